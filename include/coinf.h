@@ -706,6 +706,152 @@ co_status co_residual_align(int64_t f, int64_t s, int64_t p, int64_t module_dela
 co_status co_chain_delay(int32_t n, const int32_t* f, const int32_t* s, const int32_t* p,
                          int64_t* f_acc, int64_t* p_acc, int64_t* s_acc, int64_t* delay);
 
+/*
+ * ------------------------------------------------------------------------
+ * Token layers: the operators of a selective state space mixer.
+ *
+ * A token sequence is time-major, (B, T, values): the layout in which the
+ * projections around these layers read and write it.  The three layers below
+ * have delay 0 and follow Definition 1: a clip, a sequence of pieces and single
+ * tokens give the same outputs from one set of parameters.  Their whole state
+ * is device memory in the stated plain layout (no header, no host counter): it
+ * may be read, copied, zeroed or gathered by the caller between calls, and a
+ * call captured in a graph advances it on every replay.  No handle, no
+ * allocation, no host synchronisation in any of them.
+ *
+ * lengths: NULL, or B device int32: stream b has min(max(lengths[b], 0), T) of
+ * the call's T tokens (prompts of unequal length; for T = 1, which streams
+ * take a step).  Tokens at or past the length are not used for anything (they
+ * may hold NaN): the outputs there are 0 and the state is that after the last
+ * token of the stream.
+ *
+ * state: NULL computes a clip from a clean (zero) state and leaves none
+ * (Principle 2, forward).  Otherwise the call continues from it and, unless
+ * update_state = 0 (Principle 3), leaves the state after its tokens there.
+ * A clean state is all zero bytes.
+ */
+
+/* One (B, T, values) tensor: the values of one token are contiguous, tokens
+ * and streams are apart by any number of elements (a slice of a wider tensor,
+ * either order of the axes).  Outputs must not overlap themselves. */
+typedef struct co_tokens {
+  void*   data;
+  int64_t batch_stride;           /* elements, >= 0 */
+  int64_t token_stride;           /* elements, >= 0 */
+} co_tokens;
+
+#define CO_ACT_SILU  2            /* v / (1 + exp(-v)); co_shortconv_* only */
+
+#define CO_SHORTCONV_MAX_TAPS  8
+#define CO_SCAN_MAX_STATE      256
+#define CO_NORM_MAX_WIDTH      32768
+
+/*
+ * Short causal convolution with its activation, a depthwise convolution over
+ * tokens:
+ *   y[b,t,c] = act(bias[c] + sum_{k<K} w[c,k] x[b,t-K+1+k,c]),
+ * where x before the call's first token is the state: the K - 1 newest inputs,
+ * oldest first, (B, K-1, C) in dtype.  weight (C, K) and bias (C) in dtype.
+ * Sums in float32, rounded once.
+ */
+typedef struct co_shortconv_desc {
+  int32_t batch;
+  int32_t channels;
+  int32_t kernel;                 /* K, 1..CO_SHORTCONV_MAX_TAPS */
+  int32_t has_bias;
+  int32_t act;                    /* CO_ACT_NONE | CO_ACT_RELU | CO_ACT_SILU */
+  int32_t dtype;                  /* CO_F32 | CO_BF16: x, y, weight, bias, state */
+} co_shortconv_desc;
+
+/* Bytes of the state (0 for K = 1).  Host only. */
+co_status co_shortconv_query(const co_shortconv_desc* desc, int64_t* state_bytes);
+
+/* T tokens of x into y (not in place). */
+co_status co_shortconv_forward_steps(const co_shortconv_desc* desc, const void* weight,
+                                     const void* bias, const co_tokens* x, int32_t T,
+                                     const int32_t* lengths, void* state, const co_tokens* y,
+                                     int32_t update_state, void* stream);
+
+/*
+ * Selective scan: H heads of P values with a P x N state each, a decay a head
+ * and token, and inputs and outputs of the state (B and C) that a group of
+ * H / G heads shares:
+ *   d_t = softplus(dt[b,t,h] + dt_bias[h])  (or without softplus, without bias)
+ *   S_t = exp(d_t A[h]) S_{t-1} + d_t x[b,t,h,:] (outer) B[b,t,g,:]
+ *   y[b,t,h,:] = S_t C[b,t,g,:] + D[h] x[b,t,h,:].
+ * x and y (B, T, H P), dt (B, T, H), B and C (B, T, G N); A, D and dt_bias
+ * float32 (H), D and dt_bias may be NULL.  State (B, H, P, N) float32.
+ * Decays are meant to be at most 1 (d_t A[h] <= 0); one below 2^-160 is taken
+ * as 2^-160, which leaves nothing of a float32 either.
+ */
+typedef struct co_scan_desc {
+  int32_t batch;
+  int32_t heads;                  /* H */
+  int32_t head_dim;               /* P */
+  int32_t state_size;             /* N, 1..CO_SCAN_MAX_STATE */
+  int32_t groups;                 /* G, divides H */
+  int32_t dt_softplus;
+  int32_t dtype;                  /* CO_F32 | CO_BF16: x, B, C, y */
+  int32_t dt_dtype;               /* CO_F32 | CO_BF16: dt */
+} co_scan_desc;
+
+typedef struct co_scan_io {
+  co_tokens x, dt, b, c, y;
+} co_scan_io;
+
+/* Bytes of the state.  Host only. */
+co_status co_scan_query(const co_scan_desc* desc, int64_t* state_bytes);
+
+/* Device workspace that a call over T tokens would like (0: none).  With less
+ * the call gives results of the same accuracy, slower.  Host only. */
+co_status co_scan_workspace_bytes(const co_scan_desc* desc, int32_t T, int64_t* bytes);
+
+/* T tokens.  workspace may be NULL; it is free for reuse once the call's work on
+ * the stream is done.  y may not overlap the inputs. */
+co_status co_scan_forward_steps(const co_scan_desc* desc, const float* A, const float* D,
+                                const float* dt_bias, const co_scan_io* io, int32_t T,
+                                const int32_t* lengths, float* state, int32_t update_state,
+                                void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Root-mean-square norm over `groups` equal parts of each row of dim values,
+ * fused with a gate z and a residual sum.  With n(v) = v / sqrt(mean(v^2) + eps)
+ * over each part and silu(z) = z / (1 + exp(-z)):
+ *   a = x, or x silu(z)                     gate CO_NORM_BEFORE
+ *   r' = r + scale a, a = r'                residual CO_NORM_BEFORE (pre-norm)
+ *   y = n(a) weight, or n(a) weight silu(z) gate CO_NORM_AFTER
+ *   r' = r + scale y                        residual CO_NORM_AFTER (post-norm)
+ * x, z and y in dtype, r and r' in residual_dtype, weight and scale float32
+ * (dim); weight and scale may be NULL (1).  y is not written with residual
+ * CO_NORM_AFTER (its pointer may be NULL), r' with residual CO_NORM_NONE.
+ * All in float32, each output rounded once; the pre-norm's y is made from the
+ * unrounded sum.  y may be x, z or (same dtype) r; r_out may be r, x or z.
+ */
+#define CO_NORM_NONE    0
+#define CO_NORM_BEFORE  1
+#define CO_NORM_AFTER   2
+
+typedef struct co_norm_desc {
+  int64_t rows;
+  int32_t dim;
+  int32_t groups;                 /* divides dim, dim / groups <= CO_NORM_MAX_WIDTH */
+  int32_t gate;                   /* CO_NORM_* */
+  int32_t residual;               /* CO_NORM_* */
+  int32_t dtype;
+  int32_t residual_dtype;
+  float   eps;                    /* >= 0 */
+} co_norm_desc;
+
+/* Rows of contiguous values, row_stride elements apart. */
+typedef struct co_rows {
+  void*   data;
+  int64_t row_stride;             /* elements, >= 0 */
+} co_rows;
+
+co_status co_norm_forward(const co_norm_desc* desc, const co_rows* x, const co_rows* gate,
+                          const co_rows* residual, const float* weight, const float* scale,
+                          const co_rows* y, const co_rows* residual_out, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

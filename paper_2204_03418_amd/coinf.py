@@ -26,7 +26,8 @@ CO_ESCRATCH = -5
 CO_F32, CO_BF16 = 0, 1
 CO_ALGO_AUTO, CO_ALGO_DIRECT, CO_ALGO_GEMM, CO_ALGO_DEPTHWISE, CO_ALGO_GEMM_REG = 0, 1, 2, 3, 4
 CO_ALGO_GEMM_WS = 5
-CO_ACT_NONE, CO_ACT_RELU = 0, 1
+CO_ACT_NONE, CO_ACT_RELU, CO_ACT_SILU = 0, 1, 2
+CO_NORM_NONE, CO_NORM_BEFORE, CO_NORM_AFTER = 0, 1, 2
 CO_POOL_AVG, CO_POOL_MAX = 0, 1
 CO_MAX_TAPS = 64
 CO_TAP_NONE, CO_TAP_START, CO_TAP_ACC, CO_TAP_EMIT, CO_TAP_EMIT_FRESH = 0, 1, 2, 3, 4
@@ -164,6 +165,48 @@ co_bneck_forward_steps_ws = _sig("co_bneck_forward_steps_ws", i32,
                                  [vp, vp, i32, vp, i32, i32, vp, i64, vp, pi32])
 co_bneck_destroy = _sig("co_bneck_destroy", i32, [vp])
 co_residual_align = _sig("co_residual_align", i32, [i64, i64, i64, i64, pi64, pi64, pi64])
+
+
+class Tokens(ctypes.Structure):
+    _fields_ = [("data", vp), ("batch_stride", i64), ("token_stride", i64)]
+
+
+class ShortConvDesc(ctypes.Structure):
+    _fields_ = [("batch", i32), ("channels", i32), ("kernel", i32), ("has_bias", i32),
+                ("act", i32), ("dtype", i32)]
+
+
+class ScanDesc(ctypes.Structure):
+    _fields_ = [("batch", i32), ("heads", i32), ("head_dim", i32), ("state_size", i32),
+                ("groups", i32), ("dt_softplus", i32), ("dtype", i32), ("dt_dtype", i32)]
+
+
+class ScanIO(ctypes.Structure):
+    _fields_ = [("x", Tokens), ("dt", Tokens), ("b", Tokens), ("c", Tokens), ("y", Tokens)]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [("rows", i64), ("dim", i32), ("groups", i32), ("gate", i32), ("residual", i32),
+                ("dtype", i32), ("residual_dtype", i32), ("eps", f32)]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("data", vp), ("row_stride", i64)]
+
+
+pTok, pRows = ctypes.POINTER(Tokens), ctypes.POINTER(Rows)
+co_shortconv_query = _sig("co_shortconv_query", i32, [ctypes.POINTER(ShortConvDesc), pi64])
+co_shortconv_forward_steps = _sig("co_shortconv_forward_steps", i32,
+                                  [ctypes.POINTER(ShortConvDesc), vp, vp, pTok, i32, vp, vp, pTok,
+                                   i32, vp])
+co_scan_query = _sig("co_scan_query", i32, [ctypes.POINTER(ScanDesc), pi64])
+co_scan_workspace_bytes = _sig("co_scan_workspace_bytes", i32,
+                               [ctypes.POINTER(ScanDesc), i32, pi64])
+co_scan_forward_steps = _sig("co_scan_forward_steps", i32,
+                             [ctypes.POINTER(ScanDesc), vp, vp, vp, ctypes.POINTER(ScanIO), i32,
+                              vp, vp, i32, vp, i64, vp])
+co_norm_forward = _sig("co_norm_forward", i32,
+                       [ctypes.POINTER(NormDesc), pRows, pRows, pRows, vp, vp, pRows, pRows, vp])
 
 
 class CoinfError(RuntimeError):
@@ -1096,3 +1139,305 @@ class Residual:
     def clean_state(self):
         self.module.clean_state()
         self.line.clean_state()
+
+
+# ------------------------------------------------------------ token layers
+# Layers over token sequences (B, T, values), time-major as the projections
+# around them write it.  Their state is a plain device tensor (self.state): it
+# may be read, copied, zeroed or indexed by stream between calls.  Delay 0.
+
+
+def _tokens(t, dtype, shape, what, into):
+    """Checks that t is a device tensor of that dtype and shape (B, T, ...)
+    whose values of one token are contiguous, and points `into` at it."""
+    if t.device.type != "cuda":
+        raise ValueError(f"{what} must be a device tensor")
+    if t.dtype is not dtype:
+        raise ValueError(f"{what} has dtype {t.dtype}, expected {dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    st = t.stride()
+    run = 1
+    for i in range(len(shape) - 1, 1, -1):
+        if shape[i] != 1:
+            if st[i] != run:
+                raise ValueError(f"{what}: the values of a token must be contiguous")
+            run *= shape[i]
+    into.data, into.batch_stride, into.token_stride = t.data_ptr(), st[0], st[1]
+
+
+def _lengths(lengths, batch):
+    if lengths is None:
+        return None
+    _need(lengths, torch.int32, (batch,), "lengths")
+    return lengths.data_ptr()
+
+
+def _vector(t, n, what, device):
+    """A float32 device vector of n parameters, or None."""
+    if t is None:
+        return None
+    if tuple(t.shape) != (n,) or t.device != device:
+        raise ValueError(f"{what} must be ({n},) on {device}")
+    return t.detach().to(torch.float32).contiguous()
+
+
+class CoShortConv:
+    """Short causal depthwise convolution over tokens with its activation
+    (co_shortconv_* ABI).
+
+    weight (C, K) or (C, 1, K) with K <= 8 and bias (C,): device tensors of one
+    dtype (float32 or bfloat16).  act: "none", "relu" or "silu".  The state
+    (B, K - 1, C) holds the newest inputs, oldest first; state: a tensor to keep
+    it in (continued from), default a new clean one.
+
+    lengths (int32 (B,) on the device): how many of a call's tokens each stream
+    has.  Outputs past them are 0, whatever the tokens there hold.
+    """
+
+    delay, t_stride = 0, 1
+
+    def __init__(self, weight, bias=None, *, batch, act="silu", state=None):
+        if weight.dim() == 3 and weight.shape[1] == 1:
+            weight = weight[:, 0]
+        if weight.dim() != 2:
+            raise ValueError("weight must be (C, K) or (C, 1, K)")
+        self.batch, self.torch_dtype = batch, weight.dtype
+        self.channels, self.kernel = weight.shape
+        _need(weight, weight.dtype, weight.shape, "weight")
+        if bias is not None:
+            _need(bias, weight.dtype, (self.channels,), "bias")
+        self.weight, self.bias = weight, bias
+        acts = {"none": CO_ACT_NONE, "relu": CO_ACT_RELU, "silu": CO_ACT_SILU}
+        self.desc = ShortConvDesc(batch, self.channels, self.kernel, 1 if bias is not None else 0,
+                                  acts[act], DTYPES[weight.dtype])
+        nb = i64()
+        check(co_shortconv_query(ctypes.byref(self.desc), ctypes.byref(nb)), "co_shortconv_query")
+        shape = (batch, self.kernel - 1, self.channels)
+        if state is None:
+            state = torch.zeros(shape, dtype=weight.dtype, device=weight.device)
+        _need(state, weight.dtype, shape, "state")
+        self.state = state
+        self._x, self._y = Tokens(), Tokens()
+        # the structures of a call are this object's: like a handle, it is one thread's
+        self._args = (ctypes.byref(self.desc), _ptr(weight), _ptr(bias), ctypes.byref(self._x),
+                      ctypes.byref(self._y))
+
+    receptive_field = property(lambda self: self.kernel)
+    t_padding = property(lambda self: self.kernel - 1)
+
+    def _run(self, x, lengths, state, update, out):
+        T = x.shape[1] if x.dim() == 3 else -1
+        shape = (self.batch, T, self.channels)
+        _tokens(x, self.torch_dtype, shape, "x", self._x)
+        if out is None:
+            out = torch.empty(shape, dtype=self.torch_dtype, device=x.device)
+        _tokens(out, self.torch_dtype, shape, "out", self._y)
+        d, w, b, px, py = self._args
+        st = co_shortconv_forward_steps(d, w, b, px, T, _lengths(lengths, self.batch), state, py,
+                                        1 if update else 0, _stream())
+        if st != CO_OK:
+            check(st, "co_shortconv_forward_steps")
+        return out
+
+    def forward_steps(self, x, lengths=None, update_state=True, out=None):
+        """The next T tokens x (B, T, C) of the streams -> (B, T, C)."""
+        return self._run(x, lengths, self.state.data_ptr(), update_state, out)
+
+    def forward_step(self, x_t, lengths=None, update_state=True, out=None):
+        """The next token x_t (B, C) of each stream (of those with length 1) -> (B, C)."""
+        out = out.unsqueeze(1) if out is not None else None
+        return self.forward_steps(x_t.unsqueeze(1), lengths, update_state, out)[:, 0]
+
+    def forward(self, x, lengths=None, out=None):
+        """Whole sequences from a clean state, which the layer's own is not touched by."""
+        return self._run(x, lengths, None, False, out)
+
+    def clean_state(self):
+        self.state.zero_()
+
+
+class CoScan:
+    """Selective state space scan (co_scan_* ABI): heads of head_dim values with
+    a head_dim x state_size state each, a decay a head and token, and B and C
+    shared by the heads of a group.
+
+    A (H,): the decay of a head is exp(dt A), so A <= 0.  D (H,): skip weight.
+    dt_bias (H,) is added to dt, then with dt_softplus softplus is taken of it.
+    dtype: of x, b, c and the output; dt has it or is float32.  state
+    (B, H, head_dim, state_size) float32, continued from; default a new clean
+    one.  lengths: as CoShortConv's.
+    """
+
+    delay, receptive_field, t_stride, t_padding = 0, 1, 1, 0
+
+    def __init__(self, A, *, batch, head_dim, state_size, groups=1, D=None, dt_bias=None,
+                 dt_softplus=False, dtype=torch.bfloat16, state=None):
+        if A.device.type != "cuda":
+            raise ValueError("A must be a device tensor")
+        H = self.heads = A.shape[0]
+        self.batch, self.head_dim, self.state_size = batch, head_dim, state_size
+        self.groups, self.torch_dtype = groups, dtype
+        self.A = _vector(A, H, "A", A.device)
+        self.D = _vector(D, H, "D", A.device)
+        self.dt_bias = _vector(dt_bias, H, "dt_bias", A.device)
+        self.desc = ScanDesc(batch, H, head_dim, state_size, groups, 1 if dt_softplus else 0,
+                             DTYPES[dtype], DTYPES[dtype])
+        nb = i64()
+        check(co_scan_query(ctypes.byref(self.desc), ctypes.byref(nb)), "co_scan_query")
+        shape = (batch, H, head_dim, state_size)
+        if state is None:
+            state = torch.zeros(shape, dtype=torch.float32, device=A.device)
+        _need(state, torch.float32, shape, "state")
+        self.state = state
+        self._io = ScanIO()
+        self._args = (ctypes.byref(self.desc), _ptr(self.A), _ptr(self.D), _ptr(self.dt_bias),
+                      ctypes.byref(self._io))
+        self._ws_bytes = {}
+
+    def workspace_bytes(self, T):
+        """Device workspace of a call over T tokens."""
+        n = self._ws_bytes.get(T)
+        if n is None:
+            nb = i64()
+            check(co_scan_workspace_bytes(self._args[0], T, ctypes.byref(nb)),
+                  "co_scan_workspace_bytes")
+            n = self._ws_bytes[T] = nb.value
+        return n
+
+    def _run(self, x, dt, b, c, lengths, state, update, out):
+        B, H, P, io = self.batch, self.heads, self.head_dim, self._io
+        T = x.shape[1] if x.dim() == 4 else -1
+        shape, bc = (B, T, H, P), (B, T, self.groups, self.state_size)
+        dtype = self.torch_dtype
+        _tokens(x, dtype, shape, "x", io.x)
+        _tokens(b, dtype, bc, "b", io.b)
+        _tokens(c, dtype, bc, "c", io.c)
+        dt_dtype = torch.float32 if dt.dtype is torch.float32 else dtype
+        _tokens(dt, dt_dtype, (B, T, H), "dt", io.dt)
+        self.desc.dt_dtype = DTYPES[dt_dtype]
+        if out is None:
+            out = torch.empty(shape, dtype=dtype, device=x.device)
+        _tokens(out, dtype, shape, "out", io.y)
+        nws = self.workspace_bytes(T)
+        ws = torch.empty(nws, dtype=torch.uint8, device=x.device) if nws else None
+        d, A, D, bias, pio = self._args
+        st = co_scan_forward_steps(d, A, D, bias, pio, T, _lengths(lengths, B), state,
+                                   1 if update else 0, _ptr(ws), nws, _stream())
+        if st != CO_OK:
+            check(st, "co_scan_forward_steps")
+        return out
+
+    def forward_steps(self, x, dt, b, c, lengths=None, update_state=True, out=None):
+        """The next T tokens: x (B, T, H, P), dt (B, T, H), b and c (B, T, G, N) -> (B, T, H, P)."""
+        return self._run(x, dt, b, c, lengths, self.state.data_ptr(), update_state, out)
+
+    def forward_step(self, x_t, dt_t, b_t, c_t, lengths=None, update_state=True, out=None):
+        """The next token of each stream (of those with length 1): the same without T."""
+        out = out.unsqueeze(1) if out is not None else None
+        return self.forward_steps(x_t.unsqueeze(1), dt_t.unsqueeze(1), b_t.unsqueeze(1),
+                                  c_t.unsqueeze(1), lengths, update_state, out)[:, 0]
+
+    def forward(self, x, dt, b, c, lengths=None, out=None):
+        """Whole sequences from a clean state, which the layer's own is not touched by."""
+        return self._run(x, dt, b, c, lengths, None, False, out)
+
+    def clean_state(self):
+        self.state.zero_()
+
+
+class CoNorm:
+    """Root-mean-square norm of the last axis, in `groups` equal parts, with a
+    gate and a residual sum in the same pass (co_norm_forward).
+
+    weight (D,) and scale (D,), the residual's: parameters, taken as float32,
+    either may be None (1; then dim says D).  gate "before" norms x silu(gate),
+    "after" multiplies the normed values.  residual "before" (a pre-norm) adds
+    scale x to the residual and norms the sum; "after" (a post-norm) adds the
+    normed values times scale.  Stateless, delay 0: forward, forward_step and
+    forward_steps are one.
+    """
+
+    delay, receptive_field, t_stride, t_padding = 0, 1, 1, 0
+    MODES = {None: CO_NORM_NONE, "before": CO_NORM_BEFORE, "after": CO_NORM_AFTER}
+
+    def __init__(self, weight=None, *, dim=None, eps=1e-5, groups=1, gate=None, residual=None,
+                 scale=None):
+        given = weight if weight is not None else scale
+        if given is None and dim is None:
+            raise ValueError("weight, scale or dim must be given")
+        self.dim = dim if dim is not None else given.shape[0]
+        if groups < 1 or self.dim % groups:
+            raise ValueError(f"groups {groups} does not divide dim {self.dim}")
+        if scale is not None and residual is None:
+            raise ValueError("scale is the residual's")
+        for t, what in ((weight, "weight"), (scale, "scale")):
+            if t is not None and t.device.type != "cuda":
+                raise ValueError(f"{what} must be a device tensor")
+        self.weight = _vector(weight, self.dim, "weight", weight.device) \
+            if weight is not None else None
+        self.scale = _vector(scale, self.dim, "scale", scale.device) if scale is not None else None
+        self.gate, self.residual = gate, residual
+        self.desc = NormDesc(0, self.dim, groups, self.MODES[gate], self.MODES[residual], CO_F32,
+                             CO_F32, eps)
+        self._x, self._z, self._r, self._y, self._o = (Rows() for _ in range(5))
+
+    def _rows(self, t, dtype, shape, what, into):
+        if t.device.type != "cuda":
+            raise ValueError(f"{what} must be a device tensor")
+        if t.dtype is not dtype:
+            raise ValueError(f"{what} has dtype {t.dtype}, expected {dtype}")
+        if t.shape != shape:
+            raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+        try:
+            rows = t if t.dim() == 2 else t.view(-1, self.dim)
+        except RuntimeError:
+            raise ValueError(f"{what}: the rows must be evenly spaced") from None
+        if rows.shape[1] != 1 and rows.stride(1) != 1:
+            raise ValueError(f"{what}: the values of a row must be contiguous")
+        into.data, into.row_stride = rows.data_ptr(), rows.stride(0)
+
+    def forward(self, x, gate=None, residual=None, out=None, residual_out=None):
+        """x (..., D), gate of its shape and dtype, residual of its shape (float32 or
+        bfloat16) -> y; (y, new residual) with residual "before"; the new residual
+        with "after".  out may be x, residual_out may be residual."""
+        if (gate is None) != (self.gate is None) or (residual is None) != (self.residual is None):
+            raise ValueError("gate and residual are given to the layers that have them")
+        shape, d = x.shape, self.desc
+        if x.dim() == 0 or shape[-1] != self.dim:
+            raise ValueError(f"x has shape {tuple(shape)}, expected (..., {self.dim})")
+        if x.dtype not in DTYPES:
+            raise ValueError(f"x has dtype {x.dtype}")
+        d.rows, d.dtype = x.numel() // self.dim, DTYPES[x.dtype]
+        byref = ctypes.byref
+        self._rows(x, x.dtype, shape, "x", self._x)
+        pz = pr = po = py = None
+        if gate is not None:
+            self._rows(gate, x.dtype, shape, "gate", self._z)
+            pz = byref(self._z)
+        if residual is not None:
+            if residual.dtype not in DTYPES:
+                raise ValueError(f"residual has dtype {residual.dtype}")
+            d.residual_dtype = DTYPES[residual.dtype]
+            self._rows(residual, residual.dtype, shape, "residual", self._r)
+            if residual_out is None:
+                residual_out = torch.empty(shape, dtype=residual.dtype, device=x.device)
+            self._rows(residual_out, residual.dtype, shape, "residual_out", self._o)
+            pr, po = byref(self._r), byref(self._o)
+        if self.residual != "after":
+            if out is None:
+                out = torch.empty(shape, dtype=x.dtype, device=x.device)
+            self._rows(out, x.dtype, shape, "out", self._y)
+            py = byref(self._y)
+        st = co_norm_forward(byref(d), byref(self._x), pz, pr, _ptr(self.weight),
+                             _ptr(self.scale), py, po, _stream())
+        if st != CO_OK:
+            check(st, "co_norm_forward")
+        if self.residual == "after":
+            return residual_out
+        return (out, residual_out) if self.residual else out
+
+    forward_step = forward_steps = forward
+
+    def clean_state(self):
+        pass

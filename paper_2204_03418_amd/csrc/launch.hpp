@@ -243,4 +243,28 @@ hipError_t launch_add_frames(const void* a, const void* x, void* y, int64_t rows
                              int32_t a_frames, int32_t x_frames, int32_t x_offset, int32_t dtype,
                              hipStream_t stream);
 
+// Token layers (short_conv.hip, scan_seq.hip, scan_chunk.hip, norm.hip); the
+// entry points (token_api.hip) have checked every argument.
+hipError_t launch_shortconv(const co_shortconv_desc& d, const void* weight, const void* bias,
+                            const co_tokens& x, int32_t T, const int32_t* lengths, void* state,
+                            const co_tokens& y, bool update, hipStream_t stream);
+
+// What a scan kernel needs beside its tensors.
+struct ScanCall {
+  co_scan_desc d;
+  co_scan_io io;
+  const float* A;
+  const float* D;
+  const float* dt_bias;
+  const int32_t* lengths;
+  float* state;  // null: from zero, none left
+  int32_t T;
+  int32_t update;
+};
+hipError_t launch_scan_seq(const ScanCall& c, hipStream_t stream);
+
+hipError_t launch_norm(const co_norm_desc& d, const co_rows& x, const co_rows& gate,
+                       const co_rows& residual, const float* weight, const float* scale,
+                       const co_rows& y, const co_rows& residual_out, hipStream_t stream);
+
 }  // namespace coinf

@@ -1,0 +1,173 @@
+// Short causal convolution over tokens with its activation:
+//   y[t,c] = act(bias[c] + sum_k w[c,k] x[t-K+1+k,c]).
+// Bound by memory: x read once, y written once, 2K flops a value.  A thread
+// takes 16 bytes of channels and a run of kRun tokens, whose K - 1 tokens
+// before it are loaded again (by the wave beside it in the workgroup, so from
+// the vector cache); all loads of a run are in flight together.
+#include "launch.hpp"
+#include "token.hpp"
+
+namespace coinf {
+
+namespace {
+
+constexpr int kRun = 8;
+
+struct ConvCall {
+  const void* weight;
+  const void* bias;
+  const void* x;
+  void* y;
+  void* state;
+  const int32_t* lengths;
+  int64_t x_batch, x_token, y_batch, y_token;
+  int32_t C, T, act, update;
+  int32_t c_blocks, t_blocks;  // of a workgroup's channels and tokens
+};
+
+__device__ __forceinline__ float activate(float v, int act) {
+  if (act == CO_ACT_SILU) return silu(v);
+  return act == CO_ACT_RELU ? fmaxf(v, 0.f) : v;
+}
+
+// V channels a thread, RUN tokens a thread; LANES threads across the channels,
+// 256 / LANES runs of tokens.
+template <typename T, int K, int V, int RUN, int LANES>
+__global__ __launch_bounds__(kBlock) void shortconv_kernel(ConvCall a) {
+  constexpr int RUNS = kBlock / LANES;
+  const int lane = threadIdx.x % LANES, seg = threadIdx.x / LANES;
+  const int cb = int(blockIdx.x % uint32_t(a.c_blocks));
+  const int rest = int(blockIdx.x / uint32_t(a.c_blocks));
+  const int tb = rest % a.t_blocks, b = rest / a.t_blocks;
+  const int64_t c = (int64_t(cb) * LANES + lane) * V;
+  const int64_t t0 = (int64_t(tb) * RUNS + seg) * RUN;  // may pass T by less than 2^9
+  if (c >= a.C || t0 >= a.T) return;
+  const int len = stream_tokens(a.lengths, b, a.T);
+  const T* x = static_cast<const T*>(a.x) + b * a.x_batch + c;
+  T* y = static_cast<T*>(a.y) + b * a.y_batch + c;
+  T* state = a.state ? static_cast<T*>(a.state) + int64_t(b) * (K - 1) * a.C + c : nullptr;
+
+  // the run and the K - 1 tokens before it: from x, or the state before token 0
+  Pack<T, V> win[RUN + K - 1];
+#pragma unroll
+  for (int i = 0; i < RUN + K - 1; ++i) {
+    const int64_t t = t0 + i - (K - 1);
+    win[i] = Pack<T, V>{};
+    if (t >= 0) {
+      if (t < len) win[i] = load_pack<T, V>(x + t * a.x_token);
+    } else if (state) {
+      win[i] = load_pack<T, V>(state + (t + K - 1) * a.C);
+    }
+  }
+  float w[V][K], bias[V];
+  {
+    Pack<T, V> raw[K];
+    const T* wp = static_cast<const T*>(a.weight) + c * K;
+#pragma unroll
+    for (int k = 0; k < K; ++k) raw[k] = load_pack<T, V>(wp + k * V);
+#pragma unroll
+    for (int i = 0; i < V * K; ++i) w[i / K][i % K] = to_f32<T>(raw[i / V].v[i % V]);
+    Pack<T, V> rb{};
+    if (a.bias) rb = load_pack<T, V>(static_cast<const T*>(a.bias) + c);
+#pragma unroll
+    for (int v = 0; v < V; ++v) bias[v] = to_f32<T>(rb.v[v]);
+  }
+#pragma unroll
+  for (int i = 0; i < RUN; ++i) {
+    const int64_t t = t0 + i;
+    if (t >= a.T) break;
+    Pack<T, V> out{};
+    if (t < len) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        float s = bias[v];
+#pragma unroll
+        for (int k = 0; k < K; ++k) s = fmaf(w[v][k], to_f32<T>(win[i + k].v[v]), s);
+        out.v[v] = from_f32<T>(activate(s, a.act));
+      }
+    }
+    store_pack<T, V>(y + t * a.y_token, out);
+  }
+  // The state is read by the threads of token 0 alone, and they write it: its
+  // j-th token is number len - (K - 1) + j of the call, or what the old state has.
+  if (K > 1 && t0 == 0 && a.update && len > 0) {
+#pragma unroll
+    for (int j = 0; j < K - 1; ++j) {
+      Pack<T, V> v{};
+      if (RUN == 1) {
+        v = win[j + 1];  // one token: the old ones move up
+      } else if (len + j >= K - 1) {
+        v = load_pack<T, V>(x + (len + j - (K - 1)) * a.x_token);
+      } else {
+#pragma unroll
+        for (int i = j + 1; i < K - 1; ++i)
+          if (i == len + j) v = win[i];
+      }
+      store_pack<T, V>(state + int64_t(j) * a.C, v);
+    }
+  }
+}
+
+template <typename T, int K, int V>
+hipError_t launch_k(ConvCall a, int32_t B, hipStream_t s) {
+  const int64_t packs = (a.C + V - 1) / V;
+  if (a.T == 1) {
+    a.c_blocks = int32_t((packs + kBlock - 1) / kBlock);
+    a.t_blocks = 1;
+    const int64_t grid = int64_t(a.c_blocks) * B;
+    if (!grid_fits(grid)) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((shortconv_kernel<T, K, V, 1, kBlock>), dim3(unsigned(grid)), dim3(kBlock),
+                       0, s, a);
+    return hipGetLastError();
+  }
+  const auto go = [&](auto kernel, int lanes) {
+    a.c_blocks = int32_t((packs + lanes - 1) / lanes);
+    a.t_blocks = (a.T - 1) / (kRun * (kBlock / lanes)) + 1;
+    const int64_t grid = int64_t(a.c_blocks) * a.t_blocks * B;
+    if (!grid_fits(grid)) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL(kernel, dim3(unsigned(grid)), dim3(kBlock), 0, s, a);
+    return hipGetLastError();
+  };
+  // one run a stream: all threads across the channels
+  if (a.T <= kRun) return go(shortconv_kernel<T, K, V, kRun, kBlock>, kBlock);
+  return go(shortconv_kernel<T, K, V, kRun, 32>, 32);
+}
+
+template <typename T, int V>
+hipError_t launch_v(const ConvCall& a, int32_t B, int32_t K, hipStream_t s) {
+  switch (K) {
+    case 1: return launch_k<T, 1, V>(a, B, s);
+    case 2: return launch_k<T, 2, V>(a, B, s);
+    case 3: return launch_k<T, 3, V>(a, B, s);
+    case 4: return launch_k<T, 4, V>(a, B, s);
+    case 5: return launch_k<T, 5, V>(a, B, s);
+    case 6: return launch_k<T, 6, V>(a, B, s);
+    case 7: return launch_k<T, 7, V>(a, B, s);
+    case 8: return launch_k<T, 8, V>(a, B, s);
+  }
+  return hipErrorInvalidValue;
+}
+
+template <typename T>
+hipError_t launch_t(const ConvCall& a, int32_t B, int32_t K, hipStream_t s) {
+  constexpr int V = kWide<T>;
+  const auto wide = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
+  // 16-byte accesses where every one of them is aligned, values otherwise
+  const bool fits = a.C % V == 0 && a.x_batch % V == 0 && a.x_token % V == 0 &&
+                    a.y_batch % V == 0 && a.y_token % V == 0 && wide(a.x) && wide(a.y) &&
+                    wide(a.weight) && wide(a.bias) && wide(a.state);
+  return fits ? launch_v<T, V>(a, B, K, s) : launch_v<T, 1>(a, B, K, s);
+}
+
+}  // namespace
+
+hipError_t launch_shortconv(const co_shortconv_desc& d, const void* weight, const void* bias,
+                            const co_tokens& x, int32_t T, const int32_t* lengths, void* state,
+                            const co_tokens& y, bool update, hipStream_t stream) {
+  ConvCall a{weight, bias, x.data, y.data, state, lengths, x.batch_stride, x.token_stride,
+             y.batch_stride, y.token_stride, d.channels, T, d.act, update && state ? 1 : 0, 0, 0};
+  if (d.dtype == CO_BF16) return launch_t<bf16_t>(a, d.batch, d.kernel, stream);
+  return launch_t<float>(a, d.batch, d.kernel, stream);
+}
+
+}  // namespace coinf
