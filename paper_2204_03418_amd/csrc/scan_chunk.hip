@@ -1,0 +1,642 @@
+// Selective scan over chunks of Q tokens on the matrix cores.  With the log
+// decays l_t = d_t A and cum_t their sums from the chunk's start, a chunk that
+// begins in state S has
+//   y_t = e^{cum_t} S C_t + sum_{s<=t} e^{cum_t - cum_s} d_s (B_s . C_t) x_s + D x_t
+//   S'  = e^{cum_Q} S + sum_s (e^{cum_Q - cum_s} d_s x_s) (outer) B_s,
+// four products of sizes Q, P and N.  A workgroup's four waves are four units of
+// a group's heads, a unit being PT * 16 of a head's P rows; they share the
+// chunk's B and C and the products B_s . C_t in LDS.  A wave keeps its state
+// in the accumulators of S' all along (S^T, rows n and columns p), which are
+// also the layout that the product with C takes it in: the depth index of a
+// matrix instruction may be permuted freely if both operands agree, so lane
+// group g holds the depths 4g..4g+3 and 16+4g..16+4g+3, exactly the rows it has
+// of two 16-row result tiles.  The same holds for B_s . C_t, whose result tiles
+// become the operand of the product with x without leaving their lanes.
+//
+// bfloat16: x, B and C are used as they are.  e^{...} d_s (B_s . C_t) and the
+// state as the operand of its product with C are rounded to bfloat16, next to
+// the rounding of y itself: each adds as much error as that one over its part
+// of y.  The weighted x of the state's sum is split into three bfloat16 terms
+// (24 bits together), so the state stays a float32 sum.  float32 inputs use the
+// float32 matrix instructions throughout.
+//
+// Long sequences of few heads are cut into segments of whole chunks that run
+// beside each other: one launch makes each segment's own sum, a small one
+// carries the states across them, and the last computes everything.
+#include <type_traits>
+
+#include "launch.hpp"
+#include "token.hpp"
+
+namespace coinf {
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kWaves = 4;
+
+struct ChunkArgs {
+  ScanCall c;
+  float* ws_state;   // (B H, segments, P, N): a segment's sum, then its first state
+  float* ws_decay;   // (B H, segments): a segment's log2 decay
+  int32_t unit_blocks;  // workgroups a group of heads
+  int32_t p_blocks;     // units a head
+  int32_t segments;
+  int32_t seg_chunks;   // chunks a segment
+};
+
+// Depth-32 operand of a 16 x 16 product: lane l holds row (or column) l % 16 and
+// the depths 16 a + 4 (l / 16) + i, a < 2, i < 4, at index 4 a + i.
+template <typename T>
+struct Frag;
+template <>
+struct Frag<bf16_t> {
+  bf16x8 v;
+};
+template <>
+struct Frag<float> {
+  float v[8];
+};
+
+__device__ __forceinline__ void mma(f32x4& acc, const Frag<bf16_t>& a, const Frag<bf16_t>& b) {
+  acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, acc, 0, 0, 0);
+}
+__device__ __forceinline__ void mma(f32x4& acc, const Frag<float>& a, const Frag<float>& b) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[i], b.v[i], acc, 0, 0, 0);
+}
+
+__device__ __forceinline__ void set(Frag<bf16_t>& f, int i, float v) { f.v[i] = __bf16(v); }
+__device__ __forceinline__ void set(Frag<float>& f, int i, float v) { f.v[i] = v; }
+__device__ __forceinline__ float get(const Frag<bf16_t>& f, int i) { return float(f.v[i]); }
+__device__ __forceinline__ float get(const Frag<float>& f, int i) { return f.v[i]; }
+
+// Rows row0..row0+15 of an LDS tile, depths along its columns from col0.
+template <typename T>
+__device__ __forceinline__ Frag<T> rows_of(const T* tile, int stride, int row0, int col0) {
+  const int l = threadIdx.x % 64;
+  const T* p = tile + (row0 + l % 16) * stride + col0 + 4 * (l / 16);
+  const Pack<T, 4> lo = load_pack<T, 4>(p), hi = load_pack<T, 4>(p + 16);
+  Frag<T> f;
+  if constexpr (sizeof(T) == 2) {
+    struct Both {
+      Pack<T, 4> lo, hi;
+    };
+    f.v = __builtin_bit_cast(bf16x8, Both{lo, hi});
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f.v[i] = lo.v[i], f.v[4 + i] = hi.v[i];
+  }
+  return f;
+}
+
+// Columns of an LDS tile, depths along its rows from row0.  four = the first of
+// the 4 neighbouring columns that lanes 4q..4q+3 of 16 take, for q = l % 4 (the
+// transposing read gathers them so); one = the column of lane l % 16.
+__device__ __forceinline__ Frag<bf16_t> cols_of(const bf16_t* tile, int stride, int row0, int four,
+                                                int one) {
+  const int l = threadIdx.x % 64;
+  const bf16_t* p = tile + (row0 + 4 * (l / 16) + l % 16 / 4) * stride + four;
+  using Lds = __attribute__((address_space(3))) s16x4;
+  struct Both {
+    s16x4 lo, hi;
+  } r;
+  r.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(p));
+  r.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(p + 16 * stride));
+  (void)one;
+  return {__builtin_bit_cast(bf16x8, r)};
+}
+__device__ __forceinline__ Frag<float> cols_of(const float* tile, int stride, int row0, int four,
+                                               int one) {
+  const int l = threadIdx.x % 64;
+  const float* p = tile + (row0 + 4 * (l / 16)) * stride + one;
+  Frag<float> f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f.v[i] = p[(16 * (i / 4) + i % 4) * stride];
+  (void)four;
+  return f;
+}
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_add(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, int(uint32_t(u)), CTRL, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, int(uint32_t(u >> 32)), CTRL, ROWS, 0xf, false);
+  return v + __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
+}
+// Sum over the lanes up to this one.
+__device__ __forceinline__ double prefix_sum(double v) {
+  v = dpp_add<0x111, 0xf>(v);  // from 1, 2, 4 and 8 lanes below, within 16
+  v = dpp_add<0x112, 0xf>(v);
+  v = dpp_add<0x114, 0xf>(v);
+  v = dpp_add<0x118, 0xf>(v);
+  v = dpp_add<0x142, 0xa>(v);  // lane 15 of the 16 below
+  v = dpp_add<0x143, 0xc>(v);  // lane 31
+  return v;
+}
+__device__ __forceinline__ double last_lane(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_readlane(int(uint32_t(u)), 63);
+  const uint32_t hi = __builtin_amdgcn_readlane(int(uint32_t(u >> 32)), 63);
+  return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
+}
+
+// 16 bytes of a row from column col of `width`, zero past it and where !on.
+template <typename T, bool WIDE>
+__device__ __forceinline__ Pack<T, kWide<T>> load_row(const T* row, int col, int width, bool on) {
+  constexpr int V = kWide<T>;
+  Pack<T, V> r{};
+  if (WIDE) {
+    if (on && col < width) r = load_pack<T, V>(row + col);
+  } else if (on) {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (col + i < width) r.v[i] = row[col + i];
+  }
+  return r;
+}
+
+template <typename T, int NT, int PT>
+struct Tile {
+  static constexpr int Q = sizeof(T) == 2 ? 64 : 32;
+  static constexpr int NW = NT * 16, PW = PT * 16;
+  // Row strides: rows read as operand rows lie 16 bytes beside a multiple of the 64 banks (or
+  // spread as well), rows that the transposing read gathers 32 bytes.
+  static constexpr int CS = NW + 16 / int(sizeof(T));
+  static constexpr int BS = sizeof(T) == 2 ? NW + 16 : CS;
+  static constexpr int XS = PW + 16 / int(sizeof(T));
+  static constexpr int QT = Q / 16, QK = Q / 32;
+  static constexpr int PAIRS = QT * (QT + 1) / 2;  // tiles of B . C at and below the diagonal
+  using Cum = std::conditional_t<sizeof(T) == 2, float, double>;
+
+  T b[Q * BS];
+  T c[Q * CS];
+  T x[kWaves][Q * XS];
+  f32x4 bc[PAIRS][64];
+  Cum cum[kWaves][Q];      // log2 decay up to and with t
+  float grow[kWaves][Q];   // e^{cum_t}
+  float step[kWaves][Q];   // d_t
+  float last[kWaves][Q];   // e^{cum_Q - cum_t} d_t
+};
+
+// FULL: outputs and final states; otherwise a segment's own sum and decay.
+template <typename T, int NT, int PT, bool FULL, bool WIDE>
+__global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a) {
+  using L = Tile<T, NT, PT>;
+  using F = Frag<T>;
+  constexpr int Q = L::Q, V = kWide<T>;
+  constexpr int NK = NT / 2;                        // depth-32 blocks of N
+  constexpr int BC_ROW = L::NW / V, BC_LOADS = Q * BC_ROW / 256;
+  constexpr int X_ROW = L::PW / V, X_LOADS = Q * X_ROW / 64;
+  static_assert(NT % 2 == 0 && Q * BC_ROW % 256 == 0 && Q * X_ROW % 64 == 0);
+  __shared__ __align__(16) unsigned char lds[sizeof(L)];
+  L& sh = *reinterpret_cast<L*>(lds);
+
+  const co_scan_desc& d = a.c.d;
+  const co_scan_io& io = a.c.io;
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  const int g16 = lane / 16, l16 = lane % 16;
+  const int per_group = d.heads / d.groups;
+  const int P = d.head_dim, N = d.state_size;
+
+  const int ub = int(blockIdx.x % uint32_t(a.unit_blocks));
+  int rest = int(blockIdx.x / uint32_t(a.unit_blocks));
+  const int group = rest % d.groups;
+  rest /= d.groups;
+  const int seg = rest % a.segments, b = rest / a.segments;
+
+  if (!FULL && seg == a.segments - 1) return;  // nothing begins after it
+  const int unit = ub * kWaves + wave;
+  const bool on = unit < per_group * a.p_blocks;    // a wave without a unit only helps
+  const int h = group * per_group + (on ? unit / a.p_blocks : 0);
+  const int p0 = on ? unit % a.p_blocks * L::PW : 0;
+  const int width = on ? min(P - p0, L::PW) : 0;    // its rows of the head
+  const int64_t bh = int64_t(b) * d.heads + h;
+
+  const int len = stream_tokens(a.c.lengths, b, a.c.T);
+  const int64_t t_begin = int64_t(seg) * a.seg_chunks * Q;
+  const int64_t t_stop = min(int64_t(a.c.T), t_begin + int64_t(a.seg_chunks) * Q);
+  const int64_t t_end = min(int64_t(len), t_stop);
+
+  const T* xg = static_cast<const T*>(io.x.data) + b * io.x.batch_stride + int64_t(h) * P + p0;
+  const T* bg = static_cast<const T*>(io.b.data) + b * io.b.batch_stride + int64_t(group) * N;
+  const T* cg = static_cast<const T*>(io.c.data) + b * io.c.batch_stride + int64_t(group) * N;
+  T* yg = static_cast<T*>(io.y.data) + b * io.y.batch_stride + int64_t(h) * P + p0;
+  const int64_t dt0 = b * io.dt.batch_stride + h;
+
+  // Row r of a unit's tile pt: with two tiles a lane's 4 + 4 result rows are neighbours.
+  const auto p_of = [](int pt, int r) { return PT == 2 ? 8 * (r / 4) + 4 * pt + r % 4 : r; };
+  const auto x_four = [&](int pt) { return PT == 2 ? 8 * (lane % 4) + 4 * pt : 4 * (lane % 4); };
+
+  // S^T: rows n = 16 nt + 4 g16 + i, columns p = p_of(pt, l16)
+  f32x4 S[NT][PT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int pt = 0; pt < PT; ++pt) S[nt][pt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const auto each_state = [&](float* base, auto&& use) {
+#pragma unroll
+    for (int pt = 0; pt < PT; ++pt) {
+      const int p = p_of(pt, l16);
+      if (p >= width) continue;
+      float* row = base + int64_t(p) * N;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const int n = 16 * nt + 4 * g16;
+        if (WIDE) {
+          if (n < N) use(*reinterpret_cast<f32x4*>(row + n), S[nt][pt]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (n + i < N) {
+              float s = S[nt][pt][i];
+              use(row[n + i], s);
+              S[nt][pt][i] = s;
+            }
+        }
+      }
+    }
+  };
+  float* first = nullptr;
+  if (FULL) {
+    if (a.segments > 1)
+      first = a.ws_state + ((bh * a.segments + seg) * P + p0) * N;
+    else if (a.c.state)
+      first = a.c.state + (bh * P + p0) * N;
+  }
+  if (first) each_state(first, [](auto& mem, auto& s) { s = mem; });
+
+  const float A2 = a.c.A[h] * kLog2e, D = a.c.D ? a.c.D[h] : 0.f;
+  const float bias = a.c.dt_bias ? a.c.dt_bias[h] : 0.f;
+  double seg_log = 0.0;
+
+  Pack<T, V> rb[BC_LOADS], rc[FULL ? BC_LOADS : 1], rx[X_LOADS];
+  float rdt = 0.f;
+  const auto fetch = [&](int64_t t0) {
+#pragma unroll
+    for (int i = 0; i < BC_LOADS; ++i) {
+      const int row = (i * 256 + tid) / BC_ROW, col = (i * 256 + tid) % BC_ROW * V;
+      const int64_t t = t0 + row;
+      rb[i] = load_row<T, WIDE>(bg + t * io.b.token_stride, col, N, t < t_end);
+      if (FULL) rc[i] = load_row<T, WIDE>(cg + t * io.c.token_stride, col, N, t < t_end);
+    }
+#pragma unroll
+    for (int i = 0; i < X_LOADS; ++i) {
+      const int row = (i * 64 + lane) / X_ROW, col = (i * 64 + lane) % X_ROW * V;
+      const int64_t t = t0 + row;
+      rx[i] = load_row<T, WIDE>(xg + t * io.x.token_stride, col, width, t < t_end);
+    }
+    const int64_t t = t0 + lane;
+    rdt = 0.f;
+    if (lane < Q && t < t_end) {
+      const int64_t at = dt0 + t * io.dt.token_stride;
+      rdt = d.dt_dtype == CO_BF16 ? bf16_to_f32(static_cast<const bf16_t*>(io.dt.data)[at])
+                                  : static_cast<const float*>(io.dt.data)[at];
+    }
+  };
+
+  if (t_begin < t_end) fetch(t_begin);
+  for (int64_t t0 = t_begin; t0 < t_end; t0 += Q) {
+    __syncthreads();  // the last chunk's tiles are read
+#pragma unroll
+    for (int i = 0; i < BC_LOADS; ++i) {
+      const int row = (i * 256 + tid) / BC_ROW, col = (i * 256 + tid) % BC_ROW * V;
+      store_pack<T, V>(sh.b + row * L::BS + col, rb[i]);
+      if (FULL) store_pack<T, V>(sh.c + row * L::CS + col, rc[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < X_LOADS; ++i) {
+      const int row = (i * 64 + lane) / X_ROW, col = (i * 64 + lane) % X_ROW * V;
+      store_pack<T, V>(sh.x[wave] + row * L::XS + col, rx[i]);
+    }
+    // decays: lane = token; 64 bits keep the differences of far sums exact
+    float dt = 0.f, log_a = 0.f;
+    if (lane < Q && t0 + lane < t_end) {
+      dt = rdt + bias;
+      if (d.dt_softplus) dt = softplus(dt);
+      log_a = fmaxf(dt * A2, -160.f);
+    }
+    const double cum = prefix_sum(double(log_a));
+    const double total = last_lane(cum);
+    seg_log += total;
+    if (lane < Q) {
+      sh.cum[wave][lane] = typename L::Cum(cum);
+      sh.grow[wave][lane] = exp2_fast(float(cum));
+      sh.step[wave][lane] = dt;
+      sh.last[wave][lane] = exp2_fast(float(total - cum)) * dt;
+    }
+    if (t0 + Q < t_end) fetch(t0 + Q);
+    __syncthreads();
+
+    if constexpr (FULL) {
+      // B . C, tile row by tile row among the waves: rows s, columns t
+      for (int i = wave; i < L::PAIRS; i += kWaves) {
+        const int tj = i >= 6 ? 3 : i >= 3 ? 2 : i >= 1 ? 1 : 0, si = i - tj * (tj + 1) / 2;
+        f32x4 acc{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < NK; ++k)
+          mma(acc, rows_of<T>(sh.b, L::BS, 16 * si, 32 * k),
+              rows_of<T>(sh.c, L::CS, 16 * tj, 32 * k));
+        sh.bc[i][lane] = acc;
+      }
+      // y^T = e^{cum_t} S C_t: rows p, columns t
+      f32x4 y[L::QT][PT];
+#pragma unroll
+      for (int j = 0; j < L::QT; ++j)
+#pragma unroll
+        for (int pt = 0; pt < PT; ++pt) y[j][pt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < NK; ++k) {
+        F s[PT];
+#pragma unroll
+        for (int pt = 0; pt < PT; ++pt)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) set(s[pt], i, S[2 * k + i / 4][pt][i % 4]);
+#pragma unroll
+        for (int j = 0; j < L::QT; ++j) {
+          const F c = rows_of<T>(sh.c, L::CS, 16 * j, 32 * k);
+#pragma unroll
+          for (int pt = 0; pt < PT; ++pt) mma(y[j][pt], s[pt], c);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < L::QT; ++j) {
+        const float e = sh.grow[wave][16 * j + l16];
+#pragma unroll
+        for (int pt = 0; pt < PT; ++pt) y[j][pt] *= e;
+      }
+      __syncthreads();
+      // the chunk's own tokens
+#pragma unroll
+      for (int k = 0; k < L::QK; ++k) {
+        F x[PT];
+#pragma unroll
+        for (int pt = 0; pt < PT; ++pt)
+          x[pt] = cols_of(sh.x[wave], L::XS, 32 * k, x_four(pt), p_of(pt, l16));
+#pragma unroll
+        for (int j = 2 * k; j < L::QT; ++j) {
+          const typename L::Cum cum_t = sh.cum[wave][16 * j + l16];
+          F m;
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const int si = 2 * k + half;
+            if (si > j) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) set(m, 4 * half + i, 0.f);
+              continue;
+            }
+            const f32x4 bc = sh.bc[j * (j + 1) / 2 + si][lane];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int s = 16 * si + 4 * g16 + i;
+              const float e = exp2_fast(float(cum_t - sh.cum[wave][s])) * sh.step[wave][s];
+              const bool seen = si < j || 4 * g16 + i <= l16;
+              set(m, 4 * half + i, seen ? e * bc[i] : 0.f);
+            }
+          }
+#pragma unroll
+          for (int pt = 0; pt < PT; ++pt) mma(y[j][pt], x[pt], m);
+        }
+      }
+      // The products with masked places take 0 x_s: a NaN or an infinity among x would reach
+      // the tokens before it.  Where one shows, the chunk's own part is summed token by token.
+      bool odd = false;
+#pragma unroll
+      for (int j = 0; j < L::QT; ++j)
+#pragma unroll
+        for (int pt = 0; pt < PT; ++pt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) odd |= y[j][pt][i] != y[j][pt][i];
+      if (__any(odd)) {
+#pragma unroll 1
+        for (int j = 0; j < L::QT; ++j) {
+          f32x4 z[PT];
+#pragma unroll
+          for (int pt = 0; pt < PT; ++pt) z[pt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = 0; k < NK; ++k)
+#pragma unroll
+            for (int pt = 0; pt < PT; ++pt) {
+              F s;
+#pragma unroll
+              for (int i = 0; i < 8; ++i) set(s, i, S[2 * k + i / 4][pt][i % 4]);
+              mma(z[pt], s, rows_of<T>(sh.c, L::CS, 16 * j, 32 * k));
+            }
+          const int t = 16 * j + l16;
+          const float e = sh.grow[wave][t];
+#pragma unroll
+          for (int pt = 0; pt < PT; ++pt) z[pt] *= e;
+          const typename L::Cum cum_t = sh.cum[wave][t];
+          for (int s = 0; s <= 16 * j + 15; ++s) {
+            if (s > t) continue;
+            const float bc = sh.bc[j * (j + 1) / 2 + s / 16][16 * (s % 16 / 4) + l16][s % 4];
+            const float m = exp2_fast(float(cum_t - sh.cum[wave][s])) * sh.step[wave][s] * bc;
+#pragma unroll
+            for (int pt = 0; pt < PT; ++pt)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                z[pt][i] = fmaf(m, to_f32<T>(sh.x[wave][s * L::XS + p_of(pt, 4 * g16 + i)]),
+                                z[pt][i]);
+          }
+#pragma unroll
+          for (int jj = 0; jj < L::QT; ++jj)
+            if (jj == j) {
+#pragma unroll
+              for (int pt = 0; pt < PT; ++pt) y[jj][pt] = z[pt];
+            }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < L::QT; ++j) {
+        const int64_t t = t0 + 16 * j + l16;
+        if (t >= t_stop) continue;
+        T* row = yg + t * io.y.token_stride;
+        const T* xr = sh.x[wave] + (16 * j + l16) * L::XS;
+        constexpr int RUN = PT * 4;  // neighbours of this lane
+        const int p = RUN * g16;
+        float out[RUN];
+#pragma unroll
+        for (int i = 0; i < RUN; ++i)
+          out[i] = fmaf(D, to_f32<T>(xr[p + i]), y[j][i / 4][i % 4]);
+        if (WIDE) {
+          constexpr int W = RUN < V ? RUN : V;
+#pragma unroll
+          for (int q = 0; q < RUN; q += W) {
+            Pack<T, W> o;
+#pragma unroll
+            for (int i = 0; i < W; ++i) o.v[i] = from_f32<T>(out[q + i]);
+            if (p + q < width) store_pack<T, W>(row + p + q, o);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < RUN; ++i)
+            if (p + i < width) row[p + i] = from_f32<T>(out[i]);
+        }
+      }
+    }
+
+    // S' = e^{cum_Q} S + B^T (weighted x)
+    const float keep = exp2_fast(float(total));
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int pt = 0; pt < PT; ++pt) S[nt][pt] *= keep;
+#pragma unroll
+    for (int k = 0; k < L::QK; ++k) {
+      constexpr int TERMS = sizeof(T) == 2 ? 3 : 1;
+      F x[PT][TERMS];
+#pragma unroll
+      for (int pt = 0; pt < PT; ++pt) {
+        const F v = cols_of(sh.x[wave], L::XS, 32 * k, x_four(pt), p_of(pt, l16));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float left = get(v, i) * sh.last[wave][32 * k + 16 * (i / 4) + 4 * g16 + i % 4];
+#pragma unroll
+          for (int term = 0; term < TERMS; ++term) {
+            set(x[pt][term], i, left);
+            left -= get(x[pt][term], i);
+          }
+        }
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const F bt = cols_of(sh.b, L::BS, 32 * k, 16 * nt + 4 * (lane % 4), 16 * nt + l16);
+#pragma unroll
+        for (int pt = 0; pt < PT; ++pt)
+#pragma unroll
+          for (int term = TERMS - 1; term >= 0; --term) mma(S[nt][pt], bt, x[pt][term]);
+      }
+    }
+  }
+
+  if (FULL) {
+    // tokens past the stream's
+    const int64_t from = t_begin < t_end ? t_begin + (t_end - t_begin + Q - 1) / Q * Q : t_begin;
+    for (int64_t t = from + lane / 16; t < t_stop; t += 4)
+      for (int p = l16; p < width; p += 16) yg[t * io.y.token_stride + p] = T{};
+    if (a.c.update && seg == a.segments - 1 && len > 0)
+      each_state(a.c.state + (bh * P + p0) * N, [](auto& mem, auto& s) { mem = s; });
+  } else {
+    each_state(a.ws_state + ((bh * a.segments + seg) * P + p0) * N,
+               [](auto& mem, auto& s) { mem = s; });
+    if (on && p0 == 0 && lane == 0) a.ws_decay[bh * a.segments + seg] = float(seg_log);
+  }
+}
+
+// Turns the segments' sums into the states that they begin with.
+__global__ __launch_bounds__(kBlock) void scan_carry_kernel(ChunkArgs a) {
+  const int64_t size = int64_t(a.c.d.head_dim) * a.c.d.state_size;
+  const int64_t i = int64_t(blockIdx.x) * kBlock + threadIdx.x;
+  if (i >= size * a.c.d.heads * a.c.d.batch) return;
+  const int64_t bh = i / size;
+  float* w = a.ws_state + bh * a.segments * size + i % size;
+  const float* decay = a.ws_decay + bh * a.segments;
+  float s = a.c.state ? a.c.state[i] : 0.f;
+  for (int k = 0; k < a.segments; ++k) {
+    const float sum = k < a.segments - 1 ? w[k * size] : 0.f;
+    w[k * size] = s;
+    if (k < a.segments - 1) s = fmaf(exp2_fast(decay[k]), s, sum);
+  }
+}
+
+template <typename T, int NT, int PT, bool WIDE>
+hipError_t launch_tiles(ChunkArgs a, hipStream_t s) {
+  const co_scan_desc& d = a.c.d;
+  a.p_blocks = (d.head_dim + 16 * PT - 1) / (16 * PT);
+  const int64_t units = int64_t(d.heads / d.groups) * a.p_blocks;
+  a.unit_blocks = int32_t((units + kWaves - 1) / kWaves);
+  const int64_t grid = int64_t(a.unit_blocks) * d.groups * d.batch;
+  if (!grid_fits(grid * a.segments)) return hipErrorInvalidConfiguration;
+  if (a.segments > 1) {
+    hipLaunchKernelGGL((scan_chunk_kernel<T, NT, PT, false, WIDE>),
+                       dim3(unsigned(grid * a.segments)), dim3(kWaves * 64), 0, s, a);
+    const int64_t values = int64_t(d.batch) * d.heads * d.head_dim * d.state_size;
+    const int64_t blocks = (values + kBlock - 1) / kBlock;
+    if (!grid_fits(blocks)) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL(scan_carry_kernel, dim3(unsigned(blocks)), dim3(kBlock), 0, s, a);
+  }
+  hipLaunchKernelGGL((scan_chunk_kernel<T, NT, PT, true, WIDE>), dim3(unsigned(grid * a.segments)),
+                     dim3(kWaves * 64), 0, s, a);
+  return hipGetLastError();
+}
+
+template <typename T, bool WIDE>
+hipError_t launch_state(const ChunkArgs& a, hipStream_t s) {
+  const int N = a.c.d.state_size;
+  // the state of a unit takes 64 registers of a lane at the most
+  if (N <= 32) return launch_tiles<T, 2, 2, WIDE>(a, s);
+  if (N <= 64) return launch_tiles<T, 4, 2, WIDE>(a, s);
+  if (N <= 128) return launch_tiles<T, 8, 2, WIDE>(a, s);
+  return launch_tiles<T, 16, 1, WIDE>(a, s);
+}
+
+template <typename T>
+hipError_t launch_t(const ChunkArgs& a, hipStream_t s) {
+  constexpr int V = kWide<T>;
+  const auto wide = [](const co_tokens& t) {
+    return reinterpret_cast<uintptr_t>(t.data) % 16 == 0 && t.batch_stride % V == 0 &&
+           t.token_stride % V == 0;
+  };
+  const co_scan_io& io = a.c.io;
+  // 16-byte accesses where every one of them is aligned, values otherwise
+  const bool fits = a.c.d.head_dim % V == 0 && a.c.d.state_size % V == 0 && wide(io.x) &&
+                    wide(io.b) && wide(io.c) && wide(io.y) &&
+                    reinterpret_cast<uintptr_t>(a.c.state) % 16 == 0 &&
+                    reinterpret_cast<uintptr_t>(a.ws_state) % 16 == 0;
+  return fits ? launch_state<T, true>(a, s) : launch_state<T, false>(a, s);
+}
+
+int chunk_tokens(const co_scan_desc& d) { return d.dtype == CO_BF16 ? 64 : 32; }
+
+// Segments of a call over T tokens, and their chunks: enough to give each of
+// 256 CUs two workgroups, of four chunks at least.
+void cut(const co_scan_desc& d, int64_t T, int64_t* segments, int64_t* seg_chunks) {
+  const int64_t Q = chunk_tokens(d), chunks = (T + Q - 1) / Q;
+  const int64_t pw = d.state_size <= 128 ? 32 : 16;
+  const int64_t units = int64_t(d.heads / d.groups) * ((d.head_dim + pw - 1) / pw);
+  const int64_t groups = (units + kWaves - 1) / kWaves * d.groups * d.batch;
+  int64_t n = (512 + groups - 1) / groups;
+  n = n < chunks / 4 ? n : chunks / 4;
+  if (n < 1) n = 1;
+  *seg_chunks = (chunks + n - 1) / n;
+  *segments = (chunks + *seg_chunks - 1) / *seg_chunks;
+}
+
+}  // namespace
+
+bool scan_chunk_takes(const co_scan_desc& d, int32_t T) { return T >= 16; }
+
+int64_t scan_chunk_workspace(const co_scan_desc& d, int32_t T) {
+  int64_t segments, seg_chunks;
+  cut(d, T, &segments, &seg_chunks);
+  if (segments < 2) return 0;
+  const int64_t bh = int64_t(d.batch) * d.heads;
+  return bh * segments * (int64_t(d.head_dim) * d.state_size + 1) * 4;
+}
+
+hipError_t launch_scan_chunk(const ScanCall& c, void* workspace, int64_t workspace_bytes,
+                             hipStream_t stream) {
+  int64_t segments, seg_chunks;
+  cut(c.d, c.T, &segments, &seg_chunks);
+  if (segments > 1 && (!workspace || workspace_bytes < scan_chunk_workspace(c.d, c.T))) {
+    segments = 1;
+    seg_chunks = (c.T + chunk_tokens(c.d) - 1) / chunk_tokens(c.d);
+  }
+  ChunkArgs a{};
+  a.c = c;
+  a.segments = int32_t(segments);
+  a.seg_chunks = int32_t(seg_chunks);
+  if (segments > 1) {
+    a.ws_state = static_cast<float*>(workspace);
+    a.ws_decay = a.ws_state + int64_t(c.d.batch) * c.d.heads * segments * c.d.head_dim *
+                                  c.d.state_size;
+  }
+  if (c.d.dtype == CO_BF16) return launch_t<bf16_t>(a, stream);
+  return launch_t<float>(a, stream);
+}
+
+}  // namespace coinf

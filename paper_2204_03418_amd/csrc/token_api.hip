@@ -106,7 +106,7 @@ co_status co_scan_query(const co_scan_desc* desc, int64_t* state_bytes) {
 
 co_status co_scan_workspace_bytes(const co_scan_desc* desc, int32_t T, int64_t* bytes) {
   if (!scan_ok(desc) || T < 0 || !bytes) return CO_EINVAL;
-  *bytes = 0;
+  *bytes = scan_chunk_takes(*desc, T) ? scan_chunk_workspace(*desc, T) : 0;
   return CO_OK;
 }
 
@@ -125,10 +125,12 @@ co_status co_scan_forward_steps(const co_scan_desc* desc, const float* A, const 
       io->y.data == io->dt.data)
     return CO_EINVAL;
   if (!aligned(A, 4) || !aligned(D, 4) || !aligned(dt_bias, 4) || !aligned(state, 4) ||
-      !aligned(lengths, 4))
+      !aligned(lengths, 4) || !aligned(workspace, 4))
     return CO_EINVAL;
   if (mul_to(mul_to(B, inner, kMaxValues), T, kMaxValues) < 0) return CO_EINVAL;
   ScanCall c{*desc, *io, A, D, dt_bias, lengths, state, T, update_state && state ? 1 : 0};
+  if (scan_chunk_takes(*desc, T))
+    return done(launch_scan_chunk(c, workspace, workspace_bytes, as_stream(stream)));
   return done(launch_scan_seq(c, as_stream(stream)));
 }
 

@@ -456,3 +456,27 @@ def test_graph_replays_advance_the_states(T):
     for y, s, k in got:
         assert torch.equal(step(), y) and torch.equal(scan.state, s) and torch.equal(conv.state, k)
         x.mul_(-1.0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_scan_nonfinite_tokens_stay_behind(dtype, bad):
+    """What is not finite at a token reaches no output before it, no other
+    stream and no other row of its head."""
+    case = (2, 150, 2, 32, 1, 32, dtype, "full", True, True)
+    v, _ = scan_inputs(case, 41)
+    y, size, S, M = scan_ref(case, v, v["state"], None)
+    v["x"][0, 83, 1, 5] = bad
+    layer = scan_layer(case, v, v["state"])
+    got = layer.forward_steps(*(v[k].to(DEV) for k in ("x", "dt", "b", "c")))
+    mark = torch.zeros(got.shape, dtype=torch.bool, device=DEV)
+    mark[0, 83:, 1, 5] = True
+    assert not torch.isfinite(got[0, 83:90, 1, 5]).any()
+    f32 = (4 * 150 + 32 + 64) * R.U32 + (U[dtype] if dtype is BF16 else 0.0)
+    keep = ~mark.cpu().numpy()
+    R.within(torch.where(mark, 0.0, got), np.where(keep, y, 0.0),
+             U[dtype] * np.abs(y) + f32 * size, "finite rows")
+    assert not torch.isfinite(layer.state[0, 1, 5]).any()
+    S[0, 1, 5] = 0.0
+    layer.state[0, 1, 5] = 0.0
+    R.within(layer.state, S, (4 * 150 + 96) * R.U32 * M + 1e-300, "finite states")
