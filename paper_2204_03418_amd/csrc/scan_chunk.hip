@@ -37,6 +37,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kWaves = 4;
+constexpr int kChunk = 32;  // Q, the depth of one matrix instruction
 
 struct ChunkArgs {
   ScanCall c;
@@ -74,6 +75,28 @@ __device__ __forceinline__ void set(Frag<bf16_t>& f, int i, float v) { f.v[i] = 
 __device__ __forceinline__ void set(Frag<float>& f, int i, float v) { f.v[i] = v; }
 __device__ __forceinline__ float get(const Frag<bf16_t>& f, int i) { return float(f.v[i]); }
 __device__ __forceinline__ float get(const Frag<float>& f, int i) { return f.v[i]; }
+
+// The operand nearest to v, and in v what is left of it.
+__device__ __forceinline__ void take(Frag<bf16_t>& f, float (&v)[8]) {
+  uint32_t pairs[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    pairs[i] = __builtin_bit_cast(
+        uint32_t, __builtin_convertvector((f32x2{v[2 * i], v[2 * i + 1]}), bf16x2));
+    v[2 * i] -= __uint_as_float(pairs[i] << 16);
+    v[2 * i + 1] -= __uint_as_float(pairs[i] & 0xffff0000u);
+  }
+  struct Four {
+    uint32_t p[4];
+  };
+  f.v = __builtin_bit_cast(bf16x8, Four{{pairs[0], pairs[1], pairs[2], pairs[3]}});
+}
+__device__ __forceinline__ void take(Frag<float>& f, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f.v[i] = v[i], v[i] = 0.f;
+}
 
 // Rows row0..row0+15 of an LDS tile, depths along its columns from col0.
 template <typename T>
@@ -128,21 +151,47 @@ __device__ __forceinline__ double dpp_add(double v) {
   const uint32_t hi = __builtin_amdgcn_update_dpp(0, int(uint32_t(u >> 32)), CTRL, ROWS, 0xf, false);
   return v + __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
 }
-// Sum over the lanes up to this one.
-__device__ __forceinline__ double prefix_sum(double v) {
+// Sum over the lanes of this half wave up to this one.
+__device__ __forceinline__ double prefix_sum32(double v) {
   v = dpp_add<0x111, 0xf>(v);  // from 1, 2, 4 and 8 lanes below, within 16
   v = dpp_add<0x112, 0xf>(v);
   v = dpp_add<0x114, 0xf>(v);
   v = dpp_add<0x118, 0xf>(v);
-  v = dpp_add<0x142, 0xa>(v);  // lane 15 of the 16 below
-  v = dpp_add<0x143, 0xc>(v);  // lane 31
-  return v;
+  return dpp_add<0x142, 0xa>(v);  // lane 15 of the 16 below
 }
-__device__ __forceinline__ double last_lane(double v) {
+template <int LANE>
+__device__ __forceinline__ double from_lane(double v) {
   const uint64_t u = __builtin_bit_cast(uint64_t, v);
-  const uint32_t lo = __builtin_amdgcn_readlane(int(uint32_t(u)), 63);
-  const uint32_t hi = __builtin_amdgcn_readlane(int(uint32_t(u >> 32)), 63);
+  const uint32_t lo = __builtin_amdgcn_readlane(int(uint32_t(u)), LANE);
+  const uint32_t hi = __builtin_amdgcn_readlane(int(uint32_t(u >> 32)), LANE);
   return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
+}
+// 2^v to a few units in the last place also where v is large.
+__device__ __forceinline__ float pow2(double v) {
+  const double n = rint(v);
+  return ldexpf(exp2_fast(float(v - n)), int(n));
+}
+
+// What two chunks of a unit do to its state.  The accumulators hold the state
+// times 2^-base: a chunk whose decays stay within 2^-kSpan of the base neither
+// scales them nor takes a power for each pair of tokens.
+constexpr double kSpan = 64.0;
+struct Span {
+  double base;    // of this chunk's tokens
+  float rescale;  // of the accumulators before the chunk
+  float keep;     // and after its outputs, for a chunk of its own (far)
+  bool far;       // its decays alone pass the span: powers for pairs of tokens
+};
+// The chunk's, with the base before it; base becomes that after it.
+__device__ __forceinline__ Span span_of(double& base, double total, double reach) {
+  Span r;
+  r.far = !(reach <= kSpan);
+  const bool fits = !r.far && fabs(base) + reach <= kSpan;
+  r.rescale = fits ? 1.f : pow2(base);
+  r.base = fits ? base : 0.0;
+  r.keep = r.far ? pow2(total) : 1.f;
+  base = r.far ? 0.0 : r.base + total;
+  return r;
 }
 
 // 16 bytes of a row from column col of `width`, zero past it and where !on.
@@ -162,14 +211,14 @@ __device__ __forceinline__ Pack<T, kWide<T>> load_row(const T* row, int col, int
 
 template <typename T, int NT, int PT>
 struct Tile {
-  static constexpr int Q = sizeof(T) == 2 ? 64 : 32;
+  static constexpr int Q = kChunk;
   static constexpr int NW = NT * 16, PW = PT * 16;
   // Row strides: rows read as operand rows lie 16 bytes beside a multiple of the 64 banks (or
   // spread as well), rows that the transposing read gathers 32 bytes.
   static constexpr int CS = NW + 16 / int(sizeof(T));
   static constexpr int BS = sizeof(T) == 2 ? NW + 16 : CS;
   static constexpr int XS = PW + 16 / int(sizeof(T));
-  static constexpr int QT = Q / 16, QK = Q / 32;
+  static constexpr int QT = Q / 16;
   static constexpr int PAIRS = QT * (QT + 1) / 2;  // tiles of B . C at and below the diagonal
   using Cum = std::conditional_t<sizeof(T) == 2, float, double>;
 
@@ -177,10 +226,9 @@ struct Tile {
   T c[Q * CS];
   T x[kWaves][Q * XS];
   f32x4 bc[PAIRS][64];
-  Cum cum[kWaves][Q];      // log2 decay up to and with t
-  float grow[kWaves][Q];   // e^{cum_t}
-  float step[kWaves][Q];   // d_t
-  float last[kWaves][Q];   // e^{cum_Q - cum_t} d_t
+  // of two chunks, a token a lane (scan_chunk_kernel)
+  Cum cum[kWaves][64];
+  float step[kWaves][64], grow[kWaves][64], weight[kWaves][64];
 };
 
 // FULL: outputs and final states; otherwise a segment's own sum and decay.
@@ -190,9 +238,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a)
   using F = Frag<T>;
   constexpr int Q = L::Q, V = kWide<T>;
   constexpr int NK = NT / 2;                        // depth-32 blocks of N
-  constexpr int BC_ROW = L::NW / V, BC_LOADS = Q * BC_ROW / 256;
+  constexpr int BC_ROW = L::NW / V, BC_LOADS = (Q * BC_ROW + 255) / 256;
   constexpr int X_ROW = L::PW / V, X_LOADS = Q * X_ROW / 64;
-  static_assert(NT % 2 == 0 && Q * BC_ROW % 256 == 0 && Q * X_ROW % 64 == 0);
+  static_assert(NT % 2 == 0 && 256 % BC_ROW == 0 && Q * X_ROW % 64 == 0 && 64 % X_ROW == 0);
   __shared__ __align__(16) unsigned char lds[sizeof(L)];
   L& sh = *reinterpret_cast<L*>(lds);
 
@@ -275,67 +323,108 @@ __global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a)
   double seg_log = 0.0;
 
   Pack<T, V> rb[BC_LOADS], rc[FULL ? BC_LOADS : 1], rx[X_LOADS];
-  float rdt = 0.f;
-  const auto fetch = [&](int64_t t0) {
+  uint32_t rdt = 0;  // raw: a conversion here would wait for every load in flight
+  // A thread's pieces of B and C lie 256 / BC_ROW tokens apart, a lane's of x 64 / X_ROW.
+  constexpr int BC_BY = 256 / BC_ROW, X_BY = 64 / X_ROW;
+  const int bc_row = tid / BC_ROW, bc_col = tid % BC_ROW * V;
+  const int x_row = lane / X_ROW, x_col = lane % X_ROW * V;
+  const T* b_at = bg + (t_begin + bc_row) * io.b.token_stride;
+  const T* c_at = cg + (t_begin + bc_row) * io.c.token_stride;
+  const T* x_at = xg + (t_begin + x_row) * io.x.token_stride;
+  int64_t dt_at = dt0 + (t_begin + lane) * io.dt.token_stride;
+  // the chunk from t0 on, and the steps of two chunks
+  const auto fetch = [&](int64_t t0, bool with_dt) {
+    const int left = int(min(t_end - t0, int64_t(Q))), dt_left = int(min(t_end - t0, int64_t(64)));
 #pragma unroll
     for (int i = 0; i < BC_LOADS; ++i) {
-      const int row = (i * 256 + tid) / BC_ROW, col = (i * 256 + tid) % BC_ROW * V;
-      const int64_t t = t0 + row;
-      rb[i] = load_row<T, WIDE>(bg + t * io.b.token_stride, col, N, t < t_end);
-      if (FULL) rc[i] = load_row<T, WIDE>(cg + t * io.c.token_stride, col, N, t < t_end);
+      const bool in = bc_row + i * BC_BY < min(left, Q);
+      rb[i] = load_row<T, WIDE>(b_at + i * BC_BY * io.b.token_stride, bc_col, N, in);
+      if (FULL) rc[i] = load_row<T, WIDE>(c_at + i * BC_BY * io.c.token_stride, bc_col, N, in);
     }
 #pragma unroll
-    for (int i = 0; i < X_LOADS; ++i) {
-      const int row = (i * 64 + lane) / X_ROW, col = (i * 64 + lane) % X_ROW * V;
-      const int64_t t = t0 + row;
-      rx[i] = load_row<T, WIDE>(xg + t * io.x.token_stride, col, width, t < t_end);
-    }
-    const int64_t t = t0 + lane;
-    rdt = 0.f;
-    if (lane < Q && t < t_end) {
-      const int64_t at = dt0 + t * io.dt.token_stride;
-      rdt = d.dt_dtype == CO_BF16 ? bf16_to_f32(static_cast<const bf16_t*>(io.dt.data)[at])
-                                  : static_cast<const float*>(io.dt.data)[at];
-    }
+    for (int i = 0; i < X_LOADS; ++i)
+      rx[i] = load_row<T, WIDE>(x_at + i * X_BY * io.x.token_stride, x_col, width,
+                                x_row + i * X_BY < left);
+    if (with_dt && lane < dt_left)
+      rdt = d.dt_dtype == CO_BF16 ? static_cast<const uint16_t*>(io.dt.data)[dt_at]
+                                  : static_cast<const uint32_t*>(io.dt.data)[dt_at];
+    b_at += Q * io.b.token_stride;
+    c_at += Q * io.c.token_stride;
+    x_at += Q * io.x.token_stride;
+    if (with_dt) dt_at += 64 * io.dt.token_stride;
   };
 
-  if (t_begin < t_end) fetch(t_begin);
+  Span now{}, later{};  // of this chunk and the next
+  double base = 0.0;
+  int half = 0;  // of the two chunks whose decays are known
+  if (t_begin < t_end) fetch(t_begin, true);
   for (int64_t t0 = t_begin; t0 < t_end; t0 += Q) {
     __syncthreads();  // the last chunk's tiles are read
 #pragma unroll
     for (int i = 0; i < BC_LOADS; ++i) {
-      const int row = (i * 256 + tid) / BC_ROW, col = (i * 256 + tid) % BC_ROW * V;
-      store_pack<T, V>(sh.b + row * L::BS + col, rb[i]);
-      if (FULL) store_pack<T, V>(sh.c + row * L::CS + col, rc[i]);
+      const int row = bc_row + i * BC_BY;
+      if (row >= Q) break;
+      store_pack<T, V>(sh.b + row * L::BS + bc_col, rb[i]);
+      if (FULL) store_pack<T, V>(sh.c + row * L::CS + bc_col, rc[i]);
     }
 #pragma unroll
-    for (int i = 0; i < X_LOADS; ++i) {
-      const int row = (i * 64 + lane) / X_ROW, col = (i * 64 + lane) % X_ROW * V;
-      store_pack<T, V>(sh.x[wave] + row * L::XS + col, rx[i]);
-    }
-    // decays: lane = token; 64 bits keep the differences of far sums exact
-    float dt = 0.f, log_a = 0.f;
-    if (lane < Q && t0 + lane < t_end) {
-      dt = rdt + bias;
-      if (d.dt_softplus) dt = softplus(dt);
-      log_a = fmaxf(dt * A2, -160.f);
-    }
-    const double cum = prefix_sum(double(log_a));
-    const double total = last_lane(cum);
-    seg_log += total;
-    if (lane < Q) {
+    for (int i = 0; i < X_LOADS; ++i)
+      store_pack<T, V>(sh.x[wave] + (x_row + i * X_BY) * L::XS + x_col, rx[i]);
+    // decays of two chunks, lane = token; 64 bits keep the differences of far sums
+    if (half == 0) {
+      const int64_t t = t0 + lane;
+      float dt = 0.f, log_a = 0.f;
+      if (t < t_end) {
+        dt = __uint_as_float(d.dt_dtype == CO_BF16 ? rdt << 16 : rdt) + bias;
+        if (d.dt_softplus) dt = softplus(dt);
+        log_a = fmaxf(dt * A2, -160.f);
+      }
+      const double cum = prefix_sum32(double(log_a));
+      const double total[2] = {from_lane<31>(cum), from_lane<63>(cum)};
+      seg_log += total[0] + total[1];
+      double reach[2] = {fabs(total[0]), fabs(total[1])};  // the furthest of the sums
+      if (!d.dt_softplus) {  // steps of either sign: the sums may turn round
+        float most = fabsf(float(cum));
+#pragma unroll
+        for (int m = 16; m > 0; m /= 2) most = fmaxf(most, __shfl_xor(most, m));
+        reach[0] = from_lane<0>(double(most));
+        reach[1] = from_lane<32>(double(most));
+      }
+      now = span_of(base, total[0], reach[0]);
+      later = span_of(base, total[1], reach[1]);
+      const bool upper = lane >= 32;
+      const double at = (upper ? later.base : now.base) + cum;
+      const bool own = upper ? later.far : now.far;
       sh.cum[wave][lane] = typename L::Cum(cum);
-      sh.grow[wave][lane] = exp2_fast(float(cum));
       sh.step[wave][lane] = dt;
-      sh.last[wave][lane] = exp2_fast(float(total - cum)) * dt;
+      sh.grow[wave][lane] = pow2(at);
+      sh.weight[wave][lane] = dt * pow2(own ? (upper ? total[1] : total[0]) - cum : -at);
+    } else {
+      now = later;
     }
-    if (t0 + Q < t_end) fetch(t0 + Q);
+    if (t0 + Q < t_end) fetch(t0 + Q, half == 1);  // in flight over this one's products
     __syncthreads();
+    const bool far = now.far;
+    const typename L::Cum* cum_of = sh.cum[wave] + 32 * half;
+    const float* step_of = sh.step[wave] + 32 * half;
+    const float* grow_of = sh.grow[wave] + 32 * half;
+    const float* weight_of = sh.weight[wave] + 32 * half;
+    F x[PT];
+#pragma unroll
+    for (int pt = 0; pt < PT; ++pt)
+      x[pt] = cols_of(sh.x[wave], L::XS, 0, x_four(pt), p_of(pt, l16));
+    if (now.rescale != 1.f) {
+      const float by = now.rescale;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int pt = 0; pt < PT; ++pt) S[nt][pt] *= by;
+    }
 
     if constexpr (FULL) {
       // B . C, tile row by tile row among the waves: rows s, columns t
       for (int i = wave; i < L::PAIRS; i += kWaves) {
-        const int tj = i >= 6 ? 3 : i >= 3 ? 2 : i >= 1 ? 1 : 0, si = i - tj * (tj + 1) / 2;
+        const int tj = i >= 1 ? 1 : 0, si = i - tj * (tj + 1) / 2;
         f32x4 acc{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < NK; ++k)
@@ -343,7 +432,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a)
               rows_of<T>(sh.c, L::CS, 16 * tj, 32 * k));
         sh.bc[i][lane] = acc;
       }
-      // y^T = e^{cum_t} S C_t: rows p, columns t
+      // y^T = S C_t: rows p, columns t
       f32x4 y[L::QT][PT];
 #pragma unroll
       for (int j = 0; j < L::QT; ++j)
@@ -363,55 +452,61 @@ __global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a)
           for (int pt = 0; pt < PT; ++pt) mma(y[j][pt], s[pt], c);
         }
       }
+      float grow[L::QT];
 #pragma unroll
-      for (int j = 0; j < L::QT; ++j) {
-        const float e = sh.grow[wave][16 * j + l16];
+      for (int j = 0; j < L::QT; ++j) grow[j] = grow_of[16 * j + l16];
+      if (far) {
 #pragma unroll
-        for (int pt = 0; pt < PT; ++pt) y[j][pt] *= e;
+        for (int j = 0; j < L::QT; ++j)
+#pragma unroll
+          for (int pt = 0; pt < PT; ++pt) y[j][pt] *= grow[j];
       }
       __syncthreads();
       // the chunk's own tokens
 #pragma unroll
-      for (int k = 0; k < L::QK; ++k) {
-        F x[PT];
+      for (int j = 0; j < L::QT; ++j) {
+        F m;
 #pragma unroll
-        for (int pt = 0; pt < PT; ++pt)
-          x[pt] = cols_of(sh.x[wave], L::XS, 32 * k, x_four(pt), p_of(pt, l16));
+        for (int si = 0; si < L::QT; ++si) {
+          if (si > j) {
 #pragma unroll
-        for (int j = 2 * k; j < L::QT; ++j) {
-          const typename L::Cum cum_t = sh.cum[wave][16 * j + l16];
-          F m;
+            for (int i = 0; i < 4; ++i) set(m, 4 * si + i, 0.f);
+            continue;
+          }
+          f32x4 v = sh.bc[j * (j + 1) / 2 + si][lane];
+          const int s0 = 16 * si + 4 * g16;
+          if (far) {
+            const typename L::Cum cum_t = cum_of[16 * j + l16];
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            const int si = 2 * k + half;
-            if (si > j) {
+            for (int i = 0; i < 4; ++i)
+              v[i] *= exp2_fast(float(cum_t - cum_of[s0 + i])) * step_of[s0 + i];
+          } else {
 #pragma unroll
-              for (int i = 0; i < 4; ++i) set(m, 4 * half + i, 0.f);
-              continue;
-            }
-            const f32x4 bc = sh.bc[j * (j + 1) / 2 + si][lane];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int s = 16 * si + 4 * g16 + i;
-              const float e = exp2_fast(float(cum_t - sh.cum[wave][s])) * sh.step[wave][s];
-              const bool seen = si < j || 4 * g16 + i <= l16;
-              set(m, 4 * half + i, seen ? e * bc[i] : 0.f);
-            }
+            for (int i = 0; i < 4; ++i) v[i] *= weight_of[s0 + i];
           }
 #pragma unroll
-          for (int pt = 0; pt < PT; ++pt) mma(y[j][pt], x[pt], m);
+          for (int i = 0; i < 4; ++i)
+            set(m, 4 * si + i, si < j || 4 * g16 + i <= l16 ? v[i] : 0.f);
         }
+#pragma unroll
+        for (int pt = 0; pt < PT; ++pt) mma(y[j][pt], x[pt], m);
+      }
+      if (!far) {
+#pragma unroll
+        for (int j = 0; j < L::QT; ++j)
+#pragma unroll
+          for (int pt = 0; pt < PT; ++pt) y[j][pt] *= grow[j];
       }
       // The products with masked places take 0 x_s: a NaN or an infinity among x would reach
       // the tokens before it.  Where one shows, the chunk's own part is summed token by token.
-      bool odd = false;
+      float any = 0.f;
 #pragma unroll
       for (int j = 0; j < L::QT; ++j)
 #pragma unroll
         for (int pt = 0; pt < PT; ++pt)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) odd |= y[j][pt][i] != y[j][pt][i];
-      if (__any(odd)) {
+          for (int i = 0; i < 4; ++i) any += y[j][pt][i];
+      if (__any(any != any)) {
 #pragma unroll 1
         for (int j = 0; j < L::QT; ++j) {
           f32x4 z[PT];
@@ -427,14 +522,14 @@ __global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a)
               mma(z[pt], s, rows_of<T>(sh.c, L::CS, 16 * j, 32 * k));
             }
           const int t = 16 * j + l16;
-          const float e = sh.grow[wave][t];
+          const float e = grow_of[t];
 #pragma unroll
           for (int pt = 0; pt < PT; ++pt) z[pt] *= e;
-          const typename L::Cum cum_t = sh.cum[wave][t];
+          const typename L::Cum cum_t = cum_of[t];
           for (int s = 0; s <= 16 * j + 15; ++s) {
             if (s > t) continue;
             const float bc = sh.bc[j * (j + 1) / 2 + s / 16][16 * (s % 16 / 4) + l16][s % 4];
-            const float m = exp2_fast(float(cum_t - sh.cum[wave][s])) * sh.step[wave][s] * bc;
+            const float m = exp2_fast(float(cum_t - cum_of[s])) * step_of[s] * bc;
 #pragma unroll
             for (int pt = 0; pt < PT; ++pt)
 #pragma unroll
@@ -480,37 +575,40 @@ __global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a)
     }
 
     // S' = e^{cum_Q} S + B^T (weighted x)
-    const float keep = exp2_fast(float(total));
+    if (far) {
+      const float keep = now.keep;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int pt = 0; pt < PT; ++pt) S[nt][pt] *= keep;
+    }
+    constexpr int TERMS = sizeof(T) == 2 ? 3 : 1;
+    F xw[PT][TERMS];
+#pragma unroll
+    for (int pt = 0; pt < PT; ++pt) {
+      float left[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        left[i] = get(x[pt], i) * weight_of[16 * (i / 4) + 4 * g16 + i % 4];
+#pragma unroll
+      for (int term = 0; term < TERMS; ++term) take(xw[pt][term], left);
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const F bt = cols_of(sh.b, L::BS, 0, 16 * nt + 4 * (lane % 4), 16 * nt + l16);
+#pragma unroll
+      for (int pt = 0; pt < PT; ++pt)
+#pragma unroll
+        for (int term = TERMS - 1; term >= 0; --term) mma(S[nt][pt], bt, xw[pt][term]);
+    }
+    half ^= 1;
+  }
+  if (base != 0.0) {
+    const float by = pow2(base);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int pt = 0; pt < PT; ++pt) S[nt][pt] *= keep;
-#pragma unroll
-    for (int k = 0; k < L::QK; ++k) {
-      constexpr int TERMS = sizeof(T) == 2 ? 3 : 1;
-      F x[PT][TERMS];
-#pragma unroll
-      for (int pt = 0; pt < PT; ++pt) {
-        const F v = cols_of(sh.x[wave], L::XS, 32 * k, x_four(pt), p_of(pt, l16));
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          float left = get(v, i) * sh.last[wave][32 * k + 16 * (i / 4) + 4 * g16 + i % 4];
-#pragma unroll
-          for (int term = 0; term < TERMS; ++term) {
-            set(x[pt][term], i, left);
-            left -= get(x[pt][term], i);
-          }
-        }
-      }
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const F bt = cols_of(sh.b, L::BS, 32 * k, 16 * nt + 4 * (lane % 4), 16 * nt + l16);
-#pragma unroll
-        for (int pt = 0; pt < PT; ++pt)
-#pragma unroll
-          for (int term = TERMS - 1; term >= 0; --term) mma(S[nt][pt], bt, x[pt][term]);
-      }
-    }
+      for (int pt = 0; pt < PT; ++pt) S[nt][pt] *= by;
   }
 
   if (FULL) {
@@ -590,12 +688,10 @@ hipError_t launch_t(const ChunkArgs& a, hipStream_t s) {
   return fits ? launch_state<T, true>(a, s) : launch_state<T, false>(a, s);
 }
 
-int chunk_tokens(const co_scan_desc& d) { return d.dtype == CO_BF16 ? 64 : 32; }
-
 // Segments of a call over T tokens, and their chunks: enough to give each of
 // 256 CUs two workgroups, of four chunks at least.
 void cut(const co_scan_desc& d, int64_t T, int64_t* segments, int64_t* seg_chunks) {
-  const int64_t Q = chunk_tokens(d), chunks = (T + Q - 1) / Q;
+  const int64_t Q = kChunk, chunks = (T + Q - 1) / Q;
   const int64_t pw = d.state_size <= 128 ? 32 : 16;
   const int64_t units = int64_t(d.heads / d.groups) * ((d.head_dim + pw - 1) / pw);
   const int64_t groups = (units + kWaves - 1) / kWaves * d.groups * d.batch;
@@ -624,7 +720,7 @@ hipError_t launch_scan_chunk(const ScanCall& c, void* workspace, int64_t workspa
   cut(c.d, c.T, &segments, &seg_chunks);
   if (segments > 1 && (!workspace || workspace_bytes < scan_chunk_workspace(c.d, c.T))) {
     segments = 1;
-    seg_chunks = (c.T + chunk_tokens(c.d) - 1) / chunk_tokens(c.d);
+    seg_chunks = (c.T + kChunk - 1) / kChunk;
   }
   ChunkArgs a{};
   a.c = c;
