@@ -802,8 +802,9 @@ typedef struct co_scan_io {
 /* Bytes of the state.  Host only. */
 co_status co_scan_query(const co_scan_desc* desc, int64_t* state_bytes);
 
-/* Device workspace that a call over T tokens would like (0: none).  With less
- * the call gives results of the same accuracy, slower.  Host only. */
+/* Device workspace (16-byte aligned) that a call over T tokens would like (0:
+ * none).  With less the call runs token by token: no less accurate, slower.
+ * Host only. */
 co_status co_scan_workspace_bytes(const co_scan_desc* desc, int32_t T, int64_t* bytes);
 
 /* T tokens.  workspace may be NULL; it is free for reuse once the call's work on

@@ -263,11 +263,10 @@ struct ScanCall {
 };
 // Token by token, any call.
 hipError_t launch_scan_seq(const ScanCall& c, hipStream_t stream);
-// In chunks on the matrix cores; workspace as co_scan_forward_steps.
+// In chunks on the matrix cores, with a workspace of so many bytes at 16-byte alignment.
 bool scan_chunk_takes(const co_scan_desc& d, int32_t T);
 int64_t scan_chunk_workspace(const co_scan_desc& d, int32_t T);
-hipError_t launch_scan_chunk(const ScanCall& c, void* workspace, int64_t workspace_bytes,
-                             hipStream_t stream);
+hipError_t launch_scan_chunk(const ScanCall& c, void* workspace, hipStream_t stream);
 
 hipError_t launch_norm(const co_norm_desc& d, const co_rows& x, const co_rows& gate,
                        const co_rows& residual, const float* weight, const float* scale,

@@ -20,9 +20,11 @@
 // (24 bits together), so the state stays a float32 sum.  float32 inputs use the
 // float32 matrix instructions throughout.
 //
-// Long sequences of few heads are cut into segments of whole chunks that run
-// beside each other: one launch makes each segment's own sum, a small one
-// carries the states across them, and the last computes everything.
+// A small launch before makes what the heads of a group and the units of a head
+// share: the products B_s . C_t, and of each chunk its decays.  Long sequences
+// of few heads are cut into segments of whole chunks that run beside each other:
+// one launch makes each segment's own sum, a small one carries the states across
+// them, and the last computes everything.
 #include <type_traits>
 
 #include "launch.hpp"
@@ -38,15 +40,31 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kWaves = 4;
 constexpr int kChunk = 32;  // Q, the depth of one matrix instruction
+constexpr int kPairs = 3;   // 16 x 16 tiles of B . C at and below the diagonal: (0,0), (0,1), (1,1)
+
+// Decays of one chunk of a head, l2 = log2 of them: what its waves read.
+struct ChunkDecay {
+  float total;  // of the chunk
+  float reach;  // the largest magnitude of the sums
+  float pad[2];
+  float grow[kChunk];    // 2^{cum_t}
+  float weight[kChunk];  // 2^{-cum_t} d_t, or 2^{total - cum_t} d_t where the reach passes kSpan
+  float step[kChunk];    // d_t
+  float cum[kChunk], cum_low[kChunk];  // cum_t = cum + cum_low
+};
+static_assert(sizeof(ChunkDecay) % 16 == 0);
 
 struct ChunkArgs {
   ScanCall c;
-  float* ws_state;   // (B H, segments, P, N): a segment's sum, then its first state
-  float* ws_decay;   // (B H, segments): a segment's log2 decay
-  int32_t unit_blocks;  // workgroups a group of heads
-  int32_t p_blocks;     // units a head
+  f32x4* ws_bc;          // (B, G, chunks, kPairs, 64 lanes): tiles of B . C
+  ChunkDecay* ws_decay;  // (B H, chunks)
+  float* ws_state;       // (B H, segments, P, N): a segment's sum, then its first state
+  float* ws_total;       // (B H, segments): a segment's log2 decay
+  int32_t chunks;
+  int32_t unit_blocks;   // workgroups a group of heads
+  int32_t p_blocks;      // units a head
   int32_t segments;
-  int32_t seg_chunks;   // chunks a segment
+  int32_t seg_chunks;    // chunks a segment
 };
 
 // Depth-32 operand of a 16 x 16 product: lane l holds row (or column) l % 16 and
@@ -71,8 +89,6 @@ __device__ __forceinline__ void mma(f32x4& acc, const Frag<float>& a, const Frag
     acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[i], b.v[i], acc, 0, 0, 0);
 }
 
-__device__ __forceinline__ void set(Frag<bf16_t>& f, int i, float v) { f.v[i] = __bf16(v); }
-__device__ __forceinline__ void set(Frag<float>& f, int i, float v) { f.v[i] = v; }
 __device__ __forceinline__ float get(const Frag<bf16_t>& f, int i) { return float(f.v[i]); }
 __device__ __forceinline__ float get(const Frag<float>& f, int i) { return f.v[i]; }
 
@@ -98,23 +114,52 @@ __device__ __forceinline__ void take(Frag<float>& f, float (&v)[8]) {
   for (int i = 0; i < 8; ++i) f.v[i] = v[i], v[i] = 0.f;
 }
 
+__device__ __forceinline__ void round_to(Frag<bf16_t>& f, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f.v[i] = __bf16(v[i]);
+}
+__device__ __forceinline__ void round_to(Frag<float>& f, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f.v[i] = v[i];
+}
+
+// Whether one of an operand's values is not finite.
+__device__ __forceinline__ bool not_finite(const Frag<bf16_t>& f) {
+  typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  const u16x8 v = __builtin_bit_cast(u16x8, f.v) & u16x8(0x7fff);
+  u16x2 most = {v[0], v[1]};
+#pragma unroll
+  for (int i = 2; i < 8; i += 2) most = __builtin_elementwise_max(most, (u16x2{v[i], v[i + 1]}));
+  return most[0] >= 0x7f80 || most[1] >= 0x7f80;
+}
+__device__ __forceinline__ bool not_finite(const Frag<float>& f) {
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(f.v[i]) & 0x7fffffffu);
+  return most >= 0x7f800000u;
+}
+
+// An operand's depths 4 g..4 g + 3 and 16 + 4 g..16 + 4 g + 3.
+__device__ __forceinline__ Frag<bf16_t> join(const Pack<bf16_t, 4>& lo, const Pack<bf16_t, 4>& hi) {
+  struct Both {
+    Pack<bf16_t, 4> lo, hi;
+  };
+  return {__builtin_bit_cast(bf16x8, Both{lo, hi})};
+}
+__device__ __forceinline__ Frag<float> join(const Pack<float, 4>& lo, const Pack<float, 4>& hi) {
+  Frag<float> f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f.v[i] = lo.v[i], f.v[4 + i] = hi.v[i];
+  return f;
+}
+
 // Rows row0..row0+15 of an LDS tile, depths along its columns from col0.
 template <typename T>
 __device__ __forceinline__ Frag<T> rows_of(const T* tile, int stride, int row0, int col0) {
   const int l = threadIdx.x % 64;
   const T* p = tile + (row0 + l % 16) * stride + col0 + 4 * (l / 16);
-  const Pack<T, 4> lo = load_pack<T, 4>(p), hi = load_pack<T, 4>(p + 16);
-  Frag<T> f;
-  if constexpr (sizeof(T) == 2) {
-    struct Both {
-      Pack<T, 4> lo, hi;
-    };
-    f.v = __builtin_bit_cast(bf16x8, Both{lo, hi});
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f.v[i] = lo.v[i], f.v[4 + i] = hi.v[i];
-  }
-  return f;
+  return join(load_pack<T, 4>(p), load_pack<T, 4>(p + 16));
 }
 
 // Columns of an LDS tile, depths along its rows from row0.  four = the first of
@@ -172,26 +217,13 @@ __device__ __forceinline__ float pow2(double v) {
   return ldexpf(exp2_fast(float(v - n)), int(n));
 }
 
-// What two chunks of a unit do to its state.  The accumulators hold the state
-// times 2^-base: a chunk whose decays stay within 2^-kSpan of the base neither
-// scales them nor takes a power for each pair of tokens.
-constexpr double kSpan = 64.0;
-struct Span {
-  double base;    // of this chunk's tokens
-  float rescale;  // of the accumulators before the chunk
-  float keep;     // and after its outputs, for a chunk of its own (far)
-  bool far;       // its decays alone pass the span: powers for pairs of tokens
-};
-// The chunk's, with the base before it; base becomes that after it.
-__device__ __forceinline__ Span span_of(double& base, double total, double reach) {
-  Span r;
-  r.far = !(reach <= kSpan);
-  const bool fits = !r.far && fabs(base) + reach <= kSpan;
-  r.rescale = fits ? 1.f : pow2(base);
-  r.base = fits ? base : 0.0;
-  r.keep = r.far ? pow2(total) : 1.f;
-  base = r.far ? 0.0 : r.base + total;
-  return r;
+// The largest log2 by which a chunk's factors are scaled (to either side): its sums keep the
+// rest of float32's range.
+constexpr float kSpan = 64.f;
+
+// A value that all lanes have.
+__device__ __forceinline__ float uniform(float v) {
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v)));
 }
 
 // 16 bytes of a row from column col of `width`, zero past it and where !on.
@@ -219,17 +251,95 @@ struct Tile {
   static constexpr int BS = sizeof(T) == 2 ? NW + 16 : CS;
   static constexpr int XS = PW + 16 / int(sizeof(T));
   static constexpr int QT = Q / 16;
-  static constexpr int PAIRS = QT * (QT + 1) / 2;  // tiles of B . C at and below the diagonal
-  using Cum = std::conditional_t<sizeof(T) == 2, float, double>;
 
   T b[Q * BS];
   T c[Q * CS];
   T x[kWaves][Q * XS];
-  f32x4 bc[PAIRS][64];
-  // of two chunks, a token a lane (scan_chunk_kernel)
-  Cum cum[kWaves][64];
-  float step[kWaves][64], grow[kWaves][64], weight[kWaves][64];
+  f32x4 bc[kPairs][64];
+  float grow[kWaves][Q], weight[kWaves][Q];  // with the base in them
 };
+
+// Makes ws_bc and ws_decay: a wave a tile of B . C, or two chunks of a head.
+template <typename T, bool WIDE>
+__global__ __launch_bounds__(kBlock) void scan_prepare_kernel(ChunkArgs a) {
+  const co_scan_desc& d = a.c.d;
+  const co_scan_io& io = a.c.io;
+  const int lane = threadIdx.x % 64, g16 = lane / 16, l16 = lane % 16;
+  const int doubles = (a.chunks + 1) / 2;
+  const int jobs = d.heads + 2 * kPairs * d.groups;
+  const int64_t id = int64_t(blockIdx.x) * (kBlock / 64) + threadIdx.x / 64;
+  const int job = int(id % jobs);
+  const int64_t rest = id / jobs;
+  const int two = int(rest % doubles), b = int(rest / doubles);
+  if (b >= d.batch) return;
+  const int len = stream_tokens(a.c.lengths, b, a.c.T);
+  if (job >= d.heads) {
+    const int j = job - d.heads, group = j / (2 * kPairs), tile = j % kPairs;
+    const int chunk = 2 * two + j / kPairs % 2;
+    if (chunk >= a.chunks) return;
+    const int N = d.state_size;
+    // rows s of B and t of C, as depth-32 operands
+    const int64_t s = int64_t(chunk) * kChunk + 16 * (tile == 2) + l16;
+    const int64_t t = int64_t(chunk) * kChunk + 16 * (tile > 0) + l16;
+    const T* bp = static_cast<const T*>(io.b.data) + b * io.b.batch_stride + int64_t(group) * N;
+    const T* cp = static_cast<const T*>(io.c.data) + b * io.c.batch_stride + int64_t(group) * N;
+    const T* rows[2] = {bp + s * io.b.token_stride, cp + t * io.c.token_stride};
+    const bool in[2] = {s < len, t < len};
+    f32x4 acc{0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < N; k += 32) {
+      Frag<T> f[2];
+#pragma unroll
+      for (int side = 0; side < 2; ++side) {
+        Pack<T, 4> half[2] = {};
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int n = k + 16 * u + 4 * g16;
+          if (WIDE) {
+            if (in[side] && n < N) half[u] = load_pack<T, 4>(rows[side] + n);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (in[side] && n + i < N) half[u].v[i] = rows[side][n + i];
+          }
+        }
+        f[side] = join(half[0], half[1]);
+      }
+      mma(acc, f[0], f[1]);
+    }
+    a.ws_bc[(((int64_t(b) * d.groups + group) * a.chunks + chunk) * kPairs + tile) * 64 + lane] =
+        acc;
+    return;
+  }
+  const int h = job;
+  const int64_t t = int64_t(two) * 64 + lane;
+  float dt = 0.f, log_a = 0.f;
+  if (t < len) {
+    const int64_t at = b * io.dt.batch_stride + t * io.dt.token_stride + h;
+    dt = d.dt_dtype == CO_BF16 ? bf16_to_f32(static_cast<const bf16_t*>(io.dt.data)[at])
+                               : static_cast<const float*>(io.dt.data)[at];
+    if (a.c.dt_bias) dt += a.c.dt_bias[h];
+    if (d.dt_softplus) dt = softplus(dt);
+    log_a = fmaxf(dt * (a.c.A[h] * kLog2e), -160.f);
+  }
+  // 64 bits keep the differences of far sums exact
+  const double cum = prefix_sum32(double(log_a));
+  const double total = lane < 32 ? from_lane<31>(cum) : from_lane<63>(cum);
+  float reach = fabsf(float(cum));  // steps of either sign may turn the sums round
+#pragma unroll
+  for (int m = 16; m > 0; m /= 2) reach = fmaxf(reach, __shfl_xor(reach, m));
+  const int chunk = 2 * two + lane / 32, q = lane % 32;
+  if (chunk >= a.chunks) return;
+  ChunkDecay& o = a.ws_decay[(int64_t(b) * d.heads + h) * a.chunks + chunk];
+  if (q == 0) {
+    o.total = float(total);
+    o.reach = reach;
+  }
+  o.grow[q] = pow2(cum);
+  o.weight[q] = dt * pow2(reach <= kSpan ? -cum : total - cum);
+  o.step[q] = dt;
+  o.cum[q] = float(cum);
+  o.cum_low[q] = float(cum - double(float(cum)));
+}
 
 // FULL: outputs and final states; otherwise a segment's own sum and decay.
 template <typename T, int NT, int PT, bool FULL, bool WIDE>
@@ -274,7 +384,6 @@ __global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a)
   const T* bg = static_cast<const T*>(io.b.data) + b * io.b.batch_stride + int64_t(group) * N;
   const T* cg = static_cast<const T*>(io.c.data) + b * io.c.batch_stride + int64_t(group) * N;
   T* yg = static_cast<T*>(io.y.data) + b * io.y.batch_stride + int64_t(h) * P + p0;
-  const int64_t dt0 = b * io.dt.batch_stride + h;
 
   // Row r of a unit's tile pt: with two tiles a lane's 4 + 4 result rows are neighbours.
   const auto p_of = [](int pt, int r) { return PT == 2 ? 8 * (r / 4) + 4 * pt + r % 4 : r; };
@@ -286,6 +395,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a)
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
     for (int pt = 0; pt < PT; ++pt) S[nt][pt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const auto scale_state = [&](float by) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int pt = 0; pt < PT; ++pt) S[nt][pt] *= by;
+  };
   const auto each_state = [&](float* base, auto&& use) {
 #pragma unroll
     for (int pt = 0; pt < PT; ++pt) {
@@ -318,26 +433,28 @@ __global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a)
   }
   if (first) each_state(first, [](auto& mem, auto& s) { s = mem; });
 
-  const float A2 = a.c.A[h] * kLog2e, D = a.c.D ? a.c.D[h] : 0.f;
-  const float bias = a.c.dt_bias ? a.c.dt_bias[h] : 0.f;
-  double seg_log = 0.0;
+  const float D = a.c.D ? a.c.D[h] : 0.f;
+  const int64_t chunk0 = int64_t(seg) * a.seg_chunks;
+  const ChunkDecay* decay = a.ws_decay + bh * a.chunks + chunk0;
+  const f32x4* bc_at =
+      a.ws_bc + ((int64_t(b) * d.groups + group) * a.chunks + chunk0) * kPairs * 64 + tid;
 
+  // The next chunk on its way from memory.  A thread's pieces of B and C lie 256 / BC_ROW tokens
+  // apart, a lane's of x 64 / X_ROW.
   Pack<T, V> rb[BC_LOADS], rc[FULL ? BC_LOADS : 1], rx[X_LOADS];
-  uint32_t rdt = 0;  // raw: a conversion here would wait for every load in flight
-  // A thread's pieces of B and C lie 256 / BC_ROW tokens apart, a lane's of x 64 / X_ROW.
+  f32x4 rbc;
+  float rdecay, rtotal, rreach;
   constexpr int BC_BY = 256 / BC_ROW, X_BY = 64 / X_ROW;
   const int bc_row = tid / BC_ROW, bc_col = tid % BC_ROW * V;
   const int x_row = lane / X_ROW, x_col = lane % X_ROW * V;
   const T* b_at = bg + (t_begin + bc_row) * io.b.token_stride;
   const T* c_at = cg + (t_begin + bc_row) * io.c.token_stride;
   const T* x_at = xg + (t_begin + x_row) * io.x.token_stride;
-  int64_t dt_at = dt0 + (t_begin + lane) * io.dt.token_stride;
-  // the chunk from t0 on, and the steps of two chunks
-  const auto fetch = [&](int64_t t0, bool with_dt) {
-    const int left = int(min(t_end - t0, int64_t(Q))), dt_left = int(min(t_end - t0, int64_t(64)));
+  const auto fetch = [&](int64_t t0) {
+    const int left = int(min(t_end - t0, int64_t(Q)));
 #pragma unroll
     for (int i = 0; i < BC_LOADS; ++i) {
-      const bool in = bc_row + i * BC_BY < min(left, Q);
+      const bool in = bc_row + i * BC_BY < left;
       rb[i] = load_row<T, WIDE>(b_at + i * BC_BY * io.b.token_stride, bc_col, N, in);
       if (FULL) rc[i] = load_row<T, WIDE>(c_at + i * BC_BY * io.c.token_stride, bc_col, N, in);
     }
@@ -345,19 +462,21 @@ __global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a)
     for (int i = 0; i < X_LOADS; ++i)
       rx[i] = load_row<T, WIDE>(x_at + i * X_BY * io.x.token_stride, x_col, width,
                                 x_row + i * X_BY < left);
-    if (with_dt && lane < dt_left)
-      rdt = d.dt_dtype == CO_BF16 ? static_cast<const uint16_t*>(io.dt.data)[dt_at]
-                                  : static_cast<const uint32_t*>(io.dt.data)[dt_at];
+    if (FULL && tid < kPairs * 64) rbc = *bc_at;
+    const ChunkDecay& c = decay[(t0 - t_begin) / Q];
+    rdecay = c.grow[lane];  // and weight behind it
+    rtotal = c.total;
+    rreach = c.reach;
     b_at += Q * io.b.token_stride;
     c_at += Q * io.c.token_stride;
     x_at += Q * io.x.token_stride;
-    if (with_dt) dt_at += 64 * io.dt.token_stride;
+    bc_at += kPairs * 64;
   };
 
-  Span now{}, later{};  // of this chunk and the next
-  double base = 0.0;
-  int half = 0;  // of the two chunks whose decays are known
-  if (t_begin < t_end) fetch(t_begin, true);
+  // The accumulators hold the state times 2^-base: a chunk whose decays stay within kSpan of the
+  // base neither scales them nor takes a power for each pair of its tokens.
+  double base = 0.0, seg_log = 0.0;
+  if (t_begin < t_end) fetch(t_begin);
   for (int64_t t0 = t_begin; t0 < t_end; t0 += Q) {
     __syncthreads();  // the last chunk's tiles are read
 #pragma unroll
@@ -370,68 +489,30 @@ __global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a)
 #pragma unroll
     for (int i = 0; i < X_LOADS; ++i)
       store_pack<T, V>(sh.x[wave] + (x_row + i * X_BY) * L::XS + x_col, rx[i]);
-    // decays of two chunks, lane = token; 64 bits keep the differences of far sums
-    if (half == 0) {
-      const int64_t t = t0 + lane;
-      float dt = 0.f, log_a = 0.f;
-      if (t < t_end) {
-        dt = __uint_as_float(d.dt_dtype == CO_BF16 ? rdt << 16 : rdt) + bias;
-        if (d.dt_softplus) dt = softplus(dt);
-        log_a = fmaxf(dt * A2, -160.f);
-      }
-      const double cum = prefix_sum32(double(log_a));
-      const double total[2] = {from_lane<31>(cum), from_lane<63>(cum)};
-      seg_log += total[0] + total[1];
-      double reach[2] = {fabs(total[0]), fabs(total[1])};  // the furthest of the sums
-      if (!d.dt_softplus) {  // steps of either sign: the sums may turn round
-        float most = fabsf(float(cum));
-#pragma unroll
-        for (int m = 16; m > 0; m /= 2) most = fmaxf(most, __shfl_xor(most, m));
-        reach[0] = from_lane<0>(double(most));
-        reach[1] = from_lane<32>(double(most));
-      }
-      now = span_of(base, total[0], reach[0]);
-      later = span_of(base, total[1], reach[1]);
-      const bool upper = lane >= 32;
-      const double at = (upper ? later.base : now.base) + cum;
-      const bool own = upper ? later.far : now.far;
-      sh.cum[wave][lane] = typename L::Cum(cum);
-      sh.step[wave][lane] = dt;
-      sh.grow[wave][lane] = pow2(at);
-      sh.weight[wave][lane] = dt * pow2(own ? (upper ? total[1] : total[0]) - cum : -at);
-    } else {
-      now = later;
+    if (FULL && tid < kPairs * 64) sh.bc[tid / 64][lane] = rbc;
+    const float total = uniform(rtotal), reach = uniform(rreach);
+    const bool far = !(reach <= kSpan);  // its decays alone pass the span
+    if (far || !(fabs(base) + reach <= kSpan)) {
+      if (base != 0.0) scale_state(pow2(base));
+      base = 0.0;
     }
-    if (t0 + Q < t_end) fetch(t0 + Q, half == 1);  // in flight over this one's products
+    (lane < Q ? sh.grow[wave] : sh.weight[wave])[lane % Q] =
+        rdecay * pow2(lane < Q ? base : -base);
+    base = far ? 0.0 : base + total;
+    seg_log += total;
+    if (t0 + Q < t_end) fetch(t0 + Q);  // in flight over this one's products
     __syncthreads();
-    const bool far = now.far;
-    const typename L::Cum* cum_of = sh.cum[wave] + 32 * half;
-    const float* step_of = sh.step[wave] + 32 * half;
-    const float* grow_of = sh.grow[wave] + 32 * half;
-    const float* weight_of = sh.weight[wave] + 32 * half;
+
     F x[PT];
 #pragma unroll
     for (int pt = 0; pt < PT; ++pt)
       x[pt] = cols_of(sh.x[wave], L::XS, 0, x_four(pt), p_of(pt, l16));
-    if (now.rescale != 1.f) {
-      const float by = now.rescale;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int pt = 0; pt < PT; ++pt) S[nt][pt] *= by;
-    }
-
     if constexpr (FULL) {
-      // B . C, tile row by tile row among the waves: rows s, columns t
-      for (int i = wave; i < L::PAIRS; i += kWaves) {
-        const int tj = i >= 1 ? 1 : 0, si = i - tj * (tj + 1) / 2;
-        f32x4 acc{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < NK; ++k)
-          mma(acc, rows_of<T>(sh.b, L::BS, 16 * si, 32 * k),
-              rows_of<T>(sh.c, L::CS, 16 * tj, 32 * k));
-        sh.bc[i][lane] = acc;
-      }
+      const ChunkDecay& dec = decay[(t0 - t_begin) / Q];
+      const auto power = [&](int t, int s) {  // e^{cum_t - cum_s} d_s
+        return exp2_fast(dec.cum[t] - dec.cum[s] + (dec.cum_low[t] - dec.cum_low[s])) *
+               dec.step[s];
+      };
       // y^T = S C_t: rows p, columns t
       f32x4 y[L::QT][PT];
 #pragma unroll
@@ -440,109 +521,75 @@ __global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a)
         for (int pt = 0; pt < PT; ++pt) y[j][pt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < NK; ++k) {
-        F s[PT];
+        F c[L::QT];
 #pragma unroll
-        for (int pt = 0; pt < PT; ++pt)
+        for (int j = 0; j < L::QT; ++j) c[j] = rows_of<T>(sh.c, L::CS, 16 * j, 32 * k);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) set(s[pt], i, S[2 * k + i / 4][pt][i % 4]);
+        for (int pt = 0; pt < PT; ++pt) {
+          float v[8];
 #pragma unroll
-        for (int j = 0; j < L::QT; ++j) {
-          const F c = rows_of<T>(sh.c, L::CS, 16 * j, 32 * k);
+          for (int i = 0; i < 8; ++i) v[i] = S[2 * k + i / 4][pt][i % 4];
+          F s;
+          round_to(s, v);
 #pragma unroll
-          for (int pt = 0; pt < PT; ++pt) mma(y[j][pt], s[pt], c);
+          for (int j = 0; j < L::QT; ++j) mma(y[j][pt], s, c[j]);
         }
       }
       float grow[L::QT];
 #pragma unroll
-      for (int j = 0; j < L::QT; ++j) grow[j] = grow_of[16 * j + l16];
-      if (far) {
+      for (int j = 0; j < L::QT; ++j) grow[j] = sh.grow[wave][16 * j + l16];
+      // The products with masked places take 0 x_s: a NaN or an infinity among x would reach the
+      // tokens before it.  Where there is one the chunk's own part is summed token by token.
+      bool odd = false;
+#pragma unroll
+      for (int pt = 0; pt < PT; ++pt) odd |= not_finite(x[pt]);
+      odd = __any(odd);
+      if (far || odd) {
 #pragma unroll
         for (int j = 0; j < L::QT; ++j)
 #pragma unroll
           for (int pt = 0; pt < PT; ++pt) y[j][pt] *= grow[j];
+#pragma unroll
+        for (int j = 0; j < L::QT; ++j) grow[j] = 1.f;
       }
-      __syncthreads();
       // the chunk's own tokens
+      if (!odd) {
 #pragma unroll
-      for (int j = 0; j < L::QT; ++j) {
-        F m;
+        for (int j = 0; j < L::QT; ++j) {
+          float v[8] = {};
 #pragma unroll
-        for (int si = 0; si < L::QT; ++si) {
-          if (si > j) {
+          for (int si = 0; si <= j; ++si) {
+            const f32x4 bc = sh.bc[j + si][lane];
+            const int s0 = 16 * si + 4 * g16;
+            f32x4 w = *reinterpret_cast<const f32x4*>(&sh.weight[wave][s0]);
+            if (far) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) set(m, 4 * si + i, 0.f);
-            continue;
-          }
-          f32x4 v = sh.bc[j * (j + 1) / 2 + si][lane];
-          const int s0 = 16 * si + 4 * g16;
-          if (far) {
-            const typename L::Cum cum_t = cum_of[16 * j + l16];
+              for (int i = 0; i < 4; ++i) w[i] = power(16 * j + l16, s0 + i);
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              v[i] *= exp2_fast(float(cum_t - cum_of[s0 + i])) * step_of[s0 + i];
-          } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] *= weight_of[s0 + i];
+              v[4 * si + i] = si < j || 4 * g16 + i <= l16 ? w[i] * bc[i] : 0.f;
           }
+          F m;
+          round_to(m, v);
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            set(m, 4 * si + i, si < j || 4 * g16 + i <= l16 ? v[i] : 0.f);
+          for (int pt = 0; pt < PT; ++pt) mma(y[j][pt], x[pt], m);
         }
+      } else {
 #pragma unroll
-        for (int pt = 0; pt < PT; ++pt) mma(y[j][pt], x[pt], m);
-      }
-      if (!far) {
-#pragma unroll
-        for (int j = 0; j < L::QT; ++j)
-#pragma unroll
-          for (int pt = 0; pt < PT; ++pt) y[j][pt] *= grow[j];
-      }
-      // The products with masked places take 0 x_s: a NaN or an infinity among x would reach
-      // the tokens before it.  Where one shows, the chunk's own part is summed token by token.
-      float any = 0.f;
-#pragma unroll
-      for (int j = 0; j < L::QT; ++j)
-#pragma unroll
-        for (int pt = 0; pt < PT; ++pt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) any += y[j][pt][i];
-      if (__any(any != any)) {
-#pragma unroll 1
         for (int j = 0; j < L::QT; ++j) {
-          f32x4 z[PT];
-#pragma unroll
-          for (int pt = 0; pt < PT; ++pt) z[pt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int k = 0; k < NK; ++k)
-#pragma unroll
-            for (int pt = 0; pt < PT; ++pt) {
-              F s;
-#pragma unroll
-              for (int i = 0; i < 8; ++i) set(s, i, S[2 * k + i / 4][pt][i % 4]);
-              mma(z[pt], s, rows_of<T>(sh.c, L::CS, 16 * j, 32 * k));
-            }
           const int t = 16 * j + l16;
-          const float e = grow_of[t];
-#pragma unroll
-          for (int pt = 0; pt < PT; ++pt) z[pt] *= e;
-          const typename L::Cum cum_t = cum_of[t];
-          for (int s = 0; s <= 16 * j + 15; ++s) {
+#pragma unroll 1
+          for (int s = 0; s < 16 * j + 16; ++s) {
             if (s > t) continue;
-            const float bc = sh.bc[j * (j + 1) / 2 + s / 16][16 * (s % 16 / 4) + l16][s % 4];
-            const float m = exp2_fast(float(cum_t - cum_of[s])) * step_of[s] * bc;
+            const float m = power(t, s) * sh.bc[j + s / 16][16 * (s % 16 / 4) + l16][s % 4];
 #pragma unroll
             for (int pt = 0; pt < PT; ++pt)
 #pragma unroll
               for (int i = 0; i < 4; ++i)
-                z[pt][i] = fmaf(m, to_f32<T>(sh.x[wave][s * L::XS + p_of(pt, 4 * g16 + i)]),
-                                z[pt][i]);
+                y[j][pt][i] = fmaf(
+                    m, to_f32<T>(sh.x[wave][s * L::XS + p_of(pt, 4 * g16 + i)]), y[j][pt][i]);
           }
-#pragma unroll
-          for (int jj = 0; jj < L::QT; ++jj)
-            if (jj == j) {
-#pragma unroll
-              for (int pt = 0; pt < PT; ++pt) y[jj][pt] = z[pt];
-            }
         }
       }
 #pragma unroll
@@ -556,7 +603,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a)
         float out[RUN];
 #pragma unroll
         for (int i = 0; i < RUN; ++i)
-          out[i] = fmaf(D, to_f32<T>(xr[p + i]), y[j][i / 4][i % 4]);
+          out[i] = fmaf(D, to_f32<T>(xr[p + i]), y[j][i / 4][i % 4] * grow[j]);
         if (WIDE) {
           constexpr int W = RUN < V ? RUN : V;
 #pragma unroll
@@ -575,13 +622,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a)
     }
 
     // S' = e^{cum_Q} S + B^T (weighted x)
-    if (far) {
-      const float keep = now.keep;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int pt = 0; pt < PT; ++pt) S[nt][pt] *= keep;
-    }
+    if (far) scale_state(pow2(double(total)));
     constexpr int TERMS = sizeof(T) == 2 ? 3 : 1;
     F xw[PT][TERMS];
 #pragma unroll
@@ -589,7 +630,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a)
       float left[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        left[i] = get(x[pt], i) * weight_of[16 * (i / 4) + 4 * g16 + i % 4];
+        left[i] = get(x[pt], i) * sh.weight[wave][16 * (i / 4) + 4 * g16 + i % 4];
 #pragma unroll
       for (int term = 0; term < TERMS; ++term) take(xw[pt][term], left);
     }
@@ -601,15 +642,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a)
 #pragma unroll
         for (int term = TERMS - 1; term >= 0; --term) mma(S[nt][pt], bt, xw[pt][term]);
     }
-    half ^= 1;
   }
-  if (base != 0.0) {
-    const float by = pow2(base);
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int pt = 0; pt < PT; ++pt) S[nt][pt] *= by;
-  }
+  if (base != 0.0) scale_state(pow2(base));
 
   if (FULL) {
     // tokens past the stream's
@@ -621,7 +655,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a)
   } else {
     each_state(a.ws_state + ((bh * a.segments + seg) * P + p0) * N,
                [](auto& mem, auto& s) { mem = s; });
-    if (on && p0 == 0 && lane == 0) a.ws_decay[bh * a.segments + seg] = float(seg_log);
+    if (on && p0 == 0 && lane == 0) a.ws_total[bh * a.segments + seg] = float(seg_log);
   }
 }
 
@@ -632,13 +666,26 @@ __global__ __launch_bounds__(kBlock) void scan_carry_kernel(ChunkArgs a) {
   if (i >= size * a.c.d.heads * a.c.d.batch) return;
   const int64_t bh = i / size;
   float* w = a.ws_state + bh * a.segments * size + i % size;
-  const float* decay = a.ws_decay + bh * a.segments;
+  const float* total = a.ws_total + bh * a.segments;
   float s = a.c.state ? a.c.state[i] : 0.f;
-  for (int k = 0; k < a.segments; ++k) {
-    const float sum = k < a.segments - 1 ? w[k * size] : 0.f;
-    w[k * size] = s;
-    if (k < a.segments - 1) s = fmaf(exp2_fast(decay[k]), s, sum);
+  const int last = a.segments - 1;
+  constexpr int AHEAD = 8;  // loads in flight
+  for (int k0 = 0; k0 < last; k0 += AHEAD) {
+    float sum[AHEAD], decay[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int k = min(k0 + u, last - 1);
+      sum[u] = w[k * size];
+      decay[u] = total[k];
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      if (k0 + u >= last) break;
+      w[(k0 + u) * size] = s;
+      s = fmaf(exp2_fast(decay[u]), s, sum[u]);
+    }
   }
+  w[last * size] = s;
 }
 
 template <typename T, int NT, int PT, bool WIDE>
@@ -648,7 +695,10 @@ hipError_t launch_tiles(ChunkArgs a, hipStream_t s) {
   const int64_t units = int64_t(d.heads / d.groups) * a.p_blocks;
   a.unit_blocks = int32_t((units + kWaves - 1) / kWaves);
   const int64_t grid = int64_t(a.unit_blocks) * d.groups * d.batch;
-  if (!grid_fits(grid * a.segments)) return hipErrorInvalidConfiguration;
+  const int64_t jobs = int64_t(d.heads + 2 * kPairs * d.groups) * ((a.chunks + 1) / 2) * d.batch;
+  const int64_t first = (jobs + kBlock / 64 - 1) / (kBlock / 64);
+  if (!grid_fits(grid * a.segments) || !grid_fits(first)) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL((scan_prepare_kernel<T, WIDE>), dim3(unsigned(first)), dim3(kBlock), 0, s, a);
   if (a.segments > 1) {
     hipLaunchKernelGGL((scan_chunk_kernel<T, NT, PT, false, WIDE>),
                        dim3(unsigned(grid * a.segments)), dim3(kWaves * 64), 0, s, a);
@@ -691,7 +741,7 @@ hipError_t launch_t(const ChunkArgs& a, hipStream_t s) {
 // Segments of a call over T tokens, and their chunks: enough to give each of
 // 256 CUs two workgroups, of four chunks at least.
 void cut(const co_scan_desc& d, int64_t T, int64_t* segments, int64_t* seg_chunks) {
-  const int64_t Q = kChunk, chunks = (T + Q - 1) / Q;
+  const int64_t chunks = (T + kChunk - 1) / kChunk;
   const int64_t pw = d.state_size <= 128 ? 32 : 16;
   const int64_t units = int64_t(d.heads / d.groups) * ((d.head_dim + pw - 1) / pw);
   const int64_t groups = (units + kWaves - 1) / kWaves * d.groups * d.batch;
@@ -702,6 +752,20 @@ void cut(const co_scan_desc& d, int64_t T, int64_t* segments, int64_t* seg_chunk
   *segments = (chunks + *seg_chunks - 1) / *seg_chunks;
 }
 
+// Where each part of the workspace lies, in bytes (all multiples of 16 but the last).
+struct Space {
+  int64_t decay, state, total, bytes;
+};
+Space space_of(const co_scan_desc& d, int64_t chunks, int64_t segments) {
+  const int64_t bh = int64_t(d.batch) * d.heads;
+  Space s;
+  s.decay = int64_t(d.batch) * d.groups * chunks * kPairs * 64 * int64_t(sizeof(f32x4));
+  s.state = s.decay + bh * chunks * int64_t(sizeof(ChunkDecay));
+  s.total = s.state + (segments > 1 ? bh * segments * d.head_dim * d.state_size * 4 : 0);
+  s.bytes = s.total + (segments > 1 ? bh * segments * 4 : 0);
+  return s;
+}
+
 }  // namespace
 
 bool scan_chunk_takes(const co_scan_desc& d, int32_t T) { return T >= 16; }
@@ -709,28 +773,24 @@ bool scan_chunk_takes(const co_scan_desc& d, int32_t T) { return T >= 16; }
 int64_t scan_chunk_workspace(const co_scan_desc& d, int32_t T) {
   int64_t segments, seg_chunks;
   cut(d, T, &segments, &seg_chunks);
-  if (segments < 2) return 0;
-  const int64_t bh = int64_t(d.batch) * d.heads;
-  return bh * segments * (int64_t(d.head_dim) * d.state_size + 1) * 4;
+  return space_of(d, (int64_t(T) + kChunk - 1) / kChunk, segments).bytes;
 }
 
-hipError_t launch_scan_chunk(const ScanCall& c, void* workspace, int64_t workspace_bytes,
-                             hipStream_t stream) {
+hipError_t launch_scan_chunk(const ScanCall& c, void* workspace, hipStream_t stream) {
   int64_t segments, seg_chunks;
   cut(c.d, c.T, &segments, &seg_chunks);
-  if (segments > 1 && (!workspace || workspace_bytes < scan_chunk_workspace(c.d, c.T))) {
-    segments = 1;
-    seg_chunks = (c.T + kChunk - 1) / kChunk;
-  }
+  const int64_t chunks = (int64_t(c.T) + kChunk - 1) / kChunk;
+  const Space at = space_of(c.d, chunks, segments);
+  char* w = static_cast<char*>(workspace);
   ChunkArgs a{};
   a.c = c;
+  a.ws_bc = reinterpret_cast<f32x4*>(w);
+  a.ws_decay = reinterpret_cast<ChunkDecay*>(w + at.decay);
+  a.ws_state = reinterpret_cast<float*>(w + at.state);
+  a.ws_total = reinterpret_cast<float*>(w + at.total);
+  a.chunks = int32_t(chunks);
   a.segments = int32_t(segments);
   a.seg_chunks = int32_t(seg_chunks);
-  if (segments > 1) {
-    a.ws_state = static_cast<float*>(workspace);
-    a.ws_decay = a.ws_state + int64_t(c.d.batch) * c.d.heads * segments * c.d.head_dim *
-                                  c.d.state_size;
-  }
   if (c.d.dtype == CO_BF16) return launch_t<bf16_t>(a, stream);
   return launch_t<float>(a, stream);
 }

@@ -125,12 +125,13 @@ co_status co_scan_forward_steps(const co_scan_desc* desc, const float* A, const 
       io->y.data == io->dt.data)
     return CO_EINVAL;
   if (!aligned(A, 4) || !aligned(D, 4) || !aligned(dt_bias, 4) || !aligned(state, 4) ||
-      !aligned(lengths, 4) || !aligned(workspace, 4))
+      !aligned(lengths, 4) || !aligned(workspace, 16))
     return CO_EINVAL;
   if (mul_to(mul_to(B, inner, kMaxValues), T, kMaxValues) < 0) return CO_EINVAL;
   ScanCall c{*desc, *io, A, D, dt_bias, lengths, state, T, update_state && state ? 1 : 0};
-  if (scan_chunk_takes(*desc, T))
-    return done(launch_scan_chunk(c, workspace, workspace_bytes, as_stream(stream)));
+  if (scan_chunk_takes(*desc, T) && workspace &&
+      workspace_bytes >= scan_chunk_workspace(*desc, T))
+    return done(launch_scan_chunk(c, workspace, as_stream(stream)));
   return done(launch_scan_seq(c, as_stream(stream)));
 }
 
