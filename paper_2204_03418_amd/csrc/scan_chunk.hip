@@ -49,8 +49,8 @@ struct ChunkDecay {
   float pad[2];
   float grow[kChunk];    // 2^{cum_t}
   float weight[kChunk];  // 2^{-cum_t} d_t, or 2^{total - cum_t} d_t where the reach passes kSpan
-  float step[kChunk];    // d_t
-  float cum[kChunk], cum_low[kChunk];  // cum_t = cum + cum_low
+  // where the reach passes kSpan: d_t, and cum_t = cum + cum_low
+  float step[kChunk], cum[kChunk], cum_low[kChunk];
 };
 static_assert(sizeof(ChunkDecay) % 16 == 0);
 
@@ -140,6 +140,21 @@ __device__ __forceinline__ bool not_finite(const Frag<float>& f) {
   return most >= 0x7f800000u;
 }
 
+// Puts 0 in the place of the values that are not finite, and in `bad` 1 for each of them.
+template <typename T>
+__device__ __forceinline__ void part_finite(Frag<T>& f, Frag<T>& bad) {
+  float keep[8], out[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float v = get(f, i);
+    const bool fine = fabsf(v) < __builtin_inff();
+    keep[i] = fine ? v : 0.f;
+    out[i] = fine ? 0.f : 1.f;
+  }
+  round_to(f, keep);
+  round_to(bad, out);
+}
+
 // An operand's depths 4 g..4 g + 3 and 16 + 4 g..16 + 4 g + 3.
 __device__ __forceinline__ Frag<bf16_t> join(const Pack<bf16_t, 4>& lo, const Pack<bf16_t, 4>& hi) {
   struct Both {
@@ -226,19 +241,32 @@ __device__ __forceinline__ float uniform(float v) {
   return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v)));
 }
 
-// 16 bytes of a row from column col of `width`, zero past it and where !on.
-template <typename T, bool WIDE>
+// kWide values of a row from column col of `width`, zero past it and where !on.
+template <typename T>
 __device__ __forceinline__ Pack<T, kWide<T>> load_row(const T* row, int col, int width, bool on) {
-  constexpr int V = kWide<T>;
-  Pack<T, V> r{};
-  if (WIDE) {
-    if (on && col < width) r = load_pack<T, V>(row + col);
-  } else if (on) {
+  Pack<T, kWide<T>> r{};
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (col + i < width) r.v[i] = row[col + i];
-  }
+  for (int i = 0; i < kWide<T>; ++i)
+    if (on && col + i < width) r.v[i] = row[col + i];
   return r;
+}
+// The same 16 bytes wide, zero out of the buffer's range.
+template <typename T>
+__device__ __forceinline__ Pack<T, kWide<T>> load_pack_at(__amdgpu_buffer_rsrc_t r, int voff,
+                                                          int soff) {
+  return __builtin_bit_cast(Pack<T, kWide<T>>,
+                            __builtin_amdgcn_raw_buffer_load_b128(r, voff, soff, 0));
+}
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <typename T, int W>
+__device__ __forceinline__ void store_pack_at(__amdgpu_buffer_rsrc_t r, int voff,
+                                              const Pack<T, W>& v) {
+  if constexpr (sizeof(v) == 16)
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, voff, 0, 0);
+  else
+    __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), r, voff, 0, 0);
 }
 
 template <typename T, int NT, int PT>
@@ -265,13 +293,11 @@ __global__ __launch_bounds__(kBlock) void scan_prepare_kernel(ChunkArgs a) {
   const co_scan_desc& d = a.c.d;
   const co_scan_io& io = a.c.io;
   const int lane = threadIdx.x % 64, g16 = lane / 16, l16 = lane % 16;
-  const int doubles = (a.chunks + 1) / 2;
-  const int jobs = d.heads + 2 * kPairs * d.groups;
-  const int64_t id = int64_t(blockIdx.x) * (kBlock / 64) + threadIdx.x / 64;
-  const int job = int(id % jobs);
-  const int64_t rest = id / jobs;
-  const int two = int(rest % doubles), b = int(rest / doubles);
-  if (b >= d.batch) return;
+  const uint32_t doubles = uint32_t(a.chunks + 1) / 2;
+  const int two = int(blockIdx.x % doubles), b = int(blockIdx.x / doubles);
+  const int job = int(blockIdx.y) * (kBlock / 64) +
+                  __builtin_amdgcn_readfirstlane(int(threadIdx.x / 64));
+  if (job >= d.heads + 2 * kPairs * d.groups) return;
   const int len = stream_tokens(a.c.lengths, b, a.c.T);
   if (job >= d.heads) {
     const int j = job - d.heads, group = j / (2 * kPairs), tile = j % kPairs;
@@ -336,6 +362,7 @@ __global__ __launch_bounds__(kBlock) void scan_prepare_kernel(ChunkArgs a) {
   }
   o.grow[q] = pow2(cum);
   o.weight[q] = dt * pow2(reach <= kSpan ? -cum : total - cum);
+  if (reach <= kSpan) return;  // what follows is for the chunks that go far
   o.step[q] = dt;
   o.cum[q] = float(cum);
   o.cum_low[q] = float(cum - double(float(cum)));
@@ -343,7 +370,7 @@ __global__ __launch_bounds__(kBlock) void scan_prepare_kernel(ChunkArgs a) {
 
 // FULL: outputs and final states; otherwise a segment's own sum and decay.
 template <typename T, int NT, int PT, bool FULL, bool WIDE>
-__global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a) {
+__global__ __launch_bounds__(kWaves * 64, !FULL && sizeof(T) == 2 ? 3 : 2) void scan_chunk_kernel(ChunkArgs a) {
   using L = Tile<T, NT, PT>;
   using F = Frag<T>;
   constexpr int Q = L::Q, V = kWide<T>;
@@ -356,7 +383,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a)
 
   const co_scan_desc& d = a.c.d;
   const co_scan_io& io = a.c.io;
-  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  const int tid = threadIdx.x, lane = tid % 64;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int g16 = lane / 16, l16 = lane % 16;
   const int per_group = d.heads / d.groups;
   const int P = d.head_dim, N = d.state_size;
@@ -437,7 +465,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a)
   const int64_t chunk0 = int64_t(seg) * a.seg_chunks;
   const ChunkDecay* decay = a.ws_decay + bh * a.chunks + chunk0;
   const f32x4* bc_at =
-      a.ws_bc + ((int64_t(b) * d.groups + group) * a.chunks + chunk0) * kPairs * 64 + tid;
+      a.ws_bc + ((int64_t(b) * d.groups + group) * a.chunks + chunk0) * kPairs * 64;
 
   // The next chunk on its way from memory.  A thread's pieces of B and C lie 256 / BC_ROW tokens
   // apart, a lane's of x 64 / X_ROW.
@@ -447,22 +475,41 @@ __global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a)
   constexpr int BC_BY = 256 / BC_ROW, X_BY = 64 / X_ROW;
   const int bc_row = tid / BC_ROW, bc_col = tid % BC_ROW * V;
   const int x_row = lane / X_ROW, x_col = lane % X_ROW * V;
-  const T* b_at = bg + (t_begin + bc_row) * io.b.token_stride;
-  const T* c_at = cg + (t_begin + bc_row) * io.c.token_stride;
-  const T* x_at = xg + (t_begin + x_row) * io.x.token_stride;
+  // this thread's places in a chunk: bytes from its first token, or out of range
+  const int es = sizeof(T);
+  const int bc_off = bc_col < N ? (bc_row * int(io.b.token_stride) + bc_col) * es : kOutOfRange;
+  const int c_off = bc_col < N ? (bc_row * int(io.c.token_stride) + bc_col) * es : kOutOfRange;
+  const int x_off = x_col < width ? (x_row * int(io.x.token_stride) + x_col) * es : kOutOfRange;
+  const T* b_at = bg + t_begin * io.b.token_stride;
+  const T* c_at = cg + t_begin * io.c.token_stride;
+  const T* x_at = xg + t_begin * io.x.token_stride;
   const auto fetch = [&](int64_t t0) {
     const int left = int(min(t_end - t0, int64_t(Q)));
+    const __amdgpu_buffer_rsrc_t br = make_rsrc(b_at, kOutOfRange), cr = make_rsrc(c_at, kOutOfRange),
+                                 xr = make_rsrc(x_at, kOutOfRange);
 #pragma unroll
     for (int i = 0; i < BC_LOADS; ++i) {
-      const bool in = bc_row + i * BC_BY < left;
-      rb[i] = load_row<T, WIDE>(b_at + i * BC_BY * io.b.token_stride, bc_col, N, in);
-      if (FULL) rc[i] = load_row<T, WIDE>(c_at + i * BC_BY * io.c.token_stride, bc_col, N, in);
+      const int row = bc_row + i * BC_BY;
+      if (WIDE) {
+        const bool in = row < left;
+        rb[i] = load_pack_at<T>(br, in ? bc_off : kOutOfRange, i * BC_BY * int(io.b.token_stride) * es);
+        if (FULL)
+          rc[i] = load_pack_at<T>(cr, in ? c_off : kOutOfRange, i * BC_BY * int(io.c.token_stride) * es);
+      } else {
+        rb[i] = load_row<T>(b_at + row * io.b.token_stride, bc_col, N, row < left);
+        if (FULL) rc[i] = load_row<T>(c_at + row * io.c.token_stride, bc_col, N, row < left);
+      }
     }
 #pragma unroll
-    for (int i = 0; i < X_LOADS; ++i)
-      rx[i] = load_row<T, WIDE>(x_at + i * X_BY * io.x.token_stride, x_col, width,
-                                x_row + i * X_BY < left);
-    if (FULL && tid < kPairs * 64) rbc = *bc_at;
+    for (int i = 0; i < X_LOADS; ++i) {
+      const int row = x_row + i * X_BY;
+      if (WIDE)
+        rx[i] = load_pack_at<T>(xr, row < left ? x_off : kOutOfRange,
+                                i * X_BY * int(io.x.token_stride) * es);
+      else
+        rx[i] = load_row<T>(x_at + row * io.x.token_stride, x_col, width, row < left);
+    }
+    if (FULL) rbc = bc_at[min(tid, kPairs * 64 - 1)];
     const ChunkDecay& c = decay[(t0 - t_begin) / Q];
     rdecay = c.grow[lane];  // and weight behind it
     rtotal = c.total;
@@ -489,7 +536,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a)
 #pragma unroll
     for (int i = 0; i < X_LOADS; ++i)
       store_pack<T, V>(sh.x[wave] + (x_row + i * X_BY) * L::XS + x_col, rx[i]);
-    if (FULL && tid < kPairs * 64) sh.bc[tid / 64][lane] = rbc;
+    if (FULL && wave < kPairs) sh.bc[wave][lane] = rbc;
     const float total = uniform(rtotal), reach = uniform(rreach);
     const bool far = !(reach <= kSpan);  // its decays alone pass the span
     if (far || !(fabs(base) + reach <= kSpan)) {
@@ -508,11 +555,6 @@ __global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a)
     for (int pt = 0; pt < PT; ++pt)
       x[pt] = cols_of(sh.x[wave], L::XS, 0, x_four(pt), p_of(pt, l16));
     if constexpr (FULL) {
-      const ChunkDecay& dec = decay[(t0 - t_begin) / Q];
-      const auto power = [&](int t, int s) {  // e^{cum_t - cum_s} d_s
-        return exp2_fast(dec.cum[t] - dec.cum[s] + (dec.cum_low[t] - dec.cum_low[s])) *
-               dec.step[s];
-      };
       // y^T = S C_t: rows p, columns t
       f32x4 y[L::QT][PT];
 #pragma unroll
@@ -538,66 +580,82 @@ __global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a)
       float grow[L::QT];
 #pragma unroll
       for (int j = 0; j < L::QT; ++j) grow[j] = sh.grow[wave][16 * j + l16];
-      // The products with masked places take 0 x_s: a NaN or an infinity among x would reach the
-      // tokens before it.  Where there is one the chunk's own part is summed token by token.
+      // the chunk's own tokens: e^{cum_t - cum_s} d_s, but for what y is scaled by in the end
+      f32x4 w[kPairs];
+      w[0] = w[1] = *reinterpret_cast<const f32x4*>(&sh.weight[wave][4 * g16]);
+      w[2] = *reinterpret_cast<const f32x4*>(&sh.weight[wave][16 + 4 * g16]);
+      if (far) {
+        const ChunkDecay& c = decay[(t0 - t_begin) / Q];
+#pragma unroll
+        for (int j = 0; j < L::QT; ++j) {
+          const float cum = c.cum[16 * j + l16], low = c.cum_low[16 * j + l16];
+#pragma unroll
+          for (int si = 0; si <= j; ++si) {
+            const int s0 = 16 * si + 4 * g16;
+            const f32x4 cs = *reinterpret_cast<const f32x4*>(&c.cum[s0]);
+            const f32x4 ls = *reinterpret_cast<const f32x4*>(&c.cum_low[s0]);
+            const f32x4 ds = *reinterpret_cast<const f32x4*>(&c.step[s0]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              w[j + si][i] = exp2_fast((cum - cs[i]) + (low - ls[i])) * ds[i];
+          }
+#pragma unroll
+          for (int pt = 0; pt < PT; ++pt) y[j][pt] *= grow[j];
+          grow[j] = 1.f;
+        }
+        scale_state(pow2(double(total)));
+      }
+      // The product takes 0 x_s for s > t: a NaN or an infinity among x would reach the tokens
+      // before it.  Where there is one the product does without it, and NaN goes to its places.
       bool odd = false;
 #pragma unroll
       for (int pt = 0; pt < PT; ++pt) odd |= not_finite(x[pt]);
       odd = __any(odd);
-      if (far || odd) {
+      F bad[PT];
+      if (odd) {
 #pragma unroll
-        for (int j = 0; j < L::QT; ++j)
-#pragma unroll
-          for (int pt = 0; pt < PT; ++pt) y[j][pt] *= grow[j];
-#pragma unroll
-        for (int j = 0; j < L::QT; ++j) grow[j] = 1.f;
-      }
-      // the chunk's own tokens
-      if (!odd) {
-#pragma unroll
-        for (int j = 0; j < L::QT; ++j) {
-          float v[8] = {};
-#pragma unroll
-          for (int si = 0; si <= j; ++si) {
-            const f32x4 bc = sh.bc[j + si][lane];
-            const int s0 = 16 * si + 4 * g16;
-            f32x4 w = *reinterpret_cast<const f32x4*>(&sh.weight[wave][s0]);
-            if (far) {
-#pragma unroll
-              for (int i = 0; i < 4; ++i) w[i] = power(16 * j + l16, s0 + i);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              v[4 * si + i] = si < j || 4 * g16 + i <= l16 ? w[i] * bc[i] : 0.f;
-          }
-          F m;
-          round_to(m, v);
-#pragma unroll
-          for (int pt = 0; pt < PT; ++pt) mma(y[j][pt], x[pt], m);
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < L::QT; ++j) {
-          const int t = 16 * j + l16;
-#pragma unroll 1
-          for (int s = 0; s < 16 * j + 16; ++s) {
-            if (s > t) continue;
-            const float m = power(t, s) * sh.bc[j + s / 16][16 * (s % 16 / 4) + l16][s % 4];
-#pragma unroll
-            for (int pt = 0; pt < PT; ++pt)
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                y[j][pt][i] = fmaf(
-                    m, to_f32<T>(sh.x[wave][s * L::XS + p_of(pt, 4 * g16 + i)]), y[j][pt][i]);
-          }
-        }
+        for (int pt = 0; pt < PT; ++pt) part_finite(x[pt], bad[pt]);
       }
 #pragma unroll
       for (int j = 0; j < L::QT; ++j) {
-        const int64_t t = t0 + 16 * j + l16;
-        if (t >= t_stop) continue;
-        T* row = yg + t * io.y.token_stride;
-        const T* xr = sh.x[wave] + (16 * j + l16) * L::XS;
+        float v[8] = {}, one[8] = {};
+#pragma unroll
+        for (int si = 0; si <= j; ++si) {
+          const f32x4 bc = sh.bc[j + si][lane];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const bool seen = si < j || 4 * g16 + i <= l16;
+            v[4 * si + i] = seen ? w[j + si][i] * bc[i] : 0.f;
+            one[4 * si + i] = seen ? 1.f : 0.f;
+          }
+        }
+        F m;
+        round_to(m, v);
+#pragma unroll
+        for (int pt = 0; pt < PT; ++pt) mma(y[j][pt], x[pt], m);
+        if (odd) {
+          round_to(m, one);
+#pragma unroll
+          for (int pt = 0; pt < PT; ++pt) {
+            f32x4 count{0.f, 0.f, 0.f, 0.f};
+            mma(count, bad[pt], m);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (count[i] > 0.f) y[j][pt][i] = __builtin_nanf("");
+          }
+        }
+      }
+      if (odd) {
+#pragma unroll
+        for (int pt = 0; pt < PT; ++pt)
+          x[pt] = cols_of(sh.x[wave], L::XS, 0, x_four(pt), p_of(pt, l16));
+      }
+      const __amdgpu_buffer_rsrc_t yr = make_rsrc(yg + t0 * io.y.token_stride, kOutOfRange);
+      const int rows_left = int(min(t_stop - t0, int64_t(Q)));
+#pragma unroll
+      for (int j = 0; j < L::QT; ++j) {
+        const int r = 16 * j + l16;
+        const T* xr = sh.x[wave] + r * L::XS;
         constexpr int RUN = PT * 4;  // neighbours of this lane
         const int p = RUN * g16;
         float out[RUN];
@@ -611,18 +669,21 @@ __global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a)
             Pack<T, W> o;
 #pragma unroll
             for (int i = 0; i < W; ++i) o.v[i] = from_f32<T>(out[q + i]);
-            if (p + q < width) store_pack<T, W>(row + p + q, o);
+            const bool in = r < rows_left && p + q < width;
+            store_pack_at<T, W>(yr, in ? (r * int(io.y.token_stride) + p + q) * es : kOutOfRange, o);
           }
         } else {
+          T* row = yg + (t0 + r) * io.y.token_stride;
 #pragma unroll
           for (int i = 0; i < RUN; ++i)
-            if (p + i < width) row[p + i] = from_f32<T>(out[i]);
+            if (r < rows_left && p + i < width) row[p + i] = from_f32<T>(out[i]);
         }
       }
+    } else {
+      if (far) scale_state(pow2(double(total)));
     }
 
     // S' = e^{cum_Q} S + B^T (weighted x)
-    if (far) scale_state(pow2(double(total)));
     constexpr int TERMS = sizeof(T) == 2 ? 3 : 1;
     F xw[PT][TERMS];
 #pragma unroll
@@ -659,33 +720,35 @@ __global__ __launch_bounds__(kWaves * 64, 2) void scan_chunk_kernel(ChunkArgs a)
   }
 }
 
-// Turns the segments' sums into the states that they begin with.
-__global__ __launch_bounds__(kBlock) void scan_carry_kernel(ChunkArgs a) {
+// Turns the segments' sums into the states that they begin with, V values a thread.
+template <int V>
+__global__ __launch_bounds__(kBlock) void scan_carry_kernel(ChunkArgs a, uint32_t head_blocks) {
+  using P = Pack<float, V>;
   const int64_t size = int64_t(a.c.d.head_dim) * a.c.d.state_size;
-  const int64_t i = int64_t(blockIdx.x) * kBlock + threadIdx.x;
-  if (i >= size * a.c.d.heads * a.c.d.batch) return;
-  const int64_t bh = i / size;
-  float* w = a.ws_state + bh * a.segments * size + i % size;
+  const int64_t bh = blockIdx.x / head_blocks;
+  const int64_t i = (int64_t(blockIdx.x % head_blocks) * kBlock + threadIdx.x) * V;
+  if (i >= size) return;
+  float* w = a.ws_state + bh * a.segments * size + i;
   const float* total = a.ws_total + bh * a.segments;
-  float s = a.c.state ? a.c.state[i] : 0.f;
+  P s{};
+  if (a.c.state) s = load_pack<float, V>(a.c.state + bh * size + i);
   const int last = a.segments - 1;
   constexpr int AHEAD = 8;  // loads in flight
   for (int k0 = 0; k0 < last; k0 += AHEAD) {
-    float sum[AHEAD], decay[AHEAD];
+    P sum[AHEAD];
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      const int k = min(k0 + u, last - 1);
-      sum[u] = w[k * size];
-      decay[u] = total[k];
-    }
+    for (int u = 0; u < AHEAD; ++u)
+      if (k0 + u < last) sum[u] = load_pack<float, V>(w + (k0 + u) * size);
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      if (k0 + u >= last) break;
-      w[(k0 + u) * size] = s;
-      s = fmaf(exp2_fast(decay[u]), s, sum[u]);
-    }
+    for (int u = 0; u < AHEAD; ++u)
+      if (k0 + u < last) {
+        store_pack<float, V>(w + (k0 + u) * size, s);
+        const float decay = exp2_fast(total[k0 + u]);
+#pragma unroll
+        for (int v = 0; v < V; ++v) s.v[v] = fmaf(decay, s.v[v], sum[u].v[v]);
+      }
   }
-  w[last * size] = s;
+  store_pack<float, V>(w + last * size, s);
 }
 
 template <typename T, int NT, int PT, bool WIDE>
@@ -695,17 +758,21 @@ hipError_t launch_tiles(ChunkArgs a, hipStream_t s) {
   const int64_t units = int64_t(d.heads / d.groups) * a.p_blocks;
   a.unit_blocks = int32_t((units + kWaves - 1) / kWaves);
   const int64_t grid = int64_t(a.unit_blocks) * d.groups * d.batch;
-  const int64_t jobs = int64_t(d.heads + 2 * kPairs * d.groups) * ((a.chunks + 1) / 2) * d.batch;
-  const int64_t first = (jobs + kBlock / 64 - 1) / (kBlock / 64);
-  if (!grid_fits(grid * a.segments) || !grid_fits(first)) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL((scan_prepare_kernel<T, WIDE>), dim3(unsigned(first)), dim3(kBlock), 0, s, a);
+  const int64_t jobs = (int64_t(d.heads) + 2 * kPairs * d.groups + kBlock / 64 - 1) / (kBlock / 64);
+  const int64_t doubles = (int64_t(a.chunks) + 1) / 2 * d.batch;
+  constexpr int CV = WIDE ? 4 : 1;  // a state row is then whole pieces of 16 bytes
+  const int64_t head_blocks =
+      (int64_t(d.head_dim) * d.state_size + CV * kBlock - 1) / (CV * kBlock);
+  if (!grid_fits(grid * a.segments) || !grid_fits(doubles * jobs) || jobs > 65535 ||
+      !grid_fits(head_blocks * d.batch * d.heads))
+    return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL((scan_prepare_kernel<T, WIDE>), dim3(unsigned(doubles), unsigned(jobs)),
+                     dim3(kBlock), 0, s, a);
   if (a.segments > 1) {
     hipLaunchKernelGGL((scan_chunk_kernel<T, NT, PT, false, WIDE>),
                        dim3(unsigned(grid * a.segments)), dim3(kWaves * 64), 0, s, a);
-    const int64_t values = int64_t(d.batch) * d.heads * d.head_dim * d.state_size;
-    const int64_t blocks = (values + kBlock - 1) / kBlock;
-    if (!grid_fits(blocks)) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL(scan_carry_kernel, dim3(unsigned(blocks)), dim3(kBlock), 0, s, a);
+    hipLaunchKernelGGL(scan_carry_kernel<CV>, dim3(unsigned(head_blocks * d.batch * d.heads)),
+                       dim3(kBlock), 0, s, a, uint32_t(head_blocks));
   }
   hipLaunchKernelGGL((scan_chunk_kernel<T, NT, PT, true, WIDE>), dim3(unsigned(grid * a.segments)),
                      dim3(kWaves * 64), 0, s, a);
@@ -727,10 +794,11 @@ hipError_t launch_t(const ChunkArgs& a, hipStream_t s) {
   constexpr int V = kWide<T>;
   const auto wide = [](const co_tokens& t) {
     return reinterpret_cast<uintptr_t>(t.data) % 16 == 0 && t.batch_stride % V == 0 &&
-           t.token_stride % V == 0;
+           t.token_stride % V == 0 && t.token_stride < (1 << 22);
   };
   const co_scan_io& io = a.c.io;
-  // 16-byte accesses where every one of them is aligned, values otherwise
+  // 16-byte accesses where every one of them is aligned and a chunk's offsets take 31 bits, values
+  // otherwise
   const bool fits = a.c.d.head_dim % V == 0 && a.c.d.state_size % V == 0 && wide(io.x) &&
                     wide(io.b) && wide(io.c) && wide(io.y) &&
                     reinterpret_cast<uintptr_t>(a.c.state) % 16 == 0 &&
