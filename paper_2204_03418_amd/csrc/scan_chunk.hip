@@ -806,17 +806,28 @@ hipError_t launch_t(const ChunkArgs& a, hipStream_t s) {
   return fits ? launch_state<T, true>(a, s) : launch_state<T, false>(a, s);
 }
 
-// Segments of a call over T tokens, and their chunks: enough to give each of
-// 256 CUs two workgroups, of four chunks at least.
+// Segments of a call over T tokens, and their chunks: the cut that is estimated to be fastest.
+// In units of a chunk's time in a workgroup that has its CU alone (2.8 us, 64 heads of 64 x 128,
+// bfloat16), two on a CU take 1.5 (4.2 us); a segment's own sum takes 0.55 of the whole (75 of
+// 135 us), and carrying the states a launch and their bytes.  Unsplit, 256 workgroups of 32
+// chunks took 73 us where two segments took 89; 32 workgroups of 512 chunks cut 8, 16 and 24
+// times 300, 240 and 263.
 void cut(const co_scan_desc& d, int64_t T, int64_t* segments, int64_t* seg_chunks) {
   const int64_t chunks = (T + kChunk - 1) / kChunk;
   const int64_t pw = d.state_size <= 128 ? 32 : 16;
   const int64_t units = int64_t(d.heads / d.groups) * ((d.head_dim + pw - 1) / pw);
   const int64_t groups = (units + kWaves - 1) / kWaves * d.groups * d.batch;
-  int64_t n = (512 + groups - 1) / groups;
-  n = n < chunks / 4 ? n : chunks / 4;
-  if (n < 1) n = 1;
-  *seg_chunks = (chunks + n - 1) / n;
+  const double states = double(d.batch) * d.heads * d.head_dim * d.state_size;
+  const auto cost = [&](int64_t n) {
+    const double wgs = double(groups) * double(n);
+    const double load = wgs <= 256 ? 1.0 : wgs <= 512 ? 1.5 : 1.5 * wgs / 512;
+    const double pass = load * double((chunks + n - 1) / n);
+    return n == 1 ? pass : 1.55 * pass + 2.0 + states * double(n) * 8 / 12e6;
+  };
+  int64_t best = 1;
+  for (int64_t n = 2; n <= chunks / 4 && n <= 64; n += n < 8 ? 1 : n < 16 ? 2 : 8)
+    if (cost(n) < cost(best)) best = n;
+  *seg_chunks = (chunks + best - 1) / best;
   *segments = (chunks + *seg_chunks - 1) / *seg_chunks;
 }
 
