@@ -815,7 +815,7 @@ co_status co_scan_forward_steps(const co_scan_desc* desc, const float* A, const 
                                 void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
- * Root-mean-square norm over `groups` equal parts of each row of dim values,
+ * Root-mean-square norm over `groups` equal parts of each token's dim values,
  * fused with a gate z and a residual sum.  With n(v) = v / sqrt(mean(v^2) + eps)
  * over each part and silu(z) = z / (1 + exp(-z)):
  *   a = x, or x silu(z)                     gate CO_NORM_BEFORE
@@ -833,7 +833,8 @@ co_status co_scan_forward_steps(const co_scan_desc* desc, const float* A, const 
 #define CO_NORM_AFTER   2
 
 typedef struct co_norm_desc {
-  int64_t rows;
+  int32_t batch;                  /* >= 0; batch tokens groups < 2^31 */
+  int32_t tokens;                 /* >= 0 */
   int32_t dim;
   int32_t groups;                 /* divides dim, dim / groups <= CO_NORM_MAX_WIDTH */
   int32_t gate;                   /* CO_NORM_* */
@@ -843,15 +844,9 @@ typedef struct co_norm_desc {
   float   eps;                    /* >= 0 */
 } co_norm_desc;
 
-/* Rows of contiguous values, row_stride elements apart. */
-typedef struct co_rows {
-  void*   data;
-  int64_t row_stride;             /* elements, >= 0 */
-} co_rows;
-
-co_status co_norm_forward(const co_norm_desc* desc, const co_rows* x, const co_rows* gate,
-                          const co_rows* residual, const float* weight, const float* scale,
-                          const co_rows* y, const co_rows* residual_out, void* stream);
+co_status co_norm_forward(const co_norm_desc* desc, const co_tokens* x, const co_tokens* gate,
+                          const co_tokens* residual, const float* weight, const float* scale,
+                          const co_tokens* y, const co_tokens* residual_out, void* stream);
 
 #ifdef __cplusplus
 }

@@ -268,8 +268,8 @@ bool scan_chunk_takes(const co_scan_desc& d, int32_t T);
 int64_t scan_chunk_workspace(const co_scan_desc& d, int32_t T);
 hipError_t launch_scan_chunk(const ScanCall& c, void* workspace, hipStream_t stream);
 
-hipError_t launch_norm(const co_norm_desc& d, const co_rows& x, const co_rows& gate,
-                       const co_rows& residual, const float* weight, const float* scale,
-                       const co_rows& y, const co_rows& residual_out, hipStream_t stream);
+hipError_t launch_norm(const co_norm_desc& d, const co_tokens& x, const co_tokens& gate,
+                       const co_tokens& residual, const float* weight, const float* scale,
+                       const co_tokens& y, const co_tokens& residual_out, hipStream_t stream);
 
 }  // namespace coinf

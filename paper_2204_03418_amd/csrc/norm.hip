@@ -13,18 +13,19 @@ namespace coinf {
 namespace {
 
 struct NormArgs {
-  const void* x;
-  const void* z;
-  const void* r;
+  co_tokens x, z, r, y, o;  // o: the new residual
   const float* weight;
   const float* scale;
-  void* y;
-  void* r_out;
-  int64_t x_row, z_row, r_row, y_row, o_row;
-  int64_t parts;  // rows * groups
-  int32_t groups, width;
+  uint32_t parts;  // tokens of all streams * groups
+  uint32_t groups, tokens;
+  int32_t width;
   float eps;
 };
+
+// Where a tensor has token t of stream b.
+__device__ __forceinline__ int64_t place(const co_tokens& v, uint32_t b, uint32_t t) {
+  return b * v.batch_stride + t * v.token_stride;
+}
 
 // V neighbouring values as float32.
 template <typename T, int V>
@@ -57,29 +58,30 @@ __device__ __forceinline__ void load_vec(const float* p, int64_t at, float (&o)[
 
 // T: x, z, y.  R: the residual.  L lanes a part, NV packs of V values a lane.
 template <typename T, typename R, int GATE, int RES, int L, int V, int NV>
-__device__ __forceinline__ void norm_parts(const NormArgs& a, int64_t part0) {
+__device__ __forceinline__ void norm_parts(const NormArgs& a, uint32_t part0) {
   constexpr int PER = L < 256 ? 256 / L : 1;  // parts a workgroup
   constexpr int WAVES = L / 64;
   // a residual of 4 bytes beside values of 2 comes in two 16-byte pieces
   constexpr int RV = V * int(sizeof(R)) > 16 ? V / 2 : V;
   const int lane = threadIdx.x % L;
-  const int64_t part = part0 + threadIdx.x / L;
+  const uint32_t part = part0 + __builtin_amdgcn_readfirstlane(threadIdx.x / L);
   const bool on = part < a.parts;
-  const int64_t row = part / a.groups;
+  const uint32_t row = part / a.groups, b = row / a.tokens, t = row % a.tokens;
   const int base = int(part % a.groups) * a.width;
+  const int64_t x0 = place(a.x, b, t) + base, z0 = GATE ? place(a.z, b, t) + base : 0;
+  const int64_t r0 = RES ? place(a.r, b, t) + base : 0, o0 = RES ? place(a.o, b, t) + base : 0;
   float v[NV][V], gate[GATE ? NV : 1][V];
   float sum = 0.f;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int e = (i * L + lane) * V;
     const bool in = on && e < a.width;
-    const int64_t at = base + e;
 #pragma unroll
     for (int k = 0; k < V; ++k) v[i][k] = 0.f;
     if (in) {
-      load_f32<T, V>(a.x, row * a.x_row + at, v[i]);
+      load_f32<T, V>(a.x.data, x0 + e, v[i]);
       if (GATE) {
-        load_f32<T, V>(a.z, row * a.z_row + at, gate[i]);
+        load_f32<T, V>(a.z.data, z0 + e, gate[i]);
 #pragma unroll
         for (int k = 0; k < V; ++k) {
           gate[i][k] = silu(gate[i][k]);
@@ -88,11 +90,11 @@ __device__ __forceinline__ void norm_parts(const NormArgs& a, int64_t part0) {
       }
       if (RES == CO_NORM_BEFORE) {
         float s[V];
-        load_vec<V>(a.scale, at, s);
+        load_vec<V>(a.scale, base + e, s);
 #pragma unroll
         for (int j = 0; j < V; j += RV) {
           float r[RV];
-          load_f32<R, RV>(a.r, row * a.r_row + at + j, r);
+          load_f32<R, RV>(a.r.data, r0 + e + j, r);
 #pragma unroll
           for (int k = 0; k < RV; ++k) v[i][j + k] = fmaf(s[j + k], v[i][j + k], r[k]);
         }
@@ -109,7 +111,7 @@ __device__ __forceinline__ void norm_parts(const NormArgs& a, int64_t part0) {
       if (e >= a.width) break;
 #pragma unroll
       for (int j = 0; j < V; j += RV)
-        store_f32<R, RV>(a.r_out, row * a.o_row + base + e + j, v[i] + j);
+        store_f32<R, RV>(a.o.data, o0 + e + j, v[i] + j);
     }
   }
 #pragma unroll
@@ -128,9 +130,8 @@ __device__ __forceinline__ void norm_parts(const NormArgs& a, int64_t part0) {
   for (int i = 0; i < NV; ++i) {
     const int e = (i * L + lane) * V;
     if (e >= a.width) break;
-    const int64_t at = base + e;
     float w[V];
-    load_vec<V>(a.weight, at, w);
+    load_vec<V>(a.weight, base + e, w);
 #pragma unroll
     for (int k = 0; k < V; ++k) {
       v[i][k] = v[i][k] * inv * w[k];
@@ -138,17 +139,17 @@ __device__ __forceinline__ void norm_parts(const NormArgs& a, int64_t part0) {
     }
     if (RES == CO_NORM_AFTER) {
       float s[V];
-      load_vec<V>(a.scale, at, s);
+      load_vec<V>(a.scale, base + e, s);
 #pragma unroll
       for (int j = 0; j < V; j += RV) {
         float r[RV];
-        load_f32<R, RV>(a.r, row * a.r_row + at + j, r);
+        load_f32<R, RV>(a.r.data, r0 + e + j, r);
 #pragma unroll
         for (int k = 0; k < RV; ++k) r[k] = fmaf(s[j + k], v[i][j + k], r[k]);
-        store_f32<R, RV>(a.r_out, row * a.o_row + at + j, r);
+        store_f32<R, RV>(a.o.data, o0 + e + j, r);
       }
     } else {
-      store_f32<T, V>(a.y, row * a.y_row + at, v[i]);
+      store_f32<T, V>(a.y.data, place(a.y, b, t) + base + e, v[i]);
     }
   }
 }
@@ -156,8 +157,8 @@ __device__ __forceinline__ void norm_parts(const NormArgs& a, int64_t part0) {
 template <typename T, typename R, int GATE, int RES, int L, int V, int NV>
 __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_kernel(NormArgs a) {
   constexpr int PER = L < 256 ? 256 / L : 1;
-  const int64_t by = int64_t(gridDim.x) * PER;
-  for (int64_t part = int64_t(blockIdx.x) * PER; part < a.parts; part += by) {
+  const uint32_t by = gridDim.x * PER;  // at most 2^23: no sum here passes 32 bits
+  for (uint32_t part = blockIdx.x * PER; part < a.parts; part += by) {
     norm_parts<T, R, GATE, RES, L, V, NV>(a, part);
     if (L > 64 && part + by < a.parts) __syncthreads();  // the waves' sums are read
   }
@@ -170,7 +171,7 @@ hipError_t launch_width(const NormArgs& a, hipStream_t s) {
   const auto go = [&](auto kernel, int L) {
     const int per = L < 256 ? 256 / L : 1;
     const int64_t most = int64_t(1) << 21;  // then a workgroup takes several
-    const int64_t grid = std::min((a.parts + per - 1) / per, most);
+    const int64_t grid = std::min((int64_t(a.parts) + per - 1) / per, most);
     hipLaunchKernelGGL(kernel, dim3(unsigned(grid)), dim3(L < 256 ? 256 : L), 0, s, a);
     return hipGetLastError();
   };
@@ -202,23 +203,24 @@ hipError_t launch_kind(const NormArgs& a, int gate, int res, hipStream_t s) {
 template <typename T, typename R>
 hipError_t launch_t(const NormArgs& a, int gate, int res, hipStream_t s) {
   constexpr int V = kWide<T>;
-  const auto wide = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
+  const auto at = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
+  const auto wide = [&](const co_tokens& t) {
+    return at(t.data) && t.batch_stride % V == 0 && t.token_stride % V == 0;
+  };
   // 16-byte accesses where every one of them is aligned, values otherwise
-  const bool fits = a.width % V == 0 && a.x_row % V == 0 && a.z_row % V == 0 &&
-                    a.r_row % V == 0 && a.y_row % V == 0 && a.o_row % V == 0 && wide(a.x) &&
-                    wide(a.z) && wide(a.r) && wide(a.weight) && wide(a.scale) && wide(a.y) &&
-                    wide(a.r_out);
+  const bool fits = a.width % V == 0 && wide(a.x) && wide(a.z) && wide(a.r) && wide(a.y) &&
+                    wide(a.o) && at(a.weight) && at(a.scale);
   return fits ? launch_kind<T, R, V>(a, gate, res, s) : launch_kind<T, R, 1>(a, gate, res, s);
 }
 
 }  // namespace
 
-hipError_t launch_norm(const co_norm_desc& d, const co_rows& x, const co_rows& gate,
-                       const co_rows& residual, const float* weight, const float* scale,
-                       const co_rows& y, const co_rows& residual_out, hipStream_t stream) {
-  const NormArgs a{x.data, gate.data, residual.data, weight, scale, y.data, residual_out.data,
-                   x.row_stride, gate.row_stride, residual.row_stride, y.row_stride,
-                   residual_out.row_stride, d.rows * d.groups, d.groups, d.dim / d.groups, d.eps};
+hipError_t launch_norm(const co_norm_desc& d, const co_tokens& x, const co_tokens& gate,
+                       const co_tokens& residual, const float* weight, const float* scale,
+                       const co_tokens& y, const co_tokens& residual_out, hipStream_t stream) {
+  const NormArgs a{x, gate, residual, y, residual_out, weight, scale,
+                   uint32_t(int64_t(d.batch) * d.tokens * d.groups), uint32_t(d.groups),
+                   uint32_t(d.tokens), d.dim / d.groups, d.eps};
   const bool r16 = d.residual && d.residual_dtype == CO_BF16;
   if (d.dtype == CO_BF16)
     return r16 ? launch_t<bf16_t, bf16_t>(a, d.gate, d.residual, stream)

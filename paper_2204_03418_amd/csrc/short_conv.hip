@@ -1,9 +1,9 @@
 // Short causal convolution over tokens with its activation:
 //   y[t,c] = act(bias[c] + sum_k w[c,k] x[t-K+1+k,c]).
 // Bound by memory: x read once, y written once, 2K flops a value.  A thread
-// takes 16 bytes of channels and a run of kRun tokens, whose K - 1 tokens
-// before it are loaded again (by the wave beside it in the workgroup, so from
-// the vector cache); all loads of a run are in flight together.
+// takes 16 bytes of channels and runs of kRun tokens, whose loads are in flight
+// together and over the run before; the K - 1 tokens before its first run it
+// loads again.
 #include "launch.hpp"
 #include "token.hpp"
 
@@ -11,7 +11,7 @@ namespace coinf {
 
 namespace {
 
-constexpr int kRun = 8;
+constexpr int kRun = 2;
 
 struct ConvCall {
   const void* weight;
@@ -22,7 +22,8 @@ struct ConvCall {
   const int32_t* lengths;
   int64_t x_batch, x_token, y_batch, y_token;
   int32_t C, T, act, update;
-  int32_t c_blocks, t_blocks;  // of a workgroup's channels and tokens
+  int32_t c_blocks, t_blocks;  // workgroups across the channels and along the tokens
+  int32_t runs;                // of a thread
 };
 
 __device__ __forceinline__ float activate(float v, int act) {
@@ -30,35 +31,44 @@ __device__ __forceinline__ float activate(float v, int act) {
   return act == CO_ACT_RELU ? fmaxf(v, 0.f) : v;
 }
 
-// V channels a thread, RUN tokens a thread; LANES threads across the channels,
-// 256 / LANES runs of tokens.
+// V channels a thread, a.runs runs of RUN tokens a thread; LANES threads across the
+// channels, 256 / LANES threads along the tokens.
 template <typename T, int K, int V, int RUN, int LANES>
 __global__ __launch_bounds__(kBlock) void shortconv_kernel(ConvCall a) {
-  constexpr int RUNS = kBlock / LANES;
+  constexpr int ROWS = kBlock / LANES;
   const int lane = threadIdx.x % LANES, seg = threadIdx.x / LANES;
   const int cb = int(blockIdx.x % uint32_t(a.c_blocks));
   const int rest = int(blockIdx.x / uint32_t(a.c_blocks));
   const int tb = rest % a.t_blocks, b = rest / a.t_blocks;
   const int64_t c = (int64_t(cb) * LANES + lane) * V;
-  const int64_t t0 = (int64_t(tb) * RUNS + seg) * RUN;  // may pass T by less than 2^9
+  const int64_t t0 = (int64_t(tb) * ROWS + seg) * RUN * a.runs;
   if (c >= a.C || t0 >= a.T) return;
   const int len = stream_tokens(a.lengths, b, a.T);
   const T* x = static_cast<const T*>(a.x) + b * a.x_batch + c;
   T* y = static_cast<T*>(a.y) + b * a.y_batch + c;
   T* state = a.state ? static_cast<T*>(a.state) + int64_t(b) * (K - 1) * a.C + c : nullptr;
 
-  // the run and the K - 1 tokens before it: from x, or the state before token 0
-  Pack<T, V> win[RUN + K - 1];
+  const auto load_run = [&](Pack<T, V>(&to)[RUN], int64_t t) {
 #pragma unroll
-  for (int i = 0; i < RUN + K - 1; ++i) {
-    const int64_t t = t0 + i - (K - 1);
-    win[i] = Pack<T, V>{};
-    if (t >= 0) {
-      if (t < len) win[i] = load_pack<T, V>(x + t * a.x_token);
-    } else if (state) {
-      win[i] = load_pack<T, V>(state + (t + K - 1) * a.C);
+    for (int i = 0; i < RUN; ++i) {
+      to[i] = Pack<T, V>{};
+      if (t + i < len) to[i] = load_pack<T, V>(x + (t + i) * a.x_token);
     }
+  };
+  // the K - 1 tokens before the run, from x, or the state before token 0
+  Pack<T, V> old[K > 1 ? K - 1 : 1], first[K > 1 ? K - 1 : 1], run[RUN];
+#pragma unroll
+  for (int i = 0; i < K - 1; ++i) {
+    const int64_t t = t0 + i - (K - 1);
+    old[i] = Pack<T, V>{};
+    if (t >= 0) {
+      if (t < len) old[i] = load_pack<T, V>(x + t * a.x_token);
+    } else if (state) {
+      old[i] = load_pack<T, V>(state + (t + K - 1) * a.C);
+    }
+    first[i] = old[i];
   }
+  load_run(run, t0);
   float w[V][K], bias[V];
   {
     Pack<T, V> raw[K];
@@ -72,21 +82,39 @@ __global__ __launch_bounds__(kBlock) void shortconv_kernel(ConvCall a) {
 #pragma unroll
     for (int v = 0; v < V; ++v) bias[v] = to_f32<T>(rb.v[v]);
   }
+  for (int r = 0; r < a.runs; ++r) {
+    const int64_t t1 = t0 + int64_t(r) * RUN;
+    if (t1 >= a.T) break;
+    Pack<T, V> next[RUN];
+    if (r + 1 < a.runs) load_run(next, t1 + RUN);  // in flight over this run's sums
 #pragma unroll
-  for (int i = 0; i < RUN; ++i) {
-    const int64_t t = t0 + i;
-    if (t >= a.T) break;
-    Pack<T, V> out{};
-    if (t < len) {
+    for (int i = 0; i < RUN; ++i) {
+      const int64_t t = t1 + i;
+      Pack<T, V> out{};
+      if (t < len) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        float s = bias[v];
+        for (int v = 0; v < V; ++v) {
+          float s = bias[v];
 #pragma unroll
-        for (int k = 0; k < K; ++k) s = fmaf(w[v][k], to_f32<T>(win[i + k].v[v]), s);
-        out.v[v] = from_f32<T>(activate(s, a.act));
+          for (int k = 0; k < K; ++k) {
+            const int at = i + k - (K - 1);
+            s = fmaf(w[v][k], to_f32<T>(at < 0 ? old[at + K - 1 < 0 ? 0 : at + K - 1].v[v]
+                                               : run[at < 0 ? 0 : at].v[v]), s);
+          }
+          out.v[v] = from_f32<T>(activate(s, a.act));
+        }
       }
+      if (t < a.T) store_pack<T, V>(y + t * a.y_token, out);
     }
-    store_pack<T, V>(y + t * a.y_token, out);
+    if (r + 1 < a.runs) {
+#pragma unroll
+      for (int i = 0; i < K - 1; ++i) {
+        const int at = RUN + i - (K - 1);  // of old and run together, RUN tokens on
+        old[i] = at < 0 ? old[at + K - 1 < 0 ? 0 : at + K - 1] : run[at < 0 ? 0 : at];
+      }
+#pragma unroll
+      for (int i = 0; i < RUN; ++i) run[i] = next[i];
+    }
   }
   // The state is read by the threads of token 0 alone, and they write it: its
   // j-th token is number len - (K - 1) + j of the call, or what the old state has.
@@ -95,13 +123,13 @@ __global__ __launch_bounds__(kBlock) void shortconv_kernel(ConvCall a) {
     for (int j = 0; j < K - 1; ++j) {
       Pack<T, V> v{};
       if (RUN == 1) {
-        v = win[j + 1];  // one token: the old ones move up
+        v = j + 1 < K - 1 ? first[j + 1 < K - 1 ? j + 1 : 0] : run[0];  // the old ones move up
       } else if (len + j >= K - 1) {
         v = load_pack<T, V>(x + (len + j - (K - 1)) * a.x_token);
       } else {
 #pragma unroll
         for (int i = j + 1; i < K - 1; ++i)
-          if (i == len + j) v = win[i];
+          if (i == len + j) v = first[i];
       }
       store_pack<T, V>(state + int64_t(j) * a.C, v);
     }
@@ -113,7 +141,7 @@ hipError_t launch_k(ConvCall a, int32_t B, hipStream_t s) {
   const int64_t packs = (a.C + V - 1) / V;
   if (a.T == 1) {
     a.c_blocks = int32_t((packs + kBlock - 1) / kBlock);
-    a.t_blocks = 1;
+    a.t_blocks = a.runs = 1;
     const int64_t grid = int64_t(a.c_blocks) * B;
     if (!grid_fits(grid)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((shortconv_kernel<T, K, V, 1, kBlock>), dim3(unsigned(grid)), dim3(kBlock),
@@ -122,14 +150,20 @@ hipError_t launch_k(ConvCall a, int32_t B, hipStream_t s) {
   }
   const auto go = [&](auto kernel, int lanes) {
     a.c_blocks = int32_t((packs + lanes - 1) / lanes);
-    a.t_blocks = (a.T - 1) / (kRun * (kBlock / lanes)) + 1;
+    a.t_blocks = (a.T - 1) / (kRun * a.runs * (kBlock / lanes)) + 1;
     const int64_t grid = int64_t(a.c_blocks) * a.t_blocks * B;
     if (!grid_fits(grid)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL(kernel, dim3(unsigned(grid)), dim3(kBlock), 0, s, a);
     return hipGetLastError();
   };
-  // one run a stream: all threads across the channels
-  if (a.T <= kRun) return go(shortconv_kernel<T, K, V, kRun, kBlock>, kBlock);
+  // More runs a thread load the tokens before them less often, where that leaves two waves for
+  // each of 1024 SIMDs.  4 x 4096 tokens of 4352 channels in bfloat16 (285 MB): one run of 8
+  // tokens a thread 91 us, 4 of 8 81 us (at half the occupancy), 8 of 4 64 us, 8 of 2 59 us.
+  const int64_t threads = packs * B * ((a.T + kRun - 1) / kRun);
+  a.runs = 8;
+  while (a.runs > 1 && threads / a.runs < 2 * 1024 * 64) a.runs /= 2;
+  // few tokens: threads across the channels
+  if (a.T <= 4 * kRun) return go(shortconv_kernel<T, K, V, kRun, 64>, 64);
   return go(shortconv_kernel<T, K, V, kRun, 32>, 32);
 }
 
@@ -165,7 +199,7 @@ hipError_t launch_shortconv(const co_shortconv_desc& d, const void* weight, cons
                             const co_tokens& x, int32_t T, const int32_t* lengths, void* state,
                             const co_tokens& y, bool update, hipStream_t stream) {
   ConvCall a{weight, bias, x.data, y.data, state, lengths, x.batch_stride, x.token_stride,
-             y.batch_stride, y.token_stride, d.channels, T, d.act, update && state ? 1 : 0, 0, 0};
+             y.batch_stride, y.token_stride, d.channels, T, d.act, update && state ? 1 : 0, 0, 0, 1};
   if (d.dtype == CO_BF16) return launch_t<bf16_t>(a, d.batch, d.kernel, stream);
   return launch_t<float>(a, d.batch, d.kernel, stream);
 }

@@ -135,31 +135,32 @@ co_status co_scan_forward_steps(const co_scan_desc* desc, const float* A, const 
   return done(launch_scan_seq(c, as_stream(stream)));
 }
 
-co_status co_norm_forward(const co_norm_desc* desc, const co_rows* x, const co_rows* gate,
-                          const co_rows* residual, const float* weight, const float* scale,
-                          const co_rows* y, const co_rows* residual_out, void* stream) {
-  if (!desc || desc->rows < 0 || desc->dim <= 0 || desc->groups <= 0 ||
+co_status co_norm_forward(const co_norm_desc* desc, const co_tokens* x, const co_tokens* gate,
+                          const co_tokens* residual, const float* weight, const float* scale,
+                          const co_tokens* y, const co_tokens* residual_out, void* stream) {
+  if (!desc || desc->batch < 0 || desc->tokens < 0 || desc->dim <= 0 || desc->groups <= 0 ||
       desc->dim % desc->groups || !dtype_ok(desc->dtype) || !dtype_ok(desc->residual_dtype))
     return CO_EINVAL;
   if (desc->gate < CO_NORM_NONE || desc->gate > CO_NORM_AFTER || desc->residual < CO_NORM_NONE ||
       desc->residual > CO_NORM_AFTER || !(desc->eps >= 0.f) || !std::isfinite(desc->eps))
     return CO_EINVAL;
   if (desc->dim / desc->groups > CO_NORM_MAX_WIDTH) return CO_ENOTSUP;
-  if (mul_to(desc->rows, desc->dim, kMaxValues) < 0) return CO_EINVAL;
-  if (desc->rows == 0) return CO_OK;
-  const auto rows_ok = [&](const co_rows* r, int32_t dtype, bool out) {
-    return r && r->data && aligned(r->data, elem(dtype)) &&
-           mul_to(r->row_stride, desc->rows, kMaxOffset) >= 0 &&
-           (!out || desc->rows < 2 || r->row_stride >= desc->dim);
+  const int64_t rows = int64_t(desc->batch) * desc->tokens;
+  if (mul_to(rows, desc->groups, INT32_MAX) < 0) return CO_ENOTSUP;
+  if (rows == 0) return CO_OK;
+  const auto in_ok = [&](const co_tokens* t, int32_t dtype) {
+    return t && tokens_ok(*t, desc->batch, desc->tokens, dtype);
   };
-  if (!rows_ok(x, desc->dtype, false)) return CO_EINVAL;
-  if (desc->gate && !rows_ok(gate, desc->dtype, false)) return CO_EINVAL;
-  if (desc->residual && (!rows_ok(residual, desc->residual_dtype, false) ||
-                         !rows_ok(residual_out, desc->residual_dtype, true)))
-    return CO_EINVAL;
-  if (desc->residual != CO_NORM_AFTER && !rows_ok(y, desc->dtype, true)) return CO_EINVAL;
+  const auto result_ok = [&](const co_tokens* t, int32_t dtype) {
+    return t && out_ok(*t, desc->batch, desc->tokens, desc->dim, dtype);
+  };
+  const int32_t dt = desc->dtype, rt = desc->residual_dtype;
+  if (!in_ok(x, dt)) return CO_EINVAL;
+  if (desc->gate && !in_ok(gate, dt)) return CO_EINVAL;
+  if (desc->residual && (!in_ok(residual, rt) || !result_ok(residual_out, rt))) return CO_EINVAL;
+  if (desc->residual != CO_NORM_AFTER && !result_ok(y, dt)) return CO_EINVAL;
   if (!aligned(weight, 4) || !aligned(scale, 4)) return CO_EINVAL;
-  const co_rows none{nullptr, 0};
+  const co_tokens none{nullptr, 0, 0};
   return done(launch_norm(*desc, *x, desc->gate ? *gate : none, desc->residual ? *residual : none,
                           weight, scale, desc->residual != CO_NORM_AFTER ? *y : none,
                           desc->residual ? *residual_out : none, as_stream(stream)));

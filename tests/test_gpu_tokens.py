@@ -357,6 +357,27 @@ def test_norm_in_place_and_zero_rows():
     assert same is keep and torch.equal(keep, new) and torch.equal(y2, y)
     none = pre.forward(x[:0], residual=r[:0])
     assert none[0].shape == (0, 3, 96)
+    none = pre.forward(x[0, :0], residual=r[0, :0])
+    assert none[1].shape == (0, 96)
+
+
+def test_norm_axes():
+    """Any number of leading axes, pieces of longer tensors, tokens before streams."""
+    g = gen(23)
+    x, z = randn(g, 3, 8, 64, dtype=BF16).to(DEV), randn(g, 3, 8, 100, dtype=BF16).to(DEV)
+    layer = coinf.CoNorm(torch.ones(64, device=DEV), gate="after")
+    want = layer.forward(x, gate=z[..., :64].contiguous())
+    assert torch.equal(layer.forward(x, gate=z[..., :64]), want)
+    assert torch.equal(layer.forward(x[:, 2:5], gate=z[:, 2:5, :64]), want[:, 2:5])
+    assert torch.equal(layer.forward(x[1, 4], gate=z[1, 4, :64]), want[1, 4])
+    assert torch.equal(layer.forward(x.view(3, 2, 4, 64), gate=z[..., :64].unflatten(1, (2, 4))),
+                       want.view(3, 2, 4, 64))
+    turn = x.transpose(0, 1).contiguous().transpose(0, 1)
+    out = torch.empty_like(turn)
+    assert torch.equal(layer.forward(turn, gate=z[..., :64], out=out), want)
+    with pytest.raises(ValueError):
+        layer.forward(x.transpose(0, 1).unflatten(0, (2, 4)),
+                      gate=z[..., :64].transpose(0, 1).unflatten(0, (2, 4)).transpose(0, 2))
 
 
 # ------------------------------------------------------------ refusals, streams, graphs
@@ -480,3 +501,64 @@ def test_scan_nonfinite_tokens_stay_behind(dtype, bad):
     S[0, 1, 5] = 0.0
     layer.state[0, 1, 5] = 0.0
     R.within(layer.state, S, (4 * 150 + 96) * R.U32 * M + 1e-300, "finite states")
+
+
+# ------------------------------------------------------------ the mixer
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_mixer_is_its_layers(dtype):
+    """The mixer's three layers against the plain forms run one after the other
+    on the rounded values between them; steps against the clip."""
+    B, T, H, P, G, N, K = 2, 70, 4, 32, 2, 32, 4
+    case = (B, T, H, P, G, N, dtype, "full", True, True)
+    g = gen(51)
+    v, _ = scan_inputs(case, 51)
+    inner, shared = H * P, G * N
+    u = randn(g, B, T, 2 * inner + 2 * shared + H, scale=0.7, dtype=dtype)
+    w = randn(g, inner + 2 * shared, K, scale=0.5, dtype=dtype)
+    nw = randn(g, inner)
+    n = torch.tensor([T, 33], dtype=torch.int32)
+    conv = coinf.CoShortConv(w.to(DEV), batch=B)
+    scan = scan_layer(case, v, None)
+    mixer = coinf.Mixer(conv, scan, coinf.CoNorm(nw.to(DEV), gate="before"))
+    assert mixer.width == u.shape[-1]
+    got = mixer.forward(u.to(DEV), n.to(DEV))
+    z, xbc, dt = u.split((inner, inner + 2 * shared, H), -1)
+    y1, s1, _ = R.shortconv(R.np64(xbc), R.np64(w), None, None, n, "silu")
+    mid = conv.forward(xbc.to(DEV), n.to(DEV))
+    R.within(mid, y1, U[dtype] * np.abs(y1) + (K + 9) * R.U32 * s1, "mixer conv")
+    x, b, c = (t.cpu() for t in mid.split((inner, shared, shared), -1))
+    parts = dict(v, x=x.unflatten(-1, (H, P)), dt=dt, b=b.unflatten(-1, (G, N)),
+                 c=c.unflatten(-1, (G, N)))
+    y = scan.forward(*(parts[k].to(DEV) for k in ("x", "dt", "b", "c")), n.to(DEV))
+    y2, s2, _, _ = scan_ref(case, parts, None, n)
+    f32 = (4 * T + N + 64) * R.U32 + (U[dtype] if dtype is BF16 else 0.0)
+    R.within(y, y2, U[dtype] * np.abs(y2) + f32 * s2, "mixer scan")
+    rows = y.flatten(2).reshape(-1, inner)
+    want, _ = R.norm(R.np64(rows), R.np64(z.reshape(-1, inner)), None, R.np64(nw), None, 1, 1e-5,
+                     "before", None)
+    R.within(got.reshape(-1, inner), want, (U[dtype] + 56 * R.U32) * np.abs(want), "mixer norm")
+    # the same tokens as a piece and single steps
+    ud, keep = u.to(DEV), got.float()
+    one = [mixer.forward_steps(ud[:, :40])]
+    one += [mixer.forward_step(ud[:, t])[:, None] for t in range(40, T)]
+    both = torch.cat(one, 1).float()
+    # one rounding of the scan's factors and one of its output each, in the norm's scale
+    assert R.relative(both[0], R.np64(keep[0])) <= (4 * U[BF16] if dtype is BF16 else 1e-5)
+    with pytest.raises(ValueError):
+        coinf.Mixer(conv, scan, coinf.CoNorm(nw.to(DEV)))
+    with pytest.raises(ValueError):
+        coinf.Mixer(conv, scan, coinf.CoNorm(dim=inner + 1, gate="before"))
+
+
+def test_example_streams_equal_clips():
+    import importlib.util
+    import os
+
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples",
+                        "stream_tokens.py")
+    spec = importlib.util.spec_from_file_location("stream_tokens", path)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    assert mod.main(longest=130, tokens=6) < 0.03
