@@ -378,8 +378,10 @@ __global__ __launch_bounds__(kWaves * 64, !FULL && sizeof(T) == 2 ? 3 : 2) void 
   constexpr int BC_ROW = L::NW / V, BC_LOADS = (Q * BC_ROW + 255) / 256;
   constexpr int X_ROW = L::PW / V, X_LOADS = Q * X_ROW / 64;
   static_assert(NT % 2 == 0 && 256 % BC_ROW == 0 && Q * X_ROW % 64 == 0 && 64 % X_ROW == 0);
-  __shared__ __align__(16) unsigned char lds[sizeof(L)];
-  L& sh = *reinterpret_cast<L*>(lds);
+  // Two tiles where two workgroups of a CU have them: the next chunk's is written over this one's
+  // products, and a chunk has one barrier.
+  constexpr int BUFS = FULL && 2 * sizeof(L) <= 80 * 1024 ? 2 : 1;
+  __shared__ __align__(16) unsigned char lds[BUFS * sizeof(L)];
 
   const co_scan_desc& d = a.c.d;
   const co_scan_io& io = a.c.io;
@@ -523,13 +525,13 @@ __global__ __launch_bounds__(kWaves * 64, !FULL && sizeof(T) == 2 ? 3 : 2) void 
   // The accumulators hold the state times 2^-base: a chunk whose decays stay within kSpan of the
   // base neither scales them nor takes a power for each pair of its tokens.
   double base = 0.0, seg_log = 0.0;
-  if (t_begin < t_end) fetch(t_begin);
-  for (int64_t t0 = t_begin; t0 < t_end; t0 += Q) {
-    __syncthreads();  // the last chunk's tiles are read
+  float rescale = 1.f, total = 0.f;  // of the accumulators before the chunk; its log decay
+  bool far = false;                  // its decays alone pass the span
+  const auto stage = [&](L& sh) {
 #pragma unroll
     for (int i = 0; i < BC_LOADS; ++i) {
       const int row = bc_row + i * BC_BY;
-      if (row >= Q) break;
+      if (Q % BC_BY && row >= Q) break;
       store_pack<T, V>(sh.b + row * L::BS + bc_col, rb[i]);
       if (FULL) store_pack<T, V>(sh.c + row * L::CS + bc_col, rc[i]);
     }
@@ -537,46 +539,38 @@ __global__ __launch_bounds__(kWaves * 64, !FULL && sizeof(T) == 2 ? 3 : 2) void 
     for (int i = 0; i < X_LOADS; ++i)
       store_pack<T, V>(sh.x[wave] + (x_row + i * X_BY) * L::XS + x_col, rx[i]);
     if (FULL && wave < kPairs) sh.bc[wave][lane] = rbc;
-    const float total = uniform(rtotal), reach = uniform(rreach);
-    const bool far = !(reach <= kSpan);  // its decays alone pass the span
-    if (far || !(fabs(base) + reach <= kSpan)) {
-      if (base != 0.0) scale_state(pow2(base));
-      base = 0.0;
-    }
+    total = uniform(rtotal);
+    const float reach = uniform(rreach);
+    far = !(reach <= kSpan);
+    const bool fits = !far && fabs(base) + reach <= kSpan;
+    rescale = fits ? 1.f : pow2(base);
+    if (!fits) base = 0.0;
     (lane < Q ? sh.grow[wave] : sh.weight[wave])[lane % Q] =
         rdecay * pow2(lane < Q ? base : -base);
     base = far ? 0.0 : base + total;
     seg_log += total;
-    if (t0 + Q < t_end) fetch(t0 + Q);  // in flight over this one's products
+  };
+  if (t_begin < t_end) fetch(t_begin);
+  if (BUFS == 2 && t_begin < t_end) {
+    stage(*reinterpret_cast<L*>(lds));
+    if (t_begin + Q < t_end) fetch(t_begin + Q);
+  }
+  int buf = 0;
+  for (int64_t t0 = t_begin; t0 < t_end; t0 += Q) {
+    L& sh = *reinterpret_cast<L*>(lds + buf);
+    if (BUFS == 1) {
+      __syncthreads();  // the last chunk's tiles are read
+      stage(sh);
+      if (t0 + Q < t_end) fetch(t0 + Q);  // in flight over this one's products
+    }
     __syncthreads();
+    if (rescale != 1.f) scale_state(rescale);
 
     F x[PT];
 #pragma unroll
     for (int pt = 0; pt < PT; ++pt)
       x[pt] = cols_of(sh.x[wave], L::XS, 0, x_four(pt), p_of(pt, l16));
     if constexpr (FULL) {
-      // y^T = S C_t: rows p, columns t
-      f32x4 y[L::QT][PT];
-#pragma unroll
-      for (int j = 0; j < L::QT; ++j)
-#pragma unroll
-        for (int pt = 0; pt < PT; ++pt) y[j][pt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int k = 0; k < NK; ++k) {
-        F c[L::QT];
-#pragma unroll
-        for (int j = 0; j < L::QT; ++j) c[j] = rows_of<T>(sh.c, L::CS, 16 * j, 32 * k);
-#pragma unroll
-        for (int pt = 0; pt < PT; ++pt) {
-          float v[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = S[2 * k + i / 4][pt][i % 4];
-          F s;
-          round_to(s, v);
-#pragma unroll
-          for (int j = 0; j < L::QT; ++j) mma(y[j][pt], s, c[j]);
-        }
-      }
       float grow[L::QT];
 #pragma unroll
       for (int j = 0; j < L::QT; ++j) grow[j] = sh.grow[wave][16 * j + l16];
@@ -599,11 +593,7 @@ __global__ __launch_bounds__(kWaves * 64, !FULL && sizeof(T) == 2 ? 3 : 2) void 
             for (int i = 0; i < 4; ++i)
               w[j + si][i] = exp2_fast((cum - cs[i]) + (low - ls[i])) * ds[i];
           }
-#pragma unroll
-          for (int pt = 0; pt < PT; ++pt) y[j][pt] *= grow[j];
-          grow[j] = 1.f;
         }
-        scale_state(pow2(double(total)));
       }
       // The product takes 0 x_s for s > t: a NaN or an infinity among x would reach the tokens
       // before it.  Where there is one the product does without it, and NaN goes to its places.
@@ -616,36 +606,77 @@ __global__ __launch_bounds__(kWaves * 64, !FULL && sizeof(T) == 2 ? 3 : 2) void 
 #pragma unroll
         for (int pt = 0; pt < PT; ++pt) part_finite(x[pt], bad[pt]);
       }
+      F m[L::QT];  // columns t, depths s
 #pragma unroll
       for (int j = 0; j < L::QT; ++j) {
-        float v[8] = {}, one[8] = {};
+        float v[8] = {};
 #pragma unroll
         for (int si = 0; si <= j; ++si) {
           const f32x4 bc = sh.bc[j + si][lane];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const bool seen = si < j || 4 * g16 + i <= l16;
-            v[4 * si + i] = seen ? w[j + si][i] * bc[i] : 0.f;
-            one[4 * si + i] = seen ? 1.f : 0.f;
+          for (int i = 0; i < 4; ++i)
+            v[4 * si + i] = si < j || 4 * g16 + i <= l16 ? w[j + si][i] * bc[i] : 0.f;
+        }
+        round_to(m[j], v);
+      }
+      // y^T = S C_t + own: rows p, columns t
+      f32x4 y[L::QT][PT];
+      const auto from_state = [&] {
+#pragma unroll
+        for (int j = 0; j < L::QT; ++j)
+#pragma unroll
+          for (int pt = 0; pt < PT; ++pt) y[j][pt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < NK; ++k) {
+          F c[L::QT];
+#pragma unroll
+          for (int j = 0; j < L::QT; ++j) c[j] = rows_of<T>(sh.c, L::CS, 16 * j, 32 * k);
+#pragma unroll
+          for (int pt = 0; pt < PT; ++pt) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = S[2 * k + i / 4][pt][i % 4];
+            F s;
+            round_to(s, v);
+#pragma unroll
+            for (int j = 0; j < L::QT; ++j) mma(y[j][pt], s, c[j]);
           }
         }
-        F m;
-        round_to(m, v);
+      };
+      const auto from_own = [&] {
 #pragma unroll
-        for (int pt = 0; pt < PT; ++pt) mma(y[j][pt], x[pt], m);
-        if (odd) {
-          round_to(m, one);
+        for (int j = 0; j < L::QT; ++j)
+#pragma unroll
+          for (int pt = 0; pt < PT; ++pt) mma(y[j][pt], x[pt], m[j]);
+      };
+      from_state();
+      if (far) {
+#pragma unroll
+        for (int j = 0; j < L::QT; ++j) {
+#pragma unroll
+          for (int pt = 0; pt < PT; ++pt) y[j][pt] *= grow[j];
+          grow[j] = 1.f;
+        }
+        scale_state(pow2(double(total)));
+      }
+      from_own();
+      if (odd) {
+#pragma unroll
+        for (int j = 0; j < L::QT; ++j) {
+          float one[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            one[i] = i / 4 < j || (i / 4 == j && 4 * g16 + i % 4 <= l16) ? 1.f : 0.f;
+          round_to(m[j], one);
 #pragma unroll
           for (int pt = 0; pt < PT; ++pt) {
             f32x4 count{0.f, 0.f, 0.f, 0.f};
-            mma(count, bad[pt], m);
+            mma(count, bad[pt], m[j]);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
               if (count[i] > 0.f) y[j][pt][i] = __builtin_nanf("");
           }
         }
-      }
-      if (odd) {
 #pragma unroll
         for (int pt = 0; pt < PT; ++pt)
           x[pt] = cols_of(sh.x[wave], L::XS, 0, x_four(pt), p_of(pt, l16));
@@ -694,6 +725,11 @@ __global__ __launch_bounds__(kWaves * 64, !FULL && sizeof(T) == 2 ? 3 : 2) void 
         left[i] = get(x[pt], i) * sh.weight[wave][16 * (i / 4) + 4 * g16 + i % 4];
 #pragma unroll
       for (int term = 0; term < TERMS; ++term) take(xw[pt][term], left);
+    }
+    buf = BUFS == 2 ? int(sizeof(L)) - buf : 0;
+    if (BUFS == 2 && t0 + Q < t_end) {  // over the products below
+      stage(*reinterpret_cast<L*>(lds + buf));
+      if (t0 + 2 * Q < t_end) fetch(t0 + 2 * Q);
     }
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
