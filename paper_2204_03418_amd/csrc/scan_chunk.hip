@@ -787,6 +787,25 @@ __global__ __launch_bounds__(kBlock) void scan_carry_kernel(ChunkArgs a, uint32_
   store_pack<float, V>(w + last * size, s);
 }
 
+// Workgroups of an uncut call with units of so many rows.
+int64_t workgroups(const co_scan_desc& d, int64_t rows) {
+  const int64_t units = int64_t(d.heads / d.groups) * ((d.head_dim + rows - 1) / rows);
+  return (units + kWaves - 1) / kWaves * d.groups * d.batch;
+}
+
+// Rows of a unit.  32 share the most between them: 64 heads of 64 x 128 in bfloat16, 16000 tokens
+// 202 us with 32 and 281 us with 16.  16 where 256 states take a lane's registers, where 32 would
+// be empty for a fifth of the units or more, and where a call has too few units to fill the card
+// however it is cut: its time is then that of one wave's chunks, which are shorter (256 tokens
+// 28.6 and 25.5 us; 3 streams of 10 heads of 40 x 20, float32, 256 tokens 27.6 and 20.4 us).
+int unit_rows(const co_scan_desc& d, int64_t T) {
+  if (d.state_size > 128) return 16;
+  const int64_t halves = (d.head_dim + 15) / 16, wholes = (d.head_dim + 31) / 32;
+  if (2 * wholes * 4 >= 5 * halves) return 16;
+  const int64_t chunks = (T + kChunk - 1) / kChunk;
+  return workgroups(d, 32) * ((chunks + 3) / 4) < 600 ? 16 : 32;
+}
+
 template <typename T, int NT, int PT, bool WIDE>
 hipError_t launch_tiles(ChunkArgs a, hipStream_t s) {
   const co_scan_desc& d = a.c.d;
@@ -818,10 +837,14 @@ hipError_t launch_tiles(ChunkArgs a, hipStream_t s) {
 template <typename T, bool WIDE>
 hipError_t launch_state(const ChunkArgs& a, hipStream_t s) {
   const int N = a.c.d.state_size;
-  // the state of a unit takes 64 registers of a lane at the most
-  if (N <= 32) return launch_tiles<T, 2, 2, WIDE>(a, s);
-  if (N <= 64) return launch_tiles<T, 4, 2, WIDE>(a, s);
-  if (N <= 128) return launch_tiles<T, 8, 2, WIDE>(a, s);
+  if (unit_rows(a.c.d, a.c.T) == 32) {
+    if (N <= 32) return launch_tiles<T, 2, 2, WIDE>(a, s);
+    if (N <= 64) return launch_tiles<T, 4, 2, WIDE>(a, s);
+    return launch_tiles<T, 8, 2, WIDE>(a, s);
+  }
+  if (N <= 32) return launch_tiles<T, 2, 1, WIDE>(a, s);
+  if (N <= 64) return launch_tiles<T, 4, 1, WIDE>(a, s);
+  if (N <= 128) return launch_tiles<T, 8, 1, WIDE>(a, s);
   return launch_tiles<T, 16, 1, WIDE>(a, s);
 }
 
@@ -850,9 +873,7 @@ hipError_t launch_t(const ChunkArgs& a, hipStream_t s) {
 // times 300, 240 and 263.
 void cut(const co_scan_desc& d, int64_t T, int64_t* segments, int64_t* seg_chunks) {
   const int64_t chunks = (T + kChunk - 1) / kChunk;
-  const int64_t pw = d.state_size <= 128 ? 32 : 16;
-  const int64_t units = int64_t(d.heads / d.groups) * ((d.head_dim + pw - 1) / pw);
-  const int64_t groups = (units + kWaves - 1) / kWaves * d.groups * d.batch;
+  const int64_t groups = workgroups(d, unit_rows(d, T));
   const double states = double(d.batch) * d.heads * d.head_dim * d.state_size;
   const auto cost = [&](int64_t n) {
     const double wgs = double(groups) * double(n);
@@ -884,12 +905,12 @@ Space space_of(const co_scan_desc& d, int64_t chunks, int64_t segments) {
 }  // namespace
 
 // Token by token a call takes about 0.3 us a token and 0.11 us a million state values and token;
-// chunks take 8 us more to begin with, and 0.2 us a million values.  Measured, us, by token and in
+// chunks take 9 us more to begin with, and 0.3 us a million values.  Measured, us, by token and in
 // chunks: 16.8 million values, 4 tokens 31 and 35, 8 tokens 40 and 36, 32 tokens 97 and 39;
 // 0.5 million, 16 tokens 10 and 13, 32 tokens 17 and 13.
 bool scan_chunk_takes(const co_scan_desc& d, int32_t T) {
   const double millions = 1e-6 * d.batch * d.heads * double(d.head_dim) * d.state_size;
-  return T * (0.3 + 0.11 * millions) > 8.0 + 0.2 * millions;
+  return T * (0.3 + 0.11 * millions) > 9.0 + 0.3 * millions;
 }
 
 int64_t scan_chunk_workspace(const co_scan_desc& d, int32_t T) {
