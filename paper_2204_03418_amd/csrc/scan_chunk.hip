@@ -287,7 +287,9 @@ struct Tile {
   float grow[kWaves][Q], weight[kWaves][Q];  // with the base in them
 };
 
-// Makes ws_bc and ws_decay: a wave a tile of B . C, or two chunks of a head.
+// Makes ws_bc and ws_decay: a wave the tiles of B . C of a chunk, or two chunks of kHeads heads.
+// Bound by latency (memory, and a new kernel's instructions), so few waves with much on the way.
+constexpr int kHeads = 4;
 template <typename T, bool WIDE>
 __global__ __launch_bounds__(kBlock) void scan_prepare_kernel(ChunkArgs a) {
   const co_scan_desc& d = a.c.d;
@@ -297,75 +299,103 @@ __global__ __launch_bounds__(kBlock) void scan_prepare_kernel(ChunkArgs a) {
   const int two = int(blockIdx.x % doubles), b = int(blockIdx.x / doubles);
   const int job = int(blockIdx.y) * (kBlock / 64) +
                   __builtin_amdgcn_readfirstlane(int(threadIdx.x / 64));
-  if (job >= d.heads + 2 * kPairs * d.groups) return;
+  const int head_jobs = (d.heads + kHeads - 1) / kHeads;
+  if (job >= head_jobs + 2 * d.groups) return;
   const int len = stream_tokens(a.c.lengths, b, a.c.T);
-  if (job >= d.heads) {
-    const int j = job - d.heads, group = j / (2 * kPairs), tile = j % kPairs;
-    const int chunk = 2 * two + j / kPairs % 2;
+  if (job >= head_jobs) {
+    const int j = job - head_jobs, group = j / 2, chunk = 2 * two + j % 2;
     if (chunk >= a.chunks) return;
     const int N = d.state_size;
-    // rows s of B and t of C, as depth-32 operands
-    const int64_t s = int64_t(chunk) * kChunk + 16 * (tile == 2) + l16;
-    const int64_t t = int64_t(chunk) * kChunk + 16 * (tile > 0) + l16;
-    const T* bp = static_cast<const T*>(io.b.data) + b * io.b.batch_stride + int64_t(group) * N;
-    const T* cp = static_cast<const T*>(io.c.data) + b * io.c.batch_stride + int64_t(group) * N;
-    const T* rows[2] = {bp + s * io.b.token_stride, cp + t * io.c.token_stride};
-    const bool in[2] = {s < len, t < len};
-    f32x4 acc{0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < N; k += 32) {
-      Frag<T> f[2];
+    // rows 0..15 and 16..31 of B and of C, as depth-32 operands
+    const T* base[2] = {
+        static_cast<const T*>(io.b.data) + b * io.b.batch_stride + int64_t(group) * N,
+        static_cast<const T*>(io.c.data) + b * io.c.batch_stride + int64_t(group) * N};
+    const int64_t stride[2] = {io.b.token_stride, io.c.token_stride};
+    f32x4 acc[kPairs] = {};
+    constexpr int AHEAD = 2;  // depth blocks on the way together
+    for (int k0 = 0; k0 < N; k0 += 32 * AHEAD) {
+      Pack<T, 4> v[AHEAD][2][2][2];
 #pragma unroll
-      for (int side = 0; side < 2; ++side) {
-        Pack<T, 4> half[2] = {};
+      for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const int n = k + 16 * u + 4 * g16;
-          if (WIDE) {
-            if (in[side] && n < N) half[u] = load_pack<T, 4>(rows[side] + n);
-          } else {
+        for (int side = 0; side < 2; ++side)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (in[side] && n + i < N) half[u].v[i] = rows[side][n + i];
+          for (int half = 0; half < 2; ++half) {
+            const int64_t t = int64_t(chunk) * kChunk + 16 * half + l16;
+            const T* row = base[side] + t * stride[side];
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+              const int n = k0 + 32 * u + 16 * w + 4 * g16;
+              Pack<T, 4>& o = v[u][side][half][w];
+              o = Pack<T, 4>{};
+              if (WIDE) {
+                if (t < len && n < N) o = load_pack<T, 4>(row + n);
+              } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                  if (t < len && n + i < N) o.v[i] = row[n + i];
+              }
+            }
           }
-        }
-        f[side] = join(half[0], half[1]);
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const auto op = [&](int side, int half) {
+          return join(v[u][side][half][0], v[u][side][half][1]);
+        };
+        mma(acc[0], op(0, 0), op(1, 0));  // rows s, columns t
+        mma(acc[1], op(0, 0), op(1, 1));
+        mma(acc[2], op(0, 1), op(1, 1));
       }
-      mma(acc, f[0], f[1]);
     }
-    a.ws_bc[(((int64_t(b) * d.groups + group) * a.chunks + chunk) * kPairs + tile) * 64 + lane] =
-        acc;
+    f32x4* o = a.ws_bc + ((int64_t(b) * d.groups + group) * a.chunks + chunk) * kPairs * 64 + lane;
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) o[64 * i] = acc[i];
     return;
   }
-  const int h = job;
   const int64_t t = int64_t(two) * 64 + lane;
-  float dt = 0.f, log_a = 0.f;
-  if (t < len) {
-    const int64_t at = b * io.dt.batch_stride + t * io.dt.token_stride + h;
-    dt = d.dt_dtype == CO_BF16 ? bf16_to_f32(static_cast<const bf16_t*>(io.dt.data)[at])
-                               : static_cast<const float*>(io.dt.data)[at];
-    if (a.c.dt_bias) dt += a.c.dt_bias[h];
-    if (d.dt_softplus) dt = softplus(dt);
-    log_a = fmaxf(dt * (a.c.A[h] * kLog2e), -160.f);
-  }
-  // 64 bits keep the differences of far sums exact
-  const double cum = prefix_sum32(double(log_a));
-  const double total = lane < 32 ? from_lane<31>(cum) : from_lane<63>(cum);
-  float reach = fabsf(float(cum));  // steps of either sign may turn the sums round
-#pragma unroll
-  for (int m = 16; m > 0; m /= 2) reach = fmaxf(reach, __shfl_xor(reach, m));
   const int chunk = 2 * two + lane / 32, q = lane % 32;
-  if (chunk >= a.chunks) return;
-  ChunkDecay& o = a.ws_decay[(int64_t(b) * d.heads + h) * a.chunks + chunk];
-  if (q == 0) {
-    o.total = float(total);
-    o.reach = reach;
+  // read whether or not the stream has the token, so that its length is not waited for first
+  const int64_t at = b * io.dt.batch_stride + min(t, int64_t(a.c.T - 1)) * io.dt.token_stride;
+  float raw[kHeads], bias[kHeads], A2[kHeads];
+#pragma unroll
+  for (int i = 0; i < kHeads; ++i) {
+    const int h = min(job * kHeads + i, d.heads - 1);
+    raw[i] = d.dt_dtype == CO_BF16 ? bf16_to_f32(static_cast<const bf16_t*>(io.dt.data)[at + h])
+                                   : static_cast<const float*>(io.dt.data)[at + h];
+    bias[i] = a.c.dt_bias ? a.c.dt_bias[h] : 0.f;
+    A2[i] = a.c.A[h] * kLog2e;
   }
-  o.grow[q] = pow2(cum);
-  o.weight[q] = dt * pow2(reach <= kSpan ? -cum : total - cum);
-  if (reach <= kSpan) return;  // what follows is for the chunks that go far
-  o.step[q] = dt;
-  o.cum[q] = float(cum);
-  o.cum_low[q] = float(cum - double(float(cum)));
+#pragma unroll
+  for (int i = 0; i < kHeads; ++i) {
+    const int h = job * kHeads + i;
+    if (h >= d.heads) break;
+    float dt = raw[i] + bias[i];
+    if (d.dt_softplus) dt = softplus(dt);
+    dt = t < len ? dt : 0.f;
+    const float log_a = t < len ? fmaxf(dt * A2[i], -160.f) : 0.f;
+    // 64 bits keep the differences of far sums exact
+    const double cum = prefix_sum32(double(log_a));
+    const double total = lane < 32 ? from_lane<31>(cum) : from_lane<63>(cum);
+    float reach = fabsf(float(cum));  // steps of either sign may turn the sums round
+    if (d.dt_softplus) {
+      reach = fabsf(float(total));
+    } else {
+#pragma unroll
+      for (int m = 16; m > 0; m /= 2) reach = fmaxf(reach, __shfl_xor(reach, m));
+    }
+    if (chunk >= a.chunks) continue;
+    ChunkDecay& o = a.ws_decay[(int64_t(b) * d.heads + h) * a.chunks + chunk];
+    if (q == 0) {
+      o.total = float(total);
+      o.reach = reach;
+    }
+    o.grow[q] = pow2(cum);
+    o.weight[q] = dt * pow2(reach <= kSpan ? -cum : total - cum);
+    if (reach <= kSpan) continue;  // what follows is for the chunks that go far
+    o.step[q] = dt;
+    o.cum[q] = float(cum);
+    o.cum_low[q] = float(cum - double(float(cum)));
+  }
 }
 
 // FULL: outputs and final states; otherwise a segment's own sum and decay.
@@ -813,7 +843,8 @@ hipError_t launch_tiles(ChunkArgs a, hipStream_t s) {
   const int64_t units = int64_t(d.heads / d.groups) * a.p_blocks;
   a.unit_blocks = int32_t((units + kWaves - 1) / kWaves);
   const int64_t grid = int64_t(a.unit_blocks) * d.groups * d.batch;
-  const int64_t jobs = (int64_t(d.heads) + 2 * kPairs * d.groups + kBlock / 64 - 1) / (kBlock / 64);
+  const int64_t jobs = ((int64_t(d.heads) + kHeads - 1) / kHeads + 2 * int64_t(d.groups) +
+                        kBlock / 64 - 1) / (kBlock / 64);
   const int64_t doubles = (int64_t(a.chunks) + 1) / 2 * d.batch;
   constexpr int CV = WIDE ? 4 : 1;  // a state row is then whole pieces of 16 bytes
   const int64_t head_blocks =

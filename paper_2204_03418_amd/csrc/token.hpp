@@ -33,9 +33,21 @@ __device__ __forceinline__ float silu(float v) {
   return v * __builtin_amdgcn_rcpf(1.f + exp2_fast(-v * kLog2e));
 }
 
-// log(1 + exp(v)): log1p keeps the relative accuracy of small results, which a
-// state sums over many tokens.
-__device__ __forceinline__ float softplus(float v) { return v > 20.f ? v : log1pf(expf(v)); }
+// log(1 + exp(v)) = max(v, 0) + log(1 + u), u = exp(-|v|), to 4e-7 of its value also where it is
+// small: a state sums it over many tokens.  exp takes what the product with log2(e) rounds off as
+// a factor; with w = 1 + u rounded, log(w) u / (w - 1) is log(1 + u) without w's rounding (Kahan).
+// 20 instructions where log1pf(expf(v)) has 137.
+__device__ __forceinline__ float softplus(float v) {
+  const float a = fmaxf(-fabsf(v), -128.f);
+  const float h = a * kLog2e;
+  const float low = fmaf(a, kLog2e, -h) + a * 1.925963033500e-8f;  // of log2(e)
+  float u = exp2_fast(h);
+  u = fmaf(u, low * 0.69314718055994530942f, u);
+  const float w = 1.f + u, d = w - 1.f;
+  const float log_w = __builtin_amdgcn_logf(w) * 0.69314718055994530942f;
+  const float l = d > 0.f ? log_w * (u * __builtin_amdgcn_rcpf(d)) : u;
+  return (v < 0.f ? 0.f : v) + l;  // NaN stays
+}
 
 // Tokens of stream b in a call over T.
 __device__ __forceinline__ int stream_tokens(const int32_t* lengths, int b, int T) {
