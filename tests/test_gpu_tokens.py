@@ -562,3 +562,106 @@ def test_example_streams_equal_clips():
     mod = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(mod)
     assert mod.main(longest=130, tokens=6) < 0.03
+
+
+# ------------------------------------------------------------ places that go wrong
+
+
+@pytest.mark.parametrize("T", [4, 150])
+@pytest.mark.parametrize("which", ["dt", "b", "c"])
+def test_scan_nonfinite_inputs_reach_nothing_before_them(which, T):
+    for dtype in (F32, BF16):
+        case = (2, T, 2, 32, 1, 32, dtype, "full", True, True)
+        v, _ = scan_inputs(case, 42)
+        s = T * 2 // 3
+        y, size, _, _ = scan_ref(case, v, v["state"], None)
+        v[which][1, s] = float("nan")
+        layer = scan_layer(case, v, v["state"])
+        got = layer.forward_steps(*(v[k].to(DEV) for k in ("x", "dt", "b", "c")))
+        assert torch.isnan(got[1, s]).all()
+        if which != "c":
+            assert torch.isnan(got[1, -1]).all() and torch.isnan(layer.state[1]).all()
+        f32 = (4 * T + 96) * R.U32 + (U[dtype] if dtype is BF16 else 0.0)
+        bound = U[dtype] * np.abs(y) + f32 * size
+        R.within(got[0], y[0], bound[0], f"other stream {which}")
+        R.within(got[1, :s], y[1, :s], bound[1, :s], f"before {which}")
+
+
+def test_lengths_out_of_range_are_all_or_none():
+    case = (3, 70, 2, 32, 1, 32, BF16, "full", True, True)
+    v, _ = scan_inputs(case, 43)
+    n, good = torch.tensor([-5, 71, 1 << 30]), torch.tensor([0, 70, 70])
+    n, good = (t.to(torch.int32).to(DEV) for t in (n, good))
+    d = [v[k].to(DEV) for k in ("x", "dt", "b", "c")]
+    layer = scan_layer(case, v, None)
+    assert torch.equal(layer.forward(*d, n), layer.forward(*d, good))
+    conv = coinf.CoShortConv(torch.ones(64, 4, dtype=BF16, device=DEV), batch=3)
+    x = d[0].flatten(2)
+    assert torch.equal(conv.forward(x, n), conv.forward(x, good))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_scan_without_workspace(dtype):
+    """The C ABI without a workspace runs the call token by token, as accurate."""
+    import ctypes
+
+    case = (2, 90, 4, 32, 1, 32, dtype, "full", True, True)
+    v, _ = scan_inputs(case, 44)
+    layer = scan_layer(case, v, v["state"])
+    d = {k: v[k].to(DEV) for k in ("x", "dt", "b", "c")}
+    assert layer.workspace_bytes(90) > 0
+    y = torch.empty_like(d["x"])
+    io = coinf.ScanIO(*(coinf.Tokens(t.data_ptr(), t.stride(0), t.stride(1))
+                        for t in (d["x"], d["dt"], d["b"], d["c"], y)))
+    for ws, nws in ((None, 0), (layer.state.data_ptr(), 16)):
+        layer.state.copy_(v["state"])
+        st = coinf.co_scan_forward_steps(
+            ctypes.byref(layer.desc), layer.A.data_ptr(), layer.D.data_ptr(),
+            layer.dt_bias.data_ptr(), ctypes.byref(io), 90, None, layer.state.data_ptr(), 1, ws,
+            nws, torch.cuda.current_stream().cuda_stream)
+        assert st == coinf.CO_OK
+        check_scan(case, y, layer.state, scan_ref(case, v, v["state"], None), "no workspace")
+
+
+def far(t, apart):
+    """t (2, T, ...) on the device with its two streams `apart` elements apart."""
+    n = t[0].numel()
+    room = torch.empty(apart + n, dtype=t.dtype, device=DEV)
+    out = room.as_strided(t.shape, (apart,) + t.stride()[1:])
+    out.copy_(t)
+    return out
+
+
+def test_offsets_past_32_bits():
+    """Streams more than 2^32 elements apart, in and out."""
+    apart = (1 << 32) + 64
+    case = (2, 70, 2, 32, 1, 32, BF16, "full", True, True)
+    v, _ = scan_inputs(case, 45)
+    layer = scan_layer(case, v, v["state"])
+    d = {k: v[k].to(DEV) for k in ("x", "dt", "b", "c")}
+    want = layer.forward(*d.values())
+    x, out = far(v["x"], apart), far(torch.zeros_like(v["x"]), apart)
+    for T in (70, 3):
+        got = layer.forward(x[:, :T], *(d[k][:, :T] for k in ("dt", "b", "c")), out=out[:, :T])
+        keep = want if T == 70 else layer.forward(*(t[:, :3] for t in d.values()))
+        assert torch.equal(got, keep)
+    conv = coinf.CoShortConv(torch.randn(64, 4, dtype=BF16, device=DEV), batch=2)
+    u, o = x.flatten(2), out.flatten(2)
+    assert torch.equal(conv.forward(u, out=o), conv.forward(d["x"].flatten(2)))
+    norm = coinf.CoNorm(dim=64, gate="before")
+    assert torch.equal(norm.forward(u, gate=u, out=o),
+                       norm.forward(d["x"].flatten(2), gate=d["x"].flatten(2)))
+
+
+def test_scan_tokens_far_apart():
+    """Tokens 2^22 elements apart and more: a chunk's offsets take more than 31 bits."""
+    case = (1, 70, 2, 32, 1, 32, F32, "full", True, True)
+    v, _ = scan_inputs(case, 46)
+    layer = scan_layer(case, v, None)
+    d = {k: v[k].to(DEV) for k in ("x", "dt", "b", "c")}
+    wide = torch.empty(70, (1 << 24) + 64, device=DEV)           # 4.7 GB
+    x = wide[:, :64].unflatten(-1, (2, 32))[None]
+    x.copy_(d["x"])
+    got = layer.forward(x, *(d[k] for k in ("dt", "b", "c")))
+    y, size, _, _ = scan_ref(case, v, None, None)
+    R.within(got, y, U[F32] * np.abs(y) + (4 * 70 + 96) * R.U32 * size, "far tokens")
