@@ -25,6 +25,20 @@
 // of few heads are cut into segments of whole chunks that run beside each other:
 // one launch makes each segment's own sum, a small one carries the states across
 // them, and the last computes everything.
+//
+// Chunks of 32 tokens: one depth of a matrix instruction, and the products
+// within a chunk (Q P) stay small beside those with the state (2 N P).  64
+// tokens took 65 registers more than two waves of a SIMD have.
+//
+// Measured: 16384 tokens of 64 heads of 64 x 128, one group, bfloat16: 283 MB and
+// 43 GFLOP of the recurrence in 200 us; the launches take 13 us (B . C, decays),
+// 73 us (segments' sums), 14 us (carry) and 131 us (outputs) when traced.  The
+// last runs its matrix products at 295 TFLOP/s, 557 with the split's three terms
+// counted; it is bound by issue and latency at two waves a SIMD (matrix
+// pipes busy a quarter of the cycles, vector units 40%, waves waiting 28%), not
+// by memory (228 MB from and to memory in it, 1.7 TB/s).  Tried and no faster:
+// three waves a SIMD (spills), eight waves a workgroup, operands read further
+// ahead, matrix and vector instructions interleaved by hand, wave priorities.
 #include <type_traits>
 
 #include "launch.hpp"
@@ -125,13 +139,16 @@ __device__ __forceinline__ void round_to(Frag<float>& f, float (&v)[8]) {
 
 // Whether one of an operand's values is not finite.
 __device__ __forceinline__ bool not_finite(const Frag<bf16_t>& f) {
-  typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
   typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-  const u16x8 v = __builtin_bit_cast(u16x8, f.v) & u16x8(0x7fff);
-  u16x2 most = {v[0], v[1]};
+  struct Words {
+    uint32_t w[4];
+  };
+  const Words v = __builtin_bit_cast(Words, f.v);
+  u16x2 most = {0, 0};
 #pragma unroll
-  for (int i = 2; i < 8; i += 2) most = __builtin_elementwise_max(most, (u16x2{v[i], v[i + 1]}));
-  return most[0] >= 0x7f80 || most[1] >= 0x7f80;
+  for (int i = 0; i < 4; ++i)  // both halves of a word at once
+    most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, v.w[i] & 0x7fff7fffu));
+  return max(most[0], most[1]) >= 0x7f80;
 }
 __device__ __forceinline__ bool not_finite(const Frag<float>& f) {
   uint32_t most = 0;
