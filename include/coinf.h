@@ -766,11 +766,19 @@ typedef struct co_shortconv_desc {
 /* Bytes of the state (0 for K = 1).  Host only. */
 co_status co_shortconv_query(const co_shortconv_desc* desc, int64_t* state_bytes);
 
-/* T tokens of x into y (not in place). */
-co_status co_shortconv_forward_steps(const co_shortconv_desc* desc, const void* weight,
-                                     const void* bias, const co_tokens* x, int32_t T,
-                                     const int32_t* lengths, void* state, const co_tokens* y,
-                                     int32_t update_state, void* stream);
+typedef struct co_shortconv_call {
+  const void*    weight;
+  const void*    bias;            /* may be NULL when !has_bias */
+  co_tokens      x, y;            /* not in place */
+  const int32_t* lengths;
+  void*          state;
+  int32_t        T;
+  int32_t        update_state;
+} co_shortconv_call;
+
+/* T tokens of x into y. */
+co_status co_shortconv_forward_steps(const co_shortconv_desc* desc, const co_shortconv_call* call,
+                                     void* stream);
 
 /*
  * Selective scan: H heads of P values with a P x N state each, a decay a head
@@ -795,9 +803,19 @@ typedef struct co_scan_desc {
   int32_t dt_dtype;               /* CO_F32 | CO_BF16: dt */
 } co_scan_desc;
 
-typedef struct co_scan_io {
-  co_tokens x, dt, b, c, y;
-} co_scan_io;
+typedef struct co_scan_call {
+  const float*   A;
+  const float*   D;
+  const float*   dt_bias;
+  co_tokens      x, dt, b, c, y;  /* y may not overlap the others */
+  const int32_t* lengths;
+  float*         state;
+  void*          workspace;       /* may be NULL; free for reuse once the call's work on the
+                                     stream is done */
+  int64_t        workspace_bytes;
+  int32_t        T;
+  int32_t        update_state;
+} co_scan_call;
 
 /* Bytes of the state.  Host only. */
 co_status co_scan_query(const co_scan_desc* desc, int64_t* state_bytes);
@@ -807,12 +825,8 @@ co_status co_scan_query(const co_scan_desc* desc, int64_t* state_bytes);
  * Host only. */
 co_status co_scan_workspace_bytes(const co_scan_desc* desc, int32_t T, int64_t* bytes);
 
-/* T tokens.  workspace may be NULL; it is free for reuse once the call's work on
- * the stream is done.  y may not overlap the inputs. */
-co_status co_scan_forward_steps(const co_scan_desc* desc, const float* A, const float* D,
-                                const float* dt_bias, const co_scan_io* io, int32_t T,
-                                const int32_t* lengths, float* state, int32_t update_state,
-                                void* workspace, int64_t workspace_bytes, void* stream);
+/* T tokens. */
+co_status co_scan_forward_steps(const co_scan_desc* desc, const co_scan_call* call, void* stream);
 
 /*
  * Root-mean-square norm over `groups` equal parts of each token's dim values,
@@ -824,7 +838,7 @@ co_status co_scan_forward_steps(const co_scan_desc* desc, const float* A, const 
  *   r' = r + scale y                        residual CO_NORM_AFTER (post-norm)
  * x, z and y in dtype, r and r' in residual_dtype, weight and scale float32
  * (dim); weight and scale may be NULL (1).  y is not written with residual
- * CO_NORM_AFTER (its pointer may be NULL), r' with residual CO_NORM_NONE.
+ * CO_NORM_AFTER, r' not with residual CO_NORM_NONE (their pointers may be NULL).
  * All in float32, each output rounded once; the pre-norm's y is made from the
  * unrounded sum.  y may be x, z or (same dtype) r; r_out may be r, x or z.
  */
@@ -844,9 +858,13 @@ typedef struct co_norm_desc {
   float   eps;                    /* >= 0 */
 } co_norm_desc;
 
-co_status co_norm_forward(const co_norm_desc* desc, const co_tokens* x, const co_tokens* gate,
-                          const co_tokens* residual, const float* weight, const float* scale,
-                          const co_tokens* y, const co_tokens* residual_out, void* stream);
+typedef struct co_norm_call {
+  co_tokens    x, gate, residual, y, residual_out;
+  const float* weight;
+  const float* scale;
+} co_norm_call;
+
+co_status co_norm_forward(const co_norm_desc* desc, const co_norm_call* call, void* stream);
 
 #ifdef __cplusplus
 }

@@ -181,8 +181,15 @@ class ScanDesc(ctypes.Structure):
                 ("groups", i32), ("dt_softplus", i32), ("dtype", i32), ("dt_dtype", i32)]
 
 
-class ScanIO(ctypes.Structure):
-    _fields_ = [("x", Tokens), ("dt", Tokens), ("b", Tokens), ("c", Tokens), ("y", Tokens)]
+class ShortConvCall(ctypes.Structure):
+    _fields_ = [("weight", vp), ("bias", vp), ("x", Tokens), ("y", Tokens), ("lengths", vp),
+                ("state", vp), ("T", i32), ("update_state", i32)]
+
+
+class ScanCall(ctypes.Structure):
+    _fields_ = [("A", vp), ("D", vp), ("dt_bias", vp), ("x", Tokens), ("dt", Tokens),
+                ("b", Tokens), ("c", Tokens), ("y", Tokens), ("lengths", vp), ("state", vp),
+                ("workspace", vp), ("workspace_bytes", i64), ("T", i32), ("update_state", i32)]
 
 
 class NormDesc(ctypes.Structure):
@@ -190,19 +197,22 @@ class NormDesc(ctypes.Structure):
                 ("residual", i32), ("dtype", i32), ("residual_dtype", i32), ("eps", f32)]
 
 
-pTok = ctypes.POINTER(Tokens)
+class NormCall(ctypes.Structure):
+    _fields_ = [("x", Tokens), ("gate", Tokens), ("residual", Tokens), ("y", Tokens),
+                ("residual_out", Tokens), ("weight", vp), ("scale", vp)]
+
+
 co_shortconv_query = _sig("co_shortconv_query", i32, [ctypes.POINTER(ShortConvDesc), pi64])
 co_shortconv_forward_steps = _sig("co_shortconv_forward_steps", i32,
-                                  [ctypes.POINTER(ShortConvDesc), vp, vp, pTok, i32, vp, vp, pTok,
-                                   i32, vp])
+                                  [ctypes.POINTER(ShortConvDesc), ctypes.POINTER(ShortConvCall),
+                                   vp])
 co_scan_query = _sig("co_scan_query", i32, [ctypes.POINTER(ScanDesc), pi64])
 co_scan_workspace_bytes = _sig("co_scan_workspace_bytes", i32,
                                [ctypes.POINTER(ScanDesc), i32, pi64])
 co_scan_forward_steps = _sig("co_scan_forward_steps", i32,
-                             [ctypes.POINTER(ScanDesc), vp, vp, vp, ctypes.POINTER(ScanIO), i32,
-                              vp, vp, i32, vp, i64, vp])
+                             [ctypes.POINTER(ScanDesc), ctypes.POINTER(ScanCall), vp])
 co_norm_forward = _sig("co_norm_forward", i32,
-                       [ctypes.POINTER(NormDesc), pTok, pTok, pTok, vp, vp, pTok, pTok, vp])
+                       [ctypes.POINTER(NormDesc), ctypes.POINTER(NormCall), vp])
 
 
 class CoinfError(RuntimeError):
@@ -1143,34 +1153,32 @@ class Residual:
 # may be read, copied, zeroed or indexed by stream between calls.  Delay 0.
 
 
-# A single token's call is a few microseconds: a layer checks the shapes, strides
-# and dtypes of its arguments when they differ from its last call's, and fills
-# the strides of the call's structures then (conv 7.7 -> 6.2, scan 10.8 -> 7.4,
-# pre-norm 13.6 -> 8.0 us a call).
-def _signature(t):
-    return None if t is None else (t.shape, t.stride(), t.dtype, t.is_cuda)
-
-
+# A single token's call is a few microseconds.  A layer keeps the structure that
+# describes its call; shapes, strides and dtypes are checked and filled in when
+# they differ from the last call's, and a like call sets the pointers alone (conv
+# 7.7 -> 5.1 us, scan 10.8 -> 6.2 us, pre-norm 13.6 -> 6.8 us a call).  Like a
+# handle, a layer is one thread's.
 _like = torch.empty_like  # 1.2 us; new_empty, for inputs that are slices, 1.5
 
 
 def _tokens(t, dtype, shape, what, into):
-    """Checks that t is a device tensor of that dtype and shape (B, T, ...)
-    whose values of one token are contiguous, and points `into` at it."""
+    """Checks that t is a device tensor of that dtype and shape (B, T, ...), or
+    (B, ...) for single tokens, whose values of one token are contiguous, and
+    fills `into` with its strides."""
     if t.device.type != "cuda":
         raise ValueError(f"{what} must be a device tensor")
     if t.dtype is not dtype:
         raise ValueError(f"{what} has dtype {t.dtype}, expected {dtype}")
-    if t.shape != shape:
+    if t.shape not in (shape, shape[:1] + shape[2:] if shape[1] == 1 else shape):
         raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     st = t.stride()
-    run = 1
-    for i in range(len(shape) - 1, 1, -1):
-        if shape[i] != 1:
+    run, lead = 1, t.dim() - len(shape) + 2
+    for i in range(t.dim() - 1, lead - 1, -1):
+        if t.shape[i] != 1:
             if st[i] != run:
                 raise ValueError(f"{what}: the values of a token must be contiguous")
-            run *= shape[i]
-    into.data, into.batch_stride, into.token_stride = t.data_ptr(), st[0], st[1]
+            run *= t.shape[i]
+    into.batch_stride, into.token_stride = st[0], st[1] if lead == 2 else 0
 
 
 def _lengths(lengths, batch):
@@ -1225,54 +1233,57 @@ class CoShortConv:
             state = torch.zeros(shape, dtype=weight.dtype, device=weight.device)
         _need(state, weight.dtype, shape, "state")
         self.state = state
-        self._x, self._y = Tokens(), Tokens()
-        # the structures of a call are this object's: like a handle, it is one thread's
-        self._args = (ctypes.byref(self.desc), _ptr(weight), _ptr(bias), ctypes.byref(self._x),
-                      ctypes.byref(self._y))
+        self._call = ShortConvCall(_ptr(weight), _ptr(bias))
+        self._x, self._y = self._call.x, self._call.y
+        self._args = ctypes.byref(self.desc), ctypes.byref(self._call)
         self._sig = None
 
     receptive_field = property(lambda self: self.kernel)
     t_padding = property(lambda self: self.kernel - 1)
 
-    def _check(self, x, out):
-        T = x.shape[1] if x.dim() == 3 else -1
-        self._shape = (self.batch, T, self.channels)
-        _tokens(x, self.torch_dtype, self._shape, "x", self._x)
+    def _check(self, x, out, step, state, update):
+        B, C, call = self.batch, self.channels, self._call
+        T = 1 if step else x.shape[1] if x.dim() == 3 else -1
+        if x.dim() != 3 - step:
+            raise ValueError(f"x has shape {tuple(x.shape)}, expected "
+                             f"{(B, C) if step else (B, 'T', C)}")
+        _tokens(x, self.torch_dtype, (B, T, C), "x", self._x)
+        self._y.batch_stride, self._y.token_stride = T * C, C
         if out is not None:
-            _tokens(out, self.torch_dtype, self._shape, "out", self._y)
-        else:
-            self._y.batch_stride, self._y.token_stride = T * self.channels, self.channels
+            if out.dim() != x.dim():
+                raise ValueError(f"out has shape {tuple(out.shape)}, expected {tuple(x.shape)}")
+            _tokens(out, self.torch_dtype, (B, T, C), "out", self._y)
+        call.T, call.state, call.update_state = T, state, update
         self._dense = x.is_contiguous()
 
-    def _run(self, x, lengths, state, update, out):
-        sig = _signature(x), _signature(out)
+    def _run(self, x, lengths, state, update, out, step=False):
+        sig = (x.shape, x.stride(), x.dtype, x.is_cuda, state, update,
+               None if out is None else (out.shape, out.stride(), out.dtype, out.is_cuda))
         if sig != self._sig:
             self._sig = None
-            self._check(x, out)
+            self._check(x, out, step, state, update)
             self._sig = sig
-        shape = self._shape
         if out is None:
-            out = _like(x) if self._dense else x.new_empty(shape)
+            out = _like(x) if self._dense else x.new_empty(x.shape)
         self._x.data, self._y.data = x.data_ptr(), out.data_ptr()
-        d, w, b, px, py = self._args
-        st = co_shortconv_forward_steps(d, w, b, px, shape[1], _lengths(lengths, self.batch),
-                                        state, py, 1 if update else 0, _stream())
+        self._call.lengths = None if lengths is None else _lengths(lengths, self.batch)
+        pd, pc = self._args
+        st = co_shortconv_forward_steps(pd, pc, _stream())
         if st != CO_OK:
             check(st, "co_shortconv_forward_steps")
         return out
 
     def forward_steps(self, x, lengths=None, update_state=True, out=None):
         """The next T tokens x (B, T, C) of the streams -> (B, T, C)."""
-        return self._run(x, lengths, self.state.data_ptr(), update_state, out)
+        return self._run(x, lengths, self.state.data_ptr(), 1 if update_state else 0, out)
 
     def forward_step(self, x_t, lengths=None, update_state=True, out=None):
         """The next token x_t (B, C) of each stream (of those with length 1) -> (B, C)."""
-        out = out.unsqueeze(1) if out is not None else None
-        return self.forward_steps(x_t.unsqueeze(1), lengths, update_state, out)[:, 0]
+        return self._run(x_t, lengths, self.state.data_ptr(), 1 if update_state else 0, out, True)
 
     def forward(self, x, lengths=None, out=None):
         """Whole sequences from a clean state, which the layer's own is not touched by."""
-        return self._run(x, lengths, None, False, out)
+        return self._run(x, lengths, None, 0, out)
 
     def clean_state(self):
         self.state.zero_()
@@ -1311,11 +1322,9 @@ class CoScan:
             state = torch.zeros(shape, dtype=torch.float32, device=A.device)
         _need(state, torch.float32, shape, "state")
         self.state = state
-        self._io = ScanIO()
-        self._args = (ctypes.byref(self.desc), _ptr(self.A), _ptr(self.D), _ptr(self.dt_bias),
-                      ctypes.byref(self._io))
-        io = self._io
-        self._parts = io.x, io.dt, io.b, io.c, io.y
+        call = self._call = ScanCall(_ptr(self.A), _ptr(self.D), _ptr(self.dt_bias))
+        self._parts = call.x, call.dt, call.b, call.c, call.y
+        self._args = ctypes.byref(self.desc), ctypes.byref(call)
         self._sig = None
 
     def workspace_bytes(self, T):
@@ -1325,58 +1334,68 @@ class CoScan:
               "co_scan_workspace_bytes")
         return nb.value
 
-    def _check(self, x, dt, b, c, out):
-        B, H, P, io = self.batch, self.heads, self.head_dim, self._io
-        T = x.shape[1] if x.dim() == 4 else -1
-        bc = (B, T, self.groups, self.state_size)
+    def _check(self, x, dt, b, c, out, step, state, update):
+        B, H, P, call = self.batch, self.heads, self.head_dim, self._call
+        T = 1 if step else x.shape[1] if x.dim() == 4 else -1
         dtype = self.torch_dtype
-        self._shape = (B, T, H, P)
-        _tokens(x, dtype, self._shape, "x", io.x)
-        _tokens(b, dtype, bc, "b", io.b)
-        _tokens(c, dtype, bc, "c", io.c)
         dt_dtype = torch.float32 if dt.dtype is torch.float32 else dtype
-        _tokens(dt, dt_dtype, (B, T, H), "dt", io.dt)
+        bc = (B, T, self.groups, self.state_size)
+        for t, kind, shape, what, into in ((x, dtype, (B, T, H, P), "x", call.x),
+                                           (dt, dt_dtype, (B, T, H), "dt", call.dt),
+                                           (b, dtype, bc, "b", call.b),
+                                           (c, dtype, bc, "c", call.c),
+                                           (out, dtype, (B, T, H, P), "out", call.y)):
+            if t is None:
+                into.batch_stride, into.token_stride = T * H * P, H * P
+                continue
+            if t.dim() != len(shape) - step:
+                raise ValueError(f"{what} has shape {tuple(t.shape)}, expected "
+                                 f"{shape[:1] + shape[2:] if step else shape}")
+            _tokens(t, kind, shape, what, into)
         self.desc.dt_dtype = DTYPES[dt_dtype]
-        if out is not None:
-            _tokens(out, dtype, self._shape, "out", io.y)
-        else:
-            io.y.batch_stride, io.y.token_stride = T * H * P, H * P
+        call.T, call.state, call.update_state = T, state, update
         self._dense = x.is_contiguous()
-        self._nws = self.workspace_bytes(T)
+        self._nws = call.workspace_bytes = self.workspace_bytes(T)
 
-    def _run(self, x, dt, b, c, lengths, state, update, out):
-        sig = _signature(x), _signature(dt), _signature(b), _signature(c), _signature(out)
+    def _run(self, x, dt, b, c, lengths, state, update, out, step=False):
+        sig = (x.shape, x.stride(), x.dtype, x.is_cuda, dt.shape, dt.stride(), dt.dtype,
+               dt.is_cuda, b.shape, b.stride(), b.dtype, b.is_cuda, c.shape, c.stride(), c.dtype,
+               c.is_cuda, state, update,
+               None if out is None else (out.shape, out.stride(), out.dtype, out.is_cuda))
         if sig != self._sig:
             self._sig = None
-            self._check(x, dt, b, c, out)
+            self._check(x, dt, b, c, out, step, state, update)
             self._sig = sig
-        shape, nws = self._shape, self._nws
         if out is None:
-            out = _like(x) if self._dense else x.new_empty(shape)
+            out = _like(x) if self._dense else x.new_empty(x.shape)
         ix, idt, ib, ic, iy = self._parts
         ix.data, idt.data, ib.data = x.data_ptr(), dt.data_ptr(), b.data_ptr()
         ic.data, iy.data = c.data_ptr(), out.data_ptr()
-        ws = torch.empty(nws, dtype=torch.uint8, device=x.device) if nws else None
-        d, A, D, bias, pio = self._args
-        st = co_scan_forward_steps(d, A, D, bias, pio, shape[1], _lengths(lengths, self.batch),
-                                   state, 1 if update else 0, _ptr(ws), nws, _stream())
+        call = self._call
+        call.lengths = None if lengths is None else _lengths(lengths, self.batch)
+        ws = None
+        if self._nws:
+            ws = torch.empty(self._nws, dtype=torch.uint8, device=x.device)
+            call.workspace = ws.data_ptr()
+        pd, pc = self._args
+        st = co_scan_forward_steps(pd, pc, _stream())
         if st != CO_OK:
             check(st, "co_scan_forward_steps")
         return out
 
     def forward_steps(self, x, dt, b, c, lengths=None, update_state=True, out=None):
         """The next T tokens: x (B, T, H, P), dt (B, T, H), b and c (B, T, G, N) -> (B, T, H, P)."""
-        return self._run(x, dt, b, c, lengths, self.state.data_ptr(), update_state, out)
+        return self._run(x, dt, b, c, lengths, self.state.data_ptr(), 1 if update_state else 0,
+                         out)
 
     def forward_step(self, x_t, dt_t, b_t, c_t, lengths=None, update_state=True, out=None):
         """The next token of each stream (of those with length 1): the same without T."""
-        out = out.unsqueeze(1) if out is not None else None
-        return self.forward_steps(x_t.unsqueeze(1), dt_t.unsqueeze(1), b_t.unsqueeze(1),
-                                  c_t.unsqueeze(1), lengths, update_state, out)[:, 0]
+        return self._run(x_t, dt_t, b_t, c_t, lengths, self.state.data_ptr(),
+                         1 if update_state else 0, out, True)
 
     def forward(self, x, dt, b, c, lengths=None, out=None):
         """Whole sequences from a clean state, which the layer's own is not touched by."""
-        return self._run(x, dt, b, c, lengths, None, False, out)
+        return self._run(x, dt, b, c, lengths, None, 0, out)
 
     def clean_state(self):
         self.state.zero_()
@@ -1416,13 +1435,10 @@ class CoNorm:
         self.gate, self.residual = gate, residual
         self.desc = NormDesc(0, 0, self.dim, groups, self.MODES[gate], self.MODES[residual], CO_F32,
                              CO_F32, eps)
-        self._x, self._z, self._r, self._y, self._o = (Tokens() for _ in range(5))
-        byref = ctypes.byref
-        self._args = (byref(self.desc), byref(self._x), byref(self._z) if gate else None,
-                      byref(self._r) if residual else None,
-                      byref(self._y) if residual != "after" else None,
-                      byref(self._o) if residual else None)
-        self._weight, self._scale = _ptr(self.weight), _ptr(self.scale)
+        call = self._call = NormCall(weight=_ptr(self.weight), scale=_ptr(self.scale))
+        self._x, self._z, self._r, self._y, self._o = (call.x, call.gate, call.residual, call.y,
+                                                       call.residual_out)
+        self._args = ctypes.byref(self.desc), ctypes.byref(call)
         self._sig = None
 
     def _rows(self, t, dtype, shape, what, into):
@@ -1433,7 +1449,7 @@ class CoNorm:
         if t.shape != shape:
             raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {tuple(shape)}")
         if t.numel() == 0:
-            into.data = into.batch_stride = into.token_stride = 0
+            into.batch_stride = into.token_stride = 0
             return
         try:
             v = t if t.dim() == 3 else t.view(-1, shape[-2] if t.dim() > 1 else 1, self.dim)
@@ -1441,36 +1457,42 @@ class CoNorm:
             raise ValueError(f"{what}: the leading axes must be evenly spaced") from None
         if self.dim != 1 and v.stride(2) != 1:
             raise ValueError(f"{what}: the values of a row must be contiguous")
-        into.data, into.batch_stride, into.token_stride = t.data_ptr(), v.stride(0), v.stride(1)
+        into.batch_stride, into.token_stride = v.stride(0), v.stride(1)
 
     def forward(self, x, gate=None, residual=None, out=None, residual_out=None):
         """x (..., D), gate of its shape and dtype, residual of its shape (float32 or
         bfloat16) -> y; (y, new residual) with residual "before"; the new residual
         with "after".  out may be x, residual_out may be residual."""
-        sig = (_signature(x), _signature(gate), _signature(residual), _signature(out),
-               _signature(residual_out))
+        sig = (x.shape, x.stride(), x.dtype, x.is_cuda,
+               None if gate is None else (gate.shape, gate.stride(), gate.dtype, gate.is_cuda),
+               None if residual is None else (residual.shape, residual.stride(), residual.dtype,
+                                              residual.is_cuda),
+               None if out is None else (out.shape, out.stride(), out.dtype, out.is_cuda),
+               None if residual_out is None else (residual_out.shape, residual_out.stride(),
+                                                  residual_out.dtype, residual_out.is_cuda))
         if sig != self._sig:
             self._sig = None
             self._check(x, gate, residual, out, residual_out)
             self._sig = sig
-        pd, px, pz, pr, py, po = self._args
+        form = self.residual
         self._x.data = x.data_ptr()
-        if pz is not None:
+        if gate is not None:
             self._z.data = gate.data_ptr()
-        if pr is not None:
+        if form is not None:
             if residual_out is None:
                 residual_out = _like(residual) if self._dense[1] else residual.new_empty(x.shape)
             self._r.data, self._o.data = residual.data_ptr(), residual_out.data_ptr()
-        if py is not None:
+        if form != "after":
             if out is None:
                 out = _like(x) if self._dense[0] else x.new_empty(x.shape)
             self._y.data = out.data_ptr()
-        st = co_norm_forward(pd, px, pz, pr, self._weight, self._scale, py, po, _stream())
+        pd, pc = self._args
+        st = co_norm_forward(pd, pc, _stream())
         if st != CO_OK:
             check(st, "co_norm_forward")
-        if py is None:
-            return residual_out
-        return out if pr is None else (out, residual_out)
+        if form is None:
+            return out
+        return residual_out if form == "after" else (out, residual_out)
 
     def _check(self, x, gate, residual, out, residual_out):
         if (gate is None) != (self.gate is None) or (residual is None) != (self.residual is None):
@@ -1535,9 +1557,9 @@ class Mixer:
         z, xbc, dt = u.split(self._columns, -1)
         s = self.scan
         x, b, c = conv(xbc).split(self._split, -1)
-        y = scan(x.unflatten(-1, (s.heads, s.head_dim)), dt,
-                 b.unflatten(-1, (s.groups, s.state_size)),
-                 c.unflatten(-1, (s.groups, s.state_size)))
+        lead = u.shape[:-1]
+        bc = lead + (s.groups, s.state_size)
+        y = scan(x.view(lead + (s.heads, s.head_dim)), dt, b.view(bc), c.view(bc))
         return self.norm.forward(y.view(z.shape), gate=z)
 
     def forward_steps(self, u, lengths=None, update_state=True):
@@ -1547,7 +1569,8 @@ class Mixer:
 
     def forward_step(self, u_t, lengths=None, update_state=True):
         """The next token u_t (B, W) of each stream (of those with length 1) -> (B, H P)."""
-        return self.forward_steps(u_t.unsqueeze(1), lengths, update_state)[:, 0]
+        return self._run(u_t, lambda v: self.conv.forward_step(v, lengths, update_state),
+                         lambda *v: self.scan.forward_step(*v, lengths, update_state))
 
     def forward(self, u, lengths=None):
         """Whole sequences from a clean state, which the mixer's own is not touched by."""

@@ -245,31 +245,21 @@ hipError_t launch_add_frames(const void* a, const void* x, void* y, int64_t rows
 
 // Token layers (short_conv.hip, scan_seq.hip, scan_chunk.hip, norm.hip); the
 // entry points (token_api.hip) have checked every argument.
-hipError_t launch_shortconv(const co_shortconv_desc& d, const void* weight, const void* bias,
-                            const co_tokens& x, int32_t T, const int32_t* lengths, void* state,
-                            const co_tokens& y, bool update, hipStream_t stream);
+hipError_t launch_shortconv(const co_shortconv_desc& d, const co_shortconv_call& c,
+                            hipStream_t stream);
 
-// What a scan kernel needs beside its tensors.
+// What a scan kernel takes.
 struct ScanCall {
   co_scan_desc d;
-  co_scan_io io;
-  const float* A;
-  const float* D;
-  const float* dt_bias;
-  const int32_t* lengths;
-  float* state;  // null: from zero, none left
-  int32_t T;
-  int32_t update;
+  co_scan_call c;
 };
 // Token by token, any call.
 hipError_t launch_scan_seq(const ScanCall& c, hipStream_t stream);
-// In chunks on the matrix cores, with a workspace of so many bytes at 16-byte alignment.
+// In chunks on the matrix cores, with a workspace of so many bytes.
 bool scan_chunk_takes(const co_scan_desc& d, int32_t T);
 int64_t scan_chunk_workspace(const co_scan_desc& d, int32_t T);
-hipError_t launch_scan_chunk(const ScanCall& c, void* workspace, hipStream_t stream);
+hipError_t launch_scan_chunk(const ScanCall& c, hipStream_t stream);
 
-hipError_t launch_norm(const co_norm_desc& d, const co_tokens& x, const co_tokens& gate,
-                       const co_tokens& residual, const float* weight, const float* scale,
-                       const co_tokens& y, const co_tokens& residual_out, hipStream_t stream);
+hipError_t launch_norm(const co_norm_desc& d, const co_norm_call& c, hipStream_t stream);
 
 }  // namespace coinf

@@ -61,7 +61,6 @@ __device__ __forceinline__ void load_vec(const float* p, int64_t at, float (&o)[
 // T: x, z, y.  R: the residual.  L lanes a part, NV packs of V values a lane.
 template <typename T, typename R, int GATE, int RES, int L, int V, int NV>
 __device__ __forceinline__ void norm_parts(const NormArgs& a, uint32_t part0) {
-  constexpr int PER = L < 256 ? 256 / L : 1;  // parts a workgroup
   constexpr int WAVES = L / 64;
   // a residual of 4 bytes beside values of 2 comes in two 16-byte pieces
   constexpr int RV = V * int(sizeof(R)) > 16 ? V / 2 : V;
@@ -158,7 +157,7 @@ __device__ __forceinline__ void norm_parts(const NormArgs& a, uint32_t part0) {
 
 template <typename T, typename R, int GATE, int RES, int L, int V, int NV>
 __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_kernel(NormArgs a) {
-  constexpr int PER = L < 256 ? 256 / L : 1;
+  constexpr int PER = L < 256 ? 256 / L : 1;  // parts a workgroup
   const uint32_t by = gridDim.x * PER;  // at most 2^23: no sum here passes 32 bits
   for (uint32_t part = blockIdx.x * PER; part < a.parts; part += by) {
     norm_parts<T, R, GATE, RES, L, V, NV>(a, part);
@@ -217,10 +216,8 @@ hipError_t launch_t(const NormArgs& a, int gate, int res, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_norm(const co_norm_desc& d, const co_tokens& x, const co_tokens& gate,
-                       const co_tokens& residual, const float* weight, const float* scale,
-                       const co_tokens& y, const co_tokens& residual_out, hipStream_t stream) {
-  const NormArgs a{x, gate, residual, y, residual_out, weight, scale,
+hipError_t launch_norm(const co_norm_desc& d, const co_norm_call& c, hipStream_t stream) {
+  const NormArgs a{c.x, c.gate, c.residual, c.y, c.residual_out, c.weight, c.scale,
                    uint32_t(int64_t(d.batch) * d.tokens * d.groups), uint32_t(d.groups),
                    uint32_t(d.tokens), d.dim / d.groups, d.eps};
   const bool r16 = d.residual && d.residual_dtype == CO_BF16;

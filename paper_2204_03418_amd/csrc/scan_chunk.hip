@@ -310,7 +310,7 @@ constexpr int kHeads = 4;
 template <typename T, bool WIDE>
 __global__ __launch_bounds__(kBlock) void scan_prepare_kernel(ChunkArgs a) {
   const co_scan_desc& d = a.c.d;
-  const co_scan_io& io = a.c.io;
+  const co_scan_call& io = a.c.c;
   const int lane = threadIdx.x % 64, g16 = lane / 16, l16 = lane % 16;
   const uint32_t doubles = uint32_t(a.chunks + 1) / 2;
   const int two = int(blockIdx.x % doubles), b = int(blockIdx.x / doubles);
@@ -318,7 +318,7 @@ __global__ __launch_bounds__(kBlock) void scan_prepare_kernel(ChunkArgs a) {
                   __builtin_amdgcn_readfirstlane(int(threadIdx.x / 64));
   const int head_jobs = (d.heads + kHeads - 1) / kHeads;
   if (job >= head_jobs + 2 * d.groups) return;
-  const int len = stream_tokens(a.c.lengths, b, a.c.T);
+  const int len = stream_tokens(a.c.c.lengths, b, a.c.c.T);
   if (job >= head_jobs) {
     const int j = job - head_jobs, group = j / 2, chunk = 2 * two + j % 2;
     if (chunk >= a.chunks) return;
@@ -372,15 +372,15 @@ __global__ __launch_bounds__(kBlock) void scan_prepare_kernel(ChunkArgs a) {
   const int64_t t = int64_t(two) * 64 + lane;
   const int chunk = 2 * two + lane / 32, q = lane % 32;
   // read whether or not the stream has the token, so that its length is not waited for first
-  const int64_t at = b * io.dt.batch_stride + min(t, int64_t(a.c.T - 1)) * io.dt.token_stride;
+  const int64_t at = b * io.dt.batch_stride + min(t, int64_t(a.c.c.T - 1)) * io.dt.token_stride;
   float raw[kHeads], bias[kHeads], A2[kHeads];
 #pragma unroll
   for (int i = 0; i < kHeads; ++i) {
     const int h = min(job * kHeads + i, d.heads - 1);
     raw[i] = d.dt_dtype == CO_BF16 ? bf16_to_f32(static_cast<const bf16_t*>(io.dt.data)[at + h])
                                    : static_cast<const float*>(io.dt.data)[at + h];
-    bias[i] = a.c.dt_bias ? a.c.dt_bias[h] : 0.f;
-    A2[i] = a.c.A[h] * kLog2e;
+    bias[i] = a.c.c.dt_bias ? a.c.c.dt_bias[h] : 0.f;
+    A2[i] = a.c.c.A[h] * kLog2e;
   }
 #pragma unroll
   for (int i = 0; i < kHeads; ++i) {
@@ -431,7 +431,7 @@ __global__ __launch_bounds__(kWaves * 64, !FULL && sizeof(T) == 2 ? 3 : 2) void 
   __shared__ __align__(16) unsigned char lds[BUFS * sizeof(L)];
 
   const co_scan_desc& d = a.c.d;
-  const co_scan_io& io = a.c.io;
+  const co_scan_call& io = a.c.c;
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int g16 = lane / 16, l16 = lane % 16;
@@ -458,9 +458,9 @@ __global__ __launch_bounds__(kWaves * 64, !FULL && sizeof(T) == 2 ? 3 : 2) void 
   const int width = on ? min(P - p0, L::PW) : 0;    // its rows of the head
   const int64_t bh = int64_t(b) * d.heads + h;
 
-  const int len = stream_tokens(a.c.lengths, b, a.c.T);
+  const int len = stream_tokens(a.c.c.lengths, b, a.c.c.T);
   const int64_t t_begin = int64_t(seg) * a.seg_chunks * Q;
-  const int64_t t_stop = min(int64_t(a.c.T), t_begin + int64_t(a.seg_chunks) * Q);
+  const int64_t t_stop = min(int64_t(a.c.c.T), t_begin + int64_t(a.seg_chunks) * Q);
   const int64_t t_end = min(int64_t(len), t_stop);
 
   const T* xg = static_cast<const T*>(io.x.data) + b * io.x.batch_stride + int64_t(h) * P + p0;
@@ -511,12 +511,12 @@ __global__ __launch_bounds__(kWaves * 64, !FULL && sizeof(T) == 2 ? 3 : 2) void 
   if (FULL) {
     if (a.segments > 1)
       first = a.ws_state + ((bh * a.segments + seg) * P + p0) * N;
-    else if (a.c.state)
-      first = a.c.state + (bh * P + p0) * N;
+    else if (a.c.c.state)
+      first = a.c.c.state + (bh * P + p0) * N;
   }
   if (first) each_state(first, [](auto& mem, auto& s) { s = mem; });
 
-  const float D = a.c.D ? a.c.D[h] : 0.f;
+  const float D = a.c.c.D ? a.c.c.D[h] : 0.f;
   const int64_t chunk0 = int64_t(seg) * a.seg_chunks;
   const ChunkDecay* decay = a.ws_decay + bh * a.chunks + chunk0;
   const f32x4* bc_at =
@@ -800,8 +800,8 @@ __global__ __launch_bounds__(kWaves * 64, !FULL && sizeof(T) == 2 ? 3 : 2) void 
     const int64_t from = t_begin < t_end ? t_begin + (t_end - t_begin + Q - 1) / Q * Q : t_begin;
     for (int64_t t = from + lane / 16; t < t_stop; t += 4)
       for (int p = l16; p < width; p += 16) yg[t * io.y.token_stride + p] = T{};
-    if (a.c.update && seg == a.segments - 1 && len > 0)
-      each_state(a.c.state + (bh * P + p0) * N, [](auto& mem, auto& s) { mem = s; });
+    if (a.c.c.state && a.c.c.update_state && seg == a.segments - 1 && len > 0)
+      each_state(a.c.c.state + (bh * P + p0) * N, [](auto& mem, auto& s) { mem = s; });
   } else {
     each_state(a.ws_state + ((bh * a.segments + seg) * P + p0) * N,
                [](auto& mem, auto& s) { mem = s; });
@@ -820,7 +820,7 @@ __global__ __launch_bounds__(kBlock) void scan_carry_kernel(ChunkArgs a, uint32_
   float* w = a.ws_state + bh * a.segments * size + i;
   const float* total = a.ws_total + bh * a.segments;
   P s{};
-  if (a.c.state) s = load_pack<float, V>(a.c.state + bh * size + i);
+  if (a.c.c.state) s = load_pack<float, V>(a.c.c.state + bh * size + i);
   const int last = a.segments - 1;
   constexpr int AHEAD = 8;  // loads in flight
   for (int k0 = 0; k0 < last; k0 += AHEAD) {
@@ -891,7 +891,7 @@ hipError_t launch_tiles(ChunkArgs a, hipStream_t s) {
 template <typename T, bool WIDE>
 hipError_t launch_state(const ChunkArgs& a, hipStream_t s) {
   const int N = a.c.d.state_size;
-  if (unit_rows(a.c.d, a.c.T) == 32) {
+  if (unit_rows(a.c.d, a.c.c.T) == 32) {
     if (N <= 32) return launch_tiles<T, 2, 2, WIDE>(a, s);
     if (N <= 64) return launch_tiles<T, 4, 2, WIDE>(a, s);
     return launch_tiles<T, 8, 2, WIDE>(a, s);
@@ -909,12 +909,12 @@ hipError_t launch_t(const ChunkArgs& a, hipStream_t s) {
     return reinterpret_cast<uintptr_t>(t.data) % 16 == 0 && t.batch_stride % V == 0 &&
            t.token_stride % V == 0 && t.token_stride < (1 << 22);
   };
-  const co_scan_io& io = a.c.io;
+  const co_scan_call& io = a.c.c;
   // 16-byte accesses where every one of them is aligned and a chunk's offsets take 31 bits, values
   // otherwise
   const bool fits = a.c.d.head_dim % V == 0 && a.c.d.state_size % V == 0 && wide(io.x) &&
                     wide(io.b) && wide(io.c) && wide(io.y) &&
-                    reinterpret_cast<uintptr_t>(a.c.state) % 16 == 0 &&
+                    reinterpret_cast<uintptr_t>(a.c.c.state) % 16 == 0 &&
                     reinterpret_cast<uintptr_t>(a.ws_state) % 16 == 0;
   return fits ? launch_state<T, true>(a, s) : launch_state<T, false>(a, s);
 }
@@ -973,12 +973,12 @@ int64_t scan_chunk_workspace(const co_scan_desc& d, int32_t T) {
   return space_of(d, (int64_t(T) + kChunk - 1) / kChunk, segments).bytes;
 }
 
-hipError_t launch_scan_chunk(const ScanCall& c, void* workspace, hipStream_t stream) {
+hipError_t launch_scan_chunk(const ScanCall& c, hipStream_t stream) {
   int64_t segments, seg_chunks;
-  cut(c.d, c.T, &segments, &seg_chunks);
-  const int64_t chunks = (int64_t(c.T) + kChunk - 1) / kChunk;
+  cut(c.d, c.c.T, &segments, &seg_chunks);
+  const int64_t chunks = (int64_t(c.c.T) + kChunk - 1) / kChunk;
   const Space at = space_of(c.d, chunks, segments);
-  char* w = static_cast<char*>(workspace);
+  char* w = static_cast<char*>(c.c.workspace);
   ChunkArgs a{};
   a.c = c;
   a.ws_bc = reinterpret_cast<f32x4*>(w);

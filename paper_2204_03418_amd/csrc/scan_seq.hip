@@ -62,7 +62,7 @@ __device__ __forceinline__ float reduce_rows(float (&v)[ROWS], int nl) {
   }
 }
 
-__device__ __forceinline__ float load_dt(const co_scan_io& io, int dt_dtype, int64_t at) {
+__device__ __forceinline__ float load_dt(const co_scan_call& io, int dt_dtype, int64_t at) {
   return dt_dtype == CO_BF16 ? bf16_to_f32(static_cast<const bf16_t*>(io.dt.data)[at])
                              : static_cast<const float*>(io.dt.data)[at];
 }
@@ -90,7 +90,7 @@ template <typename T, int NL, int ROWS, bool WIDE, bool ONE>
 __global__ __launch_bounds__(kBlock) void scan_seq_kernel(SeqArgs a) {
   constexpr int GROUPS = kBlock / NL;
   const co_scan_desc& d = a.c.d;
-  const co_scan_io& io = a.c.io;
+  const co_scan_call& io = a.c.c;
   const int nl = threadIdx.x % NL, group = threadIdx.x / NL;
   const int pb = int(blockIdx.x % uint32_t(a.p_blocks));
   const int bh = int(blockIdx.x / uint32_t(a.p_blocks));
@@ -98,14 +98,14 @@ __global__ __launch_bounds__(kBlock) void scan_seq_kernel(SeqArgs a) {
   const int g = h / (d.heads / d.groups);
   const int P = d.head_dim, N = d.state_size;
   const int p0 = (pb * GROUPS + group) * ROWS;
-  const int len = stream_tokens(a.c.lengths, b, a.c.T);
+  const int len = stream_tokens(a.c.c.lengths, b, a.c.c.T);
 
   const T* xp = static_cast<const T*>(io.x.data) + b * io.x.batch_stride + int64_t(h) * P + p0;
   const T* bp = static_cast<const T*>(io.b.data) + b * io.b.batch_stride + int64_t(g) * N;
   const T* cp = static_cast<const T*>(io.c.data) + b * io.c.batch_stride + int64_t(g) * N;
   T* yp = static_cast<T*>(io.y.data) + b * io.y.batch_stride + int64_t(h) * P + p0;
   const int64_t dt0 = b * io.dt.batch_stride + h;
-  float* sp = a.c.state ? a.c.state + (int64_t(bh) * P + p0) * N : nullptr;
+  float* sp = a.c.c.state ? a.c.c.state + (int64_t(bh) * P + p0) * N : nullptr;
 
   const auto load_token = [&](int t) {
     Token<T, ROWS> k;
@@ -134,8 +134,8 @@ __global__ __launch_bounds__(kBlock) void scan_seq_kernel(SeqArgs a) {
       for (int j = 0; j < 4; ++j) S[r][j] = v.v[j];
     }
   }
-  const float A2 = a.c.A[h] * kLog2e, D = a.c.D ? a.c.D[h] : 0.f;
-  const float bias = a.c.dt_bias ? a.c.dt_bias[h] : 0.f;
+  const float A2 = a.c.c.A[h] * kLog2e, D = a.c.c.D ? a.c.c.D[h] : 0.f;
+  const float bias = a.c.c.dt_bias ? a.c.c.dt_bias[h] : 0.f;
   constexpr int STEP = NL / ROWS;  // lanes that end with the same row
   const int row = nl / STEP;
   // d_t and e^{d_t A}: of 64 tokens at once, a token a lane, in every wave
@@ -174,10 +174,10 @@ __global__ __launch_bounds__(kBlock) void scan_seq_kernel(SeqArgs a) {
     if (ONE) break;
     now = next;
   }
-  for (int t = len; t < a.c.T; ++t)
+  for (int t = len; t < a.c.c.T; ++t)
     if (nl % STEP == 0 && p0 + row < P) yp[t * io.y.token_stride + row] = T{};
 
-  if (a.c.update && len > 0) {
+  if (a.c.c.state && a.c.c.update_state && len > 0) {
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
       if (p0 + r >= P) break;
@@ -203,7 +203,7 @@ hipError_t launch_rows(const ScanCall& c, bool wide, hipStream_t s) {
     hipLaunchKernelGGL(kernel, dim3(unsigned(grid)), dim3(kBlock), 0, s, a);
     return hipGetLastError();
   };
-  if (c.T == 1)
+  if (c.c.T == 1)
     return wide ? go(scan_seq_kernel<T, NL, ROWS, true, true>)
                 : go(scan_seq_kernel<T, NL, ROWS, false, true>);
   return wide ? go(scan_seq_kernel<T, NL, ROWS, true, false>)
@@ -232,8 +232,8 @@ hipError_t launch_t(const ScanCall& c, hipStream_t s) {
     return at(t.data, n * sizeof(T)) && t.batch_stride % n == 0 && t.token_stride % n == 0;
   };
   // a state row, and the rows that a thread has of x, in whole pieces
-  const bool wide = N % 4 == 0 && c.d.head_dim % 8 == 0 && at(c.state, 16) && by(c.io.b, 4) &&
-                    by(c.io.c, 4) && by(c.io.x, 8);
+  const bool wide = N % 4 == 0 && c.d.head_dim % 8 == 0 && at(c.c.state, 16) && by(c.c.b, 4) &&
+                    by(c.c.c, 4) && by(c.c.x, 8);
   if (N <= 16) return launch_lanes<T, 4>(c, wide, s);
   if (N <= 32) return launch_lanes<T, 8>(c, wide, s);
   if (N <= 64) return launch_lanes<T, 16>(c, wide, s);

@@ -196,11 +196,11 @@ hipError_t launch_t(const ConvCall& a, int32_t B, int32_t K, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_shortconv(const co_shortconv_desc& d, const void* weight, const void* bias,
-                            const co_tokens& x, int32_t T, const int32_t* lengths, void* state,
-                            const co_tokens& y, bool update, hipStream_t stream) {
-  ConvCall a{weight, bias, x.data, y.data, state, lengths, x.batch_stride, x.token_stride,
-             y.batch_stride, y.token_stride, d.channels, T, d.act, update && state ? 1 : 0, 0, 0, 1};
+hipError_t launch_shortconv(const co_shortconv_desc& d, const co_shortconv_call& c,
+                            hipStream_t stream) {
+  const ConvCall a{c.weight, d.has_bias ? c.bias : nullptr, c.x.data, c.y.data, c.state, c.lengths,
+                   c.x.batch_stride, c.x.token_stride, c.y.batch_stride, c.y.token_stride,
+                   d.channels, c.T, d.act, c.update_state && c.state ? 1 : 0, 0, 0, 1};
   if (d.dtype == CO_BF16) return launch_t<bf16_t>(a, d.batch, d.kernel, stream);
   return launch_t<float>(a, d.batch, d.kernel, stream);
 }

@@ -78,24 +78,21 @@ co_status co_shortconv_query(const co_shortconv_desc* desc, int64_t* state_bytes
   return CO_OK;
 }
 
-co_status co_shortconv_forward_steps(const co_shortconv_desc* desc, const void* weight,
-                                     const void* bias, const co_tokens* x, int32_t T,
-                                     const int32_t* lengths, void* state, const co_tokens* y,
-                                     int32_t update_state, void* stream) {
-  if (!shortconv_ok(desc) || T < 0 || !x || !y || !weight) return CO_EINVAL;
-  if (desc->has_bias && !bias) return CO_EINVAL;
+co_status co_shortconv_forward_steps(const co_shortconv_desc* desc, const co_shortconv_call* call,
+                                     void* stream) {
+  if (!shortconv_ok(desc) || !call || call->T < 0 || !call->weight) return CO_EINVAL;
+  if (desc->has_bias && !call->bias) return CO_EINVAL;
+  const int32_t T = call->T, dt = desc->dtype;
   if (T == 0) return CO_OK;
-  const int32_t dt = desc->dtype;
-  if (!tokens_ok(*x, desc->batch, T, dt) || !out_ok(*y, desc->batch, T, desc->channels, dt))
+  if (!tokens_ok(call->x, desc->batch, T, dt) ||
+      !out_ok(call->y, desc->batch, T, desc->channels, dt) || call->x.data == call->y.data)
     return CO_EINVAL;
-  if (x->data == y->data) return CO_EINVAL;
-  if (!aligned(weight, elem(dt)) || !aligned(bias, elem(dt)) || !aligned(state, elem(dt)) ||
-      !aligned(lengths, 4))
+  if (!aligned(call->weight, elem(dt)) || !aligned(call->bias, elem(dt)) ||
+      !aligned(call->state, elem(dt)) || !aligned(call->lengths, 4))
     return CO_EINVAL;
   if (mul_to(mul_to(desc->batch, desc->channels, kMaxValues), T, kMaxValues) < 0)
     return CO_EINVAL;
-  return done(launch_shortconv(*desc, weight, desc->has_bias ? bias : nullptr, *x, T, lengths,
-                               state, *y, update_state != 0, as_stream(stream)));
+  return done(launch_shortconv(*desc, *call, as_stream(stream)));
 }
 
 co_status co_scan_query(const co_scan_desc* desc, int64_t* state_bytes) {
@@ -110,34 +107,31 @@ co_status co_scan_workspace_bytes(const co_scan_desc* desc, int32_t T, int64_t* 
   return CO_OK;
 }
 
-co_status co_scan_forward_steps(const co_scan_desc* desc, const float* A, const float* D,
-                                const float* dt_bias, const co_scan_io* io, int32_t T,
-                                const int32_t* lengths, float* state, int32_t update_state,
-                                void* workspace, int64_t workspace_bytes, void* stream) {
-  if (!scan_ok(desc) || T < 0 || !io || !A || workspace_bytes < 0) return CO_EINVAL;
+co_status co_scan_forward_steps(const co_scan_desc* desc, const co_scan_call* call, void* stream) {
+  if (!scan_ok(desc) || !call || call->T < 0 || !call->A || call->workspace_bytes < 0)
+    return CO_EINVAL;
+  const int32_t B = desc->batch, T = call->T, dt = desc->dtype;
   if (T == 0) return CO_OK;
-  const int32_t B = desc->batch, dt = desc->dtype;
   const int32_t inner = desc->heads * desc->head_dim;
-  if (!tokens_ok(io->x, B, T, dt) || !tokens_ok(io->b, B, T, dt) || !tokens_ok(io->c, B, T, dt) ||
-      !tokens_ok(io->dt, B, T, desc->dt_dtype) || !out_ok(io->y, B, T, inner, dt))
+  if (!tokens_ok(call->x, B, T, dt) || !tokens_ok(call->b, B, T, dt) ||
+      !tokens_ok(call->c, B, T, dt) || !tokens_ok(call->dt, B, T, desc->dt_dtype) ||
+      !out_ok(call->y, B, T, inner, dt))
     return CO_EINVAL;
-  if (io->y.data == io->x.data || io->y.data == io->b.data || io->y.data == io->c.data ||
-      io->y.data == io->dt.data)
+  const void* y = call->y.data;
+  if (y == call->x.data || y == call->b.data || y == call->c.data || y == call->dt.data)
     return CO_EINVAL;
-  if (!aligned(A, 4) || !aligned(D, 4) || !aligned(dt_bias, 4) || !aligned(state, 4) ||
-      !aligned(lengths, 4) || !aligned(workspace, 16))
+  if (!aligned(call->A, 4) || !aligned(call->D, 4) || !aligned(call->dt_bias, 4) ||
+      !aligned(call->state, 4) || !aligned(call->lengths, 4) || !aligned(call->workspace, 16))
     return CO_EINVAL;
   if (mul_to(mul_to(B, inner, kMaxValues), T, kMaxValues) < 0) return CO_EINVAL;
-  ScanCall c{*desc, *io, A, D, dt_bias, lengths, state, T, update_state && state ? 1 : 0};
-  if (scan_chunk_takes(*desc, T) && workspace &&
-      workspace_bytes >= scan_chunk_workspace(*desc, T))
-    return done(launch_scan_chunk(c, workspace, as_stream(stream)));
+  const ScanCall c{*desc, *call};
+  if (scan_chunk_takes(*desc, T) && call->workspace &&
+      call->workspace_bytes >= scan_chunk_workspace(*desc, T))
+    return done(launch_scan_chunk(c, as_stream(stream)));
   return done(launch_scan_seq(c, as_stream(stream)));
 }
 
-co_status co_norm_forward(const co_norm_desc* desc, const co_tokens* x, const co_tokens* gate,
-                          const co_tokens* residual, const float* weight, const float* scale,
-                          const co_tokens* y, const co_tokens* residual_out, void* stream) {
+co_status co_norm_forward(const co_norm_desc* desc, const co_norm_call* call, void* stream) {
   if (!desc || desc->batch < 0 || desc->tokens < 0 || desc->dim <= 0 || desc->groups <= 0 ||
       desc->dim % desc->groups || !dtype_ok(desc->dtype) || !dtype_ok(desc->residual_dtype))
     return CO_EINVAL;
@@ -145,25 +139,23 @@ co_status co_norm_forward(const co_norm_desc* desc, const co_tokens* x, const co
       desc->residual > CO_NORM_AFTER || !(desc->eps >= 0.f) || !std::isfinite(desc->eps))
     return CO_EINVAL;
   if (desc->dim / desc->groups > CO_NORM_MAX_WIDTH) return CO_ENOTSUP;
-  const int64_t rows = int64_t(desc->batch) * desc->tokens;
-  if (mul_to(rows, desc->groups, INT32_MAX) < 0) return CO_ENOTSUP;
-  if (rows == 0) return CO_OK;
-  const auto in_ok = [&](const co_tokens* t, int32_t dtype) {
-    return t && tokens_ok(*t, desc->batch, desc->tokens, dtype);
-  };
-  const auto result_ok = [&](const co_tokens* t, int32_t dtype) {
-    return t && out_ok(*t, desc->batch, desc->tokens, desc->dim, dtype);
-  };
-  const int32_t dt = desc->dtype, rt = desc->residual_dtype;
-  if (!in_ok(x, dt)) return CO_EINVAL;
-  if (desc->gate && !in_ok(gate, dt)) return CO_EINVAL;
-  if (desc->residual && (!in_ok(residual, rt) || !result_ok(residual_out, rt))) return CO_EINVAL;
-  if (desc->residual != CO_NORM_AFTER && !result_ok(y, dt)) return CO_EINVAL;
-  if (!aligned(weight, 4) || !aligned(scale, 4)) return CO_EINVAL;
+  const int32_t B = desc->batch, T = desc->tokens, dt = desc->dtype, rt = desc->residual_dtype;
+  if (mul_to(int64_t(B) * T, desc->groups, INT32_MAX) < 0) return CO_ENOTSUP;
+  if (B == 0 || T == 0) return CO_OK;
+  if (!call || !tokens_ok(call->x, B, T, dt)) return CO_EINVAL;
+  if (desc->gate && !tokens_ok(call->gate, B, T, dt)) return CO_EINVAL;
+  if (desc->residual &&
+      (!tokens_ok(call->residual, B, T, rt) || !out_ok(call->residual_out, B, T, desc->dim, rt)))
+    return CO_EINVAL;
+  if (desc->residual != CO_NORM_AFTER && !out_ok(call->y, B, T, desc->dim, dt)) return CO_EINVAL;
+  if (!aligned(call->weight, 4) || !aligned(call->scale, 4)) return CO_EINVAL;
+  // what the form does not have takes no part in the choice of a kernel
+  co_norm_call c = *call;
   const co_tokens none{nullptr, 0, 0};
-  return done(launch_norm(*desc, *x, desc->gate ? *gate : none, desc->residual ? *residual : none,
-                          weight, scale, desc->residual != CO_NORM_AFTER ? *y : none,
-                          desc->residual ? *residual_out : none, as_stream(stream)));
+  if (!desc->gate) c.gate = none;
+  if (!desc->residual) c.residual = c.residual_out = none;
+  if (desc->residual == CO_NORM_AFTER) c.y = none;
+  return done(launch_norm(*desc, c, as_stream(stream)));
 }
 
 }  // extern "C"

@@ -611,14 +611,14 @@ def test_scan_without_workspace(dtype):
     d = {k: v[k].to(DEV) for k in ("x", "dt", "b", "c")}
     assert layer.workspace_bytes(90) > 0
     y = torch.empty_like(d["x"])
-    io = coinf.ScanIO(*(coinf.Tokens(t.data_ptr(), t.stride(0), t.stride(1))
-                        for t in (d["x"], d["dt"], d["b"], d["c"], y)))
+    parts = [coinf.Tokens(t.data_ptr(), t.stride(0), t.stride(1))
+             for t in (d["x"], d["dt"], d["b"], d["c"], y)]
     for ws, nws in ((None, 0), (layer.state.data_ptr(), 16)):
         layer.state.copy_(v["state"])
-        st = coinf.co_scan_forward_steps(
-            ctypes.byref(layer.desc), layer.A.data_ptr(), layer.D.data_ptr(),
-            layer.dt_bias.data_ptr(), ctypes.byref(io), 90, None, layer.state.data_ptr(), 1, ws,
-            nws, torch.cuda.current_stream().cuda_stream)
+        call = coinf.ScanCall(layer.A.data_ptr(), layer.D.data_ptr(), layer.dt_bias.data_ptr(),
+                              *parts, None, layer.state.data_ptr(), ws, nws, 90, 1)
+        st = coinf.co_scan_forward_steps(ctypes.byref(layer.desc), ctypes.byref(call),
+                                         torch.cuda.current_stream().cuda_stream)
         assert st == coinf.CO_OK
         check_scan(case, y, layer.state, scan_ref(case, v, v["state"], None), "no workspace")
 
@@ -665,3 +665,49 @@ def test_scan_tokens_far_apart():
     got = layer.forward(x, *(d[k] for k in ("dt", "b", "c")))
     y, size, _, _ = scan_ref(case, v, None, None)
     R.within(got, y, U[F32] * np.abs(y) + (4 * 70 + 96) * R.U32 * size, "far tokens")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_single_token_forms(dtype):
+    """forward_step is forward_steps of one token, bit for bit: slices, an out
+    tensor, streams without a token, no update; and its refusals."""
+    g = gen(61)
+    B, H, P, G, N = 3, 4, 16, 2, 20
+    n = torch.tensor([1, 0, 1], dtype=torch.int32, device=DEV)
+    wide = randn(g, B, H * P + 2 * G * N + H, dtype=dtype).to(DEV)
+    x, b, c, dt = wide.split((H * P, G * N, G * N, H), -1)
+    x, b, c = x.view(B, H, P), b.view(B, G, N), c.view(B, G, N)
+    w = randn(g, H * P, 3, dtype=dtype).to(DEV)
+    xc = wide[:, 5:5 + H * P]
+    convs = [coinf.CoShortConv(w, batch=B) for _ in range(2)]
+    scans = [coinf.CoScan(-torch.ones(H, device=DEV), batch=B, head_dim=P, state_size=N, groups=G,
+                          dtype=dtype) for _ in range(2)]
+    for lengths, update in ((None, True), (n, True), (None, False), (n, False)):
+        out = torch.full((B, 2 * H * P), 7., dtype=dtype, device=DEV)
+        want = convs[0].forward_steps(xc[:, None], lengths, update)[:, 0]
+        got = convs[1].forward_step(xc, lengths, update, out=out[:, 3:3 + H * P])
+        assert torch.equal(got, want) and torch.equal(out[:, 3:3 + H * P], want)
+        assert (out[:, :3] == 7).all() and (out[:, 3 + H * P:] == 7).all()
+        assert torch.equal(convs[0].state, convs[1].state)
+        want = scans[0].forward_steps(x[:, None], dt[:, None], b[:, None], c[:, None], lengths,
+                                      update)[:, 0]
+        got = scans[1].forward_step(x, dt, b, c, lengths, update)
+        assert torch.equal(got, want) and torch.equal(scans[0].state, scans[1].state)
+        out = torch.full((B, 2, H, P), 7., dtype=dtype, device=DEV)
+        scans[1].forward_step(x, dt, b, c, lengths, False, out=out[:, 1])
+        assert (out[:, 0] == 7).all()
+    conv, scan = convs[0], scans[0]
+    for f in (lambda: conv.forward_step(xc[:, None]), lambda: conv.forward_steps(xc),
+              lambda: conv.forward(xc), lambda: conv.forward_step(xc[:2]),
+              lambda: conv.forward_step(xc, out=torch.empty_like(xc)[:, None]),
+              lambda: scan.forward_step(x[:, None], dt, b, c),
+              lambda: scan.forward_step(x, dt[:, None], b, c),
+              lambda: scan.forward_step(x, dt, b[:, None], c),
+              lambda: scan.forward_step(x, dt, b, c[:, :1]),
+              lambda: scan.forward_steps(x, dt, b, c),
+              lambda: scan.forward_step(x, dt, b, c, out=torch.empty_like(x)[:, None])):
+        with pytest.raises(ValueError):
+            f()
+    # a refused call leaves the next one's arguments checked anew
+    assert torch.equal(conv.forward_step(xc, update_state=False),
+                       convs[1].forward_step(xc, update_state=False))

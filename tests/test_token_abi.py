@@ -64,8 +64,8 @@ def test_scan_descriptors_refused(bad):
 
 
 def call_conv(d, x=(P, 80, 8), y=(2 * P, 80, 8), T=10, weight=P, bias=P, lengths=None, state=P):
-    return C.co_shortconv_forward_steps(ref(d), weight, bias, ref(C.Tokens(*x)), T, lengths, state,
-                                        ref(C.Tokens(*y)), 1, None)
+    c = C.ShortConvCall(weight, bias, C.Tokens(*x), C.Tokens(*y), lengths, state, T, 1)
+    return C.co_shortconv_forward_steps(ref(d), ref(c), None)
 
 
 def test_shortconv_arguments():
@@ -89,8 +89,9 @@ def test_shortconv_arguments():
 def call_scan(d, T=10, A=P, ws=None, nws=0, state=P, **io):
     t = dict(x=(P, 640, 64), dt=(P, 40, 4), b=(P, 640, 64), c=(P, 640, 64), y=(2 * P, 640, 64))
     t.update(io)
-    s = C.ScanIO(*(C.Tokens(*t[k]) for k in ("x", "dt", "b", "c", "y")))
-    return C.co_scan_forward_steps(ref(d), A, None, None, ref(s), T, None, state, 1, ws, nws, None)
+    c = C.ScanCall(A, None, None, *(C.Tokens(*t[k]) for k in ("x", "dt", "b", "c", "y")), None,
+                   state, ws, nws, T, 1)
+    return C.co_scan_forward_steps(ref(d), ref(c), None)
 
 
 def test_scan_arguments():
@@ -100,8 +101,8 @@ def test_scan_arguments():
                 dict(y=(2 * P, 640, 63)), dict(y=(2 * P, 639, 64)), dict(state=P + 2),
                 dict(ws=P + 4, nws=1 << 20)):
         assert call_scan(scan(), **bad) == C.CO_EINVAL, bad
-    assert C.co_scan_forward_steps(ref(scan()), P, None, None, None, 10, None, P, 1, None, 0,
-                                   None) == C.CO_EINVAL
+    assert C.co_scan_forward_steps(ref(scan()), None, None) == C.CO_EINVAL
+    assert C.co_scan_forward_steps(None, ref(C.ScanCall()), None) == C.CO_EINVAL
 
 
 def test_scan_workspace():
@@ -114,9 +115,10 @@ def test_scan_workspace():
         assert C.co_scan_workspace_bytes(ref(d), T, ref(n)) == C.CO_OK
         sizes.append(n.value)
     assert sizes[:3] == [0, 0, 0] and 0 < sizes[3] < sizes[4] < sizes[5] < sizes[6]
-    # decays of a chunk of 32 tokens and a head: 656 bytes; B . C: 3072; states of at most 64 parts
+    # decays of a chunk of 32 tokens and a head: 656 bytes; B . C: 3 tiles of 64 lanes; states of
+    # at most 64 parts
     chunks = 1 << 15
-    most = chunks * (64 * 656 + 3072) + 64 * 64 * (64 * 128 + 1) * 4
+    most = chunks * (64 * 656 + 3 * 64 * 16) + 64 * 64 * (64 * 128 + 1) * 4
     assert sizes[6] <= most
     assert C.co_scan_workspace_bytes(ref(d), -1, ref(n)) == C.CO_EINVAL
     assert C.co_scan_workspace_bytes(ref(d), 5, None) == C.CO_EINVAL
@@ -124,8 +126,8 @@ def test_scan_workspace():
 
 def call_norm(d, x=(P, 48, 16), gate=None, residual=None, y=(P, 48, 16), out=None, weight=P,
               scale=None):
-    t = [ref(C.Tokens(*v)) if v else None for v in (x, gate, residual, y, out)]
-    return C.co_norm_forward(ref(d), t[0], t[1], t[2], weight, scale, t[3], t[4], None)
+    t = [C.Tokens(*v) if v else C.Tokens() for v in (x, gate, residual, y, out)]
+    return C.co_norm_forward(ref(d), ref(C.NormCall(*t, weight, scale)), None)
 
 
 def test_norm_arguments():
