@@ -31,14 +31,15 @@
 // tokens took 65 registers more than two waves of a SIMD have.
 //
 // Measured: 16384 tokens of 64 heads of 64 x 128, one group, bfloat16: 283 MB and
-// 43 GFLOP of the recurrence in 200 us; the launches take 13 us (B . C, decays),
-// 73 us (segments' sums), 14 us (carry) and 131 us (outputs) when traced.  The
-// last runs its matrix products at 295 TFLOP/s, 557 with the split's three terms
+// 43 GFLOP of the recurrence in 192 us; the launches take 13 us (B . C, decays),
+// 69 us (segments' sums), 14 us (carry) and 122 us (outputs) when traced.  The
+// last runs its matrix products at 317 TFLOP/s, 598 with the split's three terms
 // counted; it is bound by issue and latency at two waves a SIMD (matrix
 // pipes busy a quarter of the cycles, vector units 40%, waves waiting 28%), not
-// by memory (228 MB from and to memory in it, 1.7 TB/s).  Tried and no faster:
+// by memory (228 MB from and to memory in it, 1.9 TB/s).  Tried and no faster:
 // three waves a SIMD (spills), eight waves a workgroup, operands read further
-// ahead, matrix and vector instructions interleaved by hand, wave priorities.
+// ahead, matrix and vector instructions interleaved by hand, sums of finer parts than
+// the segments at three and four waves a SIMD.
 #include <type_traits>
 
 #include "launch.hpp"
@@ -609,7 +610,17 @@ __global__ __launch_bounds__(kWaves * 64, !FULL && sizeof(T) == 2 ? 3 : 2) void 
     if (t_begin + Q < t_end) fetch(t_begin + Q);
   }
   int buf = 0;
+  // Of two workgroups of a CU the older one's waves go first: it was done after 85 us of 105, and
+  // the younger one ran its last chunks alone.  So in long segments the younger, of the grid's
+  // second half, goes first over half of its chunks, and both end together (16384 tokens of 64
+  // heads of 64 x 128: outputs 131 -> 122 us, sums 75 -> 69; in turns of one chunk 125 to 135; in
+  // segments of 8 chunks, float32, all launches 59 -> 64).
+  const int64_t t_even = a.seg_chunks >= 16 && blockIdx.x >= gridDim.x / 2
+                             ? t_begin + (t_end - t_begin) / (2 * Q) * Q
+                             : t_begin;
+  if (t_even > t_begin) __builtin_amdgcn_s_setprio(1);
   for (int64_t t0 = t_begin; t0 < t_end; t0 += Q) {
+    if (t0 == t_even) __builtin_amdgcn_s_setprio(0);
     L& sh = *reinterpret_cast<L*>(lds + buf);
     if (BUFS == 1) {
       __syncthreads();  // the last chunk's tiles are read
