@@ -858,14 +858,16 @@ int64_t workgroups(const co_scan_desc& d, int64_t rows) {
 }
 
 // Rows of a unit.  32 share the most between them: 64 heads of 64 x 128 in bfloat16, 16000 tokens
-// 202 us with 32 and 281 us with 16.  16 where 256 states take a lane's registers, where 32 would
-// be empty for a fifth of the units or more, and where a call has too few units to fill the card
-// however it is cut: its time is then that of one wave's chunks, which are shorter (256 tokens
-// 28.6 and 25.5 us; 3 streams of 10 heads of 40 x 20, float32, 256 tokens 27.6 and 20.4 us).
+// 202 us with 32 and 281 us with 16.  16 where 256 states take a lane's registers, where a fifth
+// or more of the waves' rows would be empty with 32 and are not with 16 (heads of 40 rows; groups
+// of three heads of 64: 16 streams of 1000 tokens of 24 such heads x 64 states 70 and 66 us, 64
+// streams of 500 of 8 groups of one head x 128 84 and 74), and where a call has too few units to
+// fill the card however it is cut: its time is then that of one wave's chunks, which are shorter
+// (256 tokens 28.6 and 25.5 us; 3 streams of 10 heads of 40 x 20, float32, 256 tokens 27.6 and
+// 20.4 us).
 int unit_rows(const co_scan_desc& d, int64_t T) {
   if (d.state_size > 128) return 16;
-  const int64_t halves = (d.head_dim + 15) / 16, wholes = (d.head_dim + 31) / 32;
-  if (2 * wholes * 4 >= 5 * halves) return 16;
+  if (2 * workgroups(d, 32) * 4 >= 5 * workgroups(d, 16)) return 16;
   const int64_t chunks = (T + kChunk - 1) / kChunk;
   return workgroups(d, 32) * ((chunks + 3) / 4) < 600 ? 16 : 32;
 }
