@@ -31,7 +31,7 @@
 // tokens took 65 registers more than two waves of a SIMD have.
 //
 // Measured: 16384 tokens of 64 heads of 64 x 128, one group, bfloat16: 283 MB and
-// 43 GFLOP of the recurrence in 192 us; the launches take 13 us (B . C, decays),
+// 43 GFLOP of the recurrence in 190 us; the launches take 12 us (B . C, decays),
 // 69 us (segments' sums), 14 us (carry) and 122 us (outputs) when traced.  The
 // last runs its matrix products at 317 TFLOP/s, 598 with the split's three terms
 // counted; it is bound by issue and latency at two waves a SIMD (matrix
@@ -306,7 +306,8 @@ struct Tile {
 };
 
 // Makes ws_bc and ws_decay: a wave the tiles of B . C of a chunk, or two chunks of kHeads heads.
-// Bound by latency (memory, and a new kernel's instructions), so few waves with much on the way.
+// Bound by latency (memory, and a new kernel's instructions), so few waves with much on the way
+// and without branches between their loads (16 ragged prompts of 8 groups 12.6 -> 9.9 us).
 constexpr int kHeads = 4;
 template <typename T, bool WIDE>
 __global__ __launch_bounds__(kBlock) void scan_prepare_kernel(ChunkArgs a) {
@@ -322,43 +323,46 @@ __global__ __launch_bounds__(kBlock) void scan_prepare_kernel(ChunkArgs a) {
   const int len = stream_tokens(a.c.c.lengths, b, a.c.c.T);
   if (job >= head_jobs) {
     const int j = job - head_jobs, group = j / 2, chunk = 2 * two + j % 2;
-    if (chunk >= a.chunks) return;
-    const int N = d.state_size;
-    // rows 0..15 and 16..31 of B and of C, as depth-32 operands
-    const T* base[2] = {
-        static_cast<const T*>(io.b.data) + b * io.b.batch_stride + int64_t(group) * N,
-        static_cast<const T*>(io.c.data) + b * io.c.batch_stride + int64_t(group) * N};
+    const int64_t t0 = int64_t(chunk) * kChunk;
+    if (t0 >= len) return;  // nobody reads it
+    const int left = int(min(len - t0, int64_t(kChunk))), N = d.state_size;
+    // rows 0..15 and 16..31 of B and of C, as depth-32 operands: both take depth 8 g16 + i as i
     const int64_t stride[2] = {io.b.token_stride, io.c.token_stride};
+    const T* base[2] = {static_cast<const T*>(io.b.data) + b * io.b.batch_stride +
+                            int64_t(group) * N + t0 * stride[0],
+                        static_cast<const T*>(io.c.data) + b * io.c.batch_stride +
+                            int64_t(group) * N + t0 * stride[1]};
     f32x4 acc[kPairs] = {};
     constexpr int AHEAD = 2;  // depth blocks on the way together
+    constexpr int V = kWide<T>, es = sizeof(T);
+    struct Eight {
+      Pack<T, V> v[8 / V];
+    };
     for (int k0 = 0; k0 < N; k0 += 32 * AHEAD) {
-      Pack<T, 4> v[AHEAD][2][2][2];
+      Eight v[AHEAD][2][2];
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
         for (int side = 0; side < 2; ++side)
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
-            const int64_t t = int64_t(chunk) * kChunk + 16 * half + l16;
-            const T* row = base[side] + t * stride[side];
+            const int row = 16 * half + l16;
 #pragma unroll
-            for (int w = 0; w < 2; ++w) {
-              const int n = k0 + 32 * u + 16 * w + 4 * g16;
-              Pack<T, 4>& o = v[u][side][half][w];
-              o = Pack<T, 4>{};
-              if (WIDE) {
-                if (t < len && n < N) o = load_pack<T, 4>(row + n);
-              } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  if (t < len && n + i < N) o.v[i] = row[n + i];
-              }
+            for (int w = 0; w < 8 / V; ++w) {
+              const int n = k0 + 32 * u + 8 * g16 + V * w;
+              if (WIDE)
+                v[u][side][half].v[w] = load_pack_at<T>(
+                    make_rsrc(base[side], kOutOfRange),
+                    row < left && n < N ? (row * int(stride[side]) + n) * es : kOutOfRange, 0);
+              else
+                v[u][side][half].v[w] =
+                    load_row<T>(base[side] + row * stride[side], n, N, row < left);
             }
           }
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
         const auto op = [&](int side, int half) {
-          return join(v[u][side][half][0], v[u][side][half][1]);
+          return __builtin_bit_cast(Frag<T>, v[u][side][half]);
         };
         mma(acc[0], op(0, 0), op(1, 0));  // rows s, columns t
         mma(acc[1], op(0, 0), op(1, 1));
@@ -383,6 +387,7 @@ __global__ __launch_bounds__(kBlock) void scan_prepare_kernel(ChunkArgs a) {
     bias[i] = a.c.c.dt_bias ? a.c.c.dt_bias[h] : 0.f;
     A2[i] = a.c.c.A[h] * kLog2e;
   }
+  if (int64_t(two) * 64 >= len) return;  // nobody reads them
 #pragma unroll
   for (int i = 0; i < kHeads; ++i) {
     const int h = job * kHeads + i;
