@@ -35,7 +35,7 @@
 // 69 us (segments' sums), 14 us (carry) and 122 us (outputs) when traced.  The
 // last runs its matrix products at 317 TFLOP/s, 598 with the split's three terms
 // counted; it is bound by issue and latency at two waves a SIMD (matrix
-// pipes busy a quarter of the cycles, vector units 40%, waves waiting 28%), not
+// pipes busy 35% of the cycles, vector units 55%, waves waiting 27%), not
 // by memory (228 MB from and to memory in it, 1.9 TB/s).  Tried and no faster:
 // three waves a SIMD (spills), eight waves a workgroup, operands read further
 // ahead, matrix and vector instructions interleaved by hand, sums of finer parts than
