@@ -13,12 +13,14 @@
 // of two 16-row result tiles.  The same holds for B_s . C_t, whose result tiles
 // become the operand of the product with x without leaving their lanes.
 //
-// bfloat16: x, B and C are used as they are.  e^{...} d_s (B_s . C_t) and the
-// state as the operand of its product with C are rounded to bfloat16, next to
-// the rounding of y itself: each adds as much error as that one over its part
-// of y.  The weighted x of the state's sum is split into three bfloat16 terms
-// (24 bits together), so the state stays a float32 sum.  float32 inputs use the
-// float32 matrix instructions throughout.
+// bfloat16: x, B and C are used as they are. What is float32 and becomes an
+// operand goes in bfloat16 terms: two (16 bits) of e^{...} d_s (B_s . C_t) and of
+// the state in its product with C, whose sums are rounded to bfloat16 once as y, 8
+// bits; three (24 bits) of the weighted x in the state's sum, which goes on being
+// summed. With one term of the first two, y was off by u times the sum of its
+// terms' magnitudes, far more than its own rounding where they cancel, and differed
+// so from single tokens (16384 tokens of 64 heads 190 us, now 215). float32
+// inputs use the float32 matrix instructions throughout.
 //
 // A small launch before makes what the heads of a group and the units of a head
 // share: the products B_s . C_t, and of each chunk its decays.  Long sequences
@@ -430,6 +432,8 @@ __global__ __launch_bounds__(kWaves * 64, !FULL && sizeof(T) == 2 ? 3 : 2) void 
   constexpr int NK = NT / 2;                        // depth-32 blocks of N
   constexpr int BC_ROW = L::NW / V, BC_LOADS = (Q * BC_ROW + 255) / 256;
   constexpr int X_ROW = L::PW / V, X_LOADS = Q * X_ROW / 64;
+  // Terms of a float32 value as an operand: of the factors of y, of the state's sum.
+  constexpr int FACTORS = sizeof(T) == 2 ? 2 : 1, TERMS = sizeof(T) == 2 ? 3 : 1;
   static_assert(NT % 2 == 0 && 256 % BC_ROW == 0 && Q * X_ROW % 64 == 0 && 64 % X_ROW == 0);
   // Two tiles where two workgroups of a CU have them: the next chunk's is written over this one's
   // products, and a chunk has one barrier.
@@ -675,7 +679,7 @@ __global__ __launch_bounds__(kWaves * 64, !FULL && sizeof(T) == 2 ? 3 : 2) void 
 #pragma unroll
         for (int pt = 0; pt < PT; ++pt) part_finite(x[pt], bad[pt]);
       }
-      F m[L::QT];  // columns t, depths s
+      F m[L::QT][FACTORS];  // columns t, depths s
 #pragma unroll
       for (int j = 0; j < L::QT; ++j) {
         float v[8] = {};
@@ -686,7 +690,8 @@ __global__ __launch_bounds__(kWaves * 64, !FULL && sizeof(T) == 2 ? 3 : 2) void 
           for (int i = 0; i < 4; ++i)
             v[4 * si + i] = si < j || 4 * g16 + i <= l16 ? w[j + si][i] * bc[i] : 0.f;
         }
-        round_to(m[j], v);
+#pragma unroll
+        for (int f = 0; f < FACTORS; ++f) take(m[j][f], v);
       }
       // y^T = S C_t + own: rows p, columns t
       f32x4 y[L::QT][PT];
@@ -705,10 +710,13 @@ __global__ __launch_bounds__(kWaves * 64, !FULL && sizeof(T) == 2 ? 3 : 2) void 
             float v[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = S[2 * k + i / 4][pt][i % 4];
-            F s;
-            round_to(s, v);
 #pragma unroll
-            for (int j = 0; j < L::QT; ++j) mma(y[j][pt], s, c[j]);
+            for (int f = 0; f < FACTORS; ++f) {
+              F s;
+              take(s, v);
+#pragma unroll
+              for (int j = 0; j < L::QT; ++j) mma(y[j][pt], s, c[j]);
+            }
           }
         }
       };
@@ -716,7 +724,9 @@ __global__ __launch_bounds__(kWaves * 64, !FULL && sizeof(T) == 2 ? 3 : 2) void 
 #pragma unroll
         for (int j = 0; j < L::QT; ++j)
 #pragma unroll
-          for (int pt = 0; pt < PT; ++pt) mma(y[j][pt], x[pt], m[j]);
+          for (int pt = 0; pt < PT; ++pt)
+#pragma unroll
+            for (int f = 0; f < FACTORS; ++f) mma(y[j][pt], x[pt], m[j][f]);
       };
       from_state();
       if (far) {
@@ -736,11 +746,12 @@ __global__ __launch_bounds__(kWaves * 64, !FULL && sizeof(T) == 2 ? 3 : 2) void 
 #pragma unroll
           for (int i = 0; i < 8; ++i)
             one[i] = i / 4 < j || (i / 4 == j && 4 * g16 + i % 4 <= l16) ? 1.f : 0.f;
-          round_to(m[j], one);
+          F ones;
+          round_to(ones, one);
 #pragma unroll
           for (int pt = 0; pt < PT; ++pt) {
             f32x4 count{0.f, 0.f, 0.f, 0.f};
-            mma(count, bad[pt], m[j]);
+            mma(count, bad[pt], ones);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
               if (count[i] > 0.f) y[j][pt][i] = __builtin_nanf("");
@@ -784,7 +795,6 @@ __global__ __launch_bounds__(kWaves * 64, !FULL && sizeof(T) == 2 ? 3 : 2) void 
     }
 
     // S' = e^{cum_Q} S + B^T (weighted x)
-    constexpr int TERMS = sizeof(T) == 2 ? 3 : 1;
     F xw[PT][TERMS];
 #pragma unroll
     for (int pt = 0; pt < PT; ++pt) {

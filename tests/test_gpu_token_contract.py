@@ -1,0 +1,54 @@
+"""What the token layers promise beyond their formulas: how exact bfloat16 is,
+what lies past a stream's length, layers in chains, and which arguments they
+refuse.
+
+Bounds as in test_gpu_tokens.py: `size` is the sum of an output's magnitudes, u
+a dtype's unit roundoff.
+"""
+import numpy as np
+import pytest
+import torch
+
+import token_ref as R
+from paper_2204_03418_amd import coinf
+from test_gpu_tokens import BF16, DEV, U, scan_inputs, scan_layer, scan_ref
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------ bfloat16
+
+
+@pytest.mark.parametrize("case", [
+    # B, T, H, P, G, N, dtype, lengths, softplus, D
+    (1, 64, 2, 32, 1, 32, BF16, "full", True, True),
+    (2, 150, 4, 64, 2, 64, BF16, "ragged", True, True),
+    (2, 90, 4, 64, 1, 128, BF16, "full", False, False),
+    (1, 130, 3, 40, 1, 20, BF16, "full", True, True),
+    (1, 100, 2, 64, 1, 256, BF16, "full", True, True),
+    (1, 900, 4, 64, 2, 128, BF16, "full", True, True),
+], ids=str)
+def test_scan_bfloat16_is_rounded_once(case):
+    """A prompt's outputs in bfloat16 are float32 sums rounded once, also where
+    the sum cancels: the float32 factors of its products keep 16 bits at least
+    (two bfloat16 terms leave u^2 of a value, u = 2^-8).  And they are those of
+    single tokens, but for that and the two roundings."""
+    T, N = case[1], case[5]
+    v, n = scan_inputs(case, 71)
+    layer = scan_layer(case, v, v["state"])
+    d = [v[k].to(DEV) for k in ("x", "dt", "b", "c")]
+    nd = None if n is None else n.to(DEV)
+    assert layer.workspace_bytes(T) > 0                         # the chunks take the call
+    got = layer.forward_steps(*d, nd, update_state=False)
+    y, size, _, _ = scan_ref(case, v, v["state"], n)
+    f32 = (4 * T + N + 64) * R.U32
+    keep = U[BF16] ** 2 + f32
+    R.within(got, y, U[BF16] * np.abs(y) + keep * size, f"bfloat16 {case}")
+    steps = []
+    for t in range(T):
+        on = None if n is None else (n > t).to(torch.int32).to(DEV)
+        steps.append(layer.forward_step(*(a[:, t] for a in d), on))
+    # each value within its own bound of the sum; what is rounded is no larger than the
+    # sum and the error before
+    most = 2 * U[BF16] * (np.abs(y) + keep * size) + (keep + f32) * size
+    R.within(got, R.np64(torch.stack(steps, 1)), most, f"bfloat16 steps {case}")
