@@ -6,13 +6,14 @@
 // loads again.  4 x 4096 tokens of 4352 channels in bfloat16: 285 MB in 59 us
 // (4.8 TB/s); one token of 64 streams 4.2 us.
 #include "launch.hpp"
+#include "short_conv.hpp"
 #include "token.hpp"
 
 namespace coinf {
 
 namespace {
 
-constexpr int kRun = 2;
+static_assert(kBlock == kConvThreads);
 
 struct ConvCall {
   const void* weight;
@@ -117,8 +118,8 @@ __global__ __launch_bounds__(kBlock) void shortconv_kernel(ConvCall a) {
       for (int i = 0; i < RUN; ++i) run[i] = next[i];
     }
   }
-  // The state is read by the threads of token 0 alone, and they write it: its
-  // j-th token is number len - (K - 1) + j of the call, or what the old state has.
+  // The state is read by the threads of token 0 alone (shortconv_cut), and they write
+  // it: its j-th token is number len - (K - 1) + j of the call, or what the old state has.
   if (K > 1 && t0 == 0 && a.update && len > 0) {
 #pragma unroll
     for (int j = 0; j < K - 1; ++j) {
@@ -139,33 +140,20 @@ __global__ __launch_bounds__(kBlock) void shortconv_kernel(ConvCall a) {
 
 template <typename T, int K, int V>
 hipError_t launch_k(ConvCall a, int32_t B, hipStream_t s) {
-  const int64_t packs = (a.C + V - 1) / V;
-  if (a.T == 1) {
-    a.c_blocks = int32_t((packs + kBlock - 1) / kBlock);
-    a.t_blocks = a.runs = 1;
-    const int64_t grid = int64_t(a.c_blocks) * B;
-    if (!grid_fits(grid)) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((shortconv_kernel<T, K, V, 1, kBlock>), dim3(unsigned(grid)), dim3(kBlock),
-                       0, s, a);
-    return hipGetLastError();
-  }
-  const auto go = [&](auto kernel, int lanes) {
-    a.c_blocks = int32_t((packs + lanes - 1) / lanes);
-    a.t_blocks = (a.T - 1) / (kRun * a.runs * (kBlock / lanes)) + 1;
+  const int64_t packs = (int64_t(a.C) + V - 1) / V;
+  const ShortConvCut cut = shortconv_cut(B, packs, a.T, K);
+  const auto go = [&](auto kernel) {
+    a.c_blocks = int32_t((packs + cut.lanes - 1) / cut.lanes);
+    a.t_blocks = cut.t_blocks;
+    a.runs = cut.runs;
     const int64_t grid = int64_t(a.c_blocks) * a.t_blocks * B;
     if (!grid_fits(grid)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL(kernel, dim3(unsigned(grid)), dim3(kBlock), 0, s, a);
     return hipGetLastError();
   };
-  // More runs a thread load the tokens before them less often, where that leaves two waves for
-  // each of 1024 SIMDs.  4 x 4096 tokens of 4352 channels in bfloat16 (285 MB): one run of 8
-  // tokens a thread 91 us, 4 of 8 81 us (at half the occupancy), 8 of 4 64 us, 8 of 2 59 us.
-  const int64_t threads = packs * B * ((a.T + kRun - 1) / kRun);
-  a.runs = 8;
-  while (a.runs > 1 && threads / a.runs < 2 * 1024 * 64) a.runs /= 2;
-  // few tokens: threads across the channels
-  if (a.T <= 4 * kRun) return go(shortconv_kernel<T, K, V, kRun, 64>, 64);
-  return go(shortconv_kernel<T, K, V, kRun, 32>, 32);
+  if (cut.run == 1) return go(shortconv_kernel<T, K, V, 1, kBlock>);
+  return cut.lanes == 64 ? go(shortconv_kernel<T, K, V, kRun, 64>)
+                         : go(shortconv_kernel<T, K, V, kRun, 32>);
 }
 
 template <typename T, int V>

@@ -52,3 +52,27 @@ def test_scan_bfloat16_is_rounded_once(case):
     # sum and the error before
     most = 2 * U[BF16] * (np.abs(y) + keep * size) + (keep + f32) * size
     R.within(got, R.np64(torch.stack(steps, 1)), most, f"bfloat16 steps {case}")
+
+
+# ------------------------------------------------------------ pieces shorter than the state
+
+
+@pytest.mark.parametrize("K", [4, 5, 6, 8])
+@pytest.mark.parametrize("T", [3, 6, 8, 13])
+def test_drafted_pieces_are_single_tokens(K, T):
+    """A few drafted tokens of many streams, twice, against single tokens bit for
+    bit: outputs and the state, which a piece reads and writes in one launch."""
+    g = torch.Generator().manual_seed(81)
+    B, C = 32, 1088
+    x = torch.randn(B, 2 * T, C, generator=g).to(BF16).to(DEV)
+    w = torch.randn(C, K, generator=g).to(BF16).to(DEV)
+    state = torch.randn(B, K - 1, C, generator=g).to(BF16).to(DEV)
+    n = torch.randint(0, T + 1, (B,), generator=g).to(torch.int32)
+    pieces, steps = (coinf.CoShortConv(w, batch=B, state=state.clone()) for _ in range(2))
+    for part, lengths in ((x[:, :T], None), (x[:, T:], n)):
+        nd = None if lengths is None else lengths.to(DEV)
+        got = pieces.forward_steps(part, nd)
+        want = torch.stack([steps.forward_step(
+            part[:, t], None if lengths is None else (lengths > t).to(torch.int32).to(DEV))
+            for t in range(T)], 1)
+        assert torch.equal(got, want) and torch.equal(pieces.state, steps.state)
