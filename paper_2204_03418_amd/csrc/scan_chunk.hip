@@ -762,7 +762,9 @@ __global__ __launch_bounds__(kWaves * 64, !FULL && sizeof(T) == 2 ? 3 : 2) void 
           x[pt] = cols_of(sh.x[wave], L::XS, 0, x_four(pt), p_of(pt, l16));
       }
       const __amdgpu_buffer_rsrc_t yr = make_rsrc(yg + t0 * io.y.token_stride, kOutOfRange);
+      // tokens of the call, and of the stream: past those the sums may be 0 times what is not finite
       const int rows_left = int(min(t_stop - t0, int64_t(Q)));
+      const int rows_own = int(min(t_end - t0, int64_t(Q)));
 #pragma unroll
       for (int j = 0; j < L::QT; ++j) {
         const int r = 16 * j + l16;
@@ -773,6 +775,10 @@ __global__ __launch_bounds__(kWaves * 64, !FULL && sizeof(T) == 2 ? 3 : 2) void 
 #pragma unroll
         for (int i = 0; i < RUN; ++i)
           out[i] = fmaf(D, to_f32<T>(xr[p + i]), y[j][i / 4][i % 4] * grow[j]);
+        if (rows_own < Q) {  // the stream ends here
+#pragma unroll
+          for (int i = 0; i < RUN; ++i) out[i] = r < rows_own ? out[i] : 0.f;
+        }
         if (WIDE) {
           constexpr int W = RUN < V ? RUN : V;
 #pragma unroll

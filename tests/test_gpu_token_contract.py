@@ -76,3 +76,31 @@ def test_drafted_pieces_are_single_tokens(K, T):
             part[:, t], None if lengths is None else (lengths > t).to(torch.int32).to(DEV))
             for t in range(T)], 1)
         assert torch.equal(got, want) and torch.equal(pieces.state, steps.state)
+
+
+# ------------------------------------------------------------ past a stream's length
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, BF16])
+@pytest.mark.parametrize("wide", [True, False])
+@pytest.mark.parametrize("which", ["x", "dt", "b", "c", "state"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_scan_past_lengths_is_zero_whatever_the_stream_holds(which, bad, wide, dtype):
+    """Outputs past a stream's length are 0 also where its own tokens or its
+    state are not finite, in one segment and in several, in pieces of 16 bytes
+    and value by value."""
+    for B, T, H in ((3, 150, 4), (3, 700, 2)):
+        P, N = (32, 32) if wide else (33, 21)
+        case = (B, T, H, P, 2, N, dtype, "full", True, True)
+        v, _ = scan_inputs(case, 72)
+        n = torch.tensor([T - 50, 41, 0], dtype=torch.int32)
+        if which == "state":
+            v["state"][:, 1, 3, 2] = bad
+        else:
+            v[which][0, T - 53], v[which][1, 3] = bad, bad
+        layer = scan_layer(case, v, v["state"])
+        assert layer.workspace_bytes(T) > 0
+        got = layer.forward_steps(*(v[k].to(DEV) for k in ("x", "dt", "b", "c")), n.to(DEV))
+        for i, k in enumerate(n.tolist()):
+            assert (got[i, k:] == 0).all(), (which, i)
+        assert not torch.isfinite(got[0, :T - 50]).all()
