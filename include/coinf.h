@@ -866,6 +866,11 @@ typedef struct co_norm_call {
 
 co_status co_norm_forward(const co_norm_desc* desc, const co_norm_call* call, void* stream);
 
+/* The same over ragged streams: tokens at or past a stream's length are not
+ * read, their outputs (y and r') are 0. */
+co_status co_norm_forward_lengths(const co_norm_desc* desc, const co_norm_call* call,
+                                  const int32_t* lengths, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -213,6 +213,8 @@ co_scan_forward_steps = _sig("co_scan_forward_steps", i32,
                              [ctypes.POINTER(ScanDesc), ctypes.POINTER(ScanCall), vp])
 co_norm_forward = _sig("co_norm_forward", i32,
                        [ctypes.POINTER(NormDesc), ctypes.POINTER(NormCall), vp])
+co_norm_forward_lengths = _sig("co_norm_forward_lengths", i32,
+                               [ctypes.POINTER(NormDesc), ctypes.POINTER(NormCall), vp, vp])
 
 
 class CoinfError(RuntimeError):
@@ -1441,7 +1443,7 @@ class CoNorm:
         self._args = ctypes.byref(self.desc), ctypes.byref(call)
         self._sig = None
 
-    def _rows(self, t, dtype, shape, what, into):
+    def _rows(self, t, dtype, shape, tokens, what, into):
         if t.device.type != "cuda":
             raise ValueError(f"{what} must be a device tensor")
         if t.dtype is not dtype:
@@ -1452,18 +1454,19 @@ class CoNorm:
             into.batch_stride = into.token_stride = 0
             return
         try:
-            v = t if t.dim() == 3 else t.view(-1, shape[-2] if t.dim() > 1 else 1, self.dim)
+            v = t if t.dim() == 3 else t.view(-1, tokens, self.dim)
         except RuntimeError:
             raise ValueError(f"{what}: the leading axes must be evenly spaced") from None
         if self.dim != 1 and v.stride(2) != 1:
             raise ValueError(f"{what}: the values of a row must be contiguous")
         into.batch_stride, into.token_stride = v.stride(0), v.stride(1)
 
-    def forward(self, x, gate=None, residual=None, out=None, residual_out=None):
+    def forward(self, x, gate=None, residual=None, out=None, residual_out=None, lengths=None):
         """x (..., D), gate of its shape and dtype, residual of its shape (float32 or
         bfloat16) -> y; (y, new residual) with residual "before"; the new residual
-        with "after".  out may be x, residual_out may be residual."""
-        sig = (x.shape, x.stride(), x.dtype, x.is_cuda,
+        with "after".  out may be x, residual_out may be residual.  lengths (of x
+        (B, T, D), or (B, D) for single tokens): as CoShortConv's."""
+        sig = (lengths is None, x.shape, x.stride(), x.dtype, x.is_cuda,
                None if gate is None else (gate.shape, gate.stride(), gate.dtype, gate.is_cuda),
                None if residual is None else (residual.shape, residual.stride(), residual.dtype,
                                               residual.is_cuda),
@@ -1472,7 +1475,7 @@ class CoNorm:
                                                   residual_out.dtype, residual_out.is_cuda))
         if sig != self._sig:
             self._sig = None
-            self._check(x, gate, residual, out, residual_out)
+            self._check(x, gate, residual, out, residual_out, lengths is not None)
             self._sig = sig
         form = self.residual
         self._x.data = x.data_ptr()
@@ -1487,14 +1490,17 @@ class CoNorm:
                 out = _like(x) if self._dense[0] else x.new_empty(x.shape)
             self._y.data = out.data_ptr()
         pd, pc = self._args
-        st = co_norm_forward(pd, pc, _stream())
+        if lengths is None:
+            st = co_norm_forward(pd, pc, _stream())
+        else:
+            st = co_norm_forward_lengths(pd, pc, _lengths(lengths, x.shape[0]), _stream())
         if st != CO_OK:
             check(st, "co_norm_forward")
         if form is None:
             return out
         return residual_out if form == "after" else (out, residual_out)
 
-    def _check(self, x, gate, residual, out, residual_out):
+    def _check(self, x, gate, residual, out, residual_out, ragged):
         if (gate is None) != (self.gate is None) or (residual is None) != (self.residual is None):
             raise ValueError("gate and residual are given to the layers that have them")
         shape, d = x.shape, self.desc
@@ -1502,23 +1508,26 @@ class CoNorm:
             raise ValueError(f"x has shape {tuple(shape)}, expected (..., {self.dim})")
         if x.dtype not in DTYPES:
             raise ValueError(f"x has dtype {x.dtype}")
-        tokens = shape[-2] if x.dim() > 1 else 1
+        if ragged and x.dim() not in (2, 3):
+            raise ValueError(f"x has shape {tuple(shape)}, expected (B, T, {self.dim}) or "
+                             f"(B, {self.dim}) beside lengths")
+        tokens = shape[-2] if x.dim() > (2 if ragged else 1) else 1
         d.tokens, d.dtype = tokens, DTYPES[x.dtype]
         d.batch = x.numel() // (tokens * self.dim) if tokens else 0
-        self._rows(x, x.dtype, shape, "x", self._x)
+        self._rows(x, x.dtype, shape, tokens, "x", self._x)
         if gate is not None:
-            self._rows(gate, x.dtype, shape, "gate", self._z)
+            self._rows(gate, x.dtype, shape, tokens, "gate", self._z)
         if residual is not None:
             if residual.dtype not in DTYPES:
                 raise ValueError(f"residual has dtype {residual.dtype}")
             d.residual_dtype = DTYPES[residual.dtype]
-            self._rows(residual, residual.dtype, shape, "residual", self._r)
+            self._rows(residual, residual.dtype, shape, tokens, "residual", self._r)
             self._o.batch_stride, self._o.token_stride = tokens * self.dim, self.dim
             if residual_out is not None:
-                self._rows(residual_out, residual.dtype, shape, "residual_out", self._o)
+                self._rows(residual_out, residual.dtype, shape, tokens, "residual_out", self._o)
         self._y.batch_stride, self._y.token_stride = tokens * self.dim, self.dim
         if out is not None:
-            self._rows(out, x.dtype, shape, "out", self._y)
+            self._rows(out, x.dtype, shape, tokens, "out", self._y)
         self._dense = x.is_contiguous(), residual is not None and residual.is_contiguous()
 
     forward_step = forward_steps = forward
@@ -1553,28 +1562,28 @@ class Mixer:
         self._split = (self.inner, shared, shared)
         self.width = sum(self._columns)
 
-    def _run(self, u, conv, scan):
+    def _run(self, u, lengths, conv, scan):
         z, xbc, dt = u.split(self._columns, -1)
         s = self.scan
         x, b, c = conv(xbc).split(self._split, -1)
         lead = u.shape[:-1]
         bc = lead + (s.groups, s.state_size)
         y = scan(x.view(lead + (s.heads, s.head_dim)), dt, b.view(bc), c.view(bc))
-        return self.norm.forward(y.view(z.shape), gate=z)
+        return self.norm.forward(y.view(z.shape), gate=z, lengths=lengths)
 
     def forward_steps(self, u, lengths=None, update_state=True):
         """The next T tokens u (B, T, W) of the streams -> (B, T, H P)."""
-        return self._run(u, lambda v: self.conv.forward_steps(v, lengths, update_state),
+        return self._run(u, lengths, lambda v: self.conv.forward_steps(v, lengths, update_state),
                          lambda *v: self.scan.forward_steps(*v, lengths, update_state))
 
     def forward_step(self, u_t, lengths=None, update_state=True):
         """The next token u_t (B, W) of each stream (of those with length 1) -> (B, H P)."""
-        return self._run(u_t, lambda v: self.conv.forward_step(v, lengths, update_state),
+        return self._run(u_t, lengths, lambda v: self.conv.forward_step(v, lengths, update_state),
                          lambda *v: self.scan.forward_step(*v, lengths, update_state))
 
     def forward(self, u, lengths=None):
         """Whole sequences from a clean state, which the mixer's own is not touched by."""
-        return self._run(u, lambda v: self.conv.forward(v, lengths),
+        return self._run(u, lengths, lambda v: self.conv.forward(v, lengths),
                          lambda *v: self.scan.forward(*v, lengths))
 
     def clean_state(self):

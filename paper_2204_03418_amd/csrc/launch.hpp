@@ -260,6 +260,7 @@ bool scan_chunk_takes(const co_scan_desc& d, int32_t T);
 int64_t scan_chunk_workspace(const co_scan_desc& d, int32_t T);
 hipError_t launch_scan_chunk(const ScanCall& c, hipStream_t stream);
 
-hipError_t launch_norm(const co_norm_desc& d, const co_norm_call& c, hipStream_t stream);
+hipError_t launch_norm(const co_norm_desc& d, const co_norm_call& c, const int32_t* lengths,
+                       hipStream_t stream);
 
 }  // namespace coinf

@@ -16,6 +16,7 @@ namespace {
 
 struct NormArgs {
   co_tokens x, z, r, y, o;  // o: the new residual
+  const int32_t* lengths;
   const float* weight;
   const float* scale;
   uint32_t parts;  // tokens of all streams * groups
@@ -66,17 +67,27 @@ __device__ __forceinline__ void norm_parts(const NormArgs& a, uint32_t part0) {
   constexpr int RV = V * int(sizeof(R)) > 16 ? V / 2 : V;
   const int lane = threadIdx.x % L;
   const uint32_t part = part0 + __builtin_amdgcn_readfirstlane(threadIdx.x / L);
-  const bool on = part < a.parts;
+  if (part >= a.parts) return;
   const uint32_t row = part / a.groups, b = row / a.tokens, t = row % a.tokens;
   const int base = int(part % a.groups) * a.width;
   const int64_t x0 = place(a.x, b, t) + base, z0 = GATE ? place(a.z, b, t) + base : 0;
   const int64_t r0 = RES ? place(a.r, b, t) + base : 0, o0 = RES ? place(a.o, b, t) + base : 0;
+  if (a.lengths && int32_t(t) >= a.lengths[b]) {  // not read; the same in all waves of the part
+    const float zero[V] = {};
+    for (int e = lane * V; e < a.width; e += L * V) {
+      if (RES != CO_NORM_AFTER) store_f32<T, V>(a.y.data, place(a.y, b, t) + base + e, zero);
+      if (RES)
+#pragma unroll
+        for (int j = 0; j < V; j += RV) store_f32<R, RV>(a.o.data, o0 + e + j, zero);
+    }
+    return;
+  }
   float v[NV][V], gate[GATE ? NV : 1][V];
   float sum = 0.f;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int e = (i * L + lane) * V;
-    const bool in = on && e < a.width;
+    const bool in = e < a.width;
 #pragma unroll
     for (int k = 0; k < V; ++k) v[i][k] = 0.f;
     if (in) {
@@ -105,7 +116,7 @@ __device__ __forceinline__ void norm_parts(const NormArgs& a, uint32_t part0) {
     for (int k = 0; k < V; ++k) sum = fmaf(v[i][k], v[i][k], sum);
   }
   // stored after all loads, which a store in between would hold up
-  if (RES == CO_NORM_BEFORE && on) {
+  if (RES == CO_NORM_BEFORE) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int e = (i * L + lane) * V;
@@ -125,7 +136,6 @@ __device__ __forceinline__ void norm_parts(const NormArgs& a, uint32_t part0) {
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) sum += part_sum[w];
   }
-  if (!on) return;
   const float inv = 1.f / sqrtf(sum / float(a.width) + a.eps);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -216,8 +226,9 @@ hipError_t launch_t(const NormArgs& a, int gate, int res, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_norm(const co_norm_desc& d, const co_norm_call& c, hipStream_t stream) {
-  const NormArgs a{c.x, c.gate, c.residual, c.y, c.residual_out, c.weight, c.scale,
+hipError_t launch_norm(const co_norm_desc& d, const co_norm_call& c, const int32_t* lengths,
+                       hipStream_t stream) {
+  const NormArgs a{c.x, c.gate, c.residual, c.y, c.residual_out, lengths, c.weight, c.scale,
                    uint32_t(int64_t(d.batch) * d.tokens * d.groups), uint32_t(d.groups),
                    uint32_t(d.tokens), d.dim / d.groups, d.eps};
   const bool r16 = d.residual && d.residual_dtype == CO_BF16;

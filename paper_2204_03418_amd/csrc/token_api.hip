@@ -132,6 +132,11 @@ co_status co_scan_forward_steps(const co_scan_desc* desc, const co_scan_call* ca
 }
 
 co_status co_norm_forward(const co_norm_desc* desc, const co_norm_call* call, void* stream) {
+  return co_norm_forward_lengths(desc, call, nullptr, stream);
+}
+
+co_status co_norm_forward_lengths(const co_norm_desc* desc, const co_norm_call* call,
+                                  const int32_t* lengths, void* stream) {
   if (!desc || desc->batch < 0 || desc->tokens < 0 || desc->dim <= 0 || desc->groups <= 0 ||
       desc->dim % desc->groups || !dtype_ok(desc->dtype) || !dtype_ok(desc->residual_dtype))
     return CO_EINVAL;
@@ -148,14 +153,15 @@ co_status co_norm_forward(const co_norm_desc* desc, const co_norm_call* call, vo
       (!tokens_ok(call->residual, B, T, rt) || !out_ok(call->residual_out, B, T, desc->dim, rt)))
     return CO_EINVAL;
   if (desc->residual != CO_NORM_AFTER && !out_ok(call->y, B, T, desc->dim, dt)) return CO_EINVAL;
-  if (!aligned(call->weight, 4) || !aligned(call->scale, 4)) return CO_EINVAL;
+  if (!aligned(call->weight, 4) || !aligned(call->scale, 4) || !aligned(lengths, 4))
+    return CO_EINVAL;
   // what the form does not have takes no part in the choice of a kernel
   co_norm_call c = *call;
   const co_tokens none{nullptr, 0, 0};
   if (!desc->gate) c.gate = none;
   if (!desc->residual) c.residual = c.residual_out = none;
   if (desc->residual == CO_NORM_AFTER) c.y = none;
-  return done(launch_norm(*desc, c, as_stream(stream)));
+  return done(launch_norm(*desc, c, lengths, as_stream(stream)));
 }
 
 }  // extern "C"

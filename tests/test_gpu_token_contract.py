@@ -104,3 +104,97 @@ def test_scan_past_lengths_is_zero_whatever_the_stream_holds(which, bad, wide, d
         for i, k in enumerate(n.tolist()):
             assert (got[i, k:] == 0).all(), (which, i)
         assert not torch.isfinite(got[0, :T - 50]).all()
+
+
+def mixer(B, g, dtype, gate="before", H=4, P=32, G=2, N=32, K=4):
+    """A mixer of small layers and the columns that it takes."""
+    inner, shared = H * P, G * N
+    w = torch.randn(inner + 2 * shared, K, generator=g).to(dtype).to(DEV) * 0.5
+    conv = coinf.CoShortConv(w, batch=B)
+    scan = coinf.CoScan(-torch.rand(H, generator=g).to(DEV) - 1, batch=B, head_dim=P, state_size=N,
+                        groups=G, dt_softplus=True, dtype=dtype)
+    norm = coinf.CoNorm(torch.randn(inner, generator=g).to(DEV), gate=gate)
+    return coinf.Mixer(conv, scan, norm)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, BF16])
+@pytest.mark.parametrize("gate", ["before", "after"])
+@pytest.mark.parametrize("T", [1, 5, 150])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_mixer_reads_nothing_past_lengths(bad, T, gate, dtype):
+    """What padded tokens hold reaches no output: zeros past the lengths, and
+    before them what finite padding gives."""
+    g = torch.Generator().manual_seed(91)
+    m = mixer(4, g, dtype, gate)
+    u = torch.randn(4, T, m.width, generator=g).to(dtype)
+    n = torch.tensor([T, 0, T // 2, min(T, 1)], dtype=torch.int32)
+    dirty = u.clone()
+    for i, k in enumerate(n.tolist()):
+        u[i, k:], dirty[i, k:] = 0.0, bad
+    u, dirty, nd = u.to(DEV), dirty.to(DEV), n.to(DEV)
+    want = m.forward(u, nd)
+    assert torch.equal(m.forward(dirty, nd), want)
+    for i, k in enumerate(n.tolist()):
+        assert (want[i, k:] == 0).all()
+    pieces = [m.forward_steps(v, nd, update_state=False) for v in (u, dirty)]
+    assert torch.equal(*pieces)
+    on = (n > 0).to(torch.int32).to(DEV)
+    steps = [m.forward_step(v[:, 0], on, update_state=False) for v in (u, dirty)]
+    assert torch.equal(*steps) and (steps[0][1] == 0).all()
+
+
+@pytest.mark.parametrize("dim,groups", [(96, 1), (90, 3), (2048, 1), (9001, 1)])
+@pytest.mark.parametrize("gate", [None, "before", "after"])
+@pytest.mark.parametrize("residual", [None, "before", "after"])
+@pytest.mark.parametrize("dtype,rdtype", [(BF16, torch.float32), (torch.float32, BF16)])
+def test_norm_lengths(dtype, rdtype, residual, gate, dim, groups):
+    """Tokens of a stream as without lengths, bit for bit; the others 0 (weights
+    and scales that are not finite among them) and unread; in place."""
+    g = torch.Generator().manual_seed(92)
+    B, T = 3, 5
+    draw = lambda t: torch.randn(B, T, dim, generator=g).to(t).to(DEV)  # noqa: E731
+    x, z, r = draw(dtype), draw(dtype), draw(rdtype)
+    w = torch.randn(dim, generator=g).to(DEV)
+    w[3] = float("inf")
+    s = torch.randn(dim, generator=g).to(DEV) if residual else None
+    layer = coinf.CoNorm(w, groups=groups, gate=gate, residual=residual, scale=s)
+    args = dict(gate=z if gate else None, residual=r if residual else None)
+    as_list = lambda v: list(v) if isinstance(v, tuple) else [v]  # noqa: E731
+    want = as_list(layer.forward(x, **args))
+    for n in ([5, 2, 0], [-3, 9, 1]):
+        nd = torch.tensor(n, dtype=torch.int32, device=DEV)
+        for t in (x, z, r):
+            for i, k in enumerate(n):
+                t[i, max(k, 0):] = float("nan")
+        got = as_list(layer.forward(x, **args, lengths=nd))
+        for a, b in zip(got, want):
+            for i, k in enumerate(n):
+                k = max(min(k, T), 0)
+                assert torch.equal(a[i, :k].nan_to_num(), b[i, :k].nan_to_num())
+                assert (a[i, k:] == 0).all()
+        # single tokens, and in place
+        on = torch.tensor([k > 1 for k in n], dtype=torch.int32, device=DEV)
+        one = as_list(layer.forward(x[:, 1], **{k: None if v is None else v[:, 1]
+                                                for k, v in args.items()}, lengths=on))
+        for a, b in zip(one, got):
+            assert torch.equal(a.nan_to_num(), b[:, 1].nan_to_num())
+        if residual != "after":
+            y = x.clone()
+            layer.forward(y, **args, out=y, lengths=nd)
+            assert torch.equal(y.nan_to_num(), got[0].nan_to_num())
+        x, z, r = draw(dtype), draw(dtype), draw(rdtype)
+        args = dict(gate=z if gate else None, residual=r if residual else None)
+        want = as_list(layer.forward(x, **args))
+
+
+def test_norm_lengths_refusals():
+    layer = coinf.CoNorm(dim=16)
+    x = torch.zeros(2, 3, 16, device=DEV)
+    n = torch.ones(2, dtype=torch.int32, device=DEV)
+    layer.forward(x, lengths=n)
+    for bad in (n.cpu(), n.long(), n[:1], torch.ones(3, dtype=torch.int32, device=DEV)):
+        with pytest.raises(ValueError):
+            layer.forward(x, lengths=bad)
+    for v in (x[0, 0], x[None]):
+        with pytest.raises(ValueError):
+            layer.forward(v, lengths=n)
