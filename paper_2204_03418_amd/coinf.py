@@ -1412,7 +1412,7 @@ class CoNorm:
     "after" multiplies the normed values.  residual "before" (a pre-norm) adds
     scale x to the residual and norms the sum; "after" (a post-norm) adds the
     normed values times scale.  Stateless, delay 0: forward, forward_step and
-    forward_steps are one.
+    forward_steps are one (update_state, which chains pass on, says nothing here).
     """
 
     delay, receptive_field, t_stride, t_padding = 0, 1, 1, 0
@@ -1530,7 +1530,11 @@ class CoNorm:
             self._rows(out, x.dtype, shape, tokens, "out", self._y)
         self._dense = x.is_contiguous(), residual is not None and residual.is_contiguous()
 
-    forward_step = forward_steps = forward
+    def forward_steps(self, x, gate=None, residual=None, out=None, residual_out=None,
+                      lengths=None, update_state=True):
+        return self.forward(x, gate, residual, out, residual_out, lengths)
+
+    forward_step = forward_steps
 
     def clean_state(self):
         pass

@@ -198,3 +198,48 @@ def test_norm_lengths_refusals():
     for v in (x[0, 0], x[None]):
         with pytest.raises(ValueError):
             layer.forward(v, lengths=n)
+
+
+# ------------------------------------------------------------ in chains
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, BF16])
+def test_token_layers_in_a_chain(dtype):
+    """A Sequential of norms, a convolution and a mixer: clips, pieces and steps
+    as its modules one after the other, with and without update_state."""
+    g = torch.Generator().manual_seed(95)
+    B, T = 2, 40
+    m = mixer(B, g, dtype)
+    w = torch.randn(m.width, 4, generator=g).to(dtype).to(DEV)
+    first = coinf.CoShortConv(w, batch=B)
+    pre, post = coinf.CoNorm(dim=m.width), coinf.CoNorm(dim=m.inner, groups=2)
+    net = coinf.Sequential(pre, first, m, post)
+    assert net.delay == 0 and net.t_stride == 1
+    x = torch.randn(B, T, m.width, generator=g).to(dtype).to(DEV)
+    want = post.forward(m.forward(first.forward(pre.forward(x))))
+    assert torch.equal(net.forward(x), want)
+    peek = net.forward_steps(x[:, :9], update_state=False)
+    assert torch.equal(net.forward_steps(x[:, :9]), peek)       # the peek left no trace
+    t9 = net.forward_step(x[:, 9], update_state=False)
+    assert torch.equal(net.forward_step(x[:, 9]), t9)
+    rest = net.forward_steps(x[:, 10:])
+    got = torch.cat((peek, t9[:, None], rest), 1)
+    # the chunks and single tokens of the scan differ by float32 sums, then by what the layers
+    # round them to: a rounding of the scan's, the gated norm's and the last norm's outputs each
+    assert R.relative(got, R.np64(want)) <= (6 * U[BF16] if dtype is BF16 else 1e-5)
+    net.clean_state()
+    assert not first.state.any() and not m.scan.state.any() and not m.conv.state.any()
+
+
+def test_norm_steps_have_the_forward_arguments():
+    g = torch.Generator().manual_seed(96)
+    layer = coinf.CoNorm(dim=32, gate="after", residual="before")
+    x, z, r = (torch.randn(2, 3, 32, generator=g).to(DEV) for _ in range(3))
+    want = layer.forward(x, z, r)
+    for f in (layer.forward_step, layer.forward_steps):
+        for update in (True, False):
+            got = f(x, z, r, update_state=update)
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+            out, new = torch.empty_like(x), torch.empty_like(r)
+            got = f(x, z, r, out, new, update_state=update)
+            assert got[0] is out and got[1] is new and torch.equal(out, want[0])
