@@ -1259,7 +1259,7 @@ class CoShortConv:
         self._dense = x.is_contiguous()
 
     def _run(self, x, lengths, state, update, out, step=False):
-        sig = (x.shape, x.stride(), x.dtype, x.is_cuda, state, update,
+        sig = (step, x.shape, x.stride(), x.dtype, x.is_cuda, state, update,
                None if out is None else (out.shape, out.stride(), out.dtype, out.is_cuda))
         if sig != self._sig:
             self._sig = None
@@ -1360,7 +1360,7 @@ class CoScan:
         self._nws = call.workspace_bytes = self.workspace_bytes(T)
 
     def _run(self, x, dt, b, c, lengths, state, update, out, step=False):
-        sig = (x.shape, x.stride(), x.dtype, x.is_cuda, dt.shape, dt.stride(), dt.dtype,
+        sig = (step, x.shape, x.stride(), x.dtype, x.is_cuda, dt.shape, dt.stride(), dt.dtype,
                dt.is_cuda, b.shape, b.stride(), b.dtype, b.is_cuda, c.shape, c.stride(), c.dtype,
                c.is_cuda, state, update,
                None if out is None else (out.shape, out.stride(), out.dtype, out.is_cuda))

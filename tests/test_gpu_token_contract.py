@@ -243,3 +243,36 @@ def test_norm_steps_have_the_forward_arguments():
             out, new = torch.empty_like(x), torch.empty_like(r)
             got = f(x, z, r, out, new, update_state=update)
             assert got[0] is out and got[1] is new and torch.equal(out, want[0])
+
+
+# ------------------------------------------------------------ arguments
+
+
+def test_wrong_rank_after_a_like_call():
+    """A call's arguments are checked for its own mode, also right after a call of
+    the other mode with the same tensors."""
+    w = torch.ones(24, 3, device=DEV)
+    conv = coinf.CoShortConv(w, batch=2)
+    x = torch.zeros(2, 24, device=DEV)
+    conv.forward_step(x)
+    for f in (conv.forward_steps, conv.forward):
+        with pytest.raises(ValueError):
+            f(x)
+        conv.forward_step(x)
+    conv.forward_steps(x[:, None])
+    with pytest.raises(ValueError):
+        conv.forward_step(x[:, None])
+    conv.forward(x[:, None])
+    with pytest.raises(ValueError):
+        conv.forward_step(x[:, None])
+    scan = coinf.CoScan(-torch.ones(3, device=DEV), batch=2, head_dim=8, state_size=4,
+                        dtype=torch.float32)
+    one = [torch.zeros(2, *s, device=DEV) for s in ((3, 8), (3,), (1, 4), (1, 4))]
+    scan.forward_step(*one)
+    for f in (scan.forward_steps, scan.forward):
+        with pytest.raises(ValueError):
+            f(*one)
+        scan.forward_step(*one)
+    scan.forward_steps(*(t[:, None] for t in one))
+    with pytest.raises(ValueError):
+        scan.forward_step(*(t[:, None] for t in one))
