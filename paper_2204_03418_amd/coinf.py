@@ -1163,12 +1163,18 @@ class Residual:
 _like = torch.empty_like  # 1.2 us; new_empty, for inputs that are slices, 1.5
 
 
-def _tokens(t, dtype, shape, what, into):
-    """Checks that t is a device tensor of that dtype and shape (B, T, ...), or
-    (B, ...) for single tokens, whose values of one token are contiguous, and
-    fills `into` with its strides."""
+def _on(t, device, what):
     if t.device.type != "cuda":
         raise ValueError(f"{what} must be a device tensor")
+    if t.device != device:
+        raise ValueError(f"{what} is on {t.device}, expected {device}")
+
+
+def _tokens(t, dtype, shape, what, into, device):
+    """Checks that t is a tensor on that device, of that dtype and shape (B, T, ...),
+    or (B, ...) for single tokens, whose values of one token are contiguous, and
+    fills `into` with its strides."""
+    _on(t, device, what)
     if t.dtype is not dtype:
         raise ValueError(f"{what} has dtype {t.dtype}, expected {dtype}")
     if t.shape not in (shape, shape[:1] + shape[2:] if shape[1] == 1 else shape):
@@ -1183,11 +1189,35 @@ def _tokens(t, dtype, shape, what, into):
     into.batch_stride, into.token_stride = st[0], st[1] if lead == 2 else 0
 
 
-def _lengths(lengths, batch):
-    if lengths is None:
-        return None
+def _lengths(lengths, batch, device):
     _need(lengths, torch.int32, (batch,), "lengths")
+    if lengths.device != device:
+        _on(lengths, device, "lengths")
     return lengths.data_ptr()
+
+
+class _TokenState:
+    """The state of a token layer: a tensor that another one of its kind may replace."""
+
+    def _keep_state(self, state, dtype, shape, device):
+        self._state_kind = dtype, shape, device
+        if state is None:
+            state = torch.zeros(shape, dtype=dtype, device=device)
+        self.state = state
+
+    @property
+    def state(self):
+        return self._state
+
+    @state.setter
+    def state(self, state):
+        dtype, shape, device = self._state_kind
+        _need(state, dtype, shape, "state")
+        _on(state, device, "state")
+        self._state = state
+
+    def clean_state(self):
+        self._state.zero_()
 
 
 def _vector(t, n, what, device):
@@ -1199,7 +1229,7 @@ def _vector(t, n, what, device):
     return t.detach().to(torch.float32).contiguous()
 
 
-class CoShortConv:
+class CoShortConv(_TokenState):
     """Short causal depthwise convolution over tokens with its activation
     (co_shortconv_* ABI).
 
@@ -1222,24 +1252,25 @@ class CoShortConv:
         self.batch, self.torch_dtype = batch, weight.dtype
         self.channels, self.kernel = weight.shape
         _need(weight, weight.dtype, weight.shape, "weight")
+        self.device = weight.device
         if bias is not None:
             _need(bias, weight.dtype, (self.channels,), "bias")
-        self.weight, self.bias = weight, bias
+            _on(bias, self.device, "bias")
+        self._weight, self._bias = weight, bias
         acts = {"none": CO_ACT_NONE, "relu": CO_ACT_RELU, "silu": CO_ACT_SILU}
         self.desc = ShortConvDesc(batch, self.channels, self.kernel, 1 if bias is not None else 0,
                                   acts[act], DTYPES[weight.dtype])
         nb = i64()
         check(co_shortconv_query(ctypes.byref(self.desc), ctypes.byref(nb)), "co_shortconv_query")
-        shape = (batch, self.kernel - 1, self.channels)
-        if state is None:
-            state = torch.zeros(shape, dtype=weight.dtype, device=weight.device)
-        _need(state, weight.dtype, shape, "state")
-        self.state = state
+        self._keep_state(state, weight.dtype, (batch, self.kernel - 1, self.channels), self.device)
         self._call = ShortConvCall(_ptr(weight), _ptr(bias))
         self._x, self._y = self._call.x, self._call.y
         self._args = ctypes.byref(self.desc), ctypes.byref(self._call)
         self._sig = None
 
+    # parameters: a call takes those that the layer was made with
+    weight = property(lambda self: self._weight)
+    bias = property(lambda self: self._bias)
     receptive_field = property(lambda self: self.kernel)
     t_padding = property(lambda self: self.kernel - 1)
 
@@ -1249,18 +1280,18 @@ class CoShortConv:
         if x.dim() != 3 - step:
             raise ValueError(f"x has shape {tuple(x.shape)}, expected "
                              f"{(B, C) if step else (B, 'T', C)}")
-        _tokens(x, self.torch_dtype, (B, T, C), "x", self._x)
+        _tokens(x, self.torch_dtype, (B, T, C), "x", self._x, self.device)
         self._y.batch_stride, self._y.token_stride = T * C, C
         if out is not None:
             if out.dim() != x.dim():
                 raise ValueError(f"out has shape {tuple(out.shape)}, expected {tuple(x.shape)}")
-            _tokens(out, self.torch_dtype, (B, T, C), "out", self._y)
+            _tokens(out, self.torch_dtype, (B, T, C), "out", self._y, self.device)
         call.T, call.state, call.update_state = T, state, update
         self._dense = x.is_contiguous()
 
     def _run(self, x, lengths, state, update, out, step=False):
-        sig = (step, x.shape, x.stride(), x.dtype, x.is_cuda, state, update,
-               None if out is None else (out.shape, out.stride(), out.dtype, out.is_cuda))
+        sig = (step, x.shape, x.stride(), x.dtype, x.get_device(), state, update,
+               None if out is None else (out.shape, out.stride(), out.dtype, out.get_device()))
         if sig != self._sig:
             self._sig = None
             self._check(x, out, step, state, update)
@@ -1268,7 +1299,7 @@ class CoShortConv:
         if out is None:
             out = _like(x) if self._dense else x.new_empty(x.shape)
         self._x.data, self._y.data = x.data_ptr(), out.data_ptr()
-        self._call.lengths = None if lengths is None else _lengths(lengths, self.batch)
+        self._call.lengths = None if lengths is None else _lengths(lengths, self.batch, self.device)
         pd, pc = self._args
         st = co_shortconv_forward_steps(pd, pc, _stream())
         if st != CO_OK:
@@ -1277,21 +1308,18 @@ class CoShortConv:
 
     def forward_steps(self, x, lengths=None, update_state=True, out=None):
         """The next T tokens x (B, T, C) of the streams -> (B, T, C)."""
-        return self._run(x, lengths, self.state.data_ptr(), 1 if update_state else 0, out)
+        return self._run(x, lengths, self._state.data_ptr(), 1 if update_state else 0, out)
 
     def forward_step(self, x_t, lengths=None, update_state=True, out=None):
         """The next token x_t (B, C) of each stream (of those with length 1) -> (B, C)."""
-        return self._run(x_t, lengths, self.state.data_ptr(), 1 if update_state else 0, out, True)
+        return self._run(x_t, lengths, self._state.data_ptr(), 1 if update_state else 0, out, True)
 
     def forward(self, x, lengths=None, out=None):
         """Whole sequences from a clean state, which the layer's own is not touched by."""
         return self._run(x, lengths, None, 0, out)
 
-    def clean_state(self):
-        self.state.zero_()
 
-
-class CoScan:
+class CoScan(_TokenState):
     """Selective state space scan (co_scan_* ABI): heads of head_dim values with
     a head_dim x state_size state each, a decay a head and token, and B and C
     shared by the heads of a group.
@@ -1312,22 +1340,24 @@ class CoScan:
         H = self.heads = A.shape[0]
         self.batch, self.head_dim, self.state_size = batch, head_dim, state_size
         self.groups, self.torch_dtype = groups, dtype
-        self.A = _vector(A, H, "A", A.device)
-        self.D = _vector(D, H, "D", A.device)
-        self.dt_bias = _vector(dt_bias, H, "dt_bias", A.device)
+        self.device = A.device
+        self._A = _vector(A, H, "A", A.device)
+        self._D = _vector(D, H, "D", A.device)
+        self._dt_bias = _vector(dt_bias, H, "dt_bias", A.device)
         self.desc = ScanDesc(batch, H, head_dim, state_size, groups, 1 if dt_softplus else 0,
                              DTYPES[dtype], DTYPES[dtype])
         nb = i64()
         check(co_scan_query(ctypes.byref(self.desc), ctypes.byref(nb)), "co_scan_query")
-        shape = (batch, H, head_dim, state_size)
-        if state is None:
-            state = torch.zeros(shape, dtype=torch.float32, device=A.device)
-        _need(state, torch.float32, shape, "state")
-        self.state = state
-        call = self._call = ScanCall(_ptr(self.A), _ptr(self.D), _ptr(self.dt_bias))
+        self._keep_state(state, torch.float32, (batch, H, head_dim, state_size), self.device)
+        call = self._call = ScanCall(_ptr(self._A), _ptr(self._D), _ptr(self._dt_bias))
         self._parts = call.x, call.dt, call.b, call.c, call.y
         self._args = ctypes.byref(self.desc), ctypes.byref(call)
         self._sig = None
+
+    # parameters: a call takes those that the layer was made with
+    A = property(lambda self: self._A)
+    D = property(lambda self: self._D)
+    dt_bias = property(lambda self: self._dt_bias)
 
     def workspace_bytes(self, T):
         """Device workspace of a call over T tokens."""
@@ -1353,17 +1383,17 @@ class CoScan:
             if t.dim() != len(shape) - step:
                 raise ValueError(f"{what} has shape {tuple(t.shape)}, expected "
                                  f"{shape[:1] + shape[2:] if step else shape}")
-            _tokens(t, kind, shape, what, into)
+            _tokens(t, kind, shape, what, into, self.device)
         self.desc.dt_dtype = DTYPES[dt_dtype]
         call.T, call.state, call.update_state = T, state, update
         self._dense = x.is_contiguous()
         self._nws = call.workspace_bytes = self.workspace_bytes(T)
 
     def _run(self, x, dt, b, c, lengths, state, update, out, step=False):
-        sig = (step, x.shape, x.stride(), x.dtype, x.is_cuda, dt.shape, dt.stride(), dt.dtype,
-               dt.is_cuda, b.shape, b.stride(), b.dtype, b.is_cuda, c.shape, c.stride(), c.dtype,
-               c.is_cuda, state, update,
-               None if out is None else (out.shape, out.stride(), out.dtype, out.is_cuda))
+        sig = (step, x.shape, x.stride(), x.dtype, x.get_device(), dt.shape, dt.stride(), dt.dtype,
+               dt.get_device(), b.shape, b.stride(), b.dtype, b.get_device(), c.shape, c.stride(),
+               c.dtype, c.get_device(), state, update,
+               None if out is None else (out.shape, out.stride(), out.dtype, out.get_device()))
         if sig != self._sig:
             self._sig = None
             self._check(x, dt, b, c, out, step, state, update)
@@ -1374,7 +1404,7 @@ class CoScan:
         ix.data, idt.data, ib.data = x.data_ptr(), dt.data_ptr(), b.data_ptr()
         ic.data, iy.data = c.data_ptr(), out.data_ptr()
         call = self._call
-        call.lengths = None if lengths is None else _lengths(lengths, self.batch)
+        call.lengths = None if lengths is None else _lengths(lengths, self.batch, self.device)
         ws = None
         if self._nws:
             ws = torch.empty(self._nws, dtype=torch.uint8, device=x.device)
@@ -1387,20 +1417,17 @@ class CoScan:
 
     def forward_steps(self, x, dt, b, c, lengths=None, update_state=True, out=None):
         """The next T tokens: x (B, T, H, P), dt (B, T, H), b and c (B, T, G, N) -> (B, T, H, P)."""
-        return self._run(x, dt, b, c, lengths, self.state.data_ptr(), 1 if update_state else 0,
+        return self._run(x, dt, b, c, lengths, self._state.data_ptr(), 1 if update_state else 0,
                          out)
 
     def forward_step(self, x_t, dt_t, b_t, c_t, lengths=None, update_state=True, out=None):
         """The next token of each stream (of those with length 1): the same without T."""
-        return self._run(x_t, dt_t, b_t, c_t, lengths, self.state.data_ptr(),
+        return self._run(x_t, dt_t, b_t, c_t, lengths, self._state.data_ptr(),
                          1 if update_state else 0, out, True)
 
     def forward(self, x, dt, b, c, lengths=None, out=None):
         """Whole sequences from a clean state, which the layer's own is not touched by."""
         return self._run(x, dt, b, c, lengths, None, 0, out)
-
-    def clean_state(self):
-        self.state.zero_()
 
 
 class CoNorm:
@@ -1431,21 +1458,24 @@ class CoNorm:
         for t, what in ((weight, "weight"), (scale, "scale")):
             if t is not None and t.device.type != "cuda":
                 raise ValueError(f"{what} must be a device tensor")
-        self.weight = _vector(weight, self.dim, "weight", weight.device) \
-            if weight is not None else None
-        self.scale = _vector(scale, self.dim, "scale", scale.device) if scale is not None else None
+        self.device = given.device if given is not None else None  # None: any input's
+        self._weight = _vector(weight, self.dim, "weight", self.device)
+        self._scale = _vector(scale, self.dim, "scale", self.device)
         self.gate, self.residual = gate, residual
         self.desc = NormDesc(0, 0, self.dim, groups, self.MODES[gate], self.MODES[residual], CO_F32,
                              CO_F32, eps)
-        call = self._call = NormCall(weight=_ptr(self.weight), scale=_ptr(self.scale))
+        call = self._call = NormCall(weight=_ptr(self._weight), scale=_ptr(self._scale))
         self._x, self._z, self._r, self._y, self._o = (call.x, call.gate, call.residual, call.y,
                                                        call.residual_out)
         self._args = ctypes.byref(self.desc), ctypes.byref(call)
         self._sig = None
 
-    def _rows(self, t, dtype, shape, tokens, what, into):
-        if t.device.type != "cuda":
-            raise ValueError(f"{what} must be a device tensor")
+    # parameters: a call takes those that the layer was made with
+    weight = property(lambda self: self._weight)
+    scale = property(lambda self: self._scale)
+
+    def _rows(self, t, dtype, shape, tokens, what, into, device):
+        _on(t, device, what)
         if t.dtype is not dtype:
             raise ValueError(f"{what} has dtype {t.dtype}, expected {dtype}")
         if t.shape != shape:
@@ -1466,13 +1496,13 @@ class CoNorm:
         bfloat16) -> y; (y, new residual) with residual "before"; the new residual
         with "after".  out may be x, residual_out may be residual.  lengths (of x
         (B, T, D), or (B, D) for single tokens): as CoShortConv's."""
-        sig = (lengths is None, x.shape, x.stride(), x.dtype, x.is_cuda,
-               None if gate is None else (gate.shape, gate.stride(), gate.dtype, gate.is_cuda),
+        sig = (lengths is None, x.shape, x.stride(), x.dtype, x.get_device(),
+               None if gate is None else (gate.shape, gate.stride(), gate.dtype, gate.get_device()),
                None if residual is None else (residual.shape, residual.stride(), residual.dtype,
-                                              residual.is_cuda),
-               None if out is None else (out.shape, out.stride(), out.dtype, out.is_cuda),
+                                              residual.get_device()),
+               None if out is None else (out.shape, out.stride(), out.dtype, out.get_device()),
                None if residual_out is None else (residual_out.shape, residual_out.stride(),
-                                                  residual_out.dtype, residual_out.is_cuda))
+                                                  residual_out.dtype, residual_out.get_device()))
         if sig != self._sig:
             self._sig = None
             self._check(x, gate, residual, out, residual_out, lengths is not None)
@@ -1493,7 +1523,7 @@ class CoNorm:
         if lengths is None:
             st = co_norm_forward(pd, pc, _stream())
         else:
-            st = co_norm_forward_lengths(pd, pc, _lengths(lengths, x.shape[0]), _stream())
+            st = co_norm_forward_lengths(pd, pc, _lengths(lengths, x.shape[0], x.device), _stream())
         if st != CO_OK:
             check(st, "co_norm_forward")
         if form is None:
@@ -1514,20 +1544,22 @@ class CoNorm:
         tokens = shape[-2] if x.dim() > (2 if ragged else 1) else 1
         d.tokens, d.dtype = tokens, DTYPES[x.dtype]
         d.batch = x.numel() // (tokens * self.dim) if tokens else 0
-        self._rows(x, x.dtype, shape, tokens, "x", self._x)
+        dev = x.device if self.device is None else self.device
+        self._rows(x, x.dtype, shape, tokens, "x", self._x, dev)
         if gate is not None:
-            self._rows(gate, x.dtype, shape, tokens, "gate", self._z)
+            self._rows(gate, x.dtype, shape, tokens, "gate", self._z, dev)
         if residual is not None:
             if residual.dtype not in DTYPES:
                 raise ValueError(f"residual has dtype {residual.dtype}")
             d.residual_dtype = DTYPES[residual.dtype]
-            self._rows(residual, residual.dtype, shape, tokens, "residual", self._r)
+            self._rows(residual, residual.dtype, shape, tokens, "residual", self._r, dev)
             self._o.batch_stride, self._o.token_stride = tokens * self.dim, self.dim
             if residual_out is not None:
-                self._rows(residual_out, residual.dtype, shape, tokens, "residual_out", self._o)
+                self._rows(residual_out, residual.dtype, shape, tokens, "residual_out", self._o,
+                           dev)
         self._y.batch_stride, self._y.token_stride = tokens * self.dim, self.dim
         if out is not None:
-            self._rows(out, x.dtype, shape, tokens, "out", self._y)
+            self._rows(out, x.dtype, shape, tokens, "out", self._y, dev)
         self._dense = x.is_contiguous(), residual is not None and residual.is_contiguous()
 
     def forward_steps(self, x, gate=None, residual=None, out=None, residual_out=None,

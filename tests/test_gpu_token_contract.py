@@ -276,3 +276,31 @@ def test_wrong_rank_after_a_like_call():
     scan.forward_steps(*(t[:, None] for t in one))
     with pytest.raises(ValueError):
         scan.forward_step(*(t[:, None] for t in one))
+
+
+def test_replaced_states_are_checked():
+    """layer.state may be another tensor of its kind, and nothing else: a call
+    reads and writes what the descriptor says."""
+    conv = coinf.CoShortConv(torch.ones(24, 3, device=DEV), batch=2)
+    scan = coinf.CoScan(-torch.ones(3, device=DEV), batch=2, head_dim=8, state_size=4,
+                        dtype=torch.float32)
+    one = [torch.ones(2, *s, device=DEV) for s in ((3, 8), (3,), (1, 4), (1, 4))]
+    for layer, step in ((conv, lambda: conv.forward_step(torch.ones(2, 24, device=DEV))),
+                        (scan, lambda: scan.forward_step(*one))):
+        old = layer.state
+        step()
+        first = old.clone()
+        for bad in (old[:1], old.bfloat16(), old.cpu(), old.transpose(0, 1), old.flatten(),
+                    old.transpose(1, 2).contiguous().transpose(1, 2)):
+            with pytest.raises(ValueError):
+                layer.state = bad
+        assert layer.state is old
+        layer.state = new = torch.zeros_like(old)
+        step()
+        assert torch.equal(new, first) and torch.equal(old, first)
+        layer.clean_state()
+        assert not new.any() and old.any()
+    for layer, name in ((conv, "weight"), (conv, "bias"), (scan, "A"), (scan, "D"),
+                        (scan, "dt_bias"), (coinf.CoNorm(dim=8), "weight")):
+        with pytest.raises(AttributeError):                     # what a call would not take
+            setattr(layer, name, None)

@@ -1,6 +1,9 @@
 """What the token layers promise, as far as the host shows it.  No GPU."""
 import ctypes
 
+import pytest
+import torch
+
 from paper_2204_03418_amd import coinf as C
 from test_token_abi import P, norm, ref
 
@@ -14,3 +17,46 @@ def test_norm_lengths_arguments():
     assert run(norm(eps=-1.0), P) == C.CO_EINVAL
     assert C.co_norm_forward_lengths(ref(norm()), None, P, None) == C.CO_EINVAL
     assert ctypes.sizeof(C.NormCall) == 5 * 24 + 16             # as co_norm_forward's callers have it
+
+
+class OnDevice:
+    """The part of a device tensor that the binding looks at, on any device."""
+
+    def __init__(self, index, shape, dtype=torch.float32):
+        self.device, self.shape, self.dtype = torch.device("cuda", index), torch.Size(shape), dtype
+        self.is_cuda = True
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return self.shape.numel()
+
+    def stride(self, axis=None):
+        st = [1]
+        for n in reversed(self.shape[1:]):
+            st.insert(0, st[0] * n)
+        return tuple(st) if axis is None else st[axis]
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return P
+
+
+def test_tensors_of_another_gpu_are_refused():
+    here, shape = torch.device("cuda", 0), torch.Size((2, 5, 8))
+    into = C.Tokens()
+    C._tokens(OnDevice(0, shape), torch.float32, shape, "x", into, here)
+    assert (into.batch_stride, into.token_stride) == (40, 8)
+    with pytest.raises(ValueError, match="cuda:1"):
+        C._tokens(OnDevice(1, shape), torch.float32, shape, "x", into, here)
+    n = (2,), torch.int32
+    assert C._lengths(OnDevice(0, *n), 2, here) == P
+    with pytest.raises(ValueError, match="cuda:1"):
+        C._lengths(OnDevice(1, *n), 2, here)
+    norm_layer = C.CoNorm(dim=8)
+    norm_layer._rows(OnDevice(1, shape), torch.float32, shape, 5, "x", into, torch.device("cuda", 1))
+    with pytest.raises(ValueError, match="cuda:1"):
+        norm_layer._rows(OnDevice(1, shape), torch.float32, shape, 5, "gate", into, here)
