@@ -64,12 +64,14 @@ struct ChunkDecay {
   float total;  // of the chunk
   float reach;  // the largest magnitude of the sums
   float pad[2];
-  float grow[kChunk];    // 2^{cum_t}
-  float weight[kChunk];  // 2^{-cum_t} d_t, or 2^{total - cum_t} d_t where the reach passes kSpan
+  // 2^{cum_t}, and from kChunk on 2^{-cum_t} d_t, or 2^{total - cum_t} d_t where the reach passes
+  // kSpan: a value for each lane of a wave
+  float factor[2 * kChunk];
   // where the reach passes kSpan: d_t, and cum_t = cum + cum_low
   float step[kChunk], cum[kChunk], cum_low[kChunk];
 };
 static_assert(sizeof(ChunkDecay) % 16 == 0);
+static_assert(std::extent_v<decltype(ChunkDecay::factor)> == 64);
 
 struct ChunkArgs {
   ScanCall c;
@@ -414,8 +416,8 @@ __global__ __launch_bounds__(kBlock) void scan_prepare_kernel(ChunkArgs a) {
       o.total = float(total);
       o.reach = reach;
     }
-    o.grow[q] = pow2(cum);
-    o.weight[q] = dt * pow2(reach <= kSpan ? -cum : total - cum);
+    o.factor[q] = pow2(cum);
+    o.factor[kChunk + q] = dt * pow2(reach <= kSpan ? -cum : total - cum);
     if (reach <= kSpan) continue;  // what follows is for the chunks that go far
     o.step[q] = dt;
     o.cum[q] = float(cum);
@@ -576,7 +578,7 @@ __global__ __launch_bounds__(kWaves * 64, !FULL && sizeof(T) == 2 ? 3 : 2) void 
     }
     if (FULL) rbc = bc_at[min(tid, kPairs * 64 - 1)];
     const ChunkDecay& c = decay[(t0 - t_begin) / Q];
-    rdecay = c.grow[lane];  // and weight behind it
+    rdecay = c.factor[lane];
     rtotal = c.total;
     rreach = c.reach;
     b_at += Q * io.b.token_stride;
