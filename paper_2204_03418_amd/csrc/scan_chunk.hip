@@ -874,6 +874,17 @@ __global__ __launch_bounds__(kBlock) void scan_carry_kernel(ChunkArgs a, uint32_
   store_pack<float, V>(w + last * size, s);
 }
 
+// The launch before the chunks has prepare_doubles x prepare_jobs workgroups, the carry
+// carry_blocks a head, V values a thread.
+int64_t prepare_doubles(const co_scan_desc& d, int64_t chunks) { return (chunks + 1) / 2 * d.batch; }
+int64_t prepare_jobs(const co_scan_desc& d) {
+  const int64_t waves = (int64_t(d.heads) + kHeads - 1) / kHeads + 2 * int64_t(d.groups);
+  return (waves + kBlock / 64 - 1) / (kBlock / 64);
+}
+int64_t carry_blocks(const co_scan_desc& d, int64_t V) {
+  return (int64_t(d.head_dim) * d.state_size + V * kBlock - 1) / (V * kBlock);
+}
+
 // Workgroups of an uncut call with units of so many rows.
 int64_t workgroups(const co_scan_desc& d, int64_t rows) {
   const int64_t units = int64_t(d.heads / d.groups) * ((d.head_dim + rows - 1) / rows);
@@ -898,19 +909,13 @@ int unit_rows(const co_scan_desc& d, int64_t T) {
 template <typename T, int NT, int PT, bool WIDE>
 hipError_t launch_tiles(ChunkArgs a, hipStream_t s) {
   const co_scan_desc& d = a.c.d;
-  a.p_blocks = (d.head_dim + 16 * PT - 1) / (16 * PT);
+  a.p_blocks = int32_t((int64_t(d.head_dim) + 16 * PT - 1) / (16 * PT));
   const int64_t units = int64_t(d.heads / d.groups) * a.p_blocks;
   a.unit_blocks = int32_t((units + kWaves - 1) / kWaves);
   const int64_t grid = int64_t(a.unit_blocks) * d.groups * d.batch;
-  const int64_t jobs = ((int64_t(d.heads) + kHeads - 1) / kHeads + 2 * int64_t(d.groups) +
-                        kBlock / 64 - 1) / (kBlock / 64);
-  const int64_t doubles = (int64_t(a.chunks) + 1) / 2 * d.batch;
+  const int64_t jobs = prepare_jobs(d), doubles = prepare_doubles(d, a.chunks);
   constexpr int CV = WIDE ? 4 : 1;  // a state row is then whole pieces of 16 bytes
-  const int64_t head_blocks =
-      (int64_t(d.head_dim) * d.state_size + CV * kBlock - 1) / (CV * kBlock);
-  if (!grid_fits(grid * a.segments) || !grid_fits(doubles * jobs) || jobs > 65535 ||
-      !grid_fits(head_blocks * d.batch * d.heads))
-    return hipErrorInvalidConfiguration;
+  const int64_t head_blocks = carry_blocks(d, CV);
   hipLaunchKernelGGL((scan_prepare_kernel<T, WIDE>), dim3(unsigned(doubles), unsigned(jobs)),
                      dim3(kBlock), 0, s, a);
   if (a.segments > 1) {
@@ -998,9 +1003,17 @@ Space space_of(const co_scan_desc& d, int64_t chunks, int64_t segments) {
 // chunks take 9 us more to begin with, and 0.3 us a million values.  Measured, us, by token and in
 // chunks: 16.8 million values, 4 tokens 31 and 35, 8 tokens 40 and 36, 32 tokens 97 and 39;
 // 0.5 million, 16 tokens 10 and 13, 32 tokens 17 and 13.
+//
+// Calls whose chunks would pass what a launch may have of workgroups go token by token.
 bool scan_chunk_takes(const co_scan_desc& d, int32_t T) {
   const double millions = 1e-6 * d.batch * d.heads * double(d.head_dim) * d.state_size;
-  return T * (0.3 + 0.11 * millions) > 9.0 + 0.3 * millions;
+  if (!(T * (0.3 + 0.11 * millions) > 9.0 + 0.3 * millions)) return false;
+  int64_t segments, seg_chunks;
+  cut(d, T, &segments, &seg_chunks);
+  const int64_t chunks = (int64_t(T) + kChunk - 1) / kChunk, jobs = prepare_jobs(d);
+  return grid_fits(workgroups(d, unit_rows(d, T)) * segments) && jobs <= 65535 &&
+         grid_fits(prepare_doubles(d, chunks) * jobs) &&
+         grid_fits(carry_blocks(d, 1) * d.batch * d.heads);
 }
 
 int64_t scan_chunk_workspace(const co_scan_desc& d, int32_t T) {

@@ -196,7 +196,9 @@ __global__ __launch_bounds__(kBlock) void scan_seq_kernel(SeqArgs a) {
 template <typename T, int NL, int ROWS>
 hipError_t launch_rows(const ScanCall& c, bool wide, hipStream_t s) {
   const int per = kBlock / NL * ROWS;
-  SeqArgs a{c, (c.d.head_dim + per - 1) / per};
+  const int64_t p_blocks = (int64_t(c.d.head_dim) + per - 1) / per;
+  if (p_blocks * per > INT32_MAX) return hipErrorInvalidConfiguration;  // rows are counted in int
+  SeqArgs a{c, int32_t(p_blocks)};
   const int64_t grid = int64_t(a.p_blocks) * c.d.heads * c.d.batch;
   if (!grid_fits(grid)) return hipErrorInvalidConfiguration;
   const auto go = [&](auto kernel) {
@@ -215,7 +217,7 @@ hipError_t launch_lanes(const ScanCall& c, bool wide, hipStream_t s) {
   // As many rows a thread as leave about four workgroups for each of 256 CUs.
   const int64_t rows = int64_t(c.d.batch) * c.d.heads * c.d.head_dim;
   const int64_t fill = rows / (int64_t(kBlock / NL) * 1024);
-  const int fit = c.d.head_dim * NL / kBlock;  // rows that one head gives a thread
+  const int64_t fit = int64_t(c.d.head_dim) * NL / kBlock;  // rows that one head gives a thread
   const int64_t most = fill < fit ? fill : fit;
   if constexpr (NL >= 8)
     if (most >= 8) return launch_rows<T, NL, 8>(c, wide, s);

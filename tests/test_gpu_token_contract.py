@@ -304,3 +304,24 @@ def test_replaced_states_are_checked():
                         (scan, "dt_bias"), (coinf.CoNorm(dim=8), "weight")):
         with pytest.raises(AttributeError):                     # what a call would not take
             setattr(layer, name, None)
+
+
+@pytest.mark.parametrize("H,G", [(1 << 20, 1), (1 << 17, 1 << 17)])
+def test_scan_of_more_heads_than_a_launch_of_chunks_has(H, G):
+    """Such a call runs token by token instead of being refused."""
+    g = torch.Generator().manual_seed(97)
+    T = 120
+    x, dt = (torch.randn(1, T, H, generator=g) for _ in range(2))
+    b, c = (torch.randn(1, T, G, 1, generator=g) for _ in range(2))
+    A = -torch.rand(H, generator=g)
+    layer = coinf.CoScan(A.to(DEV), batch=1, head_dim=1, state_size=1, groups=G, dt_softplus=True,
+                         dtype=torch.float32)
+    got = layer.forward_steps(*(t.to(DEV) for t in (x.unsqueeze(-1), dt, b, c)))
+    d = torch.nn.functional.softplus(dt.double().to(DEV), threshold=60.0)[0]
+    xd, bd, cd = x.double().to(DEV)[0], b.double().to(DEV)[0, :, :, 0], c.double().to(DEV)[0, :, :, 0]
+    S = M = torch.zeros(H, dtype=torch.float64, device=DEV)
+    for t in range(T):
+        a, u = torch.exp(d[t] * A.double().to(DEV)), d[t] * xd[t] * bd[t]
+        S, M = a * S + u, a * M + u.abs()
+        off = (got[0, t, :, 0] - S * cd[t]).abs()
+        assert (off <= (4 * T + 65) * R.U32 * (M * cd[t].abs())).all(), t

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2204_03418_amd import coinf as C
-from test_token_abi import P, norm, ref
+from test_token_abi import P, norm, ref, scan
 
 
 def test_norm_lengths_arguments():
@@ -60,3 +60,16 @@ def test_tensors_of_another_gpu_are_refused():
     norm_layer._rows(OnDevice(1, shape), torch.float32, shape, 5, "x", into, torch.device("cuda", 1))
     with pytest.raises(ValueError, match="cuda:1"):
         norm_layer._rows(OnDevice(1, shape), torch.float32, shape, 5, "gate", into, here)
+
+
+@pytest.mark.parametrize("big", [
+    dict(batch=1, heads=1 << 20, head_dim=1, state_size=1, groups=1),
+    dict(batch=1, heads=1 << 17, head_dim=4, state_size=16, groups=1 << 17),
+    dict(batch=1 << 12, heads=1 << 13, head_dim=1, state_size=1, groups=1 << 13)], ids=str)
+def test_scan_workspace_of_calls_too_wide_for_chunks(big):
+    """What a launch of the chunked form cannot hold runs token by token, which
+    wants no workspace."""
+    n = C.i64(-1)
+    assert C.co_scan_workspace_bytes(ref(scan(**big)), 1000, ref(n)) == C.CO_OK and n.value == 0
+    small = dict(big, batch=1, heads=16, groups=min(big["groups"], 16))
+    assert C.co_scan_workspace_bytes(ref(scan(**small)), 1000, ref(n)) == C.CO_OK and n.value > 0
