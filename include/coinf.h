@@ -840,7 +840,8 @@ co_status co_scan_forward_steps(const co_scan_desc* desc, const co_scan_call* ca
  * (dim); weight and scale may be NULL (1).  y is not written with residual
  * CO_NORM_AFTER, r' not with residual CO_NORM_NONE (their pointers may be NULL).
  * All in float32, each output rounded once; the pre-norm's y is made from the
- * unrounded sum.  y may be x, z or (same dtype) r; r_out may be r, x or z.
+ * unrounded sum.  y and r' may be in place of x, z or r (values of the same size
+ * at the same strides), not of each other.
  */
 #define CO_NORM_NONE    0
 #define CO_NORM_BEFORE  1

@@ -2,6 +2,7 @@
 // Stateless host side: every call checks its arguments, picks a kernel and
 // enqueues it; a negative status means nothing ran.
 #include <cmath>
+#include <initializer_list>
 
 #include "device.hpp"
 #include "launch.hpp"
@@ -41,6 +42,15 @@ bool out_ok(const co_tokens& t, int32_t B, int32_t T, int64_t width, int32_t dty
   if (T == 1 || B == 1) return true;
   return t.batch_stride >= (T - 1) * t.token_stride + width ||
          t.token_stride >= (B - 1) * t.batch_stride + width;
+}
+
+// Whether an output may be written while workgroups still read an input: they are apart, or it is
+// in place, every value where the input has it.
+bool in_place_ok(const co_tokens& out, int32_t out_dtype, const co_tokens& in, int32_t in_dtype,
+                 int32_t B, int32_t T) {
+  return out.data != in.data ||
+         (elem(out_dtype) == elem(in_dtype) && (B == 1 || out.batch_stride == in.batch_stride) &&
+          (T == 1 || out.token_stride == in.token_stride));
 }
 
 // A call too large for one launch is refused by its launcher.
@@ -161,6 +171,14 @@ co_status co_norm_forward_lengths(const co_norm_desc* desc, const co_norm_call* 
   if (!desc->gate) c.gate = none;
   if (!desc->residual) c.residual = c.residual_out = none;
   if (desc->residual == CO_NORM_AFTER) c.y = none;
+  for (const co_tokens* out : {&c.y, &c.residual_out}) {
+    const int32_t ot = out == &c.y ? dt : rt;
+    if (!out->data) continue;
+    if (!in_place_ok(*out, ot, c.x, dt, B, T) || !in_place_ok(*out, ot, c.gate, dt, B, T) ||
+        !in_place_ok(*out, ot, c.residual, rt, B, T))
+      return CO_EINVAL;
+  }
+  if (c.y.data && c.y.data == c.residual_out.data) return CO_EINVAL;
   return done(launch_norm(*desc, c, lengths, as_stream(stream)));
 }
 

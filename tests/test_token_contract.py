@@ -73,3 +73,22 @@ def test_scan_workspace_of_calls_too_wide_for_chunks(big):
     assert C.co_scan_workspace_bytes(ref(scan(**big)), 1000, ref(n)) == C.CO_OK and n.value == 0
     small = dict(big, batch=1, heads=16, groups=min(big["groups"], 16))
     assert C.co_scan_workspace_bytes(ref(scan(**small)), 1000, ref(n)) == C.CO_OK and n.value > 0
+
+
+def test_norm_in_place_means_the_same_places():
+    """An output at an input's address but with other strides or another element
+    size would be written over rows that are still to be read."""
+    def call(d, x=(P, 48, 16), gate=None, residual=None, y=(8 * P, 48, 16), out=None):
+        t = [C.Tokens(*v) if v else C.Tokens() for v in (x, gate, residual, y, out)]
+        return C.co_norm_forward(ref(d), ref(C.NormCall(*t, None, None)), None)
+
+    sizes = dict(batch=2, tokens=3, dim=16)
+    turned = (P, 16, 32)                                        # streams beside each other
+    assert call(norm(**sizes), y=turned) == C.CO_EINVAL
+    assert call(norm(**sizes, gate=1), gate=(3 * P, 48, 16), y=(3 * P, 96, 16)) == C.CO_EINVAL
+    both = dict(sizes, residual=1, dtype=C.CO_BF16, residual_dtype=C.CO_F32)
+    assert call(norm(**both), residual=(4 * P, 48, 16), out=(P, 48, 16)) == C.CO_EINVAL
+    assert call(norm(**both), residual=(4 * P, 48, 16), y=(4 * P, 48, 16),
+                out=(5 * P, 48, 16)) == C.CO_EINVAL
+    assert call(norm(**sizes, residual=1), residual=(4 * P, 48, 16), y=(5 * P, 48, 16),
+                out=(5 * P, 48, 16)) == C.CO_EINVAL             # both outputs in one place
