@@ -713,7 +713,8 @@ co_status co_chain_delay(int32_t n, const int32_t* f, const int32_t* s, const in
  * A token sequence is time-major, (B, T, values): the layout in which the
  * projections around these layers read and write it.  The three layers below
  * have delay 0 and follow Definition 1: a clip, a sequence of pieces and single
- * tokens give the same outputs from one set of parameters.  Their whole state
+ * tokens give the same outputs from one set of parameters, bit for bit but for
+ * the scan's, whose sums a piece may take in another order (see there).  Their whole state
  * is device memory in the stated plain layout (no header, no host counter): it
  * may be read, copied, zeroed or gathered by the caller between calls, and a
  * call captured in a graph advances it on every replay.  No handle, no
@@ -789,8 +790,16 @@ co_status co_shortconv_forward_steps(const co_shortconv_desc* desc, const co_sho
  *   y[b,t,h,:] = S_t C[b,t,g,:] + D[h] x[b,t,h,:].
  * x and y (B, T, H P), dt (B, T, H), B and C (B, T, G N); A, D and dt_bias
  * float32 (H), D and dt_bias may be NULL.  State (B, H, P, N) float32.
- * Decays are meant to be at most 1 (d_t A[h] <= 0); one below 2^-160 is taken
- * as 2^-160, which leaves nothing of a float32 either.
+ * Decays are meant to be at most 1 (d_t A[h] <= 0); one that is, or over several
+ * tokens gets, below float32's least normal value, 2^-126, may count as 0.
+ *
+ * Sums are float32.  Token by token they are taken in order.  Longer calls with
+ * a workspace take 32 tokens at a time (a sum then differs by its order alone,
+ * and with CO_BF16 by 2^-16 of the sum of its terms' magnitudes), and keep
+ * states and inputs times up to 2^64 in between: a state, or a d x B, of 2^63 and
+ * more may overflow there.  What a value that is not finite reaches (its token's
+ * outputs and later ones of its row, that row of the state; all rows for dt, B
+ * and C) is not finite, infinity or NaN; it reaches nothing else.
  */
 typedef struct co_scan_desc {
   int32_t batch;
