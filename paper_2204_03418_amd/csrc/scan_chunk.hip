@@ -13,14 +13,15 @@
 // of two 16-row result tiles.  The same holds for B_s . C_t, whose result tiles
 // become the operand of the product with x without leaving their lanes.
 //
-// bfloat16: x, B and C are used as they are. What is float32 and becomes an
+// bfloat16: x, B and C are used as they are.  What is float32 and becomes an
 // operand goes in bfloat16 terms: two (16 bits) of e^{...} d_s (B_s . C_t) and of
 // the state in its product with C, whose sums are rounded to bfloat16 once as y, 8
 // bits; three (24 bits) of the weighted x in the state's sum, which goes on being
-// summed. With one term of the first two, y was off by u times the sum of its
-// terms' magnitudes, far more than its own rounding where they cancel, and differed
-// so from single tokens (16384 tokens of 64 heads 190 us, now 215). float32
-// inputs use the float32 matrix instructions throughout.
+// summed.  With one term of the first two, y was off by u times the sum of its
+// terms' magnitudes, far more than its own rounding where they cancel, and
+// differed as much from single tokens (16384 tokens of 64 heads: 190 us with one
+// term, 200 to 215 with two).  float32 inputs use the float32 matrix instructions
+// throughout.
 //
 // A small launch before makes what the heads of a group and the units of a head
 // share: the products B_s . C_t, and of each chunk its decays.  Long sequences
@@ -33,12 +34,12 @@
 // tokens took 65 registers more than two waves of a SIMD have.
 //
 // Measured: 16384 tokens of 64 heads of 64 x 128, one group, bfloat16: 283 MB and
-// 43 GFLOP of the recurrence in 190 us; the launches take 12 us (B . C, decays),
-// 69 us (segments' sums), 14 us (carry) and 122 us (outputs) when traced.  The
-// last runs its matrix products at 317 TFLOP/s, 598 with the split's three terms
-// counted; it is bound by issue and latency at two waves a SIMD (matrix
-// pipes busy 35% of the cycles, vector units 55%, waves waiting 27%), not
-// by memory (228 MB from and to memory in it, 1.9 TB/s).  Tried and no faster:
+// 43 GFLOP of the recurrence in 200 us; the launches take 12 us (B . C, decays),
+// 71 us (segments' sums), 14 us (carry) and 151 us (outputs) when traced.  The
+// last runs its matrix instructions at 626 TFLOP/s (256 without the further terms
+// of the split operands); it is bound by issue and latency at two waves a SIMD
+// (matrix pipes busy 38% of the cycles, vector units 68%, waves waiting 21%), not
+// by memory (327 MB from and to memory in it, 2.2 TB/s).  Tried and no faster:
 // three waves a SIMD (spills), eight waves a workgroup, operands read further
 // ahead, matrix and vector instructions interleaved by hand, sums of finer parts than
 // the segments at three and four waves a SIMD.
@@ -451,8 +452,8 @@ __global__ __launch_bounds__(kWaves * 64, !FULL && sizeof(T) == 2 ? 3 : 2) void 
   const int P = d.head_dim, N = d.state_size;
 
   // Workgroups go to the 8 XCDs in turn.  In long segments those that read the same B and C go to
-  // one, whose L2 then has them (16 ragged prompts of 24 heads 57.0 -> 56.1 us, 16384 tokens of 64
-  // heads 133 -> 129 us); in segments of 8 chunks that was slower (1000 tokens 41 -> 49 us).
+  // one, whose L2 then has them (16 ragged prompts of 24 heads 72.7 -> 69.9 us, 16384 tokens of 64
+  // heads 205 either way); in segments of 8 chunks that is slower (1000 tokens 42 -> 50 us).
   const uint32_t eighth = gridDim.x / 8;
   const bool together = gridDim.x % 8 == 0 && a.seg_chunks >= 16;
   const uint32_t place = together ? blockIdx.x % 8 * eighth + blockIdx.x / 8 : blockIdx.x;
@@ -624,8 +625,7 @@ __global__ __launch_bounds__(kWaves * 64, !FULL && sizeof(T) == 2 ? 3 : 2) void 
   // Of two workgroups of a CU the older one's waves go first: it was done after 85 us of 105, and
   // the younger one ran its last chunks alone.  So in long segments the younger, of the grid's
   // second half, goes first over half of its chunks, and both end together (16384 tokens of 64
-  // heads of 64 x 128: outputs 131 -> 122 us, sums 75 -> 69; in turns of one chunk 125 to 135; in
-  // segments of 8 chunks, float32, all launches 59 -> 64).
+  // heads of 64 x 128, all launches: 215 -> 205 us; in segments of 8 chunks no faster).
   const int64_t t_even = a.seg_chunks >= 16 && blockIdx.x >= gridDim.x / 2
                              ? t_begin + (t_end - t_begin) / (2 * Q) * Q
                              : t_begin;
@@ -892,13 +892,13 @@ int64_t workgroups(const co_scan_desc& d, int64_t rows) {
 }
 
 // Rows of a unit.  32 share the most between them: 64 heads of 64 x 128 in bfloat16, 16000 tokens
-// 202 us with 32 and 281 us with 16.  16 where 256 states take a lane's registers, where a fifth
+// 202 us with 32 and 303 us with 16.  16 where 256 states take a lane's registers, where a fifth
 // or more of the waves' rows would be empty with 32 and are not with 16 (heads of 40 rows; groups
-// of three heads of 64: 16 streams of 1000 tokens of 24 such heads x 64 states 70 and 66 us, 64
-// streams of 500 of 8 groups of one head x 128 84 and 74), and where a call has too few units to
-// fill the card however it is cut: its time is then that of one wave's chunks, which are shorter
-// (256 tokens 28.6 and 25.5 us; 3 streams of 10 heads of 40 x 20, float32, 256 tokens 27.6 and
-// 20.4 us).
+// of three heads of 64: 16 streams of 1000 tokens of 24 such heads x 64 states 83 and 80 us, of
+// ragged ones 80 and 70; 64 streams of 500 of 8 groups of one head x 128 87 and 73), and where a
+// call has too few units to fill the card however it is cut: its time is then that of one wave's
+// chunks, which are shorter (256 tokens 33 and 26 us; 3 streams of 10 heads of 40 x 20, float32,
+// 256 tokens 29 and 22 us).
 int unit_rows(const co_scan_desc& d, int64_t T) {
   if (d.state_size > 128) return 16;
   if (2 * workgroups(d, 32) * 4 >= 5 * workgroups(d, 16)) return 16;
@@ -961,11 +961,13 @@ hipError_t launch_t(const ChunkArgs& a, hipStream_t s) {
 }
 
 // Segments of a call over T tokens, and their chunks: the cut that is estimated to be fastest.
-// In units of a chunk's time in a workgroup that has its CU alone (2.8 us, 64 heads of 64 x 128,
-// bfloat16), two on a CU take 1.5 (4.2 us); a segment's own sum takes 0.55 of the whole (75 of
-// 135 us), and carrying the states a launch and their bytes.  Unsplit, 256 workgroups of 32
-// chunks took 73 us where two segments took 89; 32 workgroups of 512 chunks cut 8, 16 and 24
-// times 300, 240 and 263.
+// In units of a chunk's time in a workgroup that has its CU alone, two on a CU take 1.5 (64 heads
+// of 64 x 128, bfloat16: 3.0 and 4.8 us); a segment's own sum takes about half of the whole (70 of
+// 155 us, 89 of 194), and carrying the states a launch and their bytes.  Chunks of other tiles and
+// types take other times, beside which the last two weigh more or less: the cut was measured for
+// 64 x 128 and 64 x 64 in bfloat16.  16 ragged prompts of 24 heads of 64 x 64, 32 chunks, 70 us
+// uncut, 73 in two segments and 76 in three (with units of 32 rows 80 and 85); 16384 tokens of 64
+// heads of 64 x 128 in 8, 16 and 24 segments 279, 206 and 234.
 void cut(const co_scan_desc& d, int64_t T, int64_t* segments, int64_t* seg_chunks) {
   const int64_t chunks = (T + kChunk - 1) / kChunk;
   const int64_t groups = workgroups(d, unit_rows(d, T));
@@ -1001,8 +1003,8 @@ Space space_of(const co_scan_desc& d, int64_t chunks, int64_t segments) {
 
 // Token by token a call takes about 0.3 us a token and 0.11 us a million state values and token;
 // chunks take 9 us more to begin with, and 0.3 us a million values.  Measured, us, by token and in
-// chunks: 16.8 million values, 4 tokens 31 and 35, 8 tokens 40 and 36, 32 tokens 97 and 39;
-// 0.5 million, 16 tokens 10 and 13, 32 tokens 17 and 13.
+// chunks: 16.8 million values, 4 tokens 29 and 37, 8 tokens 38 and 37, 32 tokens 97 and 39;
+// 0.5 million, 16 tokens 10 and 12, 32 tokens 17 and 12.
 //
 // Calls whose chunks would pass what a launch may have of workgroups go token by token.
 bool scan_chunk_takes(const co_scan_desc& d, int32_t T) {

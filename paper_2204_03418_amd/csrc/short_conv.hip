@@ -3,8 +3,9 @@
 // Bound by memory: x read once, y written once, 2K flops a value.  A thread
 // takes 16 bytes of channels and runs of kRun tokens, whose loads are in flight
 // together and over the run before; the K - 1 tokens before its first run it
-// loads again.  4 x 4096 tokens of 4352 channels in bfloat16: 285 MB in 59 us
-// (4.8 TB/s); one token of 64 streams 4.2 us.
+// loads again.  4 x 4096 tokens of 4352 channels in bfloat16: 285 MB, 313 with what
+// is loaded twice, in 58 us (5.4 TB/s); six tokens of 32 streams 6.0 us, one token
+// of 64 streams 4.3 us.
 #include "launch.hpp"
 #include "short_conv.hpp"
 #include "token.hpp"
