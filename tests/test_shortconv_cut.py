@@ -10,7 +10,7 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.fixture(scope="module")
-def checker(tmp_path_factory):
+def walk(tmp_path_factory):
     if shutil.which("g++") is None:
         pytest.skip("needs g++")
     exe = str(tmp_path_factory.mktemp("cut") / "cut")
@@ -20,13 +20,13 @@ def checker(tmp_path_factory):
     return exe
 
 
-def test_state_is_read_by_its_writers_alone(checker):
-    r = subprocess.run([checker], capture_output=True, text=True, timeout=60)
+def test_state_is_read_by_its_writers_alone(walk):
+    r = subprocess.run([walk], capture_output=True, text=True, timeout=60)
     assert r.returncode == 0, r.stdout + r.stderr
 
 
-def test_threads_shorter_than_the_state_are_found(checker):
+def test_threads_shorter_than_the_state_are_found(walk):
     """The check itself: runs chosen without regard to the taps read the state
     from threads that do not write it, at 4 taps and more."""
-    r = subprocess.run([checker, "old"], capture_output=True, text=True, timeout=60)
+    r = subprocess.run([walk, "old"], capture_output=True, text=True, timeout=60)
     assert r.returncode == 1 and r.stdout.startswith("K 4 "), r.stdout
