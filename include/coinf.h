@@ -881,6 +881,206 @@ co_status co_norm_forward(const co_norm_desc* desc, const co_norm_call* call, vo
 co_status co_norm_forward_lengths(const co_norm_desc* desc, const co_norm_call* call,
                                   const int32_t* lengths, void* stream);
 
+/*
+ * ------------------------------------------------------------------------
+ * Attention over token streams: rotary positions, a cache of keys and values in
+ * 4 bits whose pages belong to streams, and attention over it.
+ *
+ * As the token layers: (B, T, values) tensors, no handle, no allocation, no host
+ * synchronisation, state in plain device memory, so a captured call advances it
+ * on every replay.  One step of a model with any number of layers:
+ *   co_pages_reserve   once: pages for the next tokens of each stream;
+ *   co_rotary_forward, co_attn_append, co_attn_forward_steps   in each layer.
+ */
+
+/*
+ * Rotary positions: the first rotary_dim values of each head are pairs
+ * (values i and i + rotary_dim / 2, or 2 i and 2 i + 1) that turn by p f_i at
+ * position p:  (u, w) -> m (u cos - w sin, w cos + u sin); the others stay.
+ * An angle is taken modulo a turn in 64-bit integers, turns[i] = f_i / (2 pi) 2^64
+ * (co_rotary_turns), so that far positions lose nothing: it is off by
+ * |p| 2^-64 turns, and the float32 sine and cosine by 2^-23.  Outputs are
+ * rounded once.  y may be in place of x (the same strides).
+ */
+#define CO_ROTARY_HALF         0
+#define CO_ROTARY_INTERLEAVED  1
+
+#define CO_ROTARY_PLAIN   0       /* f_i = base^(-2 i / R), R = rotary_dim */
+#define CO_ROTARY_LINEAR  1       /* f_i / factor */
+#define CO_ROTARY_BASE    2       /* base factor^(R / (R - 2)) in base's place; R > 2 */
+#define CO_ROTARY_PARTS   3       /* k f_i + (1 - k) f_i / factor, k = the turns that f_i makes in
+                                     `original` positions, from `low` (0) to `high` (1) */
+
+typedef struct co_rotary_scaling {
+  int32_t kind;                   /* CO_ROTARY_* */
+  double  factor;                 /* > 0 */
+  double  original, low, high;    /* low < high */
+} co_rotary_scaling;
+
+/* The rotary_dim / 2 angles of a position.  base > 0; scaling may be NULL (plain).  Host only. */
+co_status co_rotary_turns(int32_t rotary_dim, double base, const co_rotary_scaling* scaling,
+                          uint64_t* turns);
+
+typedef struct co_rotary_desc {
+  int32_t batch;
+  int32_t heads[2];               /* of two tensors; heads[1] may be 0 */
+  int32_t head_dim;
+  int32_t rotary_dim;             /* even, 2..head_dim, <= CO_ATTN_MAX_HEAD */
+  int32_t layout;                 /* CO_ROTARY_HALF | CO_ROTARY_INTERLEAVED */
+  int32_t dtype;                  /* CO_F32 | CO_BF16 */
+  float   magnitude;              /* m */
+} co_rotary_desc;
+
+typedef struct co_rotary_call {
+  const uint64_t* turns;          /* device, rotary_dim / 2 */
+  const int32_t*  positions;      /* token t of stream b has positions[b position_batch_stride +
+                                     t position_token_stride] + (position_each ? 0 : t);
+                                     NULL: t */
+  int64_t         position_batch_stride, position_token_stride;
+  int32_t         position_each;
+  int32_t         T;
+  const int32_t*  lengths;        /* as the token layers' */
+  co_tokens       x[2], y[2];     /* (B, T, heads[i] head_dim) */
+} co_rotary_call;
+
+co_status co_rotary_forward(const co_rotary_desc* desc, const co_rotary_call* call, void* stream);
+
+/*
+ * Pages.  A pool of pages of page_tokens tokens each, for every layer of a model
+ * the same: (layers, pages, page_bytes).  Position p of stream b lies in the page
+ * table[b][p / page_tokens mod stream_pages], at p mod page_tokens.  Streams may
+ * share pages; refs counts the table entries of a page, and what a stream writes
+ * is its own: reserve gives it a copy of a page that others hold too.
+ *
+ * In a page, kv head after kv head, NB = ceil(head_dim / 32) blocks of channels:
+ *   codes of K  (page_tokens / 16, NB, 16, 16 bytes)   tile, block, token, two channels a byte,
+ *   codes of V  the same                               the lower one in the low half
+ *   scales of K (page_tokens / 16, NB, 16 bytes)       tile, block, token
+ *   scales of V the same
+ * A value is c 2^(s - 127): c by its code's lower three bits 0, 0.5, 1, 1.5, 2, 3, 4, 6
+ * and its highest bit the sign; s the block's scale byte, and s = 255: NaN.
+ * Channels past head_dim are 0.
+ */
+#define CO_ATTN_MAX_HEAD  256
+
+typedef struct co_pages_desc {
+  int32_t batch;                  /* B streams */
+  int32_t pages;                  /* of the pool, a layer */
+  int32_t page_tokens;            /* 16, 32, 64, 128 or 256 */
+  int32_t stream_pages;           /* entries of a stream's row of the table */
+  int32_t layers;
+  int32_t kv_heads;
+  int32_t head_dim;               /* 1..CO_ATTN_MAX_HEAD */
+} co_pages_desc;
+
+typedef struct co_pages_info {
+  int64_t page_bytes;
+  int64_t pool_bytes;
+  int64_t workspace_bytes;        /* of any of the calls below */
+} co_pages_info;
+
+/* State (pool to refused) and workspace (16-byte aligned; free for reuse once the
+ * call's work on the stream is done), all device memory.  A clean state: table -1,
+ * everything else 0 (the pool may hold anything). */
+typedef struct co_pages {
+  void*    pool;
+  int32_t* table;                 /* (B, stream_pages); -1: none */
+  int32_t* tokens;                /* (B): the stream's length, its next token's position */
+  int32_t* first;                 /* (B): the lowest position that it still holds */
+  int32_t* refs;                  /* (pages) */
+  int32_t* base;                  /* (B): tokens before the newest reserve */
+  int32_t* granted;               /* (B): tokens that the newest reserve gave */
+  int32_t* refused;               /* (B): tokens that reserves refused, summed */
+  void*    workspace;
+} co_pages;
+
+/* Host only. */
+co_status co_pages_query(const co_pages_desc* desc, co_pages_info* info);
+
+/*
+ * Pages for the next n = min(max(lengths[b], 0), T) tokens of each stream (lengths
+ * NULL: T): base = tokens, tokens += granted.  With keep > 0 a stream's positions
+ * below base + 1 - keep are given up first (a window of `keep` tokens sees none
+ * of them), and pages wholly below are freed.  Streams are served in order,
+ * each wholly (granted = n) or not at all (granted = 0, refused += n): the free
+ * pages must suffice for it and all before it that the table's rows have room
+ * for.  New pages are the lowest free ones.  A page that another stream holds
+ * too is replaced by a new one, to which the tiles (16 tokens) of tokens that
+ * the stream holds are copied in every layer; such a page is freed, where that
+ * was its last use, for the next call.
+ */
+co_status co_pages_reserve(const co_pages_desc* desc, const co_pages* pages, int32_t T,
+                           const int32_t* lengths, int32_t keep, void* stream);
+
+/* tokens = min(tokens, max(lengths[b], 0)): gives up a stream's newest tokens and frees the pages
+ * wholly past the end.  lengths may be base.  Sets base = tokens and granted = 0. */
+co_status co_pages_truncate(const co_pages_desc* desc, const co_pages* pages,
+                            const int32_t* lengths, void* stream);
+
+/* Every stream b at once becomes what stream source[b] was (and shares its
+ * pages): b stays, any other source in 0..B-1 forks it, all others empty stream b.
+ * Pages that nobody holds any more are free, those past a stream's end too.  Sets base = tokens
+ * and granted = 0. */
+co_status co_pages_select(const co_pages_desc* desc, const co_pages* pages, const int32_t* source,
+                          void* stream);
+
+/* Moves the pages in use that lie above their number to the free places below it, both in
+ * ascending order, in every layer: afterwards the used ones are the lowest. */
+co_status co_pages_compact(const co_pages_desc* desc, const co_pages* pages, void* stream);
+
+/*
+ * Attention of `heads` query heads over the kv_heads that they share (query head h
+ * reads kv head h / (heads / kv_heads)): token t of a stream's n = min(granted[b], T)
+ * has position p = base[b] + t and
+ *   y = sum_j softmax_j(scale q . k_j) v_j  over  max(first[b], p - window + 1) <= j <= p
+ * (window 0: none) as far as the table has a page for j.  Outputs of tokens past n, and
+ * of those that see nothing, are 0.
+ */
+typedef struct co_attn_desc {
+  int32_t batch;
+  int32_t heads;                  /* a multiple of kv_heads */
+  int32_t kv_heads;
+  int32_t head_dim;
+  int32_t pages, page_tokens, stream_pages;  /* as co_pages_desc's */
+  int32_t window;                 /* >= 0 */
+  int32_t dtype;                  /* CO_F32 | CO_BF16: q, k, v, y */
+  float   scale;
+} co_attn_desc;
+
+/* The pages of one layer: pool points to the layer's.  granted NULL: T; first NULL: 0. */
+typedef struct co_attn_cache {
+  void*          pool;
+  const int32_t* table;
+  const int32_t* base;
+  const int32_t* granted;
+  const int32_t* first;
+} co_attn_cache;
+
+/*
+ * Puts the tokens k and v (B, T, kv_heads head_dim) into their pages: a block of 32
+ * channels has the scale 2^e, e the least in -120..125 with max |x| <= 7 2^e (so
+ * that what is cut at 6 is off by no more than half a step), and its values go to
+ * the nearest code, of two the even one.  A block with a value that is not finite
+ * is NaN.  Tokens past n, and those without a page, go nowhere.
+ */
+co_status co_attn_append(const co_attn_desc* desc, const co_attn_cache* cache, const co_tokens* k,
+                         const co_tokens* v, int32_t T, void* stream);
+
+/* What positions from[b] .. from[b] + T - 1 of the cache stand for, into k and v
+ * (B, T, kv_heads head_dim); 0 where first <= position < base + n does not hold (n = granted[b];
+ * cache->granted must be given) or the table has no page. */
+co_status co_attn_read(const co_attn_desc* desc, const co_attn_cache* cache, const int32_t* from,
+                       const co_tokens* k, const co_tokens* v, int32_t T, void* stream);
+
+/* Device workspace (16-byte aligned) that a call over T tokens wants (0: none); less is refused.
+ * Host only. */
+co_status co_attn_workspace_bytes(const co_attn_desc* desc, int32_t T, int64_t* bytes);
+
+/* Attention of the tokens q (B, T, heads head_dim), appended before, into y. */
+co_status co_attn_forward_steps(const co_attn_desc* desc, const co_attn_cache* cache,
+                                const co_tokens* q, const co_tokens* y, int32_t T,
+                                void* workspace, int64_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

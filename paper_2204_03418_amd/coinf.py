@@ -29,6 +29,8 @@ CO_ALGO_GEMM_WS = 5
 CO_ACT_NONE, CO_ACT_RELU, CO_ACT_SILU = 0, 1, 2
 CO_NORM_NONE, CO_NORM_BEFORE, CO_NORM_AFTER = 0, 1, 2
 CO_POOL_AVG, CO_POOL_MAX = 0, 1
+CO_ROTARY_HALF, CO_ROTARY_INTERLEAVED = 0, 1
+CO_ROTARY_PLAIN, CO_ROTARY_LINEAR, CO_ROTARY_BASE, CO_ROTARY_PARTS = 0, 1, 2, 3
 CO_MAX_TAPS = 64
 CO_TAP_NONE, CO_TAP_START, CO_TAP_ACC, CO_TAP_EMIT, CO_TAP_EMIT_FRESH = 0, 1, 2, 3, 4
 
@@ -215,6 +217,67 @@ co_norm_forward = _sig("co_norm_forward", i32,
                        [ctypes.POINTER(NormDesc), ctypes.POINTER(NormCall), vp])
 co_norm_forward_lengths = _sig("co_norm_forward_lengths", i32,
                                [ctypes.POINTER(NormDesc), ctypes.POINTER(NormCall), vp, vp])
+
+
+class RotaryScaling(ctypes.Structure):
+    _fields_ = [("kind", i32), ("factor", ctypes.c_double), ("original", ctypes.c_double),
+                ("low", ctypes.c_double), ("high", ctypes.c_double)]
+
+
+class RotaryDesc(ctypes.Structure):
+    _fields_ = [("batch", i32), ("heads", I32x2), ("head_dim", i32), ("rotary_dim", i32),
+                ("layout", i32), ("dtype", i32), ("magnitude", f32)]
+
+
+class RotaryCall(ctypes.Structure):
+    _fields_ = [("turns", vp), ("positions", vp), ("position_batch_stride", i64),
+                ("position_token_stride", i64), ("position_each", i32), ("T", i32),
+                ("lengths", vp), ("x", Tokens * 2), ("y", Tokens * 2)]
+
+
+class PagesDesc(ctypes.Structure):
+    _fields_ = [("batch", i32), ("pages", i32), ("page_tokens", i32), ("stream_pages", i32),
+                ("layers", i32), ("kv_heads", i32), ("head_dim", i32)]
+
+
+class PagesInfo(ctypes.Structure):
+    _fields_ = [("page_bytes", i64), ("pool_bytes", i64), ("workspace_bytes", i64)]
+
+
+class Pages(ctypes.Structure):
+    _fields_ = [(k, vp) for k in ("pool", "table", "tokens", "first", "refs", "base", "granted",
+                                  "refused", "workspace")]
+
+
+class AttnDesc(ctypes.Structure):
+    _fields_ = [("batch", i32), ("heads", i32), ("kv_heads", i32), ("head_dim", i32),
+                ("pages", i32), ("page_tokens", i32), ("stream_pages", i32), ("window", i32),
+                ("dtype", i32), ("scale", f32)]
+
+
+class AttnCache(ctypes.Structure):
+    _fields_ = [(k, vp) for k in ("pool", "table", "base", "granted", "first")]
+
+
+_pages_args = [ctypes.POINTER(PagesDesc), ctypes.POINTER(Pages)]
+_attn_args = [ctypes.POINTER(AttnDesc), ctypes.POINTER(AttnCache)]
+_pTokens = ctypes.POINTER(Tokens)
+co_rotary_turns = _sig("co_rotary_turns", i32, [i32, ctypes.c_double,
+                                                ctypes.POINTER(RotaryScaling), vp])
+co_rotary_forward = _sig("co_rotary_forward", i32,
+                         [ctypes.POINTER(RotaryDesc), ctypes.POINTER(RotaryCall), vp])
+co_pages_query = _sig("co_pages_query", i32,
+                      [ctypes.POINTER(PagesDesc), ctypes.POINTER(PagesInfo)])
+co_pages_reserve = _sig("co_pages_reserve", i32, _pages_args + [i32, vp, i32, vp])
+co_pages_truncate = _sig("co_pages_truncate", i32, _pages_args + [vp, vp])
+co_pages_select = _sig("co_pages_select", i32, _pages_args + [vp, vp])
+co_pages_compact = _sig("co_pages_compact", i32, _pages_args + [vp])
+co_attn_append = _sig("co_attn_append", i32, _attn_args + [_pTokens, _pTokens, i32, vp])
+co_attn_read = _sig("co_attn_read", i32, _attn_args + [vp, _pTokens, _pTokens, i32, vp])
+co_attn_workspace_bytes = _sig("co_attn_workspace_bytes", i32,
+                               [ctypes.POINTER(AttnDesc), i32, pi64])
+co_attn_forward_steps = _sig("co_attn_forward_steps", i32,
+                             _attn_args + [_pTokens, _pTokens, i32, vp, i64, vp])
 
 
 class CoinfError(RuntimeError):
@@ -1625,3 +1688,414 @@ class Mixer:
     def clean_state(self):
         self.conv.clean_state()
         self.scan.clean_state()
+
+
+# ------------------------------------------------- attention over token streams
+# Rotary positions, pages of a cache in 4 bits, and attention over it.  As the
+# token layers: plain device tensors as state, argument checks kept between like
+# calls, one thread a layer.
+
+
+def _enqueue(device, what, fn, *args):
+    """Calls an entry point on the current stream of the layer's device."""
+    if _current_device is not None and torch.cuda.is_initialized() and \
+            _current_device() == device.index:
+        st = fn(*args, _stream())
+    else:
+        with torch.cuda.device(device):
+            st = fn(*args, _stream())
+    if st != CO_OK:
+        check(st, what)
+
+
+def _device(device):
+    """A GPU with its index."""
+    device = torch.device(device)
+    if device.type != "cuda":
+        raise ValueError(f"device is {device}, expected a GPU")
+    return device if device.index is not None else torch.device("cuda",
+                                                                torch.cuda.current_device())
+
+
+def _key(t):
+    return None if t is None else (t.shape, t.stride(), t.dtype, t.get_device())
+
+
+class CoRotary:
+    """Rotary positions (co_rotary_forward): the first rotary_dim values of each head
+    are pairs that turn with the position, base^(-2 i / rotary_dim) radians of it.
+
+    layout: "half" (values i and i + rotary_dim / 2 are a pair) or "interleaved"
+    (2 i and 2 i + 1).  scaling, for contexts longer than trained ones: None, or a dict
+    of kind "linear" (all angles divided by factor), "base" (a base so much larger that the
+    slowest angle is divided by it) or "parts" (angles that make less than low turns
+    in `original` positions are divided, those that make more than high stay, those
+    between in part), with factor and, for "parts", original, low and high.  magnitude
+    multiplies what turns.  Stateless, delay 0.
+    """
+
+    delay, receptive_field, t_stride, t_padding = 0, 1, 1, 0
+    LAYOUTS = {"half": CO_ROTARY_HALF, "interleaved": CO_ROTARY_INTERLEAVED}
+    SCALINGS = {"linear": (CO_ROTARY_LINEAR, ()), "base": (CO_ROTARY_BASE, ()),
+                "parts": (CO_ROTARY_PARTS, ("original", "low", "high"))}
+
+    def __init__(self, head_dim, *, rotary_dim=None, base=10000.0, layout="half", scaling=None,
+                 magnitude=1.0, device="cuda"):
+        self.head_dim = head_dim
+        self.rotary_dim = head_dim if rotary_dim is None else rotary_dim
+        if layout not in self.LAYOUTS:
+            raise ValueError(f"layout {layout!r}, expected one of {sorted(self.LAYOUTS)}")
+        if not 2 <= self.rotary_dim <= head_dim or self.rotary_dim % 2:
+            raise ValueError(f"rotary_dim {self.rotary_dim} of {head_dim} values: expected an even "
+                             f"part of them")
+        how = None
+        if scaling is not None:
+            kind = scaling.get("kind")
+            if kind not in self.SCALINGS:
+                raise ValueError(f"scaling kind {kind!r}, expected one of {sorted(self.SCALINGS)}")
+            number, more = self.SCALINGS[kind]
+            want = {"kind", "factor", *more}
+            if set(scaling) != want:
+                raise ValueError(f"scaling {kind!r} has {sorted(want)}")
+            how = RotaryScaling(number, *(float(scaling[k]) if k in scaling else 0.0
+                                          for k in ("factor", "original", "low", "high")))
+        turns = (ctypes.c_uint64 * (self.rotary_dim // 2))()
+        check(co_rotary_turns(self.rotary_dim, float(base),
+                              None if how is None else ctypes.byref(how), turns),
+              "co_rotary_turns")
+        self.device = _device(device)
+        self._turns = torch.tensor([ctypes.c_int64(v).value for v in turns],
+                                   dtype=torch.int64).to(self.device)
+        self.desc = RotaryDesc(0, I32x2(0, 0), head_dim, self.rotary_dim, self.LAYOUTS[layout],
+                               CO_F32, float(magnitude))
+        self._call = RotaryCall(turns=_ptr(self._turns))
+        self._args = ctypes.byref(self.desc), ctypes.byref(self._call)
+        self._sig = None
+
+    def _check(self, x, k, positions, lengths, out, k_out, step):
+        d, call = self.desc, self._call
+        if x.dtype not in DTYPES:
+            raise ValueError(f"x has dtype {x.dtype}")
+        d.dtype = DTYPES[x.dtype]
+        if k is None and k_out is not None:
+            raise ValueError("k_out is k's")
+        if x.dim() != 4 - step:
+            raise ValueError(f"x has shape {tuple(x.shape)}, expected "
+                             f"{('B', 'H', 'D') if step else ('B', 'T', 'H', 'D')}")
+        B, T = x.shape[0], 1 if step else x.shape[1]
+        d.batch, call.T = B, T
+        d.heads[1] = 0
+        self._dense = []
+        for i, (t, o, what) in enumerate(((x, out, "x"), (k, k_out, "k"))):
+            if t is None:
+                continue
+            if t.dim() != x.dim():
+                raise ValueError(f"{what} has shape {tuple(t.shape)}, expected as x's")
+            shape = torch.Size((B, T, t.shape[-2], self.head_dim))
+            _tokens(t, x.dtype, shape, what, call.x[i], self.device)
+            d.heads[i] = t.shape[-2]
+            width = t.shape[-2] * self.head_dim
+            call.y[i].batch_stride, call.y[i].token_stride = T * width, width
+            if o is not None:
+                if o.dim() != x.dim():
+                    raise ValueError(f"out has shape {tuple(o.shape)}, expected as {what}'s")
+                _tokens(o, x.dtype, shape, "out", call.y[i], self.device)
+            self._dense.append(t.is_contiguous())
+        if positions is not None:
+            _on(positions, self.device, "positions")
+            if positions.dtype is not torch.int32:
+                raise ValueError(f"positions has dtype {positions.dtype}, expected torch.int32")
+            each = positions.dim() == 2
+            if positions.shape not in ((B,), (B, T)):
+                raise ValueError(f"positions has shape {tuple(positions.shape)}, expected ({B},) or "
+                                 f"({B}, {T})")
+            call.position_batch_stride = positions.stride(0)
+            call.position_token_stride = positions.stride(1) if each else 0
+            call.position_each = 1 if each else 0
+
+    def _run(self, x, k, positions, lengths, out, k_out, step):
+        sig = (step, _key(x), _key(k), _key(positions), _key(out), _key(k_out))
+        if sig != self._sig:
+            self._sig = None
+            self._check(x, k, positions, lengths, out, k_out, step)
+            self._sig = sig
+        call = self._call
+        if out is None:
+            out = _like(x) if self._dense[0] else x.new_empty(x.shape)
+        call.x[0].data, call.y[0].data = x.data_ptr(), out.data_ptr()
+        if k is not None:
+            if k_out is None:
+                k_out = _like(k) if self._dense[1] else k.new_empty(k.shape)
+            call.x[1].data, call.y[1].data = k.data_ptr(), k_out.data_ptr()
+        call.positions = None if positions is None else positions.data_ptr()
+        call.lengths = None if lengths is None else _lengths(lengths, x.shape[0], self.device)
+        if x.numel() or (k is not None and k.numel()):
+            _enqueue(self.device, "co_rotary_forward", co_rotary_forward, *self._args)
+        return out if k is None else (out, k_out)
+
+    def forward(self, x, k=None, *, positions=None, lengths=None, out=None, k_out=None):
+        """x (B, T, H, D), and k (B, T, H', D) in the same launch -> x, or (x, k), turned.
+        positions, int32 on the device: (B,) of each stream's first token, or (B, T); default 0,
+        1, ...  out may be x, k_out may be k.  lengths: as CoShortConv's."""
+        return self._run(x, k, positions, lengths, out, k_out, 0)
+
+    forward_steps = forward
+
+    def forward_step(self, x_t, k_t=None, *, positions=None, lengths=None, out=None, k_out=None):
+        """The same of single tokens, (B, H, D)."""
+        return self._run(x_t, k_t, positions, lengths, out, k_out, 1)
+
+    def clean_state(self):
+        pass
+
+
+class CoPages:
+    """Pages of a cache of keys and values in 4 bits (co_pages_* ABI), for all layers of a
+    model: which stream holds which tokens where.
+
+    A pool of `pages` pages of page_tokens tokens (16 to 256) in each of the layers; a
+    stream holds at most stream_pages of them at once, as many as its length or, with
+    reserve's keep, its window needs.  Everything is a plain device tensor, and no call
+    waits for the device:
+
+    pool (layers, pages, page_bytes) uint8; table (batch, stream_pages) int32, position p of
+    stream b in page table[b, p // page_tokens % stream_pages]; tokens, first (batch,), a
+    stream's length and the lowest position it still holds; refs (pages,), how many streams hold
+    a page; base, granted (batch,), the length before the newest reserve and what it
+    gave; refused (batch,), what reserves refused, summed.  state: a dict of any of them
+    to keep and continue from; default clean ones.
+    """
+
+    def __init__(self, *, batch, pages, stream_pages, kv_heads, head_dim, page_tokens=64, layers=1,
+                 device=None, state=None):
+        self.batch, self.pages, self.stream_pages = batch, pages, stream_pages
+        self.kv_heads, self.head_dim = kv_heads, head_dim
+        self.page_tokens, self.layers = page_tokens, layers
+        self.desc = PagesDesc(batch, pages, page_tokens, stream_pages, layers, kv_heads, head_dim)
+        info = PagesInfo()
+        check(co_pages_query(ctypes.byref(self.desc), ctypes.byref(info)), "co_pages_query")
+        self.page_bytes, self._nws = info.page_bytes, info.workspace_bytes
+        state = {} if state is None else dict(state)
+        if device is None:
+            given = next(iter(state.values()), None)
+            device = "cuda" if given is None else given.device
+        self.device = _device(device)
+        shapes = dict(pool=(layers, pages, self.page_bytes), table=(batch, stream_pages),
+                      tokens=(batch,), first=(batch,), refs=(pages,), base=(batch,),
+                      granted=(batch,), refused=(batch,))
+        if not set(state) <= set(shapes):
+            raise ValueError(f"state has {sorted(state)}, expected some of {sorted(shapes)}")
+        self._state = {}
+        for name, shape in shapes.items():
+            dtype = torch.uint8 if name == "pool" else torch.int32
+            t = state.get(name)
+            if t is None:
+                t = (torch.empty if name == "pool" else torch.zeros)(shape, dtype=dtype,
+                                                                     device=self.device)
+                if name == "table":
+                    t.fill_(-1)
+            _need(t, dtype, shape, name)
+            _on(t, self.device, name)
+            self._state[name] = t
+        self._call = Pages(*(_ptr(self._state[k]) for k in shapes))
+        self._args = ctypes.byref(self.desc), ctypes.byref(self._call)
+        self._T = None  # tokens of the newest reserve
+
+    pool = property(lambda self: self._state["pool"])
+    table = property(lambda self: self._state["table"])
+    tokens = property(lambda self: self._state["tokens"])
+    first = property(lambda self: self._state["first"])
+    refs = property(lambda self: self._state["refs"])
+    base = property(lambda self: self._state["base"])
+    granted = property(lambda self: self._state["granted"])
+    refused = property(lambda self: self._state["refused"])
+
+    def _run(self, what, fn, *args):
+        ws = torch.empty(self._nws, dtype=torch.uint8, device=self.device)
+        self._call.workspace = ws.data_ptr()
+        _enqueue(self.device, what, fn, *self._args, *args)
+
+    def reserve(self, T, lengths=None, keep=0):
+        """Pages for the next T tokens of each stream (lengths, as CoShortConv's, of
+        them), which its layers then append and attend to -> granted: how many each stream got, all
+        it asked for or none where pages are short.  keep > 0: positions that no
+        window of `keep` tokens sees any more are given up first.  Pages that other streams
+        hold too are copied, not written."""
+        self._run("co_pages_reserve", co_pages_reserve, T,
+                  None if lengths is None else _lengths(lengths, self.batch, self.device), keep)
+        self._T = T
+        return self.granted
+
+    def truncate(self, tokens):
+        """Gives up each stream's tokens from position tokens[b] (int32 on the device) on; with
+        tokens=self.base those of the newest reserve, as after rejected drafts."""
+        self._run("co_pages_truncate", co_pages_truncate,
+                  _lengths(tokens, self.batch, self.device))
+        self._T = None
+
+    def select(self, source):
+        """Every stream b at once becomes what stream source[b] (int32 on the device) was, and shares
+        its pages: itself, another one (a fork), or with -1 an empty stream, whose pages
+        are free where nobody else holds them."""
+        self._run("co_pages_select", co_pages_select, _lengths(source, self.batch, self.device))
+        self._T = None
+
+    def compact(self):
+        """Moves the pages in use to the lowest indexes of the pool, in every layer."""
+        self._run("co_pages_compact", co_pages_compact)
+
+    def clean_state(self):
+        for name, t in self._state.items():
+            if name == "table":
+                t.fill_(-1)
+            elif name != "pool":
+                t.zero_()
+        self._T = None
+
+
+class CoAttention:
+    """Causal attention over token streams (co_attn_* ABI): keys and values go into
+    one layer of a CoPages in 4 bits, and each token attends to what its stream
+    holds up to itself, or to the newest `window` tokens of that.
+
+    heads: query heads, a multiple of the pages' kv_heads, which neighbouring ones share.
+    scale: of the products, default head_dim ** -0.5.  dtype: of q, k, v and the output.
+    A step of a model: pages.reserve(T, lengths), then each layer's forward_steps; tokens that
+    the reserve did not grant give 0.  Delay 0; the state is the pages'.
+    """
+
+    delay, t_stride, t_padding = 0, 1, 0
+
+    def __init__(self, pages, layer=0, *, heads, window=None, scale=None, dtype=torch.bfloat16):
+        if not 0 <= layer < pages.layers:
+            raise ValueError(f"layer {layer} of {pages.layers}")
+        if window is not None and window < 1:
+            raise ValueError(f"window {window}")
+        if dtype not in DTYPES:
+            raise ValueError(f"dtype {dtype}")
+        self.pages, self.layer, self.heads, self.window = pages, layer, heads, window
+        self.batch, self.kv_heads, self.head_dim = pages.batch, pages.kv_heads, pages.head_dim
+        self.torch_dtype, self.device = dtype, pages.device
+        self.scale = self.head_dim ** -0.5 if scale is None else float(scale)
+        self.desc = self._desc(pages.pages, pages.stream_pages)
+        check(co_attn_workspace_bytes(ctypes.byref(self.desc), 0, ctypes.byref(i64())),
+              "co_attn_workspace_bytes")
+        pool = pages.pool[layer]
+        self._cache = AttnCache(_ptr(pool), _ptr(pages.table), _ptr(pages.base),
+                                _ptr(pages.granted), _ptr(pages.first))
+        self._q, self._k, self._v, self._y = (Tokens() for _ in range(4))
+        self._ref = {t: ctypes.byref(getattr(self, t)) for t in ("_q", "_k", "_v", "_y")}
+        self._args = ctypes.byref(self.desc), ctypes.byref(self._cache)
+        self._append_sig = self._attend_sig = None
+
+    receptive_field = property(lambda self: self.window)  # None: all that a stream holds
+
+    def _desc(self, pages, stream_pages):
+        return AttnDesc(self.batch, self.heads, self.kv_heads, self.head_dim, pages,
+                        self.pages.page_tokens, stream_pages, self.window or 0,
+                        DTYPES[self.torch_dtype], self.scale)
+
+    def _tokens(self, t, heads, what, into, step):
+        shape = (self.batch, 1 if step else t.shape[1] if t.dim() == 4 else -1, heads,
+                 self.head_dim)
+        if t.dim() != 4 - step:
+            raise ValueError(f"{what} has shape {tuple(t.shape)}, expected "
+                             f"{shape[:1] + shape[2:] if step else shape[:1] + ('T',) + shape[2:]}")
+        _tokens(t, self.torch_dtype, torch.Size(shape), what, into, self.device)
+        return shape[1]
+
+    def _reserved(self, T):
+        if self.pages._T is not None and T != self.pages._T:
+            raise ValueError(f"{T} tokens, but the newest reserve was for {self.pages._T}")
+
+    def _append(self, k, v, step, args):
+        sig = step, _key(k), _key(v)
+        if sig != self._append_sig:
+            self._append_sig = None
+            T = self._tokens(k, self.kv_heads, "k", self._k, step)
+            if self._tokens(v, self.kv_heads, "v", self._v, step) != T:
+                raise ValueError(f"k has {T} tokens, v {v.shape[1]}")
+            self._append_T = T
+            self._append_sig = sig
+        self._k.data, self._v.data = k.data_ptr(), v.data_ptr()
+        if self._append_T:
+            _enqueue(self.device, "co_attn_append", co_attn_append, *args, self._ref["_k"],
+                     self._ref["_v"], self._append_T)
+        return self._append_T
+
+    def _attend(self, q, out, step, desc, args):
+        sig = step, _key(q), _key(out), desc.stream_pages
+        if sig != self._attend_sig:
+            self._attend_sig = None
+            T = self._tokens(q, self.heads, "q", self._q, step)
+            width = self.heads * self.head_dim
+            self._y.batch_stride, self._y.token_stride = T * width, width
+            if out is not None and self._tokens(out, self.heads, "out", self._y, step) != T:
+                raise ValueError(f"q has {T} tokens, out {out.shape[1]}")
+            nb = i64()
+            check(co_attn_workspace_bytes(ctypes.byref(desc), T, ctypes.byref(nb)),
+                  "co_attn_workspace_bytes")
+            self._attend_T, self._nws, self._dense = T, nb.value, q.is_contiguous()
+            self._attend_sig = sig
+        if out is None:
+            out = _like(q) if self._dense else q.new_empty(q.shape)
+        ws = None
+        if self._nws:
+            ws = torch.empty(self._nws, dtype=torch.uint8, device=self.device)
+        self._q.data, self._y.data = q.data_ptr(), out.data_ptr()
+        if self._attend_T:
+            _enqueue(self.device, "co_attn_forward_steps", co_attn_forward_steps, *args,
+                     self._ref["_q"], self._ref["_y"], self._attend_T, _ptr(ws), self._nws)
+        return out
+
+    def append(self, k, v):
+        """Puts k and v (B, T, kv_heads, D) of the newest reserve's tokens into the cache."""
+        self._reserved(k.shape[1] if k.dim() == 4 else 1)
+        self._append(k, v, 0, self._args)
+
+    def attend(self, q, out=None):
+        """The newest reserve's tokens q (B, T, heads, D), appended before, over the cache ->
+        (B, T, heads, D)."""
+        self._reserved(q.shape[1] if q.dim() == 4 else 1)
+        return self._attend(q, out, 0, self.desc, self._args)
+
+    def forward_steps(self, q, k, v, out=None):
+        """append and attend."""
+        self.append(k, v)
+        return self.attend(q, out)
+
+    def forward_step(self, q_t, k_t, v_t, out=None):
+        """The same of single tokens, (B, heads, D) and (B, kv_heads, D)."""
+        self._reserved(1)
+        self._append(k_t, v_t, 1, self._args)
+        return self._attend(q_t, out, 1, self.desc, self._args)
+
+    def forward(self, q, k, v, lengths=None, out=None):
+        """Whole sequences from their start, through a cache of the call's own: the layer's pages are
+        not touched.  lengths: as CoShortConv's."""
+        P, B = self.pages.page_tokens, self.batch
+        T = q.shape[1] if q.dim() == 4 else 0
+        if k.dim() == 4 and k.shape[1] != T:
+            raise ValueError(f"q has {T} tokens, k {k.shape[1]}")
+        each = max(1, -(-T // P))
+        desc = self._desc(B * each, each)
+        pool = torch.empty(B * each * self.pages.page_bytes, dtype=torch.uint8, device=self.device)
+        table = torch.arange(B * each, dtype=torch.int32, device=self.device)
+        base = torch.zeros(B, dtype=torch.int32, device=self.device)
+        cache = AttnCache(_ptr(pool), _ptr(table), _ptr(base),
+                          None if lengths is None else _lengths(lengths, B, self.device), None)
+        args = ctypes.byref(desc), ctypes.byref(cache)
+        self._append(k, v, 0, args)
+        return self._attend(q, out, 0, desc, args)
+
+    def read(self, first, T):
+        """What the cache holds at positions first[b] .. first[b] + T - 1 (first int32 on the device) of
+        each stream -> keys and values (B, T, kv_heads, D), 0 where it holds nothing."""
+        shape = self.batch, T, self.kv_heads, self.head_dim
+        k, v = (torch.empty(shape, dtype=self.torch_dtype, device=self.device) for _ in range(2))
+        width = self.kv_heads * self.head_dim
+        into = [Tokens(t.data_ptr(), T * width, width) for t in (k, v)]
+        if T:
+            _enqueue(self.device, "co_attn_read", co_attn_read, *self._args,
+                     _lengths(first, self.batch, self.device), *map(ctypes.byref, into), T)
+        return k, v

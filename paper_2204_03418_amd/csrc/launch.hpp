@@ -263,4 +263,26 @@ hipError_t launch_scan_chunk(const ScanCall& c, hipStream_t stream);
 hipError_t launch_norm(const co_norm_desc& d, const co_norm_call& c, const int32_t* lengths,
                        hipStream_t stream);
 
+// Attention over token streams (rotary.hip, pages.hip, cache.hip, attend.hip); the entry points
+// (attn_api.hip) have checked every argument.
+hipError_t launch_rotary(const co_rotary_desc& d, const co_rotary_call& c, hipStream_t stream);
+
+int64_t page_bytes(const co_pages_desc& d);
+int64_t pages_workspace(const co_pages_desc& d);
+hipError_t launch_pages_reserve(const co_pages_desc& d, const co_pages& s, int32_t T,
+                                const int32_t* lengths, int32_t keep, hipStream_t stream);
+hipError_t launch_pages_truncate(const co_pages_desc& d, const co_pages& s, const int32_t* lengths,
+                                 hipStream_t stream);
+hipError_t launch_pages_select(const co_pages_desc& d, const co_pages& s, const int32_t* source,
+                               hipStream_t stream);
+hipError_t launch_pages_compact(const co_pages_desc& d, const co_pages& s, hipStream_t stream);
+
+hipError_t launch_attn_append(const co_attn_desc& d, const co_attn_cache& c, const co_tokens& k,
+                              const co_tokens& v, int32_t T, hipStream_t stream);
+hipError_t launch_attn_read(const co_attn_desc& d, const co_attn_cache& c, const int32_t* from,
+                            const co_tokens& k, const co_tokens& v, int32_t T, hipStream_t stream);
+int64_t attend_workspace(const co_attn_desc& d, int32_t T);
+hipError_t launch_attend(const co_attn_desc& d, const co_attn_cache& c, const co_tokens& q,
+                         const co_tokens& y, int32_t T, void* workspace, hipStream_t stream);
+
 }  // namespace coinf
