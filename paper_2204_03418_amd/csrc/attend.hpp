@@ -1,0 +1,168 @@
+// What the attention kernels share.
+#pragma once
+
+#include <type_traits>
+
+#include "cache.hpp"
+#include "launch.hpp"
+#include "token.hpp"
+
+namespace coinf {
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+struct AttendArgs {
+  co_attn_desc d;
+  co_attn_cache c;
+  co_tokens q, y;
+  int32_t T;
+  PageHead lay;
+  int64_t page_bytes;
+  float scale_log2;    // > 0
+  float slack;         // of scores: kSlack
+  float q_sign;        // -1, 0 or 1: the scale's
+  int32_t group;       // query heads a kv head
+  FastDiv by_group, by_W;
+  int32_t page_shift;  // log2 of a page's tokens
+  int32_t row_tiles;   // of a stream's tokens * group
+  FastDiv by_row_tiles, by_splits, by_kv;
+  int32_t pairs;       // streams * kv heads
+  int32_t splits;      // parts of a unit's keys at most
+  int32_t wide;        // q and y in pieces of 16 bytes
+  float* part;         // (units, splits, rows, NB * 32) values, then (.., rows) reference score and sum
+  float2* part_stat;
+};
+
+// Keys: tokens of a tile, the least tiles of a part.
+constexpr int kKeys = 64;
+constexpr int kMinTiles = 4;
+
+// Weights are 2^{x + kLift}, x <= kSlack over the row's reference: 2^15, below 16-bit floats' highest.
+// Their least step is 2^-24, 2^-35 of the row's reference.
+constexpr float kLift = 11.f, kSlack = 4.f;
+// Values are c 2^{s - E + kValueLift}, s <= E: below 6 2^12.
+constexpr int kValueLift = 12, kValueSlack = 4;
+
+// What a stream's rows see.
+struct Span {
+  int64_t base;
+  int n;         // tokens of the call
+  int64_t lowest;
+  __device__ Span(const AttendArgs& a, int b)
+      : base(a.c.base[b]),
+        n(base < 0 ? 0 : stream_tokens(a.c.granted, b, a.T)),
+        lowest(a.c.first ? max(a.c.first[b], 0) : 0) {}
+  // first and last key of a token, whole or past it
+  __device__ int64_t lo(const AttendArgs& a, int t) const {
+    const int64_t w = a.d.window ? base + t - a.d.window + 1 : 0;
+    return max(max(w, lowest), int64_t(0));
+  }
+};
+
+// Tiles of keys first..end - 1 of a unit's part `split`; parts: of the unit.
+struct Part {
+  int first, end, parts;
+  __device__ Part(int64_t lo, int64_t hi, int splits, int split) {
+    const int t0 = int(lo / kKeys), t1 = lo < hi ? int((hi + kKeys - 1) / kKeys) : t0;
+    const int each = max((t1 - t0 + splits - 1) / splits, kMinTiles);
+    parts = max((t1 - t0 + each - 1) / each, 1);
+    first = min(t0 + split * each, t1);
+    end = min(first + each, t1);
+  }
+};
+
+// Four values of channels c.. of a row, 0 past D.
+template <typename T>
+__device__ __forceinline__ void load4(const T* row, int c, int D, bool wide, float* v) {
+  if (wide) {
+    Pack<T, 4> p{};
+    if (c < D) p = load_pack<T, 4>(row + c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = to_f32<T>(p.v[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = c + i < D ? to_f32<T>(row[c + i]) : 0.f;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store4(T* row, int c, int D, bool wide, const float* v) {
+  if (wide) {
+    Pack<T, 4> p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p.v[i] = from_f32<T>(v[i]);
+    if (c < D) store_pack<T, 4>(row + c, p);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (c + i < D) row[c + i] = from_f32<T>(v[i]);
+  }
+}
+
+__device__ __forceinline__ float exponent_to_f32(int biased) {
+  return __uint_as_float(uint32_t(min(max(biased, 0), 254)) << 23);
+}
+
+// The 8-bit terms of 16 values, 2^{e - 4 k} the scale of term k: words[k] 16 bytes.  Two hold a
+// bfloat16 exactly down to 2^-17 of the block's largest, six a float32 to 2^-24 of it.
+template <int TERMS>
+__device__ __forceinline__ void to_terms(float (&v)[16], int scale_byte, i32x4 (&words)[TERMS]) {
+#pragma unroll
+  for (int k = 0; k < TERMS; ++k) {
+    const float scale = exponent_to_f32(scale_byte - 4 * k);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      s16x2 p = {0, 0};
+      p = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(p, v[4 * w], v[4 * w + 1], scale, false);
+      p = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(p, v[4 * w + 2], v[4 * w + 3], scale, true);
+      const int word = __builtin_bit_cast(int, p);
+      words[k][w] = word;
+      if (k + 1 < TERMS) {
+        const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(word, scale, false);
+        const f32x2 hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(word, scale, true);
+        v[4 * w] -= lo[0], v[4 * w + 1] -= lo[1], v[4 * w + 2] -= hi[0], v[4 * w + 3] -= hi[1];
+      }
+    }
+  }
+}
+
+// The scale byte of a block of queries whose largest magnitude has the bits `most`: that lies in
+// 2^7..2^8 of it (below 2^-80: multiples of 2^-96).
+__device__ __forceinline__ int query_scale(uint32_t most) {
+  return max(int(most >> 23) - 7, 40);
+}
+
+template <typename T>
+constexpr int kQueryTerms = sizeof(T) == 2 ? 2 : 6;
+template <typename T>
+constexpr int kWeightTerms = sizeof(T) == 2 ? 1 : 2;
+
+// Sixteen codes as 16-bit floats times 2^{s - E + kValueLift}.
+__device__ __forceinline__ void decode16(uint32_t lo, uint32_t hi, float scale, f16x8 (&o)[2]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t w = i ? hi : lo;
+    const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 0);
+    const f16x2 b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 1);
+    const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 2);
+    const f16x2 d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 3);
+    o[i] = f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+  }
+}
+
+// Four rows of 16 columns of an LDS tile of 16-bit values, turned: lane j of 16 gets column j.
+// p: this lane's row j / 4 and columns 4 (j % 4).
+__device__ __forceinline__ s16x4 turned4(const _Float16* p) {
+  using Lds = __attribute__((address_space(3))) s16x4;
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(p));
+}
+
+
+}  // namespace coinf

@@ -84,12 +84,13 @@ def attend_bound(y, sizes, n, D, u, weights):
     """What may be between an attention's output over n keys and y: its rounding, u; a weight's, `weights`
     (its own and the sum's); the sum of n terms in float32; in a weight the error of
     its score, D + 16 roundings of a sum of magnitudes `worst`, twice (numerator and sum);
-    and weights that are multiples of 2^-39 of the largest, off by half of that (16-bit
-    floats to 2^15: their least step is 2^-24)."""
+    and weights that are multiples of 2^-35 of the largest at most, off by half of that: they are
+    16-bit floats, whose least step is 2^-24, and a row's reference, which its largest
+    weight is not below, is 2^11."""
     size, worst, reach = sizes
     score = np.minimum((D + 16) * U32 * worst, 300.0)      # past that a weight says nothing
     return (u * np.abs(y) + size * (2 * weights + (n + 64) * U32 + 2 * np.expm1(2 * score))
-            + 2.0 ** -40 * reach)
+            + 2.0 ** -36 * reach)
 
 
 class Streams:
