@@ -165,4 +165,11 @@ __device__ __forceinline__ s16x4 turned4(const _Float16* p) {
 }
 
 
+// Calls of at most kFewTiles * 16 rows, in column tiles of 16.
+constexpr int kFewTiles = 2;
+void launch_attend_few(const AttendArgs& a, int NB, int tiles, hipStream_t stream);
+// The others.
+void launch_attend_rows(const AttendArgs& a, int NB, hipStream_t stream);
+constexpr int kRows = 128;  // of a workgroup
+
 }  // namespace coinf

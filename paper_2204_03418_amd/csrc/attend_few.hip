@@ -1,0 +1,454 @@
+// Attention of few rows (single and drafted tokens) over the cache: bound by the
+// cache's bytes.  A workgroup takes a part of one stream's keys of a kv head, and its
+// four waves go over it 32 keys at a time, each by itself and without barriers: keys come
+// from memory as the operand that they are, values pass through the wave's own LDS to be
+// turned.  The products are as in the kernel of many rows, in 16 x 16 tiles, a column
+// tile for each 16 rows.  At the end the waves' sums are joined in LDS, and the parts' in
+// a launch of their own.
+#include <algorithm>
+
+#include "attend.hpp"
+
+namespace coinf {
+
+namespace {
+
+constexpr int kWaves = kBlock / 64;
+constexpr int kStep = 32;  // keys
+
+template <typename T, int NB>
+struct Few {
+  static constexpr int QT = kQueryTerms<T>, PT = kWeightTerms<T>;
+  // a matrix instruction has four slots of 32 channels: four blocks of a term, or two of two terms,
+  // or one of four
+  static constexpr int NBP = NB <= 2 ? NB : (NB + 3) / 4 * 4;
+  static constexpr int FRAGS = NBP >= 4 ? NBP / 4 : 1;
+  static constexpr int MMA = NBP >= 4 ? QT * FRAGS : NBP == 2 ? QT / 2 : (QT + 3) / 4;
+  static constexpr int CHUNKS = NB * kStep;  // 16 bytes of values of a step
+  static constexpr int VC = (CHUNKS + 63) / 64;
+  static constexpr int VS = NB * 32 + 16;    // rows 32 bytes beside a multiple of the banks
+  // of a slot of fragment f
+  static __device__ int block(int f, int slot) {
+    return NBP >= 4 ? 4 * f + slot : NBP == 2 ? slot % 2 : 0;
+  }
+};
+
+// One wave's values, and at the end its sums (16 rows of NB * 32, 64 bytes more each).
+template <typename T, int NB>
+struct FewLds {
+  union {
+    alignas(16) _Float16 v[kStep * Few<T, NB>::VS];
+    alignas(16) float o[16 * (NB * 32 + 16)];
+  };
+};
+
+template <typename T, int NB, int CT>
+__global__ __launch_bounds__(kBlock) void attend_few_kernel(AttendArgs a) {
+  using F = Few<T, NB>;
+  __shared__ FewLds<T, NB> lds[kWaves];
+  __shared__ float2 stats[kWaves][16];
+  const int lane = threadIdx.x % 64, col = lane % 16, g = lane / 16;
+  const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / 64);
+  const int split = blockIdx.x / a.pairs, pair = blockIdx.x - split * a.pairs;
+  const int b = fdiv(pair, a.by_kv), kv = pair - b * a.d.kv_heads;
+  const Span span(a, b);
+  const int rows = span.n * a.group;
+  const auto token_of = [&](int row) { return fdiv(row, a.by_group); };
+  const auto out_row = [&](int row) {
+    const int t = token_of(row), head = kv * a.group + row - t * a.group;
+    return static_cast<T*>(a.y.data) + b * a.y.batch_stride + t * a.y.token_stride +
+           int64_t(head) * a.d.head_dim;
+  };
+  if (split == 0) {  // outputs of tokens that the stream does not have
+    const float none[4] = {};
+    for (int i = threadIdx.x; i < (a.T - span.n) * a.group * (NB * 8); i += kBlock)
+      store4<T>(out_row(rows + i / (NB * 8)), i % (NB * 8) * 4, a.d.head_dim, a.wide, none);
+  }
+  if (rows == 0) return;
+  const Part part(span.lo(a, 0), span.base + span.n, a.splits, split);
+  if (split >= part.parts) return;
+
+  // queries, as 8-bit terms
+  i32x8 qo[CT][F::MMA];
+  int qs[CT][F::MMA];
+  bool q_bad[CT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    const int row = 16 * c + col;
+    const bool live = row < rows;
+    const int t = token_of(live ? row : 0), head = kv * a.group + (live ? row - t * a.group : 0);
+    const T* q = static_cast<const T*>(a.q.data) + b * a.q.batch_stride + t * a.q.token_stride +
+                 int64_t(head) * a.d.head_dim;
+    q_bad[c] = false;
+#pragma unroll
+    for (int f = 0; f < F::FRAGS; ++f) {
+      int byte[2];
+      i32x4 words[2][F::QT];
+      // this lane's halves of 16 channels: of slots g / 2 and 2 + g / 2
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        if (w == 1 && F::NBP <= 2) {  // the same block again
+          byte[1] = byte[0];
+#pragma unroll
+          for (int k = 0; k < F::QT; ++k) words[1][k] = words[0][k];
+          continue;
+        }
+        const int blk = F::NBP == 2 ? g / 2 : F::block(f, 2 * w + g / 2);
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          load4<T>(q, live ? blk * 32 + 16 * (g % 2) + 4 * i : a.d.head_dim, a.d.head_dim, a.wide,
+                   v + 4 * i);
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          v[i] *= a.q_sign;
+          most = max(most, __float_as_uint(v[i]) & 0x7fffffffu);
+        }
+        most = max(most, uint32_t(__shfl_xor(int(most), 16)));
+        const bool bad = most >= 0x7f800000u;
+        q_bad[c] |= bad;
+        byte[w] = bad ? 127 : query_scale(most);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = bad ? 0.f : v[i];
+        to_terms<F::QT>(v, byte[w], words[w]);
+      }
+      // scales: of slot g, which lanes of group 2 (g % 2) have
+      const int b0 = __shfl(byte[0], col + 32 * (g % 2)), b1 = __shfl(byte[1], col + 32 * (g % 2));
+      const int mine = g / 2 ? b1 : b0;
+#pragma unroll
+      for (int k = 0; k < F::MMA / F::FRAGS; ++k) {
+        const int j = k * F::FRAGS + f;
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if constexpr (F::NBP >= 4) {
+              qo[c][j][4 * w + i] = words[w][k][i];
+            } else if constexpr (F::NBP == 2) {
+              qo[c][j][4 * w + i] = words[w][2 * k + w][i];
+            } else {
+              const int t0 = 4 * k + 2 * w;
+              const int lo = t0 < F::QT ? words[w][t0 < F::QT ? t0 : 0][i] : 0;
+              const int hi = t0 + 1 < F::QT ? words[w][t0 + 1 < F::QT ? t0 + 1 : 0][i] : 0;
+              qo[c][j][4 * w + i] = g / 2 ? hi : lo;
+            }
+          }
+        qs[c][j] = mine - 4 * (F::NBP >= 4 ? k : F::NBP == 2 ? 2 * k + g / 2 : 4 * k + g);
+      }
+    }
+    // all lanes of a column
+    q_bad[c] |= __shfl_xor(int(q_bad[c]), 16) != 0;
+    q_bad[c] |= __shfl_xor(int(q_bad[c]), 32) != 0;
+  }
+
+  const char* pool = static_cast<const char*>(a.c.pool) + int64_t(kv) * a.lay.bytes();
+  const int32_t* table = a.c.table + int64_t(b) * a.d.stream_pages;
+  constexpr int tile_bytes = NB * 256;
+  const int sub_mask = a.lay.P / kCacheTile - 1;
+  const auto page_of = [&](int tile) {  // of 16 tokens
+    const int lp = tile >> (a.page_shift - 4);
+    const int p = table[lp - fdiv(lp, a.by_W) * a.d.stream_pages];
+    return __builtin_amdgcn_readfirstlane(p >= 0 && p < a.d.pages ? p : -1);
+  };
+  int page[2];
+  i32x4 rk[2][F::FRAGS], rv[F::VC];
+  int rks[2][F::FRAGS], rvs[F::VC], has;  // has: bit i: tile i has a page
+  const auto fetch_pages = [&](int step) {
+    page[0] = page_of(2 * step);
+    page[1] = page_of(2 * step + 1);
+  };
+  const auto fetch = [&](int step) {
+    has = (page[0] >= 0) | (page[1] >= 0) << 1;
+    const char* p[2];
+    int in[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      in[i] = (2 * step + i) & sub_mask;
+      p[i] = pool + (page[i] >= 0 ? page[i] : 0) * a.page_bytes;
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int f = 0; f < F::FRAGS; ++f) {
+        const int blk = F::block(f, g);
+        rk[i][f] = i32x4{0, 0, 0, 0};
+        rks[i][f] = 127;
+        if (page[i] >= 0 && blk < NB) {
+          const int at = blk * 16 + col;
+          rk[i][f] = *reinterpret_cast<const i32x4*>(p[i] + in[i] * tile_bytes + at * 16);
+          rks[i][f] = uint8_t(p[i][a.lay.scales(0) + in[i] * NB * 16 + at]);
+        }
+      }
+#pragma unroll
+    for (int i = 0; i < F::VC; ++i) {
+      const int c = lane + 64 * i, tile = c / (NB * 16), rest = c - tile * NB * 16;
+      rv[i] = i32x4{0, 0, 0, 0};
+      rvs[i] = 0;
+      if (c < F::CHUNKS && (tile ? page[1] : page[0]) >= 0) {
+        const char* q = tile ? p[1] : p[0];
+        const int n = tile ? in[1] : in[0];
+        rv[i] = *reinterpret_cast<const i32x4*>(q + a.lay.codes(1) + n * tile_bytes + rest * 16);
+        rvs[i] = uint8_t(q[a.lay.scales(1) + n * NB * 16 + rest]);
+      }
+    }
+  };
+
+  f32x4 o[CT][NB * 2];
+  float m[CT], l[CT];
+  int E = 0;
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    m[c] = -1e30f;
+    l[c] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NB * 2; ++i) o[c][i] = f32x4{};
+  }
+  const int64_t hi = span.base + span.n;
+  const int64_t lo_all = span.lo(a, span.n - 1), hi_all = span.base;  // that all rows see
+  int64_t my_lo[CT], my_hi[CT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    const int row = 16 * c + col, t = token_of(row);
+    my_lo[c] = span.lo(a, t);
+    my_hi[c] = row < rows ? span.base + t : -1;
+  }
+  _Float16* vbuf = lds[wave].v;
+  const int end = min(part.end * 2, int((hi + kStep - 1) / kStep));
+  int step = part.first * 2 + wave;
+  if (step < end) {
+    fetch_pages(step);
+    fetch(step);
+    if (step + kWaves < end) fetch_pages(step + kWaves);
+  }
+  for (; step < end; step += kWaves) {
+    const int64_t pos0 = int64_t(step) * kStep;
+    const int pages = has;
+    // scores: the keys are used up first
+    f32x4 sc[CT][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        sc[c][i] = f32x4{};
+#pragma unroll
+        for (int j = 0; j < F::MMA; ++j) {
+          const i32x4 w = rk[i][j % F::FRAGS];
+          sc[c][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+              i32x8{w[0], w[1], w[2], w[3], 0, 0, 0, 0}, qo[c][j], sc[c][i], 4, 0, 0,
+              rks[i][j % F::FRAGS], 0, qs[c][j]);
+        }
+      }
+    // values, as 16-bit floats into LDS
+    const int from = int(min(max(span.lowest - pos0, int64_t(0)), int64_t(kStep)));
+    const int to = int(min(hi - pos0, int64_t(kStep)));
+    int top_s = 0;
+    bool bad = false;
+    int vs[F::VC];
+#pragma unroll
+    for (int i = 0; i < F::VC; ++i) {
+      const int c = lane + 64 * i, tile = c / (NB * 16), tok = tile * 16 + c % 16;
+      const bool on = c < F::CHUNKS && tok >= from && tok < to && (pages >> tile & 1);
+      bad |= on && rvs[i] == 255;
+      vs[i] = on && rvs[i] != 255 ? rvs[i] : 0;
+      top_s = max(top_s, vs[i]);
+    }
+    if (__any(top_s > E)) {
+#pragma unroll
+      for (int k = 1; k < 64; k *= 2) top_s = max(top_s, __shfl_xor(top_s, k));
+      const int next = __builtin_amdgcn_readfirstlane(top_s) + kValueSlack;
+      if (E) {
+        const float down = exponent_to_f32(127 + E - next);
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+          for (int i = 0; i < NB * 2; ++i) o[c][i] *= down;
+      }
+      E = next;
+    }
+#pragma unroll
+    for (int i = 0; i < F::VC; ++i) {
+      const int c = lane + 64 * i, tile = c / (NB * 16), rest = c - tile * NB * 16;
+      if (c >= F::CHUNKS) break;
+      const float scale = vs[i] ? exponent_to_f32(127 + vs[i] - E + kValueLift) : 0.f;
+      _Float16* dst = vbuf + (tile * 16 + rest % 16) * F::VS + rest / 16 * 32;
+      f16x8 w[2];
+      decode16(rv[i][0], rv[i][1], scale, w);
+      *reinterpret_cast<f16x8*>(dst) = w[0];
+      *reinterpret_cast<f16x8*>(dst + 8) = w[1];
+      decode16(rv[i][2], rv[i][3], scale, w);
+      *reinterpret_cast<f16x8*>(dst + 16) = w[0];
+      *reinterpret_cast<f16x8*>(dst + 24) = w[1];
+    }
+    int raw[F::VC];
+#pragma unroll
+    for (int i = 0; i < F::VC; ++i) raw[i] = rvs[i];
+    if (step + kWaves < end) {
+      fetch(step + kWaves);
+      if (step + 2 * kWaves < end) fetch_pages(step + 2 * kWaves);
+    }
+    const bool whole = pos0 >= lo_all && pos0 + kStep - 1 <= hi_all && pages == 3;
+    f16x8 p[CT][F::PT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      if (!whole || 16 * (c + 1) > rows) {
+        const int first = int(min(max(my_lo[c] - pos0, int64_t(-1)), int64_t(kStep)));
+        const int last = int(min(max(my_hi[c] - pos0, int64_t(-1)), int64_t(kStep)));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int k = 16 * (i / 4) + 4 * g + i % 4;
+          const bool see = k >= first && k <= last && (pages >> (i / 4) & 1);
+          sc[c][i / 4][i % 4] = see ? sc[c][i / 4][i % 4] : -__builtin_inff();
+        }
+      }
+      float top = sc[c][0][0];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) top = fmaxf(top, sc[c][i / 4][i % 4]);
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      if (__any(top > m[c] + a.slack)) {
+        const float next = fmaxf(top, m[c]);
+        const float down = exp2_fast((m[c] - next) * a.scale_log2);
+        l[c] *= down;
+#pragma unroll
+        for (int i = 0; i < NB * 2; ++i) o[c][i] *= down;
+        m[c] = next;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        f32x2 w;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          w[k] = exp2_fast(fmaf(sc[c][(i + k) / 4][(i + k) % 4] - m[c], a.scale_log2, kLift));
+#pragma unroll
+        for (int k = 0; k < F::PT; ++k) {
+          const f16x2 r = __builtin_convertvector(w, f16x2);
+          p[c][k][i] = r[0];
+          p[c][k][i + 1] = r[1];
+          l[c] = __builtin_amdgcn_fdot2(r, f16x2{1, 1}, l[c], false);
+          if (k + 1 < F::PT) w -= __builtin_convertvector(r, f32x2);
+        }
+      }
+    }
+    __builtin_amdgcn_wave_barrier();  // a wave's LDS instructions stay in order
+    const _Float16* base = vbuf + (4 * g + col / 4) * F::VS + 4 * (col % 4);
+#pragma unroll
+    for (int i = 0; i < NB * 2; ++i) {
+      struct Both {
+        s16x4 lo, hi;
+      } r;
+      r.lo = turned4(base + 16 * i);
+      r.hi = turned4(base + 16 * F::VS + 16 * i);
+      const f16x8 v = __builtin_bit_cast(f16x8, r);
+#pragma unroll
+      for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int k = 0; k < F::PT; ++k)
+          o[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[c][k], o[c][i], 0, 0, 0);
+    }
+    __builtin_amdgcn_wave_barrier();
+    if (__any(bad)) {  // blocks that are not finite, to the rows that see their tokens
+#pragma unroll
+      for (int i = 0; i < F::VC; ++i)
+        for (int k = 0; k < 64; ++k) {
+          const int c = k + 64 * i;
+          if (c >= F::CHUNKS) break;
+          if (__builtin_amdgcn_readlane(raw[i], k) != 255) continue;
+          const int tile = c / (NB * 16), blk = c % (NB * 16) / 16;
+          const int64_t pos = pos0 + tile * 16 + c % 16;
+#pragma unroll
+          for (int q = 0; q < CT; ++q) {
+            const bool see = pos >= my_lo[q] && pos <= my_hi[q] && (pages >> tile & 1);
+            const float nan = see ? __builtin_nanf("") : 0.f;
+#pragma unroll
+            for (int n = 0; n < NB * 2; ++n)
+              if (n / 2 == blk) o[q][n] += nan;
+          }
+        }
+    }
+  }
+
+  // the waves' sums together, a column tile at a time
+  constexpr int OS = NB * 32 + 16;
+  const float up = exponent_to_f32(E - kValueSlack);
+  const float less = exponent_to_f32(127 + kValueSlack - kValueLift);
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    if (16 * c >= rows) break;
+    l[c] += __shfl_xor(l[c], 16);
+    l[c] += __shfl_xor(l[c], 32);
+    const float inv = l[c] > 0.f || l[c] != l[c] ? 1.f / l[c] : 0.f;
+    const float nan = q_bad[c] && l[c] > 0.f ? __builtin_nanf("") : 0.f;
+    if (c) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NB * 2; ++i) {
+      Pack<float, 4> v;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v.v[k] = o[c][i][k] * inv * less * up + nan;
+      store_pack<float, 4>(lds[wave].o + col * OS + 16 * i + 4 * g, v);
+    }
+    if (g == 0) stats[wave][col] = {m[c], l[c]};
+    __syncthreads();
+    for (int i = threadIdx.x; i < 16 * NB * 8; i += kBlock) {
+      const int r = i / (NB * 8), ch = i % (NB * 8) * 4, row = 16 * c + r;
+      if (row >= rows) break;
+      float top = -__builtin_inff(), sum = 0.f, v[4] = {};
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, stats[w][r].x);
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float2 st = stats[w][r];
+        if (st.y == 0.f) continue;  // sees nothing there
+        const float weight = exp2_fast((st.x - top) * a.scale_log2) * st.y;
+        sum += weight;
+        const Pack<float, 4> x = load_pack<float, 4>(lds[w].o + r * OS + ch);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = fmaf(weight, x.v[k], v[k]);
+      }
+      const float all = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] *= all;
+      if (part.parts == 1) {
+        store4<T>(out_row(row), ch, a.d.head_dim, a.wide, v);
+      } else {
+        const int64_t at = (int64_t(pair) * a.splits + split) * (CT * 16) + row;
+        store_pack<float, 4>(a.part + at * (NB * 32) + ch, Pack<float, 4>{{v[0], v[1], v[2], v[3]}});
+        if (ch == 0) a.part_stat[at] = {top, sum};
+      }
+    }
+  }
+}
+
+template <typename T, int NB>
+void run(const AttendArgs& a, int tiles, unsigned grid, hipStream_t s) {
+  if (tiles == 1)
+    attend_few_kernel<T, NB, 1><<<grid, kBlock, 0, s>>>(a);
+  else
+    attend_few_kernel<T, NB, 2><<<grid, kBlock, 0, s>>>(a);
+}
+
+template <typename T>
+void run(const AttendArgs& a, int NB, int tiles, unsigned grid, hipStream_t s) {
+  switch (NB) {
+    case 1: run<T, 1>(a, tiles, grid, s); break;
+    case 2: run<T, 2>(a, tiles, grid, s); break;
+    case 3: run<T, 3>(a, tiles, grid, s); break;
+    case 4: run<T, 4>(a, tiles, grid, s); break;
+    case 5: run<T, 5>(a, tiles, grid, s); break;
+    case 6: run<T, 6>(a, tiles, grid, s); break;
+    case 7: run<T, 7>(a, tiles, grid, s); break;
+    default: run<T, 8>(a, tiles, grid, s); break;
+  }
+}
+
+}  // namespace
+
+void launch_attend_few(const AttendArgs& a, int NB, int tiles, hipStream_t stream) {
+  const unsigned grid = unsigned(a.pairs) * a.splits;
+  if (a.d.dtype == CO_BF16)
+    run<bf16_t>(a, NB, tiles, grid, stream);
+  else
+    run<float>(a, NB, tiles, grid, stream);
+}
+
+}  // namespace coinf

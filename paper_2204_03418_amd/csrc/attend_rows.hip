@@ -10,15 +10,11 @@
 // LDS holds and moves a quarter of the bytes.  Values become 16-bit floats in LDS, once a
 // workgroup (exactly, but for what is below 2^-35 of its tile's largest scale), and the
 // weights 16-bit floats with 11 bits (two terms, 22 bits, for float32).
-#include <algorithm>
-
 #include "attend.hpp"
 
 namespace coinf {
 
 namespace {
-
-constexpr int kRows = 128;
 
 template <typename T, int NB>
 struct Rows {
@@ -428,46 +424,6 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
   if (half == 0) a.part_stat[at] = {m, l};
 }
 
-// Joins the parts of a row: a wave a row.
-template <typename T>
-__global__ __launch_bounds__(kBlock) void attend_join_kernel(AttendArgs a, int rows_of, int width,
-                                                             int64_t all_rows) {
-  const int64_t r = int64_t(blockIdx.x) * (kBlock / 64) + threadIdx.x / 64;
-  if (r >= all_rows) return;
-  const int lane = threadIdx.x % 64;
-  const int64_t unit = r / rows_of;
-  const int in = int(r - unit * rows_of);
-  const int pair = fdiv(int(unit), a.by_row_tiles), rt = int(unit) - pair * a.row_tiles;
-  const int b = fdiv(pair, a.by_kv), kv = pair - b * a.d.kv_heads;
-  const Span span(a, b);
-  const int rows = span.n * a.group, row0 = rt * rows_of, row = row0 + in;
-  if (row >= rows) return;
-  const int t = fdiv(row, a.by_group), head = kv * a.group + row - t * a.group;
-  const int t_last = fdiv(min(row0 + rows_of, rows) - 1, a.by_group);
-  const Part part(span.lo(a, fdiv(row0, a.by_group)), span.base + t_last + 1, a.splits, 0);
-  if (part.parts == 1) return;
-  const int64_t at = unit * a.splits * rows_of + in;
-  float top = -__builtin_inff();
-  for (int s = 0; s < part.parts; ++s) top = fmaxf(top, a.part_stat[at + int64_t(s) * rows_of].x);
-  float sum = 0.f, v[4] = {};
-  for (int s = 0; s < part.parts; ++s) {
-    const int64_t i = at + int64_t(s) * rows_of;
-    const float2 stat = a.part_stat[i];
-    if (stat.y == 0.f) continue;  // sees nothing there
-    const float w = exp2_fast((stat.x - top) * a.scale_log2) * stat.y;
-    sum += w;
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (lane + 64 * k < width) v[k] = fmaf(w, a.part[i * width + lane + 64 * k], v[k]);
-  }
-  T* y = static_cast<T*>(a.y.data) + b * a.y.batch_stride + t * a.y.token_stride +
-         int64_t(head) * a.d.head_dim;
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (lane + 64 * k < a.d.head_dim) y[lane + 64 * k] = from_f32<T>(v[k] * inv);
-}
-
 template <typename T>
 void run(const AttendArgs& a, int NB, unsigned grid, hipStream_t s) {
   switch (NB) {
@@ -480,77 +436,16 @@ void run(const AttendArgs& a, int NB, unsigned grid, hipStream_t s) {
     case 7: attend_rows_kernel<T, 7><<<grid, kBlock, 0, s>>>(a); break;
     default: attend_rows_kernel<T, 8><<<grid, kBlock, 0, s>>>(a); break;
   }
-  if (a.splits > 1) {
-    const int64_t rows = int64_t(a.pairs) * a.row_tiles * kRows;
-    attend_join_kernel<T><<<unsigned((rows + 3) / 4), kBlock, 0, s>>>(a, kRows, NB * 32, rows);
-  }
-}
-
-// How the rows of a call are cut.
-struct Cut {
-  int64_t pairs, row_tiles, splits;
-  int64_t units() const { return pairs * row_tiles; }
-};
-
-// Workgroups that the card holds: two a CU.  A call of fewer units has its keys cut in parts.
-Cut cut_of(const co_attn_desc& d, int32_t T) {
-  Cut c;
-  c.pairs = int64_t(d.batch) * d.kv_heads;
-  c.row_tiles = (int64_t(T) * (d.heads / d.kv_heads) + kRows - 1) / kRows;
-  const int64_t keys = std::min<int64_t>(int64_t(d.stream_pages) * d.page_tokens,
-                                         d.window ? int64_t(d.window) + T + kKeys : INT64_MAX);
-  const int64_t parts = (keys + kKeys * kMinTiles - 1) / (kKeys * kMinTiles);
-  c.splits = std::max<int64_t>(1, std::min<int64_t>(512 / c.units(), parts));
-  return c;
 }
 
 }  // namespace
 
-int64_t attend_workspace(const co_attn_desc& d, int32_t T) {
-  if (T == 0) return 0;
-  const Cut c = cut_of(d, T);
-  if (c.splits == 1) return 0;
-  return c.units() * c.splits * kRows * (cache_blocks(d.head_dim) * 32 + 2) * 4;
-}
-
-hipError_t launch_attend(const co_attn_desc& d, const co_attn_cache& cache, const co_tokens& q,
-                         const co_tokens& y, int32_t T, void* workspace, hipStream_t stream) {
-  AttendArgs a{d, cache, q, y, T};
-  const int NB = cache_blocks(d.head_dim);
-  a.lay = {d.page_tokens, NB};
-  a.page_bytes = int64_t(a.lay.bytes()) * d.kv_heads;
-  const float scale = d.scale * kLog2e;
-  a.q_sign = scale > 0 ? 1.f : scale < 0 ? -1.f : 0.f;
-  a.scale_log2 = scale == 0 ? 1.f : fabsf(scale);
-  a.slack = kSlack / a.scale_log2;
-  a.group = d.heads / d.kv_heads;
-  const Cut c = cut_of(d, T);
-  if (int64_t(T) * a.group + kRows >= INT32_MAX || c.units() * c.splits >= 1 << 24 ||
-      c.units() * kRows / 4 >= 1 << 24)
-    return hipErrorInvalidConfiguration;
-  a.by_group = make_fastdiv(a.group);
-  a.by_W = make_fastdiv(d.stream_pages);
-  a.by_kv = make_fastdiv(d.kv_heads);
-  while ((1 << a.page_shift) < d.page_tokens) ++a.page_shift;
-  a.pairs = int32_t(c.pairs);
-  a.row_tiles = int32_t(c.row_tiles);
-  a.splits = int32_t(c.splits);
-  a.by_row_tiles = make_fastdiv(a.row_tiles);
-  a.by_splits = make_fastdiv(a.splits);
-  const int es = d.dtype == CO_BF16 ? 2 : 4;
-  a.wide = 1;
-  for (const co_tokens* v : {&q, &y})
-    if ((v->batch_stride | v->token_stride | d.head_dim |
-         int64_t(reinterpret_cast<uintptr_t>(v->data) / es)) % 4)
-      a.wide = 0;
-  a.part = static_cast<float*>(workspace);
-  a.part_stat = reinterpret_cast<float2*>(a.part + c.units() * c.splits * kRows * NB * 32);
-  const unsigned grid = unsigned(c.units() * c.splits);
-  if (d.dtype == CO_BF16)
+void launch_attend_rows(const AttendArgs& a, int NB, hipStream_t stream) {
+  const unsigned grid = unsigned(int64_t(a.pairs) * a.row_tiles * a.splits);
+  if (a.d.dtype == CO_BF16)
     run<bf16_t>(a, NB, grid, stream);
   else
     run<float>(a, NB, grid, stream);
-  return hipGetLastError();
 }
 
 }  // namespace coinf
