@@ -53,31 +53,47 @@ constexpr int kValueLift = 12, kValueSlack = 4;
 
 // What a stream's rows see.
 struct Span {
-  int64_t base;
-  int n;         // tokens of the call
-  int64_t lowest;
-  __device__ Span(const AttendArgs& a, int b)
-      : base(a.c.base[b]),
-        n(base < 0 ? 0 : stream_tokens(a.c.granted, b, a.T)),
-        lowest(a.c.first ? max(a.c.first[b], 0) : 0) {}
-  // first and last key of a token, whole or past it
-  __device__ int64_t lo(const AttendArgs& a, int t) const {
-    const int64_t w = a.d.window ? base + t - a.d.window + 1 : 0;
-    return max(max(w, lowest), int64_t(0));
+  int base, n;  // n: tokens of the call
+  int lowest;
+  __device__ Span(const AttendArgs& a, int b) : base(a.c.base[b]) {
+    // positions stay below 2^31
+    n = base < 0 ? 0 : min(stream_tokens(a.c.granted, b, a.T), INT32_MAX - 2 * kKeys - base);
+    n = max(n, 0);
+    lowest = a.c.first ? max(a.c.first[b], 0) : 0;
+  }
+  // a token's first key
+  __device__ int lo(const AttendArgs& a, int t) const {
+    const int w = a.d.window ? base - a.d.window + 1 + t : 0;
+    return max(w, lowest);
   }
 };
 
-// Tiles of keys first..end - 1 of a unit's part `split`; parts: of the unit.
+// Tiles first..end - 1 of a unit's part `split` of the keys lo..hi - 1; parts: of the unit.
 struct Part {
   int first, end, parts;
-  __device__ Part(int64_t lo, int64_t hi, int splits, int split) {
-    const int t0 = int(lo / kKeys), t1 = lo < hi ? int((hi + kKeys - 1) / kKeys) : t0;
+  __device__ Part(int lo, int hi, int splits, int split) {
+    const int t0 = lo / kKeys, t1 = lo < hi ? (hi + kKeys - 1) / kKeys : t0;
     const int each = max((t1 - t0 + splits - 1) / splits, kMinTiles);
     parts = max((t1 - t0 + each - 1) / each, 1);
     first = min(t0 + split * each, t1);
     end = min(first + each, t1);
   }
 };
+
+// The largest of the lanes' values.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_max(int v) {
+  return max(v, __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ int wave_max(int v) {  // v >= 0
+  v = dpp_max<0x111, 0xf>(v);  // from 1, 2, 4 and 8 lanes below, within 16
+  v = dpp_max<0x112, 0xf>(v);
+  v = dpp_max<0x114, 0xf>(v);
+  v = dpp_max<0x118, 0xf>(v);
+  v = dpp_max<0x142, 0xa>(v);  // lane 15 of the 16 below
+  v = dpp_max<0x143, 0xc>(v);  // lane 31
+  return __builtin_amdgcn_readlane(v, 63);
+}
 
 // Four values of channels c.. of a row, 0 past D.
 template <typename T>

@@ -204,9 +204,9 @@ __global__ __launch_bounds__(kBlock) void attend_few_kernel(AttendArgs a) {
 #pragma unroll
     for (int i = 0; i < NB * 2; ++i) o[c][i] = f32x4{};
   }
-  const int64_t hi = span.base + span.n;
-  const int64_t lo_all = span.lo(a, span.n - 1), hi_all = span.base;  // that all rows see
-  int64_t my_lo[CT], my_hi[CT];
+  const int hi = span.base + span.n;
+  const int lo_all = span.lo(a, span.n - 1), hi_all = span.base;  // that all rows see
+  int my_lo[CT], my_hi[CT];
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
     const int row = 16 * c + col, t = token_of(row);
@@ -214,7 +214,7 @@ __global__ __launch_bounds__(kBlock) void attend_few_kernel(AttendArgs a) {
     my_hi[c] = row < rows ? span.base + t : -1;
   }
   _Float16* vbuf = lds[wave].v;
-  const int end = min(part.end * 2, int((hi + kStep - 1) / kStep));
+  const int end = min(part.end * 2, (hi + kStep - 1) / kStep);
   int step = part.first * 2 + wave;
   if (step < end) {
     fetch_pages(step);
@@ -222,7 +222,7 @@ __global__ __launch_bounds__(kBlock) void attend_few_kernel(AttendArgs a) {
     if (step + kWaves < end) fetch_pages(step + kWaves);
   }
   for (; step < end; step += kWaves) {
-    const int64_t pos0 = int64_t(step) * kStep;
+    const int pos0 = step * kStep;
     const int pages = has;
     // scores: the keys are used up first
     f32x4 sc[CT][2];
@@ -240,8 +240,7 @@ __global__ __launch_bounds__(kBlock) void attend_few_kernel(AttendArgs a) {
         }
       }
     // values, as 16-bit floats into LDS
-    const int from = int(min(max(span.lowest - pos0, int64_t(0)), int64_t(kStep)));
-    const int to = int(min(hi - pos0, int64_t(kStep)));
+    const int from = span.lowest - pos0, to = hi - pos0;
     int top_s = 0;
     bool bad = false;
     int vs[F::VC];
@@ -254,9 +253,7 @@ __global__ __launch_bounds__(kBlock) void attend_few_kernel(AttendArgs a) {
       top_s = max(top_s, vs[i]);
     }
     if (__any(top_s > E)) {
-#pragma unroll
-      for (int k = 1; k < 64; k *= 2) top_s = max(top_s, __shfl_xor(top_s, k));
-      const int next = __builtin_amdgcn_readfirstlane(top_s) + kValueSlack;
+      const int next = wave_max(top_s) + kValueSlack;
       if (E) {
         const float down = exponent_to_f32(127 + E - next);
 #pragma unroll
@@ -292,8 +289,7 @@ __global__ __launch_bounds__(kBlock) void attend_few_kernel(AttendArgs a) {
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       if (!whole || 16 * (c + 1) > rows) {
-        const int first = int(min(max(my_lo[c] - pos0, int64_t(-1)), int64_t(kStep)));
-        const int last = int(min(max(my_hi[c] - pos0, int64_t(-1)), int64_t(kStep)));
+        const int first = my_lo[c] - pos0, last = my_hi[c] - pos0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int k = 16 * (i / 4) + 4 * g + i % 4;
@@ -355,7 +351,7 @@ __global__ __launch_bounds__(kBlock) void attend_few_kernel(AttendArgs a) {
           if (c >= F::CHUNKS) break;
           if (__builtin_amdgcn_readlane(raw[i], k) != 255) continue;
           const int tile = c / (NB * 16), blk = c % (NB * 16) / 16;
-          const int64_t pos = pos0 + tile * 16 + c % 16;
+          const int pos = pos0 + tile * 16 + c % 16;
 #pragma unroll
           for (int q = 0; q < CT; ++q) {
             const bool see = pos >= my_lo[q] && pos <= my_hi[q] && (pages >> tile & 1);

@@ -16,36 +16,41 @@ namespace coinf {
 
 namespace {
 
+constexpr int kSubs = kKeys / kCacheTile;  // tiles of the pages in one of keys: a wave each
+static_assert(kSubs == kBlock / 64);
+
 template <typename T, int NB>
 struct Rows {
   static constexpr int QT = kQueryTerms<T>, PT = kWeightTerms<T>;
   static constexpr bool EVEN = NB % 2 == 0;
-  static constexpr int MMA = QT * NB / 2;              // of a 32 x 32 tile of scores, depth 64
-  static constexpr int FRAGS = EVEN ? NB / 2 : NB;     // of keys
-  static constexpr int CHUNKS = NB * kKeys;            // 16 bytes of codes of a tile
-  static constexpr int PER = (CHUNKS + kBlock - 1) / kBlock;
-  static constexpr int WORDS = (CHUNKS / 4 + 63) / 64;  // of scales a lane
-  static constexpr int VS = NB * 32 + 32;              // rows 64 bytes apart modulo the banks
+  static constexpr int MMA = QT * NB / 2;           // of a 32 x 32 tile of scores, depth 64
+  static constexpr int FRAGS = EVEN ? NB / 2 : NB;  // of keys
+  static constexpr int CHUNKS = NB * kCacheTile;    // 16 bytes of codes of 16 tokens
+  static constexpr int PER = (CHUNKS + 63) / 64;
+  static constexpr int VS = NB * 32 + 32;           // rows 64 bytes apart modulo the banks
   // term and block of the half h of instruction j
   static __device__ int term(int j, int h) { return EVEN ? 2 * j / NB : 2 * (j / NB) + h; }
   static __device__ int block(int j, int h) { return EVEN ? 2 * j % NB + h : j % NB; }
 };
 
+constexpr int kNoPage = 1, kNotFinite = 2;  // of 16 tokens
+
 template <typename T, int NB>
 struct RowsLds {
   using R = Rows<T, NB>;
-  alignas(16) uint8_t k[2][R::CHUNKS * 16];
+  alignas(16) uint8_t k[2][kSubs * R::CHUNKS * 16];
   alignas(16) _Float16 v[2][kKeys * R::VS];
-  uint32_t ks[2][R::CHUNKS / 4], vs[2][R::CHUNKS / 4];
-  int32_t pages[2];  // bit i: 16 tokens i have a page
-  int32_t bad[2];    // the tile, where a value is not finite
+  uint8_t ks[2][kSubs * R::CHUNKS], vs[2][kSubs * R::CHUNKS];
+  alignas(16) int32_t flags[2][kSubs];
+  alignas(16) int32_t top[4][kSubs];  // the largest scale of the values, by tile modulo 4
 };
 
 template <typename T, int NB>
 __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(AttendArgs a) {
   using R = Rows<T, NB>;
   __shared__ RowsLds<T, NB> s;
-  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, col = lane % 32, half = lane / 32;
+  const int tid = threadIdx.x, lane = tid % 64, col = lane % 32, half = lane / 32;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
 
   // which unit: all parts and row tiles of a pair on one XCD where the pairs allow it, the rows
   // that see most first
@@ -126,93 +131,80 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
     }
   }
 
-  // one thread's 16 bytes of keys and of values of a tile, on their way
+  // The keys' way: pages three tiles ahead, scales of values two, codes one.  A wave brings 16 of a
+  // tile's tokens, from one page.
   const char* pool = static_cast<const char*>(a.c.pool) + int64_t(kv) * a.lay.bytes();
   const int32_t* table = a.c.table + int64_t(b) * a.d.stream_pages;
-  const int tile_bytes = NB * 256;
-  i32x4 rk[R::PER], rv[R::PER];
-  uint32_t rks[R::WORDS], rvs[R::WORDS];
-  int page[R::PER], page_w[R::WORDS];
-  // the pages of a tile's chunks and words of scales
-  const auto page_of = [&](int tile, int sub) {
-    const int64_t pos = int64_t(tile) * kKeys + sub * kCacheTile;
-    const int lp = int(pos >> a.page_shift);
-    const int p = table[lp - fdiv(lp, a.by_W) * a.d.stream_pages];
+  const int sub_mask = a.lay.P / kCacheTile - 1;
+  const auto load_page = [&](int tile) {
+    const int lp = (tile * kSubs + wave) >> (a.page_shift - 4);
+    return table[lp - fdiv(lp, a.by_W) * a.d.stream_pages];
+  };
+  const auto page_ok = [&](int p) {
+    p = __builtin_amdgcn_readfirstlane(p);
     return p >= 0 && p < a.d.pages ? p : -1;
   };
-  const auto fetch_pages = [&](int tile) {
+  // `part` of the page, for this wave's 16 tokens of the tile
+  const auto place = [&](int page, int tile, int part, int bytes) {
+    return pool + page * a.page_bytes + part + ((tile * kSubs + wave) & sub_mask) * bytes;
+  };
+  const int hi = span.base + span.n;
+  i32x4 rk[R::PER], rv[R::PER];
+  int rks[R::PER], rvs[R::PER], rvs_next[R::PER];
+  const auto fetch_codes = [&](int page, int tile) {
 #pragma unroll
     for (int i = 0; i < R::PER; ++i) {
-      const int c = tid + i * kBlock;
-      page[i] = c < R::CHUNKS ? page_of(tile, c / (NB * 16)) : -1;
-    }
-#pragma unroll
-    for (int i = 0; i < R::WORDS; ++i) {
-      const int w = lane + 64 * i;
-      page_w[i] = w < R::CHUNKS / 4 ? page_of(tile, w / (NB * 4)) : -1;
+      const int c = lane + 64 * i;
+      rk[i] = rv[i] = i32x4{0, 0, 0, 0};
+      rks[i] = 127;
+      if (page >= 0 && c < R::CHUNKS) {
+        rk[i] = *reinterpret_cast<const i32x4*>(
+            place(page, tile, a.lay.codes(0), R::CHUNKS * 16) + c * 16);
+        rv[i] = *reinterpret_cast<const i32x4*>(
+            place(page, tile, a.lay.codes(1), R::CHUNKS * 16) + c * 16);
+        rks[i] = uint8_t(place(page, tile, a.lay.scales(0), R::CHUNKS)[c]);
+      }
     }
   };
-  const auto fetch = [&](int tile) {
-    const int in = int(int64_t(tile) * kKeys & (a.lay.P - 1)) / kCacheTile;  // of a page's tiles
-    const int sub_mask = a.lay.P / kCacheTile - 1;
+  const auto fetch_scales = [&](int page, int tile) {
 #pragma unroll
     for (int i = 0; i < R::PER; ++i) {
-      const int c = tid + i * kBlock, sub = c / (NB * 16), rest = c - sub * NB * 16;
-      rk[i] = rv[i] = i32x4{0, 0, 0, 0};
-      if (page[i] >= 0) {
-        const char* p = pool + page[i] * a.page_bytes + ((in + sub) & sub_mask) * tile_bytes +
-                        rest * 16;
-        rk[i] = *reinterpret_cast<const i32x4*>(p);
-        rv[i] = *reinterpret_cast<const i32x4*>(p + a.lay.codes(1));
-      }
+      const int c = lane + 64 * i;
+      rvs_next[i] = 0;
+      if (page >= 0 && c < R::CHUNKS)
+        rvs_next[i] = uint8_t(place(page, tile, a.lay.scales(1), R::CHUNKS)[c]);
     }
+  };
+  // scales of the stream's own tokens: what else a page holds may be anything
+  const auto post_scales = [&](int tile) {
+    const int pos0 = tile * kKeys + wave * kCacheTile;
+    const int from = span.lowest - pos0, to = hi - pos0;
+    int top = 0;
 #pragma unroll
-    for (int i = 0; i < R::WORDS; ++i) {
-      const int w = lane + 64 * i, sub = w / (NB * 4), rest = w - sub * NB * 4;
-      rks[i] = rvs[i] = 0;
-      if (page_w[i] >= 0) {
-        const char* p = pool + page_w[i] * a.page_bytes + ((in + sub) & sub_mask) * NB * 16 +
-                        rest * 4;
-        if (wave == 0) rks[i] = *reinterpret_cast<const uint32_t*>(p + a.lay.scales(0));
-        rvs[i] = *reinterpret_cast<const uint32_t*>(p + a.lay.scales(1));
-      }
+    for (int i = 0; i < R::PER; ++i) {
+      const int tok = lane % 16;
+      rvs_next[i] = tok >= from && tok < to ? rvs_next[i] : 0;
+      top = max(top, rvs_next[i] == 255 ? 0 : rvs_next[i]);
     }
+    top = wave_max(top);
+    if (lane == 0) s.top[tile & 3][wave] = top;
   };
 
-  const int64_t hi = span.base + span.n;
   f32x16 o[NB];
 #pragma unroll
   for (int i = 0; i < NB; ++i) o[i] = f32x16{};
-  float m = -1e30f, l = 0.f;  // the row's reference score, and its sum
-  int E = 0;                  // the values' exponent, 0: none yet
+  // The row's reference score, and its sum.  The products begin at -reference (all 16 alike): what
+  // they give is the difference.  over: what a difference may reach, everything before the first.
+  f32x16 below = f32x16{};
+  float l = 0.f, over = -3e38f;
+  int E = 0;  // the values' exponent, 0: none yet
 
   // what was fetched into LDS
-  const auto fill = [&](int tile, int buf) {
-    const int64_t pos0 = int64_t(tile) * kKeys;
-    // keys of the stream: what else a page holds may be anything
-    const int from = int(min(max(span.lowest - pos0, int64_t(0)), int64_t(kKeys)));
-    const int to = int(min(hi - pos0, int64_t(kKeys)));
-    int top = 0;
-    uint32_t bytes[R::WORDS];
-#pragma unroll
-    for (int i = 0; i < R::WORDS; ++i) {
-      const int w = lane + 64 * i, tok = w / (NB * 4) * 16 + w % 4 * 4;
-      bytes[i] = rvs[i];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int v = bytes[i] >> (8 * k) & 255;
-        const bool on = tok + k >= from && tok + k < to && v != 255;
-        top = max(top, on ? v : 0);
-      }
-      if (wave == 0 && w < R::CHUNKS / 4) {
-        s.ks[buf][w] = rks[i];
-        s.vs[buf][w] = bytes[i];
-      }
-    }
-    if (__any(top > E)) {
-#pragma unroll
-      for (int k = 1; k < 64; k *= 2) top = max(top, __shfl_xor(top, k));
-      const int next = __builtin_amdgcn_readfirstlane(top) + kValueSlack;
+  const auto fill = [&](int page, int tile, int buf) {
+    const i32x4 t4 = *reinterpret_cast<const i32x4*>(s.top[tile & 3]);
+    const int top = __builtin_amdgcn_readfirstlane(max(max(t4[0], t4[1]), max(t4[2], t4[3])));
+    if (top > E) {
+      const int next = top + kValueSlack;
       if (E) {
         const float down = exponent_to_f32(127 + E - next);
 #pragma unroll
@@ -220,21 +212,19 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
       }
       E = next;
     }
+    bool bad = false;
 #pragma unroll
     for (int i = 0; i < R::PER; ++i) {
-      const int c = tid + i * kBlock, sub = c / (NB * 16), rest = c - sub * NB * 16;
-      const int tok = sub * 16 + rest % 16, blk = rest / 16;
-      // the chunk's scale is byte c of the words, which all waves have
-      const uint32_t word = R::WORDS == 1 || c < 256
-                                ? uint32_t(__shfl(int(bytes[0]), c / 4 % 64))
-                                : uint32_t(__shfl(int(bytes[R::WORDS - 1]), c / 4 % 64));
+      const int c = lane + 64 * i;
       if (c >= R::CHUNKS) break;
-      const int v = word >> (8 * (c % 4)) & 255;
-      *reinterpret_cast<i32x4*>(s.k[buf] + c * 16) = rk[i];
-      const bool on = tok >= from && tok < to && page[i] >= 0;
-      if (on && v == 255) s.bad[buf] = tile;
-      const float scale = on && v != 255 ? exponent_to_f32(127 + v - E + kValueLift) : 0.f;
-      _Float16* dst = s.v[buf] + tok * R::VS + blk * 32;
+      *reinterpret_cast<i32x4*>(s.k[buf] + (wave * R::CHUNKS + c) * 16) = rk[i];
+      s.ks[buf][wave * R::CHUNKS + c] = uint8_t(rks[i]);
+      s.vs[buf][wave * R::CHUNKS + c] = uint8_t(rvs[i]);
+      const bool no = rvs[i] == 255;
+      bad |= no;
+      // a scale of 0 is far below any other
+      const float scale = exponent_to_f32(no || rvs[i] == 0 ? 0 : 127 + rvs[i] - E + kValueLift);
+      _Float16* dst = s.v[buf] + (wave * kCacheTile + c % 16) * R::VS + c / 16 * 32;
       f16x8 w[2];
       decode16(rv[i][0], rv[i][1], scale, w);
       *reinterpret_cast<f16x8*>(dst) = w[0];
@@ -243,45 +233,47 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
       *reinterpret_cast<f16x8*>(dst + 16) = w[0];
       *reinterpret_cast<f16x8*>(dst + 24) = w[1];
     }
-    if (wave == 0) {
-      // one lane of each 16 tokens' first chunk or word
-      uint32_t on = 0;
-#pragma unroll
-      for (int i = 0; i < R::WORDS; ++i) {
-        const int w = lane + 64 * i;
-        if (w < R::CHUNKS / 4 && w % (NB * 4) == 0 && page_w[i] >= 0) on |= 1u << (w / (NB * 4));
-      }
-#pragma unroll
-      for (int k = 1; k < 64; k *= 2) on |= uint32_t(__shfl_xor(int(on), k));
-      if (lane == 0) s.pages[buf] = int(on);
-    }
+    const int flags = (page < 0 ? kNoPage : 0) | (__any(bad) ? kNotFinite : 0);
+    if (lane == 0) s.flags[buf][wave] = flags;
   };
 
-  // the wave's rows: keys that some of them see
+  // the wave's rows: their tokens, and the keys that some and that all of them see
+  const int wave_rows = min(row0 + wave * 32 + 32, rows) - (row0 + wave * 32);
   const int wt0 = fdiv(row0 + wave * 32, a.by_group);
-  const int wrows = min(row0 + wave * 32 + 32, rows);
-  const int wt1 = fdiv(max(wrows, 1) - 1, a.by_group);
-  const bool wave_on = row0 + wave * 32 < rows;
-  const int64_t wave_lo = span.lo(a, wt0), wave_hi = span.base + wt1;   // both included
-  const int64_t wave_lo_all = span.lo(a, wt1), wave_hi_all = span.base + wt0;  // that all see
-  const int64_t my_lo = span.lo(a, t), my_hi = live ? span.base + t : -1;
+  const int wt1 = fdiv(row0 + wave * 32 + max(wave_rows, 1) - 1, a.by_group);
+  const int some_lo = span.lo(a, wt0), some_hi = wave_rows > 0 ? span.base + wt1 : -1;
+  const int all_lo = span.lo(a, wt1), all_hi = span.base + wt0;
+  const int my_lo = span.lo(a, t), my_hi = live ? span.base + t : -1;
 
-  if (tid < 2) s.bad[tid] = -1;
+  int page0 = -1, page1 = -1, page2 = -1, coming = -1;  // of the next tiles
   if (part.first < part.end) {
-    fetch_pages(part.first);
-    fetch(part.first);
-    __syncthreads();  // bad
-    fill(part.first, 0);
-    if (part.first + 1 < part.end) fetch_pages(part.first + 1);
+    page0 = page_ok(load_page(part.first));
+    if (part.first + 1 < part.end) page1 = page_ok(load_page(part.first + 1));
+    if (part.first + 2 < part.end) coming = load_page(part.first + 2);
+    fetch_scales(page0, part.first);
+    fetch_codes(page0, part.first);
+    post_scales(part.first);
+#pragma unroll
+    for (int i = 0; i < R::PER; ++i) rvs[i] = rvs_next[i];
+    fetch_scales(page1, part.first + 1);
+    if (part.first + 1 < part.end) post_scales(part.first + 1);
+    page2 = page_ok(coming);
+    __syncthreads();
+    fill(page0, part.first, 0);
   }
   __syncthreads();
 
   for (int tile = part.first; tile < part.end; ++tile) {
     const int buf = (tile - part.first) & 1;
-    const bool more = tile + 1 < part.end;
-    if (more) fetch(tile + 1);
-    const int64_t pos0 = int64_t(tile) * kKeys;
-    if (wave_on && pos0 <= wave_hi && pos0 + kKeys > wave_lo) {
+    const int pos0 = tile * kKeys;
+    if (tile + 3 < part.end) coming = load_page(tile + 3);
+    if (tile + 1 < part.end) {
+#pragma unroll
+      for (int i = 0; i < R::PER; ++i) rvs[i] = rvs_next[i];
+      fetch_codes(page1, tile + 1);
+      if (tile + 2 < part.end) fetch_scales(page2, tile + 2);
+    }
+    if (pos0 <= some_hi && pos0 + kKeys > some_lo) {
       f32x16 sc[2];
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
@@ -293,26 +285,24 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
           const int at = ((2 * g + col / 16) * NB + blk) * 16 + col % 16;
           const i32x4 w = *reinterpret_cast<const i32x4*>(s.k[buf] + at * 16);
           kf[f] = i32x8{w[0], w[1], w[2], w[3], 0, 0, 0, 0};
-          ks[f] = reinterpret_cast<const uint8_t*>(s.ks[buf])[at];
+          ks[f] = s.ks[buf][at];
         }
-        sc[g] = f32x16{};
+        sc[g] = below;
 #pragma unroll
         for (int j = 0; j < R::MMA; ++j)
           sc[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
               kf[j % R::FRAGS], qo[j], sc[g], 4, 0, 0, ks[j % R::FRAGS], 0, qs[j]);
       }
-      const bool whole = pos0 + kKeys - 1 <= wave_hi_all && pos0 >= wave_lo_all &&
-                         s.pages[buf] == 15;
-      if (!whole) {
-        const int pages = s.pages[buf];
-        const int from = int(min(max(my_lo - pos0, int64_t(-1)), int64_t(kKeys)));
-        const int to = int(min(max(my_hi - pos0, int64_t(-1)), int64_t(kKeys)));
+      const i32x4 f4 = *reinterpret_cast<const i32x4*>(s.flags[buf]);
+      const int flags = __builtin_amdgcn_readfirstlane(f4[0] | f4[1] | f4[2] | f4[3]);
+      if (pos0 + kKeys - 1 > all_hi || pos0 < all_lo || (flags & kNoPage)) {
+        const int from = my_lo - pos0, to = my_hi - pos0;
 #pragma unroll
         for (int g = 0; g < 2; ++g)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int k = 32 * g + 8 * (i / 4) + 4 * half + i % 4;
-            const bool see = k >= from && k <= to && (pages >> (k / 16) & 1);
+            const bool see = k >= from && k <= to && !(f4[2 * g + i / 8] & kNoPage);
             sc[g][i] = see ? sc[g][i] : -__builtin_inff();
           }
       }
@@ -320,22 +310,27 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
 #pragma unroll
       for (int i = 1; i < 16; ++i) top = fmaxf(fmaxf(top, sc[0][i]), sc[1][i]);
       top = fmaxf(top, __shfl_xor(top, 32));
-      if (__any(top > m + a.slack)) {
-        const float next = fmaxf(top, m);
-        const float down = exp2_fast((m - next) * a.scale_log2);
+      if (__any(top > over)) {
+        const float more = top > over ? top : 0.f;
+        const float down = over < 0.f ? 1.f : exp2_fast(-more * a.scale_log2);
+        over = top > over ? a.slack : over;
         l *= down;
 #pragma unroll
         for (int i = 0; i < NB; ++i) o[i] *= down;
-        m = next;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          sc[0][i] -= more;
+          sc[1][i] -= more;
+          below[i] -= more;
+        }
       }
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
         f16x8 p[R::PT][2];
 #pragma unroll
         for (int i = 0; i < 16; i += 2) {
-          // the difference first: far scores have no digits to lose
-          f32x2 w = {exp2_fast(fmaf(sc[g][i] - m, a.scale_log2, kLift)),
-                     exp2_fast(fmaf(sc[g][i + 1] - m, a.scale_log2, kLift))};
+          f32x2 w = {exp2_fast(fmaf(sc[g][i], a.scale_log2, kLift)),
+                     exp2_fast(fmaf(sc[g][i + 1], a.scale_log2, kLift))};
 #pragma unroll
           for (int k = 0; k < R::PT; ++k) {
             const f16x2 r = __builtin_convertvector(w, f16x2);
@@ -365,12 +360,12 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
           }
         }
       }
-      if (s.bad[buf] == tile) {  // a block that is not finite, to the rows that see its token
-        for (int c = 0; c < R::CHUNKS; ++c) {
-          if (reinterpret_cast<const uint8_t*>(s.vs[buf])[c] != 255) continue;
-          const int tok = c / (NB * 16) * 16 + c % 16, blk = c % (NB * 16) / 16;
-          const int64_t pos = pos0 + tok;
-          const bool see = pos >= my_lo && pos <= my_hi && (s.pages[buf] >> (tok / 16) & 1);
+      if (flags & kNotFinite) {  // a block that is not finite, to the rows that see its token
+        for (int c = 0; c < kSubs * R::CHUNKS; ++c) {
+          if (s.vs[buf][c] != 255) continue;
+          const int sub = c / R::CHUNKS, blk = c % R::CHUNKS / 16;
+          const int pos = pos0 + sub * 16 + c % 16;
+          const bool see = pos >= my_lo && pos <= my_hi && !(s.flags[buf][sub] & kNoPage);
           const float nan = see ? __builtin_nanf("") : 0.f;
 #pragma unroll
           for (int i = 0; i < NB; ++i)
@@ -380,9 +375,11 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
         }
       }
     }
-    if (more) {
-      fill(tile + 1, buf ^ 1);
-      if (tile + 2 < part.end) fetch_pages(tile + 2);
+    if (tile + 1 < part.end) {
+      fill(page1, tile + 1, buf ^ 1);
+      if (tile + 2 < part.end) post_scales(tile + 2);
+      page1 = page2;
+      page2 = page_ok(coming);
     }
     __syncthreads();
   }
@@ -421,7 +418,7 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
                                  value(blk, i + 3)}};
       store_pack<float, 4>(o_part + blk * 32 + 2 * i + 4 * half, v);
     }
-  if (half == 0) a.part_stat[at] = {m, l};
+  if (half == 0) a.part_stat[at] = {-below[0], l};
 }
 
 template <typename T>
