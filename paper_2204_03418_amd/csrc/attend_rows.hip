@@ -33,14 +33,14 @@ struct Rows {
   static __device__ int block(int j, int h) { return EVEN ? 2 * j % NB + h : j % NB; }
 };
 
-constexpr int kNoPage = 1, kNotFinite = 2;  // of 16 tokens
+constexpr int kNoPage = 1, kNotFinite = 2;  // flags of 16 tokens
 
 template <typename T, int NB>
 struct RowsLds {
   using R = Rows<T, NB>;
-  alignas(16) uint8_t k[2][kSubs * R::CHUNKS * 16];
+  alignas(16) uint8_t k[3][kSubs * R::CHUNKS * 16];  // by tile modulo 3, the others modulo 2
   alignas(16) _Float16 v[2][kKeys * R::VS];
-  uint8_t ks[2][kSubs * R::CHUNKS], vs[2][kSubs * R::CHUNKS];
+  uint8_t ks[3][kSubs * R::CHUNKS], vs[2][kSubs * R::CHUNKS];
   alignas(16) int32_t flags[2][kSubs];
   alignas(16) int32_t top[4][kSubs];  // the largest scale of the values, by tile modulo 4
 };
@@ -131,8 +131,8 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
     }
   }
 
-  // The keys' way: pages three tiles ahead, scales of values two, codes one.  A wave brings 16 of a
-  // tile's tokens, from one page.
+  // The keys' way: pages three tiles ahead, codes of keys and scales of values two, codes of values
+  // one.  A wave brings 16 of a tile's tokens, from one page.
   const char* pool = static_cast<const char*>(a.c.pool) + int64_t(kv) * a.lay.bytes();
   const int32_t* table = a.c.table + int64_t(b) * a.d.stream_pages;
   const int sub_mask = a.lay.P / kCacheTile - 1;
@@ -151,40 +151,45 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
   const int hi = span.base + span.n;
   i32x4 rk[R::PER], rv[R::PER];
   int rks[R::PER], rvs[R::PER], rvs_next[R::PER];
-  const auto fetch_codes = [&](int page, int tile) {
+  const auto fetch_keys = [&](int page, int tile) {  // and the values' scales
 #pragma unroll
     for (int i = 0; i < R::PER; ++i) {
       const int c = lane + 64 * i;
-      rk[i] = rv[i] = i32x4{0, 0, 0, 0};
+      rk[i] = i32x4{0, 0, 0, 0};
       rks[i] = 127;
+      rvs_next[i] = 0;
       if (page >= 0 && c < R::CHUNKS) {
         rk[i] = *reinterpret_cast<const i32x4*>(
             place(page, tile, a.lay.codes(0), R::CHUNKS * 16) + c * 16);
-        rv[i] = *reinterpret_cast<const i32x4*>(
-            place(page, tile, a.lay.codes(1), R::CHUNKS * 16) + c * 16);
         rks[i] = uint8_t(place(page, tile, a.lay.scales(0), R::CHUNKS)[c]);
+        rvs_next[i] = uint8_t(place(page, tile, a.lay.scales(1), R::CHUNKS)[c]);
       }
     }
   };
-  const auto fetch_scales = [&](int page, int tile) {
+  const auto fetch_values = [&](int page, int tile) {
 #pragma unroll
     for (int i = 0; i < R::PER; ++i) {
       const int c = lane + 64 * i;
-      rvs_next[i] = 0;
+      rv[i] = i32x4{0, 0, 0, 0};
       if (page >= 0 && c < R::CHUNKS)
-        rvs_next[i] = uint8_t(place(page, tile, a.lay.scales(1), R::CHUNKS)[c]);
+        rv[i] = *reinterpret_cast<const i32x4*>(
+            place(page, tile, a.lay.codes(1), R::CHUNKS * 16) + c * 16);
     }
   };
-  // scales of the stream's own tokens: what else a page holds may be anything
-  const auto post_scales = [&](int tile) {
+  // The keys into LDS, and the largest of the values' scales: of the stream's own tokens, what else
+  // a page holds may be anything.
+  const auto fill_keys = [&](int tile, int slot) {
     const int pos0 = tile * kKeys + wave * kCacheTile;
     const int from = span.lowest - pos0, to = hi - pos0;
     int top = 0;
 #pragma unroll
     for (int i = 0; i < R::PER; ++i) {
-      const int tok = lane % 16;
+      const int c = lane + 64 * i, tok = lane % 16;
       rvs_next[i] = tok >= from && tok < to ? rvs_next[i] : 0;
       top = max(top, rvs_next[i] == 255 ? 0 : rvs_next[i]);
+      if (c >= R::CHUNKS) break;
+      *reinterpret_cast<i32x4*>(s.k[slot] + (wave * R::CHUNKS + c) * 16) = rk[i];
+      s.ks[slot][wave * R::CHUNKS + c] = uint8_t(rks[i]);
     }
     top = wave_max(top);
     if (lane == 0) s.top[tile & 3][wave] = top;
@@ -199,26 +204,13 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
   float l = 0.f, over = -3e38f;
   int E = 0;  // the values' exponent, 0: none yet
 
-  // what was fetched into LDS
-  const auto fill = [&](int page, int tile, int buf) {
-    const i32x4 t4 = *reinterpret_cast<const i32x4*>(s.top[tile & 3]);
-    const int top = __builtin_amdgcn_readfirstlane(max(max(t4[0], t4[1]), max(t4[2], t4[3])));
-    if (top > E) {
-      const int next = top + kValueSlack;
-      if (E) {
-        const float down = exponent_to_f32(127 + E - next);
-#pragma unroll
-        for (int i = 0; i < NB; ++i) o[i] *= down;
-      }
-      E = next;
-    }
+  // the values into LDS
+  const auto fill_values = [&](int page, int buf) {
     bool bad = false;
 #pragma unroll
     for (int i = 0; i < R::PER; ++i) {
       const int c = lane + 64 * i;
       if (c >= R::CHUNKS) break;
-      *reinterpret_cast<i32x4*>(s.k[buf] + (wave * R::CHUNKS + c) * 16) = rk[i];
-      s.ks[buf][wave * R::CHUNKS + c] = uint8_t(rks[i]);
       s.vs[buf][wave * R::CHUNKS + c] = uint8_t(rvs[i]);
       const bool no = rvs[i] == 255;
       bad |= no;
@@ -236,6 +228,19 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
     const int flags = (page < 0 ? kNoPage : 0) | (__any(bad) ? kNotFinite : 0);
     if (lane == 0) s.flags[buf][wave] = flags;
   };
+  // the values' exponent for a tile; the sums follow it
+  const auto follow = [&](int tile) {
+    const i32x4 t4 = *reinterpret_cast<const i32x4*>(s.top[tile & 3]);
+    const int top = __builtin_amdgcn_readfirstlane(max(max(t4[0], t4[1]), max(t4[2], t4[3])));
+    if (top <= E) return;
+    const int next = top + kValueSlack;
+    if (E) {
+      const float down = exponent_to_f32(127 + E - next);
+#pragma unroll
+      for (int i = 0; i < NB; ++i) o[i] *= down;
+    }
+    E = next;
+  };
 
   // the wave's rows: their tokens, and the keys that some and that all of them see
   const int wave_rows = min(row0 + wave * 32 + 32, rows) - (row0 + wave * 32);
@@ -245,127 +250,149 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
   const int all_lo = span.lo(a, wt1), all_hi = span.base + wt0;
   const int my_lo = span.lo(a, t), my_hi = live ? span.base + t : -1;
 
+  // scores of 32 keys, half g of the tile in `slot`
+  f32x16 sc[2];
+  const auto score = [&](int g, int slot) {
+    i32x8 kf[R::FRAGS];
+    int ks[R::FRAGS];
+#pragma unroll
+    for (int f = 0; f < R::FRAGS; ++f) {
+      const int blk = R::EVEN ? 2 * f + half : f;
+      const int at = ((2 * g + col / 16) * NB + blk) * 16 + col % 16;
+      const i32x4 w = *reinterpret_cast<const i32x4*>(s.k[slot] + at * 16);
+      kf[f] = i32x8{w[0], w[1], w[2], w[3], 0, 0, 0, 0};
+      ks[f] = s.ks[slot][at];
+    }
+    sc[g] = below;
+#pragma unroll
+    for (int j = 0; j < R::MMA; ++j)
+      sc[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+          kf[j % R::FRAGS], qo[j], sc[g], 4, 0, 0, ks[j % R::FRAGS], 0, qs[j]);
+  };
+  // the scores of half g within the row's keys and the reference
+  const auto settle = [&](int g, int pos0, bool edge, int no_page) {
+    if (edge) {
+      const int from = my_lo - pos0, to = my_hi - pos0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int k = 32 * g + 8 * (i / 4) + 4 * half + i % 4;
+        const bool see = k >= from && k <= to && !(no_page >> (2 * g + i / 8) & 1);
+        sc[g][i] = see ? sc[g][i] : -__builtin_inff();
+      }
+    }
+    float top = sc[g][0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[g][i]);
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top),
+                                                       false, false);
+    top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+    if (__any(top > over)) {
+      const float more = top > over ? top : 0.f;
+      const float down = over < 0.f ? 1.f : exp2_fast(-more * a.scale_log2);
+      over = top > over ? a.slack : over;
+      l *= down;
+#pragma unroll
+      for (int i = 0; i < NB; ++i) o[i] *= down;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        sc[g][i] -= more;
+        below[i] -= more;
+      }
+    }
+  };
+  // the weights of half g
+  f16x8 p[R::PT][2];
+  const auto weigh = [&](int g) {
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      f32x2 w = {exp2_fast(fmaf(sc[g][i], a.scale_log2, kLift)),
+                 exp2_fast(fmaf(sc[g][i + 1], a.scale_log2, kLift))};
+#pragma unroll
+      for (int k = 0; k < R::PT; ++k) {
+        const f16x2 r = __builtin_convertvector(w, f16x2);
+        p[k][i / 8][i % 8] = r[0];
+        p[k][i / 8][i % 8 + 1] = r[1];
+        // the sum of the weights as they are used
+        l = __builtin_amdgcn_fdot2(r, f16x2{1, 1}, l, false);
+        if (k + 1 < R::PT) w -= __builtin_convertvector(r, f32x2);
+      }
+    }
+  };
+  const auto sum = [&](int g, int buf) {
+    const int j16 = lane % 16;
+    const _Float16* base = s.v[buf] + (32 * g + 4 * half + j16 / 4) * R::VS +
+                           16 * (lane / 16 % 2) + 4 * (j16 % 4);
+#pragma unroll
+    for (int d = 0; d < 2; ++d) {
+#pragma unroll
+      for (int blk = 0; blk < NB; ++blk) {
+        struct Both {
+          s16x4 lo, hi;
+        } r;
+        r.lo = turned4(base + 16 * d * R::VS + 32 * blk);
+        r.hi = turned4(base + (16 * d + 8) * R::VS + 32 * blk);
+        const f16x8 v = __builtin_bit_cast(f16x8, r);
+#pragma unroll
+        for (int k = 0; k < R::PT; ++k)
+          o[blk] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[k][d], o[blk], 0, 0, 0);
+      }
+    }
+  };
+
   int page0 = -1, page1 = -1, page2 = -1, coming = -1;  // of the next tiles
   if (part.first < part.end) {
     page0 = page_ok(load_page(part.first));
     if (part.first + 1 < part.end) page1 = page_ok(load_page(part.first + 1));
     if (part.first + 2 < part.end) coming = load_page(part.first + 2);
-    fetch_scales(page0, part.first);
-    fetch_codes(page0, part.first);
-    post_scales(part.first);
+    fetch_values(page0, part.first);
+    fetch_keys(page0, part.first);
+    fill_keys(part.first, 0);
 #pragma unroll
     for (int i = 0; i < R::PER; ++i) rvs[i] = rvs_next[i];
-    fetch_scales(page1, part.first + 1);
-    if (part.first + 1 < part.end) post_scales(part.first + 1);
+    if (part.first + 1 < part.end) {
+      fetch_keys(page1, part.first + 1);
+      fill_keys(part.first + 1, 1);
+    }
     page2 = page_ok(coming);
     __syncthreads();
-    fill(page0, part.first, 0);
+    follow(part.first);
+    fill_values(page0, 0);
+    score(0, 0);
   }
   __syncthreads();
 
+  int slot = 0;  // of the tile's keys
   for (int tile = part.first; tile < part.end; ++tile) {
     const int buf = (tile - part.first) & 1;
     const int pos0 = tile * kKeys;
+    const int slot1 = slot == 2 ? 0 : slot + 1, slot2 = slot1 == 2 ? 0 : slot1 + 1;
     if (tile + 3 < part.end) coming = load_page(tile + 3);
     if (tile + 1 < part.end) {
 #pragma unroll
       for (int i = 0; i < R::PER; ++i) rvs[i] = rvs_next[i];
-      fetch_codes(page1, tile + 1);
-      if (tile + 2 < part.end) fetch_scales(page2, tile + 2);
+      fetch_values(page1, tile + 1);
+      if (tile + 2 < part.end) fetch_keys(page2, tile + 2);
     }
     if (pos0 <= some_hi && pos0 + kKeys > some_lo) {
-      f32x16 sc[2];
-#pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        i32x8 kf[R::FRAGS];
-        int ks[R::FRAGS];
-#pragma unroll
-        for (int f = 0; f < R::FRAGS; ++f) {
-          const int blk = R::EVEN ? 2 * f + half : f;
-          const int at = ((2 * g + col / 16) * NB + blk) * 16 + col % 16;
-          const i32x4 w = *reinterpret_cast<const i32x4*>(s.k[buf] + at * 16);
-          kf[f] = i32x8{w[0], w[1], w[2], w[3], 0, 0, 0, 0};
-          ks[f] = s.ks[buf][at];
-        }
-        sc[g] = below;
-#pragma unroll
-        for (int j = 0; j < R::MMA; ++j)
-          sc[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-              kf[j % R::FRAGS], qo[j], sc[g], 4, 0, 0, ks[j % R::FRAGS], 0, qs[j]);
-      }
       const i32x4 f4 = *reinterpret_cast<const i32x4*>(s.flags[buf]);
-      const int flags = __builtin_amdgcn_readfirstlane(f4[0] | f4[1] | f4[2] | f4[3]);
-      if (pos0 + kKeys - 1 > all_hi || pos0 < all_lo || (flags & kNoPage)) {
-        const int from = my_lo - pos0, to = my_hi - pos0;
-#pragma unroll
-        for (int g = 0; g < 2; ++g)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int k = 32 * g + 8 * (i / 4) + 4 * half + i % 4;
-            const bool see = k >= from && k <= to && !(f4[2 * g + i / 8] & kNoPage);
-            sc[g][i] = see ? sc[g][i] : -__builtin_inff();
-          }
-      }
-      float top = fmaxf(sc[0][0], sc[1][0]);
-#pragma unroll
-      for (int i = 1; i < 16; ++i) top = fmaxf(fmaxf(top, sc[0][i]), sc[1][i]);
-      top = fmaxf(top, __shfl_xor(top, 32));
-      if (__any(top > over)) {
-        const float more = top > over ? top : 0.f;
-        const float down = over < 0.f ? 1.f : exp2_fast(-more * a.scale_log2);
-        over = top > over ? a.slack : over;
-        l *= down;
-#pragma unroll
-        for (int i = 0; i < NB; ++i) o[i] *= down;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          sc[0][i] -= more;
-          sc[1][i] -= more;
-          below[i] -= more;
-        }
-      }
-#pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        f16x8 p[R::PT][2];
-#pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-          f32x2 w = {exp2_fast(fmaf(sc[g][i], a.scale_log2, kLift)),
-                     exp2_fast(fmaf(sc[g][i + 1], a.scale_log2, kLift))};
-#pragma unroll
-          for (int k = 0; k < R::PT; ++k) {
-            const f16x2 r = __builtin_convertvector(w, f16x2);
-            p[k][i / 8][i % 8] = r[0];
-            p[k][i / 8][i % 8 + 1] = r[1];
-            // the sum of the weights as they are used
-            l = __builtin_amdgcn_fdot2(r, f16x2{1, 1}, l, false);
-            if (k + 1 < R::PT) w -= __builtin_convertvector(r, f32x2);
-          }
-        }
-        const int j16 = lane % 16;
-        const _Float16* base = s.v[buf] + (32 * g + 4 * half + j16 / 4) * R::VS +
-                               16 * (lane / 16 % 2) + 4 * (j16 % 4);
-#pragma unroll
-        for (int blk = 0; blk < NB; ++blk) {
-#pragma unroll
-          for (int d = 0; d < 2; ++d) {
-            struct Both {
-              s16x4 lo, hi;
-            } r;
-            r.lo = turned4(base + 16 * d * R::VS + 32 * blk);
-            r.hi = turned4(base + (16 * d + 8) * R::VS + 32 * blk);
-            const f16x8 v = __builtin_bit_cast(f16x8, r);
-#pragma unroll
-            for (int k = 0; k < R::PT; ++k)
-              o[blk] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[k][d], o[blk], 0, 0, 0);
-          }
-        }
-      }
-      if (flags & kNotFinite) {  // a block that is not finite, to the rows that see its token
+      const int flags = __builtin_amdgcn_readfirstlane(f4[0] | f4[1] << 2 | f4[2] << 4 | f4[3] << 6);
+      const int no_page = (flags & 1) | (flags >> 1 & 2) | (flags >> 2 & 4) | (flags >> 3 & 8);
+      const bool edge = pos0 + kKeys - 1 > all_hi || pos0 < all_lo || no_page;
+      settle(0, pos0, edge, no_page);
+      // the next half's scores beside these weights
+      score(1, slot);
+      weigh(0);
+      sum(0, buf);
+      settle(1, pos0, edge, no_page);
+      score(0, slot1);  // past the last tile: whatever is there, and not used
+      weigh(1);
+      sum(1, buf);
+      if (flags & 0xaa) {  // a block that is not finite, to the rows that see its token
         for (int c = 0; c < kSubs * R::CHUNKS; ++c) {
           if (s.vs[buf][c] != 255) continue;
           const int sub = c / R::CHUNKS, blk = c % R::CHUNKS / 16;
           const int pos = pos0 + sub * 16 + c % 16;
-          const bool see = pos >= my_lo && pos <= my_hi && !(s.flags[buf][sub] & kNoPage);
+          const bool see = pos >= my_lo && pos <= my_hi && !(no_page >> sub & 1);
           const float nan = see ? __builtin_nanf("") : 0.f;
 #pragma unroll
           for (int i = 0; i < NB; ++i)
@@ -374,13 +401,17 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
               for (int k = 0; k < 16; ++k) o[i][k] += nan;
         }
       }
+    } else if (tile + 1 < part.end) {
+      score(0, slot1);
     }
     if (tile + 1 < part.end) {
-      fill(page1, tile + 1, buf ^ 1);
-      if (tile + 2 < part.end) post_scales(tile + 2);
+      follow(tile + 1);
+      fill_values(page1, buf ^ 1);
+      if (tile + 2 < part.end) fill_keys(tile + 2, slot2);
       page1 = page2;
       page2 = page_ok(coming);
     }
+    slot = slot1;
     __syncthreads();
   }
 
