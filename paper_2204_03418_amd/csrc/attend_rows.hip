@@ -40,9 +40,9 @@ struct RowsLds {
   using R = Rows<T, NB>;
   alignas(16) uint8_t k[3][kSubs * R::CHUNKS * 16];  // by tile modulo 3, the others modulo 2
   alignas(16) _Float16 v[2][kKeys * R::VS];
-  uint8_t ks[3][kSubs * R::CHUNKS], vs[2][kSubs * R::CHUNKS];
+  uint8_t ks[3][kSubs * R::CHUNKS];
+  alignas(16) uint8_t vs[4][kSubs * R::CHUNKS];  // by tile modulo 4, 0 of keys not the stream's
   alignas(16) int32_t flags[2][kSubs];
-  alignas(16) int32_t top[4][kSubs];  // the largest scale of the values, by tile modulo 4
 };
 
 template <typename T, int NB>
@@ -132,10 +132,11 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
   }
 
   // The keys' way: pages three tiles ahead, codes of keys and scales of values two, codes of values
-  // one.  A wave brings 16 of a tile's tokens, from one page.
+  // one.  A wave brings 16 of a tile's tokens, from one page: nothing of them is read out of
+  // a page's range, and without a page they are 0.
   const char* pool = static_cast<const char*>(a.c.pool) + int64_t(kv) * a.lay.bytes();
   const int32_t* table = a.c.table + int64_t(b) * a.d.stream_pages;
-  const int sub_mask = a.lay.P / kCacheTile - 1;
+  const int sub_mask = a.lay.P / kCacheTile - 1, head_bytes = a.lay.bytes();
   const auto load_page = [&](int tile) {
     const int lp = (tile * kSubs + wave) >> (a.page_shift - 4);
     return table[lp - fdiv(lp, a.by_W) * a.d.stream_pages];
@@ -144,55 +145,61 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
     p = __builtin_amdgcn_readfirstlane(p);
     return p >= 0 && p < a.d.pages ? p : -1;
   };
-  // `part` of the page, for this wave's 16 tokens of the tile
-  const auto place = [&](int page, int tile, int part, int bytes) {
-    return pool + page * a.page_bytes + part + ((tile * kSubs + wave) & sub_mask) * bytes;
+  const auto page_rsrc = [&](int page) {
+    return make_rsrc(pool + max(page, 0) * a.page_bytes, page < 0 ? 0 : head_bytes);
   };
+  // which 16 tokens of the page are this wave's of the tile
+  const auto place = [&](int tile) { return (tile * kSubs + wave) & sub_mask; };
+  int at16[R::PER], at1[R::PER];  // this lane's bytes of 16 tokens' codes and scales
+#pragma unroll
+  for (int i = 0; i < R::PER; ++i) {
+    const int c = lane + 64 * i;
+    at16[i] = c < R::CHUNKS ? c * 16 : kOutOfRange;
+    at1[i] = c < R::CHUNKS ? c : kOutOfRange;
+  }
   const int hi = span.base + span.n;
   i32x4 rk[R::PER], rv[R::PER];
   int rks[R::PER], rvs[R::PER], rvs_next[R::PER];
   const auto fetch_keys = [&](int page, int tile) {  // and the values' scales
+    const auto r = page_rsrc(page);
+    const int n = place(tile);
 #pragma unroll
     for (int i = 0; i < R::PER; ++i) {
-      const int c = lane + 64 * i;
-      rk[i] = i32x4{0, 0, 0, 0};
-      rks[i] = 127;
-      rvs_next[i] = 0;
-      if (page >= 0 && c < R::CHUNKS) {
-        rk[i] = *reinterpret_cast<const i32x4*>(
-            place(page, tile, a.lay.codes(0), R::CHUNKS * 16) + c * 16);
-        rks[i] = uint8_t(place(page, tile, a.lay.scales(0), R::CHUNKS)[c]);
-        rvs_next[i] = uint8_t(place(page, tile, a.lay.scales(1), R::CHUNKS)[c]);
-      }
+      rk[i] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                            r, at16[i], n * (R::CHUNKS * 16), 0));
+      rks[i] = uint8_t(__builtin_amdgcn_raw_buffer_load_b8(
+          r, at1[i], a.lay.scales(0) + n * R::CHUNKS, 0));
+      rvs_next[i] = uint8_t(__builtin_amdgcn_raw_buffer_load_b8(
+          r, at1[i], a.lay.scales(1) + n * R::CHUNKS, 0));
     }
   };
   const auto fetch_values = [&](int page, int tile) {
+    const auto r = page_rsrc(page);
+    const int n = place(tile);
+#pragma unroll
+    for (int i = 0; i < R::PER; ++i)
+      rv[i] = __builtin_bit_cast(
+          i32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                     r, at16[i], a.lay.codes(1) + n * (R::CHUNKS * 16), 0));
+  };
+  // The keys and the values' scales into LDS: the scales of the stream's own tokens, what else a
+  // page holds may be anything.
+  const auto fill_keys = [&](int tile, int slot) {
+    const int pos0 = tile * kKeys + wave * kCacheTile;
+    if (pos0 < span.lowest || pos0 + kCacheTile > hi) {
+      const int tok = lane % 16;
+#pragma unroll
+      for (int i = 0; i < R::PER; ++i)
+        rvs_next[i] = tok >= span.lowest - pos0 && tok < hi - pos0 ? rvs_next[i] : 0;
+    }
 #pragma unroll
     for (int i = 0; i < R::PER; ++i) {
       const int c = lane + 64 * i;
-      rv[i] = i32x4{0, 0, 0, 0};
-      if (page >= 0 && c < R::CHUNKS)
-        rv[i] = *reinterpret_cast<const i32x4*>(
-            place(page, tile, a.lay.codes(1), R::CHUNKS * 16) + c * 16);
-    }
-  };
-  // The keys into LDS, and the largest of the values' scales: of the stream's own tokens, what else
-  // a page holds may be anything.
-  const auto fill_keys = [&](int tile, int slot) {
-    const int pos0 = tile * kKeys + wave * kCacheTile;
-    const int from = span.lowest - pos0, to = hi - pos0;
-    int top = 0;
-#pragma unroll
-    for (int i = 0; i < R::PER; ++i) {
-      const int c = lane + 64 * i, tok = lane % 16;
-      rvs_next[i] = tok >= from && tok < to ? rvs_next[i] : 0;
-      top = max(top, rvs_next[i] == 255 ? 0 : rvs_next[i]);
       if (c >= R::CHUNKS) break;
       *reinterpret_cast<i32x4*>(s.k[slot] + (wave * R::CHUNKS + c) * 16) = rk[i];
       s.ks[slot][wave * R::CHUNKS + c] = uint8_t(rks[i]);
+      s.vs[tile & 3][wave * R::CHUNKS + c] = uint8_t(rvs_next[i]);
     }
-    top = wave_max(top);
-    if (lane == 0) s.top[tile & 3][wave] = top;
   };
 
   f32x16 o[NB];
@@ -211,11 +218,10 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
     for (int i = 0; i < R::PER; ++i) {
       const int c = lane + 64 * i;
       if (c >= R::CHUNKS) break;
-      s.vs[buf][wave * R::CHUNKS + c] = uint8_t(rvs[i]);
-      const bool no = rvs[i] == 255;
-      bad |= no;
-      // a scale of 0 is far below any other
-      const float scale = exponent_to_f32(no || rvs[i] == 0 ? 0 : 127 + rvs[i] - E + kValueLift);
+      bad |= rvs[i] == 255;
+      // without a scale: 0
+      const int e = max(127 + kValueLift + rvs[i] - E, 0);
+      const float scale = __uint_as_float(uint32_t(rvs[i] == 0 || rvs[i] == 255 ? 0 : e) << 23);
       _Float16* dst = s.v[buf] + (wave * kCacheTile + c % 16) * R::VS + c / 16 * 32;
       f16x8 w[2];
       decode16(rv[i][0], rv[i][1], scale, w);
@@ -230,10 +236,33 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
   };
   // the values' exponent for a tile; the sums follow it
   const auto follow = [&](int tile) {
-    const i32x4 t4 = *reinterpret_cast<const i32x4*>(s.top[tile & 3]);
-    const int top = __builtin_amdgcn_readfirstlane(max(max(t4[0], t4[1]), max(t4[2], t4[3])));
-    if (top <= E) return;
-    const int next = top + kValueSlack;
+    constexpr int WORDS = kSubs * R::CHUNKS / 4;  // of scales
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 top = {0, 0};
+#pragma unroll
+    for (int i = 0; i < (WORDS + 63) / 64; ++i) {
+      const int w = lane + 64 * i;
+      const uint32_t v =
+          reinterpret_cast<const uint32_t*>(s.vs[tile & 3])[WORDS % 64 ? min(w, WORDS - 1) : w];
+      top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, v & 0xff00ffu));
+      top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, v >> 8 & 0xff00ffu));
+    }
+    if (!__any(max(top[0], top[1]) > E)) return;
+    int most = 0;  // but for those that are not finite
+#pragma unroll
+    for (int i = 0; i < (WORDS + 63) / 64; ++i) {
+      const int w = lane + 64 * i;
+      const uint32_t v =
+          reinterpret_cast<const uint32_t*>(s.vs[tile & 3])[WORDS % 64 ? min(w, WORDS - 1) : w];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int e = v >> (8 * k) & 255;
+        most = max(most, e == 255 ? 0 : e);
+      }
+    }
+    most = wave_max(most);
+    if (most <= E) return;
+    const int next = most + kValueSlack;
     if (E) {
       const float down = exponent_to_f32(127 + E - next);
 #pragma unroll
@@ -252,9 +281,7 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
 
   // scores of 32 keys, half g of the tile in `slot`
   f32x16 sc[2];
-  const auto score = [&](int g, int slot) {
-    i32x8 kf[R::FRAGS];
-    int ks[R::FRAGS];
+  const auto load_keys = [&](int g, int slot, i32x8 (&kf)[R::FRAGS], int (&ks)[R::FRAGS]) {
 #pragma unroll
     for (int f = 0; f < R::FRAGS; ++f) {
       const int blk = R::EVEN ? 2 * f + half : f;
@@ -263,6 +290,11 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
       kf[f] = i32x8{w[0], w[1], w[2], w[3], 0, 0, 0, 0};
       ks[f] = s.ks[slot][at];
     }
+  };
+  const auto score = [&](int g, int slot) {
+    i32x8 kf[R::FRAGS];
+    int ks[R::FRAGS];
+    load_keys(g, slot, kf, ks);
     sc[g] = below;
 #pragma unroll
     for (int j = 0; j < R::MMA; ++j)
@@ -300,11 +332,26 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
       }
     }
   };
-  // the weights of half g
-  f16x8 p[R::PT][2];
-  const auto weigh = [&](int g) {
-#pragma unroll
-    for (int i = 0; i < 16; i += 2) {
+  // The weights of half g and what they add, beside the scores of half `other` of the tile in `slot`:
+  // a matrix instruction of the scores, then a part of the weights, which take the vector unit
+  // about as long as it takes the matrix unit.
+  const auto advance = [&](int g, int buf, int other, int slot) {
+    i32x8 kf[R::FRAGS];
+    int ks[R::FRAGS];
+    load_keys(other, slot, kf, ks);
+    const int j16 = lane % 16;
+    const _Float16* base = s.v[buf] + (32 * g + 4 * half + j16 / 4) * R::VS +
+                           16 * (lane / 16 % 2) + 4 * (j16 % 4);
+    const auto values = [&](int d, int blk) {
+      struct Both {
+        s16x4 lo, hi;
+      } r;
+      r.lo = turned4(base + 16 * d * R::VS + 32 * blk);
+      r.hi = turned4(base + (16 * d + 8) * R::VS + 32 * blk);
+      return __builtin_bit_cast(f16x8, r);
+    };
+    f16x8 p[R::PT][2];
+    const auto weigh = [&](int i) {  // weights i and i + 1
       f32x2 w = {exp2_fast(fmaf(sc[g][i], a.scale_log2, kLift)),
                  exp2_fast(fmaf(sc[g][i + 1], a.scale_log2, kLift))};
 #pragma unroll
@@ -316,27 +363,26 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
         l = __builtin_amdgcn_fdot2(r, f16x2{1, 1}, l, false);
         if (k + 1 < R::PT) w -= __builtin_convertvector(r, f32x2);
       }
-    }
-  };
-  const auto sum = [&](int g, int buf) {
-    const int j16 = lane % 16;
-    const _Float16* base = s.v[buf] + (32 * g + 4 * half + j16 / 4) * R::VS +
-                           16 * (lane / 16 % 2) + 4 * (j16 % 4);
+    };
+    sc[other] = below;
 #pragma unroll
-    for (int d = 0; d < 2; ++d) {
+    for (int j = 0; j < R::MMA; ++j) {
+      sc[other] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+          kf[j % R::FRAGS], qo[j], sc[other], 4, 0, 0, ks[j % R::FRAGS], 0, qs[j]);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 8 * j / R::MMA; i < 8 * (j + 1) / R::MMA; ++i) weigh(2 * i);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int d = 0; d < 2; ++d)
 #pragma unroll
       for (int blk = 0; blk < NB; ++blk) {
-        struct Both {
-          s16x4 lo, hi;
-        } r;
-        r.lo = turned4(base + 16 * d * R::VS + 32 * blk);
-        r.hi = turned4(base + (16 * d + 8) * R::VS + 32 * blk);
-        const f16x8 v = __builtin_bit_cast(f16x8, r);
+        const f16x8 v = values(d, blk);
 #pragma unroll
         for (int k = 0; k < R::PT; ++k)
           o[blk] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[k][d], o[blk], 0, 0, 0);
       }
-    }
   };
 
   int page0 = -1, page1 = -1, page2 = -1, coming = -1;  // of the next tiles
@@ -349,21 +395,19 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
     fill_keys(part.first, 0);
 #pragma unroll
     for (int i = 0; i < R::PER; ++i) rvs[i] = rvs_next[i];
-    if (part.first + 1 < part.end) {
-      fetch_keys(page1, part.first + 1);
-      fill_keys(part.first + 1, 1);
-    }
+    fetch_keys(page1, part.first + 1);
+    fill_keys(part.first + 1, 1);
     page2 = page_ok(coming);
     __syncthreads();
     follow(part.first);
-    fill_values(page0, 0);
+    fill_values(page0, part.first & 1);
     score(0, 0);
   }
   __syncthreads();
 
   int slot = 0;  // of the tile's keys
   for (int tile = part.first; tile < part.end; ++tile) {
-    const int buf = (tile - part.first) & 1;
+    const int buf = tile & 1;
     const int pos0 = tile * kKeys;
     const int slot1 = slot == 2 ? 0 : slot + 1, slot2 = slot1 == 2 ? 0 : slot1 + 1;
     if (tile + 3 < part.end) coming = load_page(tile + 3);
@@ -379,17 +423,12 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
       const int no_page = (flags & 1) | (flags >> 1 & 2) | (flags >> 2 & 4) | (flags >> 3 & 8);
       const bool edge = pos0 + kKeys - 1 > all_hi || pos0 < all_lo || no_page;
       settle(0, pos0, edge, no_page);
-      // the next half's scores beside these weights
-      score(1, slot);
-      weigh(0);
-      sum(0, buf);
+      advance(0, buf, 1, slot);
       settle(1, pos0, edge, no_page);
-      score(0, slot1);  // past the last tile: whatever is there, and not used
-      weigh(1);
-      sum(1, buf);
+      advance(1, buf, 0, slot1);  // past the last tile: whatever is there, and not used
       if (flags & 0xaa) {  // a block that is not finite, to the rows that see its token
         for (int c = 0; c < kSubs * R::CHUNKS; ++c) {
-          if (s.vs[buf][c] != 255) continue;
+          if (s.vs[tile & 3][c] != 255) continue;
           const int sub = c / R::CHUNKS, blk = c % R::CHUNKS / 16;
           const int pos = pos0 + sub * 16 + c % 16;
           const bool see = pos >= my_lo && pos <= my_hi && !(no_page >> sub & 1);
