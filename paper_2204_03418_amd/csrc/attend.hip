@@ -7,44 +7,60 @@ namespace coinf {
 
 namespace {
 
-// Joins the parts of a row: a wave a row.
+// Joins the parts of a row: four values a lane, `lanes` (a power of two, 4 lanes >= width) a row.
 template <typename T>
 __global__ __launch_bounds__(kBlock) void attend_join_kernel(AttendArgs a, int rows_of, int width,
-                                                             int64_t all_rows) {
-  const int64_t r = int64_t(blockIdx.x) * (kBlock / 64) + threadIdx.x / 64;
+                                                             int lanes, int64_t all_rows) {
+  const int64_t r = (int64_t(blockIdx.x) * kBlock + threadIdx.x) / lanes;
   if (r >= all_rows) return;
-  const int lane = threadIdx.x % 64;
-  const int64_t unit = r / rows_of;
-  const int in = int(r - unit * rows_of);
-  const int pair = fdiv(int(unit), a.by_row_tiles), rt = int(unit) - pair * a.row_tiles;
+  const int ch = int(threadIdx.x) % lanes * 4;
+  const int unit = int(r / rows_of), in = int(r - int64_t(unit) * rows_of);
+  const int pair = fdiv(unit, a.by_row_tiles), rt = unit - pair * a.row_tiles;
   const int b = fdiv(pair, a.by_kv), kv = pair - b * a.d.kv_heads;
   const Span span(a, b);
   const int rows = span.n * a.group, row0 = rt * rows_of, row = row0 + in;
-  if (row >= rows) return;
+  if (row >= rows || ch >= width) return;
   const int t = fdiv(row, a.by_group), head = kv * a.group + row - t * a.group;
   const int t_last = fdiv(min(row0 + rows_of, rows) - 1, a.by_group);
-  const Part part(span.lo(a, fdiv(row0, a.by_group)), span.base + t_last + 1, a.splits, 0);
+  const Part part(span.lo(a, fdiv(row0, a.by_group)), span.base + t_last + 1, a.keys, a.splits, 0);
   if (part.parts == 1) return;
-  const int64_t at = unit * a.splits * rows_of + in;
-  float top = -__builtin_inff();
-  for (int s = 0; s < part.parts; ++s) top = fmaxf(top, a.part_stat[at + int64_t(s) * rows_of].x);
-  float sum = 0.f, v[4] = {};
-  for (int s = 0; s < part.parts; ++s) {
-    const int64_t i = at + int64_t(s) * rows_of;
-    const float2 stat = a.part_stat[i];
-    if (stat.y == 0.f) continue;  // sees nothing there
-    const float w = exp2_fast((stat.x - top) * a.scale_log2) * stat.y;
-    sum += w;
+  const int64_t at = int64_t(unit) * a.splits * rows_of + in;
+  // eight parts on their way at a time
+  constexpr int AHEAD = 8;
+  float top = -__builtin_inff(), sum = 0.f, v[4] = {};
+  for (int s0 = 0; s0 < part.parts; s0 += AHEAD) {
+    float2 stat[AHEAD];
+    Pack<float, 4> x[AHEAD];
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (lane + 64 * k < width) v[k] = fmaf(w, a.part[i * width + lane + 64 * k], v[k]);
+    for (int s = 0; s < AHEAD; ++s) {
+      const int64_t i = at + int64_t(min(s0 + s, part.parts - 1)) * rows_of;
+      stat[s] = a.part_stat[i];
+      if (s0 + s >= part.parts) stat[s].y = 0.f;
+      x[s] = load_pack<float, 4>(a.part + i * width + ch);
+    }
+    float next = top;
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s) next = stat[s].y == 0.f ? next : fmaxf(next, stat[s].x);
+    const float down = top == next ? 1.f : exp2_fast((top - next) * a.scale_log2);
+    sum *= down;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] *= down;
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s) {
+      if (stat[s].y == 0.f) continue;  // sees nothing there
+      const float w = exp2_fast((stat[s].x - next) * a.scale_log2) * stat[s].y;
+      sum += w;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = fmaf(w, x[s].v[k], v[k]);
+    }
+    top = next;
   }
   T* y = static_cast<T*>(a.y.data) + b * a.y.batch_stride + t * a.y.token_stride +
          int64_t(head) * a.d.head_dim;
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (lane + 64 * k < a.d.head_dim) y[lane + 64 * k] = from_f32<T>(v[k] * inv);
+  for (int k = 0; k < 4; ++k) v[k] *= inv;
+  store4<T>(y, ch, a.d.head_dim, a.wide, v);
 }
 
 // How the rows of a call are cut.
@@ -59,13 +75,18 @@ Cut cut_of(const co_attn_desc& d, int32_t T) {
   Cut c;
   c.pairs = int64_t(d.batch) * d.kv_heads;
   const int64_t rows = int64_t(T) * (d.heads / d.kv_heads);
-  c.few = rows <= kFewTiles * 16 ? int((rows + 15) / 16) : 0;
-  c.rows = c.few ? c.few * 16 : kRows;
-  c.row_tiles = (rows + c.rows - 1) / c.rows;
   const int64_t keys = std::min<int64_t>(int64_t(d.stream_pages) * d.page_tokens,
-                                         d.window ? int64_t(d.window) + T + kKeys : INT64_MAX);
-  const int64_t parts = (keys + kKeys * kMinTiles - 1) / (kKeys * kMinTiles);
-  c.splits = std::max<int64_t>(1, std::min<int64_t>((c.few ? 1024 : 512) / c.units(), parts));
+                                         d.window ? int64_t(d.window) + T + kMostKeys : INT64_MAX);
+  c.few = rows <= kFewTiles * 16 ? int((rows + 15) / 16) : 0;
+  // 256 rows go over 128 keys in 3.9 us, two workgroups of 128 in 4.4 us, but nothing runs beside
+  // the start and end of the former: they take more than 6000 keys or so to be made up for
+  // (512 tokens over 32768: 258 and 291 us; 4 prompts of 4096: 593 and 574)
+  const int most = d.dtype == CO_BF16 ? kWideBlocks<bf16_t> : kWideBlocks<float>;
+  c.rows = c.few ? c.few * 16 : rows > 128 && keys >= 8192 && cache_blocks(d.head_dim) <= most
+                                    ? 256 : 128;
+  c.row_tiles = (rows + c.rows - 1) / c.rows;
+  const int64_t parts = (keys + kPartKeys - 1) / kPartKeys;
+  c.splits = std::max<int64_t>(1, std::min<int64_t>((c.few ? 1024 : c.rows == 128 ? 512 : 256) / c.units(), parts));
   return c;
 }
 
@@ -90,7 +111,7 @@ hipError_t launch_attend(const co_attn_desc& d, const co_attn_cache& cache, cons
   a.slack = kSlack / a.scale_log2;
   a.group = d.heads / d.kv_heads;
   const Cut c = cut_of(d, T);
-  if (int64_t(T) * a.group + kRows >= INT32_MAX || c.units() * c.splits >= 1 << 24 ||
+  if (int64_t(T) * a.group + c.rows >= INT32_MAX || c.units() * c.splits >= 1 << 24 ||
       c.units() * c.rows / 4 >= 1 << 24)
     return hipErrorInvalidConfiguration;
   a.by_group = make_fastdiv(a.group);
@@ -100,6 +121,7 @@ hipError_t launch_attend(const co_attn_desc& d, const co_attn_cache& cache, cons
   a.pairs = int32_t(c.pairs);
   a.row_tiles = int32_t(c.row_tiles);
   a.splits = int32_t(c.splits);
+  a.keys = c.few ? kFewKeys : int32_t(c.rows / 2);
   a.by_row_tiles = make_fastdiv(a.row_tiles);
   a.by_splits = make_fastdiv(a.splits);
   const int es = d.dtype == CO_BF16 ? 2 : 4;
@@ -113,14 +135,16 @@ hipError_t launch_attend(const co_attn_desc& d, const co_attn_cache& cache, cons
   if (c.few)
     launch_attend_few(a, NB, c.few, stream);
   else
-    launch_attend_rows(a, NB, stream);
+    launch_attend_rows(a, NB, int(c.rows), stream);
   if (a.splits > 1) {
     const int64_t rows = c.units() * c.rows;
-    const unsigned grid = unsigned((rows + 3) / 4);
+    const int lanes = NB <= 1 ? 8 : NB <= 2 ? 16 : NB <= 4 ? 32 : 64;
+    const unsigned grid = unsigned((rows * lanes + kBlock - 1) / kBlock);
     if (d.dtype == CO_BF16)
-      attend_join_kernel<bf16_t><<<grid, kBlock, 0, stream>>>(a, int(c.rows), NB * 32, rows);
+      attend_join_kernel<bf16_t>
+          <<<grid, kBlock, 0, stream>>>(a, int(c.rows), NB * 32, lanes, rows);
     else
-      attend_join_kernel<float><<<grid, kBlock, 0, stream>>>(a, int(c.rows), NB * 32, rows);
+      attend_join_kernel<float><<<grid, kBlock, 0, stream>>>(a, int(c.rows), NB * 32, lanes, rows);
   }
   return hipGetLastError();
 }

@@ -36,14 +36,15 @@ struct AttendArgs {
   FastDiv by_row_tiles, by_splits, by_kv;
   int32_t pairs;       // streams * kv heads
   int32_t splits;      // parts of a unit's keys at most
+  int32_t keys;        // of a tile
   int32_t wide;        // q and y in pieces of 16 bytes
   float* part;         // (units, splits, rows, NB * 32) values, then (.., rows) reference score and sum
   float2* part_stat;
 };
 
-// Keys: tokens of a tile, the least tiles of a part.
-constexpr int kKeys = 64;
-constexpr int kMinTiles = 4;
+// Keys of a tile at most, and of a part at least.
+constexpr int kMostKeys = 128;
+constexpr int kPartKeys = 256;
 
 // Weights are 2^{x + kLift}, x <= kSlack over the row's reference: 2^15, below 16-bit floats' highest.
 // Their least step is 2^-24, 2^-35 of the row's reference.
@@ -57,7 +58,7 @@ struct Span {
   int lowest;
   __device__ Span(const AttendArgs& a, int b) : base(a.c.base[b]) {
     // positions stay below 2^31
-    n = base < 0 ? 0 : min(stream_tokens(a.c.granted, b, a.T), INT32_MAX - 2 * kKeys - base);
+    n = base < 0 ? 0 : min(stream_tokens(a.c.granted, b, a.T), INT32_MAX - 4 * kMostKeys - base);
     n = max(n, 0);
     lowest = a.c.first ? max(a.c.first[b], 0) : 0;
   }
@@ -68,12 +69,13 @@ struct Span {
   }
 };
 
-// Tiles first..end - 1 of a unit's part `split` of the keys lo..hi - 1; parts: of the unit.
+// Tiles first..end - 1, of `keys` each, of a unit's part `split` of the keys lo..hi - 1; parts: of
+// the unit.
 struct Part {
   int first, end, parts;
-  __device__ Part(int lo, int hi, int splits, int split) {
-    const int t0 = lo / kKeys, t1 = lo < hi ? (hi + kKeys - 1) / kKeys : t0;
-    const int each = max((t1 - t0 + splits - 1) / splits, kMinTiles);
+  __device__ Part(int lo, int hi, int keys, int splits, int split) {
+    const int t0 = lo / keys, t1 = lo < hi ? (hi + keys - 1) / keys : t0;
+    const int each = max((t1 - t0 + splits - 1) / splits, kPartKeys / keys);
     parts = max((t1 - t0 + each - 1) / each, 1);
     first = min(t0 + split * each, t1);
     end = min(first + each, t1);
@@ -160,17 +162,13 @@ constexpr int kQueryTerms = sizeof(T) == 2 ? 2 : 6;
 template <typename T>
 constexpr int kWeightTerms = sizeof(T) == 2 ? 1 : 2;
 
-// Sixteen codes as 16-bit floats times 2^{s - E + kValueLift}.
-__device__ __forceinline__ void decode16(uint32_t lo, uint32_t hi, float scale, f16x8 (&o)[2]) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const uint32_t w = i ? hi : lo;
-    const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 0);
-    const f16x2 b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 1);
-    const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 2);
-    const f16x2 d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 3);
-    o[i] = f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-  }
+// Eight codes as 16-bit floats, times the scale.
+__device__ __forceinline__ f16x8 decode8(uint32_t w, float scale) {
+  const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 0);
+  const f16x2 b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 1);
+  const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 2);
+  const f16x2 d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 3);
+  return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
 // Four rows of 16 columns of an LDS tile of 16-bit values, turned: lane j of 16 gets column j.
@@ -182,10 +180,12 @@ __device__ __forceinline__ s16x4 turned4(const _Float16* p) {
 
 
 // Calls of at most kFewTiles * 16 rows, in column tiles of 16.
-constexpr int kFewTiles = 2;
+constexpr int kFewTiles = 2, kFewKeys = 64;
 void launch_attend_few(const AttendArgs& a, int NB, int tiles, hipStream_t stream);
-// The others.
-void launch_attend_rows(const AttendArgs& a, int NB, hipStream_t stream);
-constexpr int kRows = 128;  // of a workgroup
+// The others, 128 or 256 rows a workgroup: 256 for heads of at most so many blocks (whose queries and
+// sums leave registers for two waves a SIMD).
+template <typename T>
+constexpr int kWideBlocks = sizeof(T) == 2 ? 4 : 2;
+void launch_attend_rows(const AttendArgs& a, int NB, int rows, hipStream_t stream);
 
 }  // namespace coinf

@@ -65,7 +65,7 @@ __global__ __launch_bounds__(kBlock) void attend_few_kernel(AttendArgs a) {
       store4<T>(out_row(rows + i / (NB * 8)), i % (NB * 8) * 4, a.d.head_dim, a.wide, none);
   }
   if (rows == 0) return;
-  const Part part(span.lo(a, 0), span.base + span.n, a.splits, split);
+  const Part part(span.lo(a, 0), span.base + span.n, a.keys, a.splits, split);
   if (split >= part.parts) return;
 
   // queries, as 8-bit terms
@@ -214,8 +214,8 @@ __global__ __launch_bounds__(kBlock) void attend_few_kernel(AttendArgs a) {
     my_hi[c] = row < rows ? span.base + t : -1;
   }
   _Float16* vbuf = lds[wave].v;
-  const int end = min(part.end * 2, (hi + kStep - 1) / kStep);
-  int step = part.first * 2 + wave;
+  const int end = min(part.end * (kFewKeys / kStep), (hi + kStep - 1) / kStep);
+  int step = part.first * (kFewKeys / kStep) + wave;
   if (step < end) {
     fetch_pages(step);
     fetch(step);
@@ -269,13 +269,8 @@ __global__ __launch_bounds__(kBlock) void attend_few_kernel(AttendArgs a) {
       if (c >= F::CHUNKS) break;
       const float scale = vs[i] ? exponent_to_f32(127 + vs[i] - E + kValueLift) : 0.f;
       _Float16* dst = vbuf + (tile * 16 + rest % 16) * F::VS + rest / 16 * 32;
-      f16x8 w[2];
-      decode16(rv[i][0], rv[i][1], scale, w);
-      *reinterpret_cast<f16x8*>(dst) = w[0];
-      *reinterpret_cast<f16x8*>(dst + 8) = w[1];
-      decode16(rv[i][2], rv[i][3], scale, w);
-      *reinterpret_cast<f16x8*>(dst + 16) = w[0];
-      *reinterpret_cast<f16x8*>(dst + 24) = w[1];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) *reinterpret_cast<f16x8*>(dst + 8 * k) = decode8(rv[i][k], scale);
     }
     int raw[F::VC];
 #pragma unroll

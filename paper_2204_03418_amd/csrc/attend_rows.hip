@@ -16,11 +16,10 @@ namespace coinf {
 
 namespace {
 
-constexpr int kSubs = kKeys / kCacheTile;  // tiles of the pages in one of keys: a wave each
-static_assert(kSubs == kBlock / 64);
-
-template <typename T, int NB>
+// A workgroup of W waves: 32 W rows, 16 W keys a tile (a wave brings 16 of them).
+template <typename T, int NB, int W>
 struct Rows {
+  static constexpr int KEYS = kCacheTile * W, HALVES = KEYS / 32;
   static constexpr int QT = kQueryTerms<T>, PT = kWeightTerms<T>;
   static constexpr bool EVEN = NB % 2 == 0;
   static constexpr int MMA = QT * NB / 2;           // of a 32 x 32 tile of scores, depth 64
@@ -33,22 +32,26 @@ struct Rows {
   static __device__ int block(int j, int h) { return EVEN ? 2 * j % NB + h : j % NB; }
 };
 
+// Has v made by here.
+__device__ __forceinline__ void hold(float& v) { asm volatile("" : "+v"(v)); }
+
 constexpr int kNoPage = 1, kNotFinite = 2;  // flags of 16 tokens
 
-template <typename T, int NB>
+template <typename T, int NB, int W>
 struct RowsLds {
-  using R = Rows<T, NB>;
-  alignas(16) uint8_t k[3][kSubs * R::CHUNKS * 16];  // by tile modulo 3, the others modulo 2
-  alignas(16) _Float16 v[2][kKeys * R::VS];
-  uint8_t ks[3][kSubs * R::CHUNKS];
-  alignas(16) uint8_t vs[4][kSubs * R::CHUNKS];  // by tile modulo 4, 0 of keys not the stream's
-  alignas(16) int32_t flags[2][kSubs];
+  using R = Rows<T, NB, W>;
+  alignas(16) uint8_t k[3][W * R::CHUNKS * 16];  // by tile modulo 3, the others modulo 2
+  alignas(16) _Float16 v[2][R::KEYS * R::VS];
+  uint8_t ks[3][W * R::CHUNKS];
+  alignas(16) uint8_t vs[4][W * R::CHUNKS];  // by tile modulo 4, 0 of keys not the stream's
+  int32_t flags[4][W];           // by tile modulo 4
 };
 
-template <typename T, int NB>
-__global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(AttendArgs a) {
-  using R = Rows<T, NB>;
-  __shared__ RowsLds<T, NB> s;
+template <typename T, int NB, int W>
+__global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_rows_kernel(AttendArgs a) {
+  using R = Rows<T, NB, W>;
+  constexpr int kRows = 32 * W, kKeys = R::KEYS;
+  __shared__ RowsLds<T, NB, W> s;
   const int tid = threadIdx.x, lane = tid % 64, col = lane % 32, half = lane / 32;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
 
@@ -88,7 +91,7 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
     return;
   }
   const int t_last = fdiv(min(row0 + kRows, rows) - 1, a.by_group);
-  const Part part(span.lo(a, fdiv(row0, a.by_group)), span.base + t_last + 1, a.splits, split);
+  const Part part(span.lo(a, fdiv(row0, a.by_group)), span.base + t_last + 1, kKeys, a.splits, split);
   if (split >= part.parts) return;
 
   // queries, as 8-bit terms
@@ -138,7 +141,7 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
   const int32_t* table = a.c.table + int64_t(b) * a.d.stream_pages;
   const int sub_mask = a.lay.P / kCacheTile - 1, head_bytes = a.lay.bytes();
   const auto load_page = [&](int tile) {
-    const int lp = (tile * kSubs + wave) >> (a.page_shift - 4);
+    const int lp = (tile * W + wave) >> (a.page_shift - 4);
     return table[lp - fdiv(lp, a.by_W) * a.d.stream_pages];
   };
   const auto page_ok = [&](int p) {
@@ -149,7 +152,7 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
     return make_rsrc(pool + max(page, 0) * a.page_bytes, page < 0 ? 0 : head_bytes);
   };
   // which 16 tokens of the page are this wave's of the tile
-  const auto place = [&](int tile) { return (tile * kSubs + wave) & sub_mask; };
+  const auto place = [&](int tile) { return (tile * W + wave) & sub_mask; };
   int at16[R::PER], at1[R::PER];  // this lane's bytes of 16 tokens' codes and scales
 #pragma unroll
   for (int i = 0; i < R::PER; ++i) {
@@ -184,7 +187,7 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
   };
   // The keys and the values' scales into LDS: the scales of the stream's own tokens, what else a
   // page holds may be anything.
-  const auto fill_keys = [&](int tile, int slot) {
+  const auto fill_keys = [&](int page, int tile, int slot) {
     const int pos0 = tile * kKeys + wave * kCacheTile;
     if (pos0 < span.lowest || pos0 + kCacheTile > hi) {
       const int tok = lane % 16;
@@ -192,6 +195,10 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
       for (int i = 0; i < R::PER; ++i)
         rvs_next[i] = tok >= span.lowest - pos0 && tok < hi - pos0 ? rvs_next[i] : 0;
     }
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < R::PER; ++i) bad |= rvs_next[i] == 255;
+    s.flags[tile & 3][wave] = (page < 0 ? kNoPage : 0) | (__any(bad) ? kNotFinite : 0);
 #pragma unroll
     for (int i = 0; i < R::PER; ++i) {
       const int c = lane + 64 * i;
@@ -208,61 +215,51 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
   // The row's reference score, and its sum.  The products begin at -reference (all 16 alike): what
   // they give is the difference.  over: what a difference may reach, everything before the first.
   f32x16 below = f32x16{};
-  float l = 0.f, over = -3e38f;
+  float l[2] = {0.f, 0.f}, over = -3e38f;
   int E = 0;  // the values' exponent, 0: none yet
 
-  // the values into LDS
-  const auto fill_values = [&](int page, int buf) {
-    bool bad = false;
+  // The values into LDS, a quarter of a lane's 32 at a time.
+  const auto fill_values = [&](int buf, int E, int piece) {
 #pragma unroll
     for (int i = 0; i < R::PER; ++i) {
       const int c = lane + 64 * i;
       if (c >= R::CHUNKS) break;
-      bad |= rvs[i] == 255;
       // without a scale: 0
       const int e = max(127 + kValueLift + rvs[i] - E, 0);
       const float scale = __uint_as_float(uint32_t(rvs[i] == 0 || rvs[i] == 255 ? 0 : e) << 23);
       _Float16* dst = s.v[buf] + (wave * kCacheTile + c % 16) * R::VS + c / 16 * 32;
-      f16x8 w[2];
-      decode16(rv[i][0], rv[i][1], scale, w);
-      *reinterpret_cast<f16x8*>(dst) = w[0];
-      *reinterpret_cast<f16x8*>(dst + 8) = w[1];
-      decode16(rv[i][2], rv[i][3], scale, w);
-      *reinterpret_cast<f16x8*>(dst + 16) = w[0];
-      *reinterpret_cast<f16x8*>(dst + 24) = w[1];
+      *reinterpret_cast<f16x8*>(dst + 8 * piece) = decode8(rv[i][piece], scale);
     }
-    const int flags = (page < 0 ? kNoPage : 0) | (__any(bad) ? kNotFinite : 0);
-    if (lane == 0) s.flags[buf][wave] = flags;
   };
-  // the values' exponent for a tile; the sums follow it
-  const auto follow = [&](int tile) {
-    constexpr int WORDS = kSubs * R::CHUNKS / 4;  // of scales
+  // the values' exponent for a tile
+  const auto exponent = [&](int tile) {
+    constexpr int WORDS = W * R::CHUNKS / 4;  // of scales
     typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    const auto word = [&](int i) {
+      const int w = lane + 64 * i;
+      return reinterpret_cast<const uint32_t*>(s.vs[tile & 3])[WORDS % 64 ? min(w, WORDS - 1) : w];
+    };
     u16x2 top = {0, 0};
 #pragma unroll
     for (int i = 0; i < (WORDS + 63) / 64; ++i) {
-      const int w = lane + 64 * i;
-      const uint32_t v =
-          reinterpret_cast<const uint32_t*>(s.vs[tile & 3])[WORDS % 64 ? min(w, WORDS - 1) : w];
-      top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, v & 0xff00ffu));
-      top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, v >> 8 & 0xff00ffu));
+      top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, word(i) & 0xff00ffu));
+      top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, word(i) >> 8 & 0xff00ffu));
     }
-    if (!__any(max(top[0], top[1]) > E)) return;
+    if (!__any(max(top[0], top[1]) > E)) return E;
     int most = 0;  // but for those that are not finite
 #pragma unroll
-    for (int i = 0; i < (WORDS + 63) / 64; ++i) {
-      const int w = lane + 64 * i;
-      const uint32_t v =
-          reinterpret_cast<const uint32_t*>(s.vs[tile & 3])[WORDS % 64 ? min(w, WORDS - 1) : w];
+    for (int i = 0; i < (WORDS + 63) / 64; ++i)
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const int e = v >> (8 * k) & 255;
+        const int e = word(i) >> (8 * k) & 255;
         most = max(most, e == 255 ? 0 : e);
       }
-    }
     most = wave_max(most);
-    if (most <= E) return;
-    const int next = most + kValueSlack;
+    return most > E ? most + kValueSlack : E;
+  };
+  // the sums follow it
+  const auto follow = [&](int next) {
+    if (next == E) return;
     if (E) {
       const float down = exponent_to_f32(127 + E - next);
 #pragma unroll
@@ -279,50 +276,51 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
   const int all_lo = span.lo(a, wt1), all_hi = span.base + wt0;
   const int my_lo = span.lo(a, t), my_hi = live ? span.base + t : -1;
 
-  // scores of 32 keys, half g of the tile in `slot`
+  // Scores of 32 keys (a half): those of two halves are held, and the largest of the newer one's.
   f32x16 sc[2];
-  const auto load_keys = [&](int g, int slot, i32x8 (&kf)[R::FRAGS], int (&ks)[R::FRAGS]) {
+  float top[2];  // of even and odd ones
+  i32x8 kf[R::FRAGS];
+  int ks[R::FRAGS];
+  const auto load_keys = [&](int h, int slot) {
 #pragma unroll
     for (int f = 0; f < R::FRAGS; ++f) {
       const int blk = R::EVEN ? 2 * f + half : f;
-      const int at = ((2 * g + col / 16) * NB + blk) * 16 + col % 16;
+      const int at = ((2 * h + col / 16) * NB + blk) * 16 + col % 16;
       const i32x4 w = *reinterpret_cast<const i32x4*>(s.k[slot] + at * 16);
       kf[f] = i32x8{w[0], w[1], w[2], w[3], 0, 0, 0, 0};
       ks[f] = s.ks[slot][at];
     }
   };
-  const auto score = [&](int g, int slot) {
-    i32x8 kf[R::FRAGS];
-    int ks[R::FRAGS];
-    load_keys(g, slot, kf, ks);
-    sc[g] = below;
-#pragma unroll
-    for (int j = 0; j < R::MMA; ++j)
-      sc[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-          kf[j % R::FRAGS], qo[j], sc[g], 4, 0, 0, ks[j % R::FRAGS], 0, qs[j]);
+  const auto score = [&](int g, int j) {  // instruction j of them
+    sc[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+        kf[j % R::FRAGS], qo[j], j ? sc[g] : below, 4, 0, 0, ks[j % R::FRAGS], 0, qs[j]);
   };
-  // the scores of half g within the row's keys and the reference
-  const auto settle = [&](int g, int pos0, bool edge, int no_page) {
+  const auto largest = [&](int g, int i0, int i1) {
+#pragma unroll
+    for (int i = i0; i < i1; ++i) top[i % 2] = i < 2 ? sc[g][i] : fmaxf(top[i % 2], sc[g][i]);
+  };
+  // half h's scores within the row's keys and the reference
+  const auto settle = [&](int h, int pos0, bool edge, int no_page) {
+    const int g = h % 2;
     if (edge) {
       const int from = my_lo - pos0, to = my_hi - pos0;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const int k = 32 * g + 8 * (i / 4) + 4 * half + i % 4;
-        const bool see = k >= from && k <= to && !(no_page >> (2 * g + i / 8) & 1);
+        const int k = 32 * h + 8 * (i / 4) + 4 * half + i % 4;
+        const bool see = k >= from && k <= to && !(no_page >> (2 * h + i / 8) & 1);
         sc[g][i] = see ? sc[g][i] : -__builtin_inff();
       }
+      largest(g, 0, 16);
     }
-    float top = sc[g][0];
-#pragma unroll
-    for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[g][i]);
-    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top),
-                                                       false, false);
-    top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
-    if (__any(top > over)) {
-      const float more = top > over ? top : 0.f;
+    const uint32_t all = __float_as_uint(fmaxf(top[0], top[1]));
+    const auto both = __builtin_amdgcn_permlane32_swap(all, all, false, false);
+    const float high = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+    if (__any(high > over)) {
+      const float more = high > over ? high : 0.f;
       const float down = over < 0.f ? 1.f : exp2_fast(-more * a.scale_log2);
-      over = top > over ? a.slack : over;
-      l *= down;
+      over = high > over ? a.slack : over;
+      l[0] *= down;
+      l[1] *= down;
 #pragma unroll
       for (int i = 0; i < NB; ++i) o[i] *= down;
 #pragma unroll
@@ -332,76 +330,115 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
       }
     }
   };
-  // The weights of half g and what they add, beside the scores of half `other` of the tile in `slot`:
-  // a matrix instruction of the scores, then a part of the weights, which take the vector unit
-  // about as long as it takes the matrix unit.
-  const auto advance = [&](int g, int buf, int other, int slot) {
-    i32x8 kf[R::FRAGS];
-    int ks[R::FRAGS];
-    load_keys(other, slot, kf, ks);
+  // Half h's weights and what they add, beside the scores of half `h_other`, whose keys are loaded; then
+  // those of half h_keys are.
+  // A matrix instruction that waits for its unit keeps the other waves' vector instructions
+  // waiting too, so a part of the vector work follows each of them, about as long as it takes:
+  // weights, the largest of the next scores, and what `beside` has (NB pieces).  The scheduler would
+  // put the matrix instructions side by side, so it is held to this order.
+  const auto advance = [&](int h, int buf, int h_other, int h_keys, int slot_keys, auto&& beside) {
+    const int g = h % 2, other = h_other % 2;
     const int j16 = lane % 16;
-    const _Float16* base = s.v[buf] + (32 * g + 4 * half + j16 / 4) * R::VS +
+    const _Float16* base = s.v[buf] + (32 * h + 4 * half + j16 / 4) * R::VS +
                            16 * (lane / 16 % 2) + 4 * (j16 % 4);
-    const auto values = [&](int d, int blk) {
+    const auto values = [&](int i) {  // 16 keys i / NB, block i % NB
+      const _Float16* v = base + 16 * (i / NB) * R::VS + 32 * (i % NB);
       struct Both {
         s16x4 lo, hi;
       } r;
-      r.lo = turned4(base + 16 * d * R::VS + 32 * blk);
-      r.hi = turned4(base + (16 * d + 8) * R::VS + 32 * blk);
+      r.lo = turned4(v);
+      r.hi = turned4(v + 8 * R::VS);
       return __builtin_bit_cast(f16x8, r);
     };
-    f16x8 p[R::PT][2];
-    const auto weigh = [&](int i) {  // weights i and i + 1
-      f32x2 w = {exp2_fast(fmaf(sc[g][i], a.scale_log2, kLift)),
-                 exp2_fast(fmaf(sc[g][i + 1], a.scale_log2, kLift))};
+    // weights in four groups of four, each a stage behind the one before: arguments, powers, operands
+    f16x8 p[R::PT][2], v[NB];
+    float x[16];
+    const auto weigh = [&](int stage) {
 #pragma unroll
-      for (int k = 0; k < R::PT; ++k) {
-        const f16x2 r = __builtin_convertvector(w, f16x2);
-        p[k][i / 8][i % 8] = r[0];
-        p[k][i / 8][i % 8 + 1] = r[1];
-        // the sum of the weights as they are used
-        l = __builtin_amdgcn_fdot2(r, f16x2{1, 1}, l, false);
-        if (k + 1 < R::PT) w -= __builtin_convertvector(r, f32x2);
+      for (int i = 4 * stage; i < 4 * stage + 4; ++i)
+        if (i < 16) x[i] = fmaf(sc[g][i], a.scale_log2, kLift);
+#pragma unroll
+      for (int i = 4 * stage - 4; i < 4 * stage; ++i)
+        if (i >= 0 && i < 16) x[i] = exp2_fast(x[i]);
+#pragma unroll
+      for (int i = 4 * stage - 8; i < 4 * stage - 4; i += 2) {
+        if (i < 0) continue;
+        f32x2 w = {x[i], x[i + 1]};
+#pragma unroll
+        for (int k = 0; k < R::PT; ++k) {
+          const f16x2 r = __builtin_convertvector(w, f16x2);
+          p[k][i / 8][i % 8] = r[0];
+          p[k][i / 8][i % 8 + 1] = r[1];
+          // the sum of the weights as they are used
+          l[i / 2 % 2] = __builtin_amdgcn_fdot2(r, f16x2{1, 1}, l[i / 2 % 2], false);
+          if (k + 1 < R::PT) w -= __builtin_convertvector(r, f32x2);
+        }
       }
     };
-    sc[other] = below;
+    const auto add = [&](int i) {
+#pragma unroll
+      for (int k = 0; k < R::PT; ++k)
+        o[i % NB] =
+            __builtin_amdgcn_mfma_f32_32x32x16_f16(v[i % NB], p[k][i / NB], o[i % NB], 0, 0, 0);
+    };
+    constexpr int STAGES = 6;
 #pragma unroll
     for (int j = 0; j < R::MMA; ++j) {
-      sc[other] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-          kf[j % R::FRAGS], qo[j], sc[other], 4, 0, 0, ks[j % R::FRAGS], 0, qs[j]);
+      score(other, j);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = 8 * j / R::MMA; i < 8 * (j + 1) / R::MMA; ++i) weigh(2 * i);
+      for (int i = STAGES * j / R::MMA; i < STAGES * (j + 1) / R::MMA; ++i) weigh(i);
+#pragma unroll
+      for (int i = NB * j / R::MMA; i < NB * (j + 1) / R::MMA; ++i) v[i] = values(i);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    load_keys(h_keys, slot_keys);
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      add(i);
+      __builtin_amdgcn_sched_barrier(0);
+      v[i] = values(NB + i);
+      beside(i);
       __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
-    for (int d = 0; d < 2; ++d)
-#pragma unroll
-      for (int blk = 0; blk < NB; ++blk) {
-        const f16x8 v = values(d, blk);
-#pragma unroll
-        for (int k = 0; k < R::PT; ++k)
-          o[blk] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[k][d], o[blk], 0, 0, 0);
-      }
+    for (int i = 0; i < NB; ++i) {
+      add(NB + i);
+      __builtin_amdgcn_sched_barrier(0);
+      largest(other, 16 * i / NB, 16 * (i + 1) / NB);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // made here, not where they are used
+    hold(top[0]);
+    hold(top[1]);
+    hold(l[0]);
+    hold(l[1]);
   };
 
-  int page0 = -1, page1 = -1, page2 = -1, coming = -1;  // of the next tiles
+  // The pages of the next tiles.  Past the part's end there are none, and what goes to LDS is 0.
+  const auto page_at = [&](int tile, int loaded) { return tile < part.end ? page_ok(loaded) : -1; };
+  int page0 = -1, page1 = -1, page2 = -1, flags = 0;
   if (part.first < part.end) {
-    page0 = page_ok(load_page(part.first));
-    if (part.first + 1 < part.end) page1 = page_ok(load_page(part.first + 1));
-    if (part.first + 2 < part.end) coming = load_page(part.first + 2);
+    page0 = page_at(part.first, load_page(part.first));
+    page1 = page_at(part.first + 1, load_page(part.first + 1));
+    page2 = page_at(part.first + 2, load_page(part.first + 2));
     fetch_values(page0, part.first);
     fetch_keys(page0, part.first);
-    fill_keys(part.first, 0);
+    fill_keys(page0, part.first, 0);
 #pragma unroll
     for (int i = 0; i < R::PER; ++i) rvs[i] = rvs_next[i];
     fetch_keys(page1, part.first + 1);
-    fill_keys(part.first + 1, 1);
-    page2 = page_ok(coming);
+    fill_keys(page1, part.first + 1, 1);
     __syncthreads();
-    follow(part.first);
-    fill_values(page0, part.first & 1);
-    score(0, 0);
+    follow(exponent(part.first));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) fill_values(part.first & 1, E, i);
+    load_keys(0, 0);
+#pragma unroll
+    for (int j = 0; j < R::MMA; ++j) score(0, j);
+    largest(0, 0, 16);
+    load_keys(1, 0);
+    flags = s.flags[part.first & 3][lane % W];
   }
   __syncthreads();
 
@@ -410,24 +447,34 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
     const int buf = tile & 1;
     const int pos0 = tile * kKeys;
     const int slot1 = slot == 2 ? 0 : slot + 1, slot2 = slot1 == 2 ? 0 : slot1 + 1;
-    if (tile + 3 < part.end) coming = load_page(tile + 3);
-    if (tile + 1 < part.end) {
+    const int coming = load_page(tile + 3);
 #pragma unroll
-      for (int i = 0; i < R::PER; ++i) rvs[i] = rvs_next[i];
-      fetch_values(page1, tile + 1);
-      if (tile + 2 < part.end) fetch_keys(page2, tile + 2);
-    }
+    for (int i = 0; i < R::PER; ++i) rvs[i] = rvs_next[i];
+    fetch_values(page1, tile + 1);
+    fetch_keys(page2, tile + 2);
+    const int no_page = int(__ballot(flags & kNoPage)) & ((1 << W) - 1);
+    const bool not_finite = __any(flags & kNotFinite);
+    int E1;
     if (pos0 <= some_hi && pos0 + kKeys > some_lo) {
-      const i32x4 f4 = *reinterpret_cast<const i32x4*>(s.flags[buf]);
-      const int flags = __builtin_amdgcn_readfirstlane(f4[0] | f4[1] << 2 | f4[2] << 4 | f4[3] << 6);
-      const int no_page = (flags & 1) | (flags >> 1 & 2) | (flags >> 2 & 4) | (flags >> 3 & 8);
       const bool edge = pos0 + kKeys - 1 > all_hi || pos0 < all_lo || no_page;
-      settle(0, pos0, edge, no_page);
-      advance(0, buf, 1, slot);
-      settle(1, pos0, edge, no_page);
-      advance(1, buf, 0, slot1);  // past the last tile: whatever is there, and not used
-      if (flags & 0xaa) {  // a block that is not finite, to the rows that see its token
-        for (int c = 0; c < kSubs * R::CHUNKS; ++c) {
+#pragma unroll
+      for (int h = 0; h < R::HALVES; ++h) {
+        settle(h, pos0, edge, no_page);
+        if (h == R::HALVES - 1) E1 = exponent(tile + 1);
+        // past the last tile: 0
+        const int h1 = (h + 1) % R::HALVES, h2 = (h + 2) % R::HALVES;
+        advance(h, buf, h1, h2, h + 2 < R::HALVES ? slot : slot1, [&](int i) {
+          // the next tiles' keys in the first but one half, values in the last, in order
+          if (h == R::HALVES - 2 && i == 0) fill_keys(page2, tile + 2, slot2);
+          if (h == R::HALVES - 1) {
+#pragma unroll
+            for (int k = 4 * i / NB; k < 4 * (i + 1) / NB; ++k)
+              fill_values(buf ^ 1, E1, k);
+          }
+        });
+      }
+      if (not_finite) {  // a block that is not finite, to the rows that see its token
+        for (int c = 0; c < W * R::CHUNKS; ++c) {
           if (s.vs[tile & 3][c] != 255) continue;
           const int sub = c / R::CHUNKS, blk = c % R::CHUNKS / 16;
           const int pos = pos0 + sub * 16 + c % 16;
@@ -440,30 +487,36 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
               for (int k = 0; k < 16; ++k) o[i][k] += nan;
         }
       }
-    } else if (tile + 1 < part.end) {
-      score(0, slot1);
+    } else {
+      E1 = exponent(tile + 1);
+      fill_keys(page2, tile + 2, slot2);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) fill_values(buf ^ 1, E1, i);
+      load_keys(0, slot1);
+#pragma unroll
+      for (int j = 0; j < R::MMA; ++j) score(0, j);
+      largest(0, 0, 16);
+      load_keys(1, slot1);
     }
-    if (tile + 1 < part.end) {
-      follow(tile + 1);
-      fill_values(page1, buf ^ 1);
-      if (tile + 2 < part.end) fill_keys(tile + 2, slot2);
-      page1 = page2;
-      page2 = page_ok(coming);
-    }
+    flags = s.flags[(tile + 1) & 3][lane % W];
+    follow(E1);
+    page1 = page2;
+    page2 = page_at(tile + 3, coming);
     slot = slot1;
     __syncthreads();
   }
 
-  l += __shfl_xor(l, 32);
+  float sum = l[0] + l[1];
+  sum += __shfl_xor(sum, 32);
   if (!live) {
     if (split == 0) no_output();
     return;
   }
-  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+  const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
   // 2^{E - 127 - kValueLift} in two steps, neither out of range
   const float up = exponent_to_f32(E - kValueSlack);
   const float less = exponent_to_f32(127 + kValueSlack - kValueLift);
-  const float bad = q_bad && l > 0.f ? __builtin_nanf("") : 0.f;
+  const float bad = q_bad && sum > 0.f ? __builtin_nanf("") : 0.f;
   const auto value = [&](int blk, int i) { return o[blk][i] * inv * less * up + bad; };
   if (part.parts == 1) {
     T* y = static_cast<T*>(a.y.data) + b * a.y.batch_stride + t * a.y.token_stride +
@@ -488,31 +541,42 @@ __global__ __launch_bounds__(kBlock, NB <= 4 ? 2 : 1) void attend_rows_kernel(At
                                  value(blk, i + 3)}};
       store_pack<float, 4>(o_part + blk * 32 + 2 * i + 4 * half, v);
     }
-  if (half == 0) a.part_stat[at] = {-below[0], l};
+  if (half == 0) a.part_stat[at] = {-below[0], sum};
+}
+
+template <typename T, int NB>
+void run(const AttendArgs& a, int rows, unsigned grid, hipStream_t s) {
+  if constexpr (NB <= kWideBlocks<T>) {
+    if (rows == 256) {
+      attend_rows_kernel<T, NB, 8><<<grid, 512, 0, s>>>(a);
+      return;
+    }
+  }
+  attend_rows_kernel<T, NB, 4><<<grid, 256, 0, s>>>(a);
 }
 
 template <typename T>
-void run(const AttendArgs& a, int NB, unsigned grid, hipStream_t s) {
+void run(const AttendArgs& a, int NB, int rows, unsigned grid, hipStream_t s) {
   switch (NB) {
-    case 1: attend_rows_kernel<T, 1><<<grid, kBlock, 0, s>>>(a); break;
-    case 2: attend_rows_kernel<T, 2><<<grid, kBlock, 0, s>>>(a); break;
-    case 3: attend_rows_kernel<T, 3><<<grid, kBlock, 0, s>>>(a); break;
-    case 4: attend_rows_kernel<T, 4><<<grid, kBlock, 0, s>>>(a); break;
-    case 5: attend_rows_kernel<T, 5><<<grid, kBlock, 0, s>>>(a); break;
-    case 6: attend_rows_kernel<T, 6><<<grid, kBlock, 0, s>>>(a); break;
-    case 7: attend_rows_kernel<T, 7><<<grid, kBlock, 0, s>>>(a); break;
-    default: attend_rows_kernel<T, 8><<<grid, kBlock, 0, s>>>(a); break;
+    case 1: run<T, 1>(a, rows, grid, s); break;
+    case 2: run<T, 2>(a, rows, grid, s); break;
+    case 3: run<T, 3>(a, rows, grid, s); break;
+    case 4: run<T, 4>(a, rows, grid, s); break;
+    case 5: run<T, 5>(a, rows, grid, s); break;
+    case 6: run<T, 6>(a, rows, grid, s); break;
+    case 7: run<T, 7>(a, rows, grid, s); break;
+    default: run<T, 8>(a, rows, grid, s); break;
   }
 }
 
 }  // namespace
 
-void launch_attend_rows(const AttendArgs& a, int NB, hipStream_t stream) {
+void launch_attend_rows(const AttendArgs& a, int NB, int rows, hipStream_t stream) {
   const unsigned grid = unsigned(int64_t(a.pairs) * a.row_tiles * a.splits);
   if (a.d.dtype == CO_BF16)
-    run<bf16_t>(a, NB, grid, stream);
+    run<bf16_t>(a, NB, rows, grid, stream);
   else
-    run<float>(a, NB, grid, stream);
+    run<float>(a, NB, rows, grid, stream);
 }
 
 }  // namespace coinf

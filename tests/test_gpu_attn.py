@@ -336,6 +336,13 @@ ATTEND = [
     (1, 300, 1500, 8, 2, 128, 64, 0, BF16, "full", 0, 0),
     (1, 70, 3000, 2, 2, 224, 64, 1000, BF16, "full", 0, 0),
     (2, 33, 17, 8, 8, 32, 256, 1, BF16, "ragged", 0, 0),
+    # long contexts, more rows than 128: wider workgroups
+    (1, 90, 9000, 4, 2, 128, 256, 0, BF16, "full", 0, 0),
+    (2, 140, 8300, 2, 2, 96, 64, 0, BF16, "ragged", 3, 1),
+    (1, 300, 8200, 2, 1, 50, 128, 8100, BF16, "full", 0, 0),
+    (2, 70, 8500, 3, 1, 32, 256, 0, F32, "ragged", 0, 0),
+    (1, 260, 8400, 1, 1, 64, 16, 0, F32, "full", 0, 0),
+    (1, 150, 8400, 2, 1, 128, 64, 0, F32, "full", 0, 0),
 ]
 
 
