@@ -22,7 +22,7 @@ __global__ __launch_bounds__(kBlock) void attend_join_kernel(AttendArgs a, int r
   if (row >= rows || ch >= width) return;
   const int t = fdiv(row, a.by_group), head = kv * a.group + row - t * a.group;
   const int t_last = fdiv(min(row0 + rows_of, rows) - 1, a.by_group);
-  const Part part(span.lo(a, fdiv(row0, a.by_group)), span.base + t_last + 1, a.keys, a.splits, 0);
+  const Part part(a, span.lo(a, fdiv(row0, a.by_group)), span.base + t_last + 1, 0);
   if (part.parts == 1) return;
   const int64_t at = int64_t(unit) * a.splits * rows_of + in;
   // eight parts on their way at a time
@@ -67,6 +67,7 @@ __global__ __launch_bounds__(kBlock) void attend_join_kernel(AttendArgs a, int r
 struct Cut {
   int64_t pairs, row_tiles, splits, rows;
   int few;  // column tiles of the kernel of few rows, or 0
+  int part_keys;  // of a part at least
   int64_t units() const { return pairs * row_tiles; }
 };
 
@@ -85,8 +86,10 @@ Cut cut_of(const co_attn_desc& d, int32_t T) {
   c.rows = c.few ? c.few * 16 : rows > 128 && keys >= 8192 && cache_blocks(d.head_dim) <= most
                                     ? 256 : 128;
   c.row_tiles = (rows + c.rows - 1) / c.rows;
-  const int64_t parts = (keys + kPartKeys - 1) / kPartKeys;
-  c.splits = std::max<int64_t>(1, std::min<int64_t>((c.few ? 1024 : c.rows == 128 ? 512 : 256) / c.units(), parts));
+  c.part_keys = c.few ? 512 : 256;
+  const int64_t parts = (keys + c.part_keys - 1) / c.part_keys;
+  const int64_t room = c.few ? 1024 : c.rows == 128 ? 512 : 256;
+  c.splits = std::max<int64_t>(1, std::min(room / c.units(), parts));
   return c;
 }
 
@@ -122,6 +125,7 @@ hipError_t launch_attend(const co_attn_desc& d, const co_attn_cache& cache, cons
   a.row_tiles = int32_t(c.row_tiles);
   a.splits = int32_t(c.splits);
   a.keys = c.few ? kFewKeys : int32_t(c.rows / 2);
+  a.part_tiles = c.part_keys / a.keys;
   a.by_row_tiles = make_fastdiv(a.row_tiles);
   a.by_splits = make_fastdiv(a.splits);
   const int es = d.dtype == CO_BF16 ? 2 : 4;

@@ -37,14 +37,13 @@ struct AttendArgs {
   int32_t pairs;       // streams * kv heads
   int32_t splits;      // parts of a unit's keys at most
   int32_t keys;        // of a tile
+  int32_t part_tiles;  // of a part at least
   int32_t wide;        // q and y in pieces of 16 bytes
   float* part;         // (units, splits, rows, NB * 32) values, then (.., rows) reference score and sum
   float2* part_stat;
 };
 
-// Keys of a tile at most, and of a part at least.
-constexpr int kMostKeys = 128;
-constexpr int kPartKeys = 256;
+constexpr int kMostKeys = 128;  // of a tile
 
 // Weights are 2^{x + kLift}, x <= kSlack over the row's reference: 2^15, below 16-bit floats' highest.
 // Their least step is 2^-24, 2^-35 of the row's reference.
@@ -69,13 +68,12 @@ struct Span {
   }
 };
 
-// Tiles first..end - 1, of `keys` each, of a unit's part `split` of the keys lo..hi - 1; parts: of
-// the unit.
+// Tiles first..end - 1 of a unit's part `split` of the keys lo..hi - 1; parts: of the unit.
 struct Part {
   int first, end, parts;
-  __device__ Part(int lo, int hi, int keys, int splits, int split) {
-    const int t0 = lo / keys, t1 = lo < hi ? (hi + keys - 1) / keys : t0;
-    const int each = max((t1 - t0 + splits - 1) / splits, kPartKeys / keys);
+  __device__ Part(const AttendArgs& a, int lo, int hi, int split) {
+    const int t0 = lo / a.keys, t1 = lo < hi ? (hi + a.keys - 1) / a.keys : t0;
+    const int each = max((t1 - t0 + a.splits - 1) / a.splits, a.part_tiles);
     parts = max((t1 - t0 + each - 1) / each, 1);
     first = min(t0 + split * each, t1);
     end = min(first + each, t1);

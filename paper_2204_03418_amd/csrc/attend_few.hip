@@ -33,6 +33,12 @@ struct Few {
   }
 };
 
+// Waves a SIMD: what a kernel's registers and LDS leave room for.
+template <typename T, int NB, int CT>
+constexpr int few_waves() {
+  return CT == 1 && (sizeof(T) == 2 || NB <= 2) && NB <= 4 ? 4 : NB <= 4 ? 2 : 1;
+}
+
 // One wave's values, and at the end its sums (16 rows of NB * 32, 64 bytes more each).
 template <typename T, int NB>
 struct FewLds {
@@ -43,7 +49,8 @@ struct FewLds {
 };
 
 template <typename T, int NB, int CT>
-__global__ __launch_bounds__(kBlock) void attend_few_kernel(AttendArgs a) {
+__global__ __launch_bounds__(kBlock, (few_waves<T, NB, CT>())) void attend_few_kernel(
+    AttendArgs a) {
   using F = Few<T, NB>;
   __shared__ FewLds<T, NB> lds[kWaves];
   __shared__ float2 stats[kWaves][16];
@@ -65,7 +72,7 @@ __global__ __launch_bounds__(kBlock) void attend_few_kernel(AttendArgs a) {
       store4<T>(out_row(rows + i / (NB * 8)), i % (NB * 8) * 4, a.d.head_dim, a.wide, none);
   }
   if (rows == 0) return;
-  const Part part(span.lo(a, 0), span.base + span.n, a.keys, a.splits, split);
+  const Part part(a, span.lo(a, 0), span.base + span.n, split);
   if (split >= part.parts) return;
 
   // queries, as 8-bit terms
@@ -142,54 +149,82 @@ __global__ __launch_bounds__(kBlock) void attend_few_kernel(AttendArgs a) {
     q_bad[c] |= __shfl_xor(int(q_bad[c]), 32) != 0;
   }
 
+  // The keys' way: pages two steps ahead, codes and scales one.  Nothing is read out of a page's
+  // range, and without a page all is 0.  The two tiles of 16 tokens of a step lie in one page, or
+  // with pages of 16 in two.
   const char* pool = static_cast<const char*>(a.c.pool) + int64_t(kv) * a.lay.bytes();
   const int32_t* table = a.c.table + int64_t(b) * a.d.stream_pages;
   constexpr int tile_bytes = NB * 256;
-  const int sub_mask = a.lay.P / kCacheTile - 1;
-  const auto page_of = [&](int tile) {  // of 16 tokens
+  const int sub_mask = a.lay.P / kCacheTile - 1, head_bytes = a.lay.bytes();
+  const bool two = a.lay.P == kCacheTile;
+  const auto load_page = [&](int tile) {  // of 16 tokens
     const int lp = tile >> (a.page_shift - 4);
-    const int p = table[lp - fdiv(lp, a.by_W) * a.d.stream_pages];
-    return __builtin_amdgcn_readfirstlane(p >= 0 && p < a.d.pages ? p : -1);
+    return table[lp - fdiv(lp, a.by_W) * a.d.stream_pages];
   };
-  int page[2];
+  const auto page_rsrc = [&](int page) {
+    return make_rsrc(pool + max(page, 0) * a.page_bytes, page < 0 ? 0 : head_bytes);
+  };
+  int at_k[F::FRAGS], at_v[F::VC], at_vs[F::VC];  // this lane's bytes of the keys' codes and the values'
+  bool tile1[F::VC];                              // whether those are of the second tile
+#pragma unroll
+  for (int f = 0; f < F::FRAGS; ++f) {
+    const int blk = F::block(f, g);
+    at_k[f] = blk < NB ? blk * 16 + col : kOutOfRange / 16;
+  }
+#pragma unroll
+  for (int i = 0; i < F::VC; ++i) {
+    const int c = lane + 64 * i, tile = c / (NB * 16), rest = c - tile * NB * 16;
+    tile1[i] = tile > 0;
+    at_v[i] = c < F::CHUNKS ? (two ? 0 : tile * tile_bytes) + rest * 16 : kOutOfRange;
+    at_vs[i] = c < F::CHUNKS ? (two ? 0 : tile * NB * 16) + rest : kOutOfRange;
+  }
+  int page[2], coming[2];
   i32x4 rk[2][F::FRAGS], rv[F::VC];
-  int rks[2][F::FRAGS], rvs[F::VC], has;  // has: bit i: tile i has a page
+  int rks[2][F::FRAGS], rvs[F::VC];
   const auto fetch_pages = [&](int step) {
-    page[0] = page_of(2 * step);
-    page[1] = page_of(2 * step + 1);
+    coming[0] = load_page(2 * step);
+    if (two) coming[1] = load_page(2 * step + 1);
+  };
+  const auto take_pages = [&] {
+    const auto ok = [&](int p) {
+      p = __builtin_amdgcn_readfirstlane(p);
+      return p >= 0 && p < a.d.pages ? p : -1;
+    };
+    page[0] = ok(coming[0]);
+    page[1] = two ? ok(coming[1]) : page[0];
   };
   const auto fetch = [&](int step) {
-    has = (page[0] >= 0) | (page[1] >= 0) << 1;
-    const char* p[2];
-    int in[2];
+    const auto r0 = page_rsrc(page[0]), r1 = page_rsrc(page[1]);
+    const int n0 = (2 * step) & sub_mask, n1 = (2 * step + 1) & sub_mask;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      in[i] = (2 * step + i) & sub_mask;
-      p[i] = pool + (page[i] >= 0 ? page[i] : 0) * a.page_bytes;
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
+      const auto r = i ? r1 : r0;
+      const int n = i ? n1 : n0;
 #pragma unroll
       for (int f = 0; f < F::FRAGS; ++f) {
-        const int blk = F::block(f, g);
-        rk[i][f] = i32x4{0, 0, 0, 0};
-        rks[i][f] = 127;
-        if (page[i] >= 0 && blk < NB) {
-          const int at = blk * 16 + col;
-          rk[i][f] = *reinterpret_cast<const i32x4*>(p[i] + in[i] * tile_bytes + at * 16);
-          rks[i][f] = uint8_t(p[i][a.lay.scales(0) + in[i] * NB * 16 + at]);
-        }
+        rk[i][f] = __builtin_bit_cast(
+            i32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at_k[f] * 16, n * tile_bytes, 0));
+        rks[i][f] = uint8_t(__builtin_amdgcn_raw_buffer_load_b8(
+            r, at_k[f], a.lay.scales(0) + n * NB * 16, 0));
       }
+    }
 #pragma unroll
     for (int i = 0; i < F::VC; ++i) {
-      const int c = lane + 64 * i, tile = c / (NB * 16), rest = c - tile * NB * 16;
-      rv[i] = i32x4{0, 0, 0, 0};
-      rvs[i] = 0;
-      if (c < F::CHUNKS && (tile ? page[1] : page[0]) >= 0) {
-        const char* q = tile ? p[1] : p[0];
-        const int n = tile ? in[1] : in[0];
-        rv[i] = *reinterpret_cast<const i32x4*>(q + a.lay.codes(1) + n * tile_bytes + rest * 16);
-        rvs[i] = uint8_t(q[a.lay.scales(1) + n * NB * 16 + rest]);
+      const int v = a.lay.codes(1) + n0 * tile_bytes, vs = a.lay.scales(1) + n0 * NB * 16;
+      rv[i] = __builtin_bit_cast(
+          i32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                     r0, two && tile1[i] ? kOutOfRange : at_v[i], v, 0));
+      rvs[i] = uint8_t(__builtin_amdgcn_raw_buffer_load_b8(
+          r0, two && tile1[i] ? kOutOfRange : at_vs[i], vs, 0));
+    }
+    if (two) {  // n0 = n1 = 0
+#pragma unroll
+      for (int i = 0; i < F::VC; ++i) {
+        rv[i] |= __builtin_bit_cast(
+            i32x4, __builtin_amdgcn_raw_buffer_load_b128(r1, tile1[i] ? at_v[i] : kOutOfRange,
+                                                         a.lay.codes(1), 0));
+        rvs[i] |= uint8_t(__builtin_amdgcn_raw_buffer_load_b8(
+            r1, tile1[i] ? at_vs[i] : kOutOfRange, a.lay.scales(1), 0));
       }
     }
   };
@@ -218,12 +253,13 @@ __global__ __launch_bounds__(kBlock) void attend_few_kernel(AttendArgs a) {
   int step = part.first * (kFewKeys / kStep) + wave;
   if (step < end) {
     fetch_pages(step);
+    take_pages();
     fetch(step);
     if (step + kWaves < end) fetch_pages(step + kWaves);
   }
   for (; step < end; step += kWaves) {
     const int pos0 = step * kStep;
-    const int pages = has;
+    const int pages = (page[0] >= 0) | (page[1] >= 0) << 1;
     // scores: the keys are used up first
     f32x4 sc[CT][2];
 #pragma unroll
@@ -240,17 +276,19 @@ __global__ __launch_bounds__(kBlock) void attend_few_kernel(AttendArgs a) {
         }
       }
     // values, as 16-bit floats into LDS
-    const int from = span.lowest - pos0, to = hi - pos0;
+    if (pos0 < span.lowest || pos0 + kStep > hi) {  // of the stream's own tokens
+#pragma unroll
+      for (int i = 0; i < F::VC; ++i) {
+        const int tok = (tile1[i] ? 16 : 0) + lane % 16;
+        rvs[i] = tok >= span.lowest - pos0 && tok < hi - pos0 ? rvs[i] : 0;
+      }
+    }
     int top_s = 0;
     bool bad = false;
-    int vs[F::VC];
 #pragma unroll
     for (int i = 0; i < F::VC; ++i) {
-      const int c = lane + 64 * i, tile = c / (NB * 16), tok = tile * 16 + c % 16;
-      const bool on = c < F::CHUNKS && tok >= from && tok < to && (pages >> tile & 1);
-      bad |= on && rvs[i] == 255;
-      vs[i] = on && rvs[i] != 255 ? rvs[i] : 0;
-      top_s = max(top_s, vs[i]);
+      bad |= rvs[i] == 255;
+      top_s = max(top_s, rvs[i] == 255 ? 0 : rvs[i]);
     }
     if (__any(top_s > E)) {
       const int next = wave_max(top_s) + kValueSlack;
@@ -267,7 +305,9 @@ __global__ __launch_bounds__(kBlock) void attend_few_kernel(AttendArgs a) {
     for (int i = 0; i < F::VC; ++i) {
       const int c = lane + 64 * i, tile = c / (NB * 16), rest = c - tile * NB * 16;
       if (c >= F::CHUNKS) break;
-      const float scale = vs[i] ? exponent_to_f32(127 + vs[i] - E + kValueLift) : 0.f;
+      // without a scale: 0
+      const int e = max(127 + kValueLift + rvs[i] - E, 0);
+      const float scale = __uint_as_float(uint32_t(rvs[i] == 0 || rvs[i] == 255 ? 0 : e) << 23);
       _Float16* dst = vbuf + (tile * 16 + rest % 16) * F::VS + rest / 16 * 32;
 #pragma unroll
       for (int k = 0; k < 4; ++k) *reinterpret_cast<f16x8*>(dst + 8 * k) = decode8(rv[i][k], scale);
@@ -276,6 +316,7 @@ __global__ __launch_bounds__(kBlock) void attend_few_kernel(AttendArgs a) {
 #pragma unroll
     for (int i = 0; i < F::VC; ++i) raw[i] = rvs[i];
     if (step + kWaves < end) {
+      take_pages();
       fetch(step + kWaves);
       if (step + 2 * kWaves < end) fetch_pages(step + 2 * kWaves);
     }

@@ -91,7 +91,7 @@ __global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_r
     return;
   }
   const int t_last = fdiv(min(row0 + kRows, rows) - 1, a.by_group);
-  const Part part(span.lo(a, fdiv(row0, a.by_group)), span.base + t_last + 1, kKeys, a.splits, split);
+  const Part part(a, span.lo(a, fdiv(row0, a.by_group)), span.base + t_last + 1, split);
   if (split >= part.parts) return;
 
   // queries, as 8-bit terms
