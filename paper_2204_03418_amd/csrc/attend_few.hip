@@ -75,80 +75,6 @@ __global__ __launch_bounds__(kBlock, (few_waves<T, NB, CT>())) void attend_few_k
   const Part part(a, span.lo(a, 0), span.base + span.n, split);
   if (split >= part.parts) return;
 
-  // queries, as 8-bit terms
-  i32x8 qo[CT][F::MMA];
-  int qs[CT][F::MMA];
-  bool q_bad[CT];
-#pragma unroll
-  for (int c = 0; c < CT; ++c) {
-    const int row = 16 * c + col;
-    const bool live = row < rows;
-    const int t = token_of(live ? row : 0), head = kv * a.group + (live ? row - t * a.group : 0);
-    const T* q = static_cast<const T*>(a.q.data) + b * a.q.batch_stride + t * a.q.token_stride +
-                 int64_t(head) * a.d.head_dim;
-    q_bad[c] = false;
-#pragma unroll
-    for (int f = 0; f < F::FRAGS; ++f) {
-      int byte[2];
-      i32x4 words[2][F::QT];
-      // this lane's halves of 16 channels: of slots g / 2 and 2 + g / 2
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        if (w == 1 && F::NBP <= 2) {  // the same block again
-          byte[1] = byte[0];
-#pragma unroll
-          for (int k = 0; k < F::QT; ++k) words[1][k] = words[0][k];
-          continue;
-        }
-        const int blk = F::NBP == 2 ? g / 2 : F::block(f, 2 * w + g / 2);
-        float v[16];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          load4<T>(q, live ? blk * 32 + 16 * (g % 2) + 4 * i : a.d.head_dim, a.d.head_dim, a.wide,
-                   v + 4 * i);
-        uint32_t most = 0;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          v[i] *= a.q_sign;
-          most = max(most, __float_as_uint(v[i]) & 0x7fffffffu);
-        }
-        most = max(most, uint32_t(__shfl_xor(int(most), 16)));
-        const bool bad = most >= 0x7f800000u;
-        q_bad[c] |= bad;
-        byte[w] = bad ? 127 : query_scale(most);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = bad ? 0.f : v[i];
-        to_terms<F::QT>(v, byte[w], words[w]);
-      }
-      // scales: of slot g, which lanes of group 2 (g % 2) have
-      const int b0 = __shfl(byte[0], col + 32 * (g % 2)), b1 = __shfl(byte[1], col + 32 * (g % 2));
-      const int mine = g / 2 ? b1 : b0;
-#pragma unroll
-      for (int k = 0; k < F::MMA / F::FRAGS; ++k) {
-        const int j = k * F::FRAGS + f;
-#pragma unroll
-        for (int w = 0; w < 2; ++w)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if constexpr (F::NBP >= 4) {
-              qo[c][j][4 * w + i] = words[w][k][i];
-            } else if constexpr (F::NBP == 2) {
-              qo[c][j][4 * w + i] = words[w][2 * k + w][i];
-            } else {
-              const int t0 = 4 * k + 2 * w;
-              const int lo = t0 < F::QT ? words[w][t0 < F::QT ? t0 : 0][i] : 0;
-              const int hi = t0 + 1 < F::QT ? words[w][t0 + 1 < F::QT ? t0 + 1 : 0][i] : 0;
-              qo[c][j][4 * w + i] = g / 2 ? hi : lo;
-            }
-          }
-        qs[c][j] = mine - 4 * (F::NBP >= 4 ? k : F::NBP == 2 ? 2 * k + g / 2 : 4 * k + g);
-      }
-    }
-    // all lanes of a column
-    q_bad[c] |= __shfl_xor(int(q_bad[c]), 16) != 0;
-    q_bad[c] |= __shfl_xor(int(q_bad[c]), 32) != 0;
-  }
-
   // The keys' way: pages two steps ahead, codes and scales one.  Nothing is read out of a page's
   // range, and without a page all is 0.  The two tiles of 16 tokens of a step lie in one page, or
   // with pages of 16 in two.
@@ -229,6 +155,90 @@ __global__ __launch_bounds__(kBlock, (few_waves<T, NB, CT>())) void attend_few_k
     }
   };
 
+  const int hi = span.base + span.n;
+  const int end = min(part.end * (kFewKeys / kStep), (hi + kStep - 1) / kStep);
+  int step = part.first * (kFewKeys / kStep) + wave;
+  if (step < end) {  // on their way beside the queries
+    fetch_pages(step);
+    take_pages();
+    fetch(step);
+    if (step + kWaves < end) fetch_pages(step + kWaves);
+  }
+
+  // queries, as 8-bit terms
+  i32x8 qo[CT][F::MMA];
+  int qs[CT][F::MMA];
+  bool q_bad[CT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    const int row = 16 * c + col;
+    const bool live = row < rows;
+    const int t = token_of(live ? row : 0), head = kv * a.group + (live ? row - t * a.group : 0);
+    const T* q = static_cast<const T*>(a.q.data) + b * a.q.batch_stride + t * a.q.token_stride +
+                 int64_t(head) * a.d.head_dim;
+    q_bad[c] = false;
+#pragma unroll
+    for (int f = 0; f < F::FRAGS; ++f) {
+      int byte[2];
+      i32x4 words[2][F::QT];
+      // this lane's halves of 16 channels: of slots g / 2 and 2 + g / 2
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        if (w == 1 && F::NBP <= 2) {  // the same block again
+          byte[1] = byte[0];
+#pragma unroll
+          for (int k = 0; k < F::QT; ++k) words[1][k] = words[0][k];
+          continue;
+        }
+        const int blk = F::NBP == 2 ? g / 2 : F::block(f, 2 * w + g / 2);
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          load4<T>(q, live ? blk * 32 + 16 * (g % 2) + 4 * i : a.d.head_dim, a.d.head_dim, a.wide,
+                   v + 4 * i);
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          v[i] *= a.q_sign;
+          most = max(most, __float_as_uint(v[i]) & 0x7fffffffu);
+        }
+        most = max(most, uint32_t(__shfl_xor(int(most), 16)));
+        const bool bad = most >= 0x7f800000u;
+        q_bad[c] |= bad;
+        byte[w] = bad ? 127 : query_scale(most);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = bad ? 0.f : v[i];
+        to_terms<F::QT>(v, byte[w], words[w]);
+      }
+      // scales: of slot g, which lanes of group 2 (g % 2) have
+      const int b0 = __shfl(byte[0], col + 32 * (g % 2)), b1 = __shfl(byte[1], col + 32 * (g % 2));
+      const int mine = g / 2 ? b1 : b0;
+#pragma unroll
+      for (int k = 0; k < F::MMA / F::FRAGS; ++k) {
+        const int j = k * F::FRAGS + f;
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if constexpr (F::NBP >= 4) {
+              qo[c][j][4 * w + i] = words[w][k][i];
+            } else if constexpr (F::NBP == 2) {
+              qo[c][j][4 * w + i] = words[w][2 * k + w][i];
+            } else {
+              const int t0 = 4 * k + 2 * w;
+              const int lo = t0 < F::QT ? words[w][t0 < F::QT ? t0 : 0][i] : 0;
+              const int hi = t0 + 1 < F::QT ? words[w][t0 + 1 < F::QT ? t0 + 1 : 0][i] : 0;
+              qo[c][j][4 * w + i] = g / 2 ? hi : lo;
+            }
+          }
+        qs[c][j] = mine - 4 * (F::NBP >= 4 ? k : F::NBP == 2 ? 2 * k + g / 2 : 4 * k + g);
+      }
+    }
+    // all lanes of a column
+    q_bad[c] |= __shfl_xor(int(q_bad[c]), 16) != 0;
+    q_bad[c] |= __shfl_xor(int(q_bad[c]), 32) != 0;
+  }
+
   f32x4 o[CT][NB * 2];
   float m[CT], l[CT];
   int E = 0;
@@ -239,7 +249,6 @@ __global__ __launch_bounds__(kBlock, (few_waves<T, NB, CT>())) void attend_few_k
 #pragma unroll
     for (int i = 0; i < NB * 2; ++i) o[c][i] = f32x4{};
   }
-  const int hi = span.base + span.n;
   const int lo_all = span.lo(a, span.n - 1), hi_all = span.base;  // that all rows see
   int my_lo[CT], my_hi[CT];
 #pragma unroll
@@ -249,14 +258,6 @@ __global__ __launch_bounds__(kBlock, (few_waves<T, NB, CT>())) void attend_few_k
     my_hi[c] = row < rows ? span.base + t : -1;
   }
   _Float16* vbuf = lds[wave].v;
-  const int end = min(part.end * (kFewKeys / kStep), (hi + kStep - 1) / kStep);
-  int step = part.first * (kFewKeys / kStep) + wave;
-  if (step < end) {
-    fetch_pages(step);
-    take_pages();
-    fetch(step);
-    if (step + kWaves < end) fetch_pages(step + kWaves);
-  }
   for (; step < end; step += kWaves) {
     const int pos0 = step * kStep;
     const int pages = (page[0] >= 0) | (page[1] >= 0) << 1;

@@ -22,6 +22,8 @@ struct CacheArgs {
   int32_t T;
   PageHead lay;
   int64_t page_bytes;
+  int32_t page_shift;
+  FastDiv by_W, by_row;  // a row: the quarter blocks of a token
 };
 
 // The scale byte of a block whose largest magnitude has the float32 bits `most`; codes follow it:
@@ -70,84 +72,108 @@ __device__ __forceinline__ void store8(T* row, int c, int D, const float (&v)[8]
   }
 }
 
-// blockIdx: tile of the call's positions, kv head and K or V, stream.
+// blockIdx: tile of the call's positions, kv head, stream.
 template <typename T, bool WIDE>
 __global__ __launch_bounds__(kBlock) void append_kernel(CacheArgs a) {
-  const int b = blockIdx.z, which = blockIdx.y & 1, h = blockIdx.y >> 1;
+  const int b = blockIdx.z, h = blockIdx.y;
   const int P = a.lay.P, NB = a.lay.NB, D = a.d.head_dim;
   const int n = stream_tokens(a.c.granted, b, a.T);
   const int64_t base = a.c.base[b];
   const int64_t pos0 = (base / kCacheTile + blockIdx.x) * kCacheTile;
   if (base < 0 || pos0 >= base + n) return;
-  const int page = a.c.table[int64_t(b) * a.d.stream_pages + pos0 / P % a.d.stream_pages];
+  const int lp = int(pos0 >> a.page_shift);
+  const int page = a.c.table[int64_t(b) * a.d.stream_pages + lp - fdiv(lp, a.by_W) * a.d.stream_pages];
   if (page < 0 || page >= a.d.pages) return;
   char* head = static_cast<char*>(a.c.pool) + page * a.page_bytes + int64_t(h) * a.lay.bytes();
-  const int tile = int(pos0 % P) / kCacheTile;
-  char* codes = head + a.lay.codes(which) + tile * a.lay.tile_bytes();
-  char* scales = head + a.lay.scales(which) + tile * NB * kCacheTile;
-  const co_tokens& io = a.kv[which];
-  const T* x = static_cast<const T*>(io.data) + b * io.batch_stride + int64_t(h) * D;
-  for (int i = threadIdx.x; i < kCacheTile * NB * 4; i += kBlock) {
-    const int tok = i / (NB * 4), rest = i - tok * NB * 4, block = rest / 4, quad = rest % 4;
-    const int64_t t = pos0 + tok - base;
-    if (t < 0 || t >= n) continue;  // the four lanes of a block alike
-    float v[8];
-    load8<T, WIDE>(x + t * io.token_stride, block * kCacheBlock + quad * 8, D, v);
-    uint32_t most = 0;
+  const int tile = int(pos0 & (P - 1)) / kCacheTile;
+  const int first = int(base - pos0), end = int(min(base + n - pos0, int64_t(kCacheTile)));
+  const T* x[2];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) most = max(most, __float_as_uint(v[k]) & 0x7fffffffu);
-    most = max(most, uint32_t(__shfl_xor(int(most), 1)));
-    most = max(most, uint32_t(__shfl_xor(int(most), 2)));
-    const int s = scale_byte(most);
-    uint32_t code = 0;
-    if (s != 255) {
-      const float scale = scale_of(s);
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[0], v[1], scale, 0);
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[2], v[3], scale, 1);
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[4], v[5], scale, 2);
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[6], v[7], scale, 3);
+  for (int w = 0; w < 2; ++w)
+    x[w] = static_cast<const T*>(a.kv[w].data) + b * a.kv[w].batch_stride + int64_t(h) * D -
+           first * a.kv[w].token_stride;
+  for (int i = threadIdx.x; i < kCacheTile * NB * 4; i += kBlock) {
+    const int tok = fdiv(i, a.by_row), rest = i - tok * NB * 4, block = rest / 4, quad = rest % 4;
+    if (tok < first || tok >= end) continue;  // the four lanes of a block alike
+    float v[2][8];
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+      load8<T, WIDE>(x[w] + tok * a.kv[w].token_stride, block * kCacheBlock + quad * 8, D, v[w]);
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      uint32_t most = 0;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) most = max(most, __float_as_uint(v[w][k]) & 0x7fffffffu);
+      most = max(most, uint32_t(__shfl_xor(int(most), 1)));
+      most = max(most, uint32_t(__shfl_xor(int(most), 2)));
+      const int s = scale_byte(most);
+      uint32_t code = 0;
+      if (s != 255) {
+        const float scale = scale_of(s);
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[w][0], v[w][1], scale, 0);
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[w][2], v[w][3], scale, 1);
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[w][4], v[w][5], scale, 2);
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[w][6], v[w][7], scale, 3);
+      }
+      const int at = block * kCacheTile + tok;
+      *reinterpret_cast<uint32_t*>(head + a.lay.codes(w) + tile * a.lay.tile_bytes() + at * 16 +
+                                   quad * 4) = code;
+      if (quad == 0) head[a.lay.scales(w) + tile * NB * kCacheTile + at] = char(s);
     }
-    *reinterpret_cast<uint32_t*>(codes + (block * kCacheTile + tok) * 16 + quad * 4) = code;
-    if (quad == 0) scales[block * kCacheTile + tok] = char(s);
   }
 }
 
-// blockIdx: 16 of the call's tokens, kv head and K or V, stream.
+// 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives, times the scale: exact in float32.
+__device__ __forceinline__ void decode8(uint32_t code, float scale, float (&v)[8]) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, scale, 0);
+  const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, scale, 1);
+  const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, scale, 2);
+  const f32x2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, scale, 3);
+  v[0] = a[0], v[1] = a[1], v[2] = b[0], v[3] = b[1];
+  v[4] = c[0], v[5] = c[1], v[6] = d[0], v[7] = d[1];
+}
+
+// blockIdx: 16 of the call's tokens, kv head, stream.
 template <typename T, bool WIDE>
 __global__ __launch_bounds__(kBlock) void read_kernel(CacheArgs a) {
-  const int b = blockIdx.z, which = blockIdx.y & 1, h = blockIdx.y >> 1;
+  const int b = blockIdx.z, h = blockIdx.y;
   const int P = a.lay.P, NB = a.lay.NB, D = a.d.head_dim;
   const int64_t lowest = a.c.first ? max(a.c.first[b], 0) : 0;
   const int64_t end = int64_t(a.c.base[b]) + max(a.c.granted[b], 0), from = a.from[b];
-  const co_tokens& io = a.kv[which];
-  T* y = static_cast<T*>(io.data) + b * io.batch_stride + int64_t(h) * D;
+  T* y[2];
+#pragma unroll
+  for (int w = 0; w < 2; ++w)
+    y[w] = static_cast<T*>(a.kv[w].data) + b * a.kv[w].batch_stride + int64_t(h) * D;
   for (int i = threadIdx.x; i < kCacheTile * NB * 4; i += kBlock) {
-    const int tok = i / (NB * 4), rest = i - tok * NB * 4, block = rest / 4, quad = rest % 4;
+    const int tok = fdiv(i, a.by_row), rest = i - tok * NB * 4, block = rest / 4, quad = rest % 4;
     const int64_t t = int64_t(blockIdx.x) * kCacheTile + tok, pos = from + t;
     if (t >= a.T) continue;
     int page = -1;
-    if (pos >= lowest && pos < end)
-      page = a.c.table[int64_t(b) * a.d.stream_pages + pos / P % a.d.stream_pages];
-    float v[8] = {};
+    if (pos >= lowest && pos < end && pos <= INT32_MAX) {
+      const int lp = int(pos) >> a.page_shift;
+      page = a.c.table[int64_t(b) * a.d.stream_pages + lp - fdiv(lp, a.by_W) * a.d.stream_pages];
+    }
+    float v[2][8] = {};
     if (page >= 0 && page < a.d.pages) {
       const char* head =
           static_cast<const char*>(a.c.pool) + page * a.page_bytes + int64_t(h) * a.lay.bytes();
-      const int in = int(pos % P), tile = in / kCacheTile, at = block * kCacheTile + in % kCacheTile;
-      const uint32_t code = *reinterpret_cast<const uint32_t*>(
-          head + a.lay.codes(which) + tile * a.lay.tile_bytes() + at * 16 + quad * 4);
-      const int s = uint8_t(head[a.lay.scales(which) + tile * NB * kCacheTile + at]);
-      const float scale = s == 255 ? __builtin_nanf("") : scale_of(s);
+      const int in = int(pos) & (P - 1), tile = in / kCacheTile;
+      const int at = block * kCacheTile + in % kCacheTile;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        // 0, 0.5, 1, 1.5, 2, 3, 4, 6: one bit of mantissa, exponents from -1, 0 and 0.5 below
-        const int c = code >> (4 * k), m = c & 7;
-        const float value = m < 2 ? 0.5f * m
-                                  : __uint_as_float(uint32_t(126 + (m >> 1)) << 23 |
-                                                    uint32_t(m & 1) << 22);
-        v[k] = (c & 8 ? -value : value) * scale;
+      for (int w = 0; w < 2; ++w) {
+        const uint32_t code = *reinterpret_cast<const uint32_t*>(
+            head + a.lay.codes(w) + tile * a.lay.tile_bytes() + at * 16 + quad * 4);
+        const int s = uint8_t(head[a.lay.scales(w) + tile * NB * kCacheTile + at]);
+        decode8(code, s == 255 ? __builtin_nanf("") : scale_of(s), v[w]);
+        if (s == 255)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[w][k] = __builtin_nanf("");
       }
     }
-    store8<T, WIDE>(y + t * io.token_stride, block * kCacheBlock + quad * 8, D, v);
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+      store8<T, WIDE>(y[w] + t * a.kv[w].token_stride, block * kCacheBlock + quad * 8, D, v[w]);
   }
 }
 
@@ -156,6 +182,9 @@ CacheArgs args(const co_attn_desc& d, const co_attn_cache& c, const co_tokens& k
   CacheArgs a{d, c, {k, v}, nullptr, T};
   a.lay = {d.page_tokens, cache_blocks(d.head_dim)};
   a.page_bytes = int64_t(a.lay.bytes()) * d.kv_heads;
+  while ((1 << a.page_shift) < d.page_tokens) ++a.page_shift;
+  a.by_W = make_fastdiv(d.stream_pages);
+  a.by_row = make_fastdiv(a.lay.NB * 4);
   return a;
 }
 
@@ -173,7 +202,7 @@ bool wide(const CacheArgs& a) {
 hipError_t launch_attn_append(const co_attn_desc& d, const co_attn_cache& c, const co_tokens& k,
                               const co_tokens& v, int32_t T, hipStream_t stream) {
   const CacheArgs a = args(d, c, k, v, T);
-  const dim3 grid(unsigned((int64_t(T) + kCacheTile - 2) / kCacheTile + 1), unsigned(d.kv_heads) * 2,
+  const dim3 grid(unsigned((int64_t(T) + kCacheTile - 2) / kCacheTile + 1), unsigned(d.kv_heads),
                   unsigned(d.batch));
   if (d.dtype == CO_BF16) {
     if (wide(a)) append_kernel<bf16_t, true><<<grid, kBlock, 0, stream>>>(a);
@@ -189,7 +218,7 @@ hipError_t launch_attn_read(const co_attn_desc& d, const co_attn_cache& c, const
                             const co_tokens& k, const co_tokens& v, int32_t T, hipStream_t stream) {
   CacheArgs a = args(d, c, k, v, T);
   a.from = from;
-  const dim3 grid(unsigned((int64_t(T) + kCacheTile - 1) / kCacheTile), unsigned(d.kv_heads) * 2,
+  const dim3 grid(unsigned((int64_t(T) + kCacheTile - 1) / kCacheTile), unsigned(d.kv_heads),
                   unsigned(d.batch));
   if (d.dtype == CO_BF16) {
     if (wide(a)) read_kernel<bf16_t, true><<<grid, kBlock, 0, stream>>>(a);

@@ -96,7 +96,6 @@ __global__ __launch_bounds__(kOne) void reserve_kernel(PagesArgs a) {
     if (refused) a.s.refused[b] += refused;
     a.copies[2 * b] = -1;
   }
-  __threadfence();
   __syncthreads();
   // pages wanted: rank by stream and position
   const int64_t items = int64_t(B) * a.most;
@@ -138,7 +137,6 @@ __global__ __launch_bounds__(kOne) void reserve_kernel(PagesArgs a) {
     found += total;
   }
   found = min(found, wanted);
-  __threadfence();
   __syncthreads();
   for (int b = tid; b < B; b += kOne) {
     const int n = a.s.granted[b];
@@ -151,7 +149,6 @@ __global__ __launch_bounds__(kOne) void reserve_kernel(PagesArgs a) {
       a.s.refused[b] += n;
     }
   }
-  __threadfence();
   __syncthreads();
   for (int64_t i = tid; i < items; i += kOne) {
     const int rank = a.rank[i];
@@ -272,24 +269,22 @@ __global__ __launch_bounds__(kBlock) void select_store_kernel(PagesArgs a, const
   }
 }
 
-// Which pages move where: one workgroup.  moves: their number, then (from, to) each; name: the new
-// index of each page that moves.
+// Which pages move where: one workgroup.  moves: their number, then (from, to) each; rank: which of
+// them a page is.
 __global__ __launch_bounds__(kOne) void compact_plan_kernel(PagesArgs a, int32_t* moves,
-                                                            int32_t* name) {
+                                                            int32_t* rank) {
   __shared__ int scratch[kOne / 64];
   constexpr int EACH = 8;
   const int n = a.d.pages, tid = threadIdx.x;
-  int used = 0;
+  int mine_used = 0, used;
   for (int p0 = 0; p0 < n; p0 += EACH * kOne) {
-    int mine = 0, total;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-      const int p = p0 + EACH * tid + i;
-      mine += p < n && a.s.refs[min(p, n - 1)] > 0;
+      const int p = p0 + i * kOne + tid;
+      mine_used += p < n && a.s.refs[min(p, n - 1)] > 0;
     }
-    prefix_before(mine, scratch, total);
-    used += total;
   }
+  prefix_before(mine_used, scratch, used);
   // the k-th free page below `used` takes the k-th used one above
   int holes = 0, movers = 0;
   for (int p0 = 0; p0 < n; p0 += EACH * kOne) {
@@ -307,21 +302,15 @@ __global__ __launch_bounds__(kOne) void compact_plan_kernel(PagesArgs a, int32_t
     for (int i = 0; i < EACH; ++i) {
       const int p = p0 + EACH * tid + i;
       if (!pick[i]) continue;
-      if (p < used)
-        moves[1 + 2 * hole++ + 1] = p;
-      else
+      if (p < used) {
+        moves[2 + 2 * hole++] = p;
+      } else {
+        rank[p] = mover;
         moves[1 + 2 * mover++] = p;
+      }
     }
     holes += total & 0xffff;
     movers += total >> 16;
-  }
-  __threadfence();
-  __syncthreads();
-  for (int i = tid; i < movers; i += kOne) {
-    const int from = moves[1 + 2 * i], to = moves[2 + 2 * i];
-    name[from] = to;
-    a.s.refs[to] = a.s.refs[from];
-    a.s.refs[from] = 0;
   }
   if (tid == 0) moves[0] = movers;
 }
@@ -330,7 +319,7 @@ constexpr int kPiece = 16384;  // bytes that a workgroup moves at a time
 
 // Moves the pages and names them anew in the table.
 __global__ __launch_bounds__(kBlock) void compact_move_kernel(PagesArgs a, const int32_t* moves,
-                                                              const int32_t* name,
+                                                              const int32_t* rank,
                                                               int64_t page_bytes) {
   const int count = moves[0];
   if (count == 0) return;
@@ -339,7 +328,14 @@ __global__ __launch_bounds__(kBlock) void compact_move_kernel(PagesArgs a, const
   for (int64_t i = blockIdx.x * int64_t(kBlock) + threadIdx.x; i < n;
        i += int64_t(gridDim.x) * kBlock) {
     const int page = a.s.table[i];
-    if (page >= used_first && page < a.d.pages) a.s.table[i] = name[page];
+    if (page < used_first || page >= a.d.pages) continue;
+    const int k = rank[page];  // anything, for a page that nobody counts
+    if (k >= 0 && k < count && moves[1 + 2 * k] == page) a.s.table[i] = moves[2 + 2 * k];
+  }
+  for (int i = blockIdx.x * kBlock + threadIdx.x; i < count; i += gridDim.x * kBlock) {
+    const int from = moves[1 + 2 * i];
+    a.s.refs[moves[2 + 2 * i]] = a.s.refs[from];
+    a.s.refs[from] = 0;
   }
   const int pieces = int((page_bytes + kPiece - 1) / kPiece);
   const int64_t units = int64_t(count) * a.d.layers * pieces;
@@ -374,7 +370,7 @@ int64_t page_bytes(const co_pages_desc& d) {
 }
 
 // reserve: ranks and a list, of a page a table entry and one more a stream at most, and copies;
-// select: rows, tokens, firsts; compact: moves and names.
+// select: rows, tokens, firsts; compact: moves and ranks.
 int64_t pages_workspace(const co_pages_desc& d) {
   const int64_t B = d.batch, items = B * (d.stream_pages + 1);
   return round16(4 * std::max(2 * items + 2 * B, 3 * int64_t(d.pages) + 1));
@@ -418,9 +414,9 @@ hipError_t launch_pages_select(const co_pages_desc& d, const co_pages& s, const 
 hipError_t launch_pages_compact(const co_pages_desc& d, const co_pages& s, hipStream_t stream) {
   const PagesArgs a{d, s, nullptr, 0, 0};
   int32_t* moves = static_cast<int32_t*>(s.workspace);
-  int32_t* name = moves + 2 * int64_t(d.pages) + 1;
-  compact_plan_kernel<<<1, kOne, 0, stream>>>(a, moves, name);
-  compact_move_kernel<<<2048, kBlock, 0, stream>>>(a, moves, name, page_bytes(d));
+  int32_t* rank = moves + 2 * int64_t(d.pages) + 1;
+  compact_plan_kernel<<<1, kOne, 0, stream>>>(a, moves, rank);
+  compact_move_kernel<<<2048, kBlock, 0, stream>>>(a, moves, rank, page_bytes(d));
   return hipGetLastError();
 }
 
