@@ -1696,14 +1696,13 @@ class Mixer:
 # calls, one thread a layer.
 
 
-def _enqueue(device, what, fn, *args):
-    """Calls an entry point on the current stream of the layer's device."""
-    if _current_device is not None and torch.cuda.is_initialized() and \
-            _current_device() == device.index:
-        st = fn(*args, _stream())
+def _enqueue(index, what, fn, *args):
+    """Calls an entry point on the current stream of a layer's GPU."""
+    if _current_raw_stream is not None and _current_device() == index:
+        st = fn(*args, _current_raw_stream(index))
     else:
-        with torch.cuda.device(device):
-            st = fn(*args, _stream())
+        with torch.cuda.device(index):
+            st = fn(*args, torch.cuda.current_stream(index).cuda_stream)
     if st != CO_OK:
         check(st, what)
 
@@ -1769,10 +1768,11 @@ class CoRotary:
         self.desc = RotaryDesc(0, I32x2(0, 0), head_dim, self.rotary_dim, self.LAYOUTS[layout],
                                CO_F32, float(magnitude))
         self._call = RotaryCall(turns=_ptr(self._turns))
+        self._x, self._y = tuple(self._call.x), tuple(self._call.y)
         self._args = ctypes.byref(self.desc), ctypes.byref(self._call)
         self._sig = None
 
-    def _check(self, x, k, positions, lengths, out, k_out, step):
+    def _check(self, x, k, positions, out, k_out, step):
         d, call = self.desc, self._call
         if x.dtype not in DTYPES:
             raise ValueError(f"x has dtype {x.dtype}")
@@ -1792,14 +1792,14 @@ class CoRotary:
             if t.dim() != x.dim():
                 raise ValueError(f"{what} has shape {tuple(t.shape)}, expected as x's")
             shape = torch.Size((B, T, t.shape[-2], self.head_dim))
-            _tokens(t, x.dtype, shape, what, call.x[i], self.device)
+            _tokens(t, x.dtype, shape, what, self._x[i], self.device)
             d.heads[i] = t.shape[-2]
             width = t.shape[-2] * self.head_dim
-            call.y[i].batch_stride, call.y[i].token_stride = T * width, width
+            self._y[i].batch_stride, self._y[i].token_stride = T * width, width
             if o is not None:
                 if o.dim() != x.dim():
                     raise ValueError(f"out has shape {tuple(o.shape)}, expected as {what}'s")
-                _tokens(o, x.dtype, shape, "out", call.y[i], self.device)
+                _tokens(o, x.dtype, shape, "out", self._y[i], self.device)
             self._dense.append(t.is_contiguous())
         if positions is not None:
             _on(positions, self.device, "positions")
@@ -1817,20 +1817,20 @@ class CoRotary:
         sig = (step, _key(x), _key(k), _key(positions), _key(out), _key(k_out))
         if sig != self._sig:
             self._sig = None
-            self._check(x, k, positions, lengths, out, k_out, step)
+            self._check(x, k, positions, out, k_out, step)
             self._sig = sig
-        call = self._call
+        call, d = self._call, self.desc
         if out is None:
             out = _like(x) if self._dense[0] else x.new_empty(x.shape)
-        call.x[0].data, call.y[0].data = x.data_ptr(), out.data_ptr()
+        self._x[0].data, self._y[0].data = x.data_ptr(), out.data_ptr()
         if k is not None:
             if k_out is None:
                 k_out = _like(k) if self._dense[1] else k.new_empty(k.shape)
-            call.x[1].data, call.y[1].data = k.data_ptr(), k_out.data_ptr()
+            self._x[1].data, self._y[1].data = k.data_ptr(), k_out.data_ptr()
         call.positions = None if positions is None else positions.data_ptr()
         call.lengths = None if lengths is None else _lengths(lengths, x.shape[0], self.device)
-        if x.numel() or (k is not None and k.numel()):
-            _enqueue(self.device, "co_rotary_forward", co_rotary_forward, *self._args)
+        if call.T and d.batch:
+            _enqueue(self.device.index, "co_rotary_forward", co_rotary_forward, *self._args)
         return out if k is None else (out, k_out)
 
     def forward(self, x, k=None, *, positions=None, lengths=None, out=None, k_out=None):
@@ -1874,7 +1874,7 @@ class CoPages:
         self.desc = PagesDesc(batch, pages, page_tokens, stream_pages, layers, kv_heads, head_dim)
         info = PagesInfo()
         check(co_pages_query(ctypes.byref(self.desc), ctypes.byref(info)), "co_pages_query")
-        self.page_bytes, self._nws = info.page_bytes, info.workspace_bytes
+        self.page_bytes = info.page_bytes
         state = {} if state is None else dict(state)
         if device is None:
             given = next(iter(state.values()), None)
@@ -1898,6 +1898,9 @@ class CoPages:
             _on(t, self.device, name)
             self._state[name] = t
         self._call = Pages(*(_ptr(self._state[k]) for k in shapes))
+        # as the state, one call's at a time
+        self._ws = torch.empty(info.workspace_bytes, dtype=torch.uint8, device=self.device)
+        self._call.workspace = self._ws.data_ptr()
         self._args = ctypes.byref(self.desc), ctypes.byref(self._call)
         self._T = None  # tokens of the newest reserve
 
@@ -1911,9 +1914,7 @@ class CoPages:
     refused = property(lambda self: self._state["refused"])
 
     def _run(self, what, fn, *args):
-        ws = torch.empty(self._nws, dtype=torch.uint8, device=self.device)
-        self._call.workspace = ws.data_ptr()
-        _enqueue(self.device, what, fn, *self._args, *args)
+        _enqueue(self.device.index, what, fn, *self._args, *args)
 
     def reserve(self, T, lengths=None, keep=0):
         """Pages for the next T tokens of each stream (lengths, as CoShortConv's, of
@@ -1983,8 +1984,9 @@ class CoAttention:
         pool = pages.pool[layer]
         self._cache = AttnCache(_ptr(pool), _ptr(pages.table), _ptr(pages.base),
                                 _ptr(pages.granted), _ptr(pages.first))
-        self._q, self._k, self._v, self._y = (Tokens() for _ in range(4))
-        self._ref = {t: ctypes.byref(getattr(self, t)) for t in ("_q", "_k", "_v", "_y")}
+        self._q, self._k, self._v, self._y, self._rk, self._rv = (Tokens() for _ in range(6))
+        self._ref = {t: ctypes.byref(getattr(self, t))
+                     for t in ("_q", "_k", "_v", "_y", "_rk", "_rv")}
         self._args = ctypes.byref(self.desc), ctypes.byref(self._cache)
         self._append_sig = self._attend_sig = None
 
@@ -2019,7 +2021,7 @@ class CoAttention:
             self._append_sig = sig
         self._k.data, self._v.data = k.data_ptr(), v.data_ptr()
         if self._append_T:
-            _enqueue(self.device, "co_attn_append", co_attn_append, *args, self._ref["_k"],
+            _enqueue(self.device.index, "co_attn_append", co_attn_append, *args, self._ref["_k"],
                      self._ref["_v"], self._append_T)
         return self._append_T
 
@@ -2044,7 +2046,7 @@ class CoAttention:
             ws = torch.empty(self._nws, dtype=torch.uint8, device=self.device)
         self._q.data, self._y.data = q.data_ptr(), out.data_ptr()
         if self._attend_T:
-            _enqueue(self.device, "co_attn_forward_steps", co_attn_forward_steps, *args,
+            _enqueue(self.device.index, "co_attn_forward_steps", co_attn_forward_steps, *args,
                      self._ref["_q"], self._ref["_y"], self._attend_T, _ptr(ws), self._nws)
         return out
 
@@ -2092,10 +2094,13 @@ class CoAttention:
         """What the cache holds at positions first[b] .. first[b] + T - 1 (first int32 on the device) of
         each stream -> keys and values (B, T, kv_heads, D), 0 where it holds nothing."""
         shape = self.batch, T, self.kv_heads, self.head_dim
-        k, v = (torch.empty(shape, dtype=self.torch_dtype, device=self.device) for _ in range(2))
+        k = torch.empty(shape, dtype=self.torch_dtype, device=self.device)
+        v = _like(k)
         width = self.kv_heads * self.head_dim
-        into = [Tokens(t.data_ptr(), T * width, width) for t in (k, v)]
+        for t, into in ((k, self._rk), (v, self._rv)):
+            into.data, into.batch_stride, into.token_stride = t.data_ptr(), T * width, width
         if T:
-            _enqueue(self.device, "co_attn_read", co_attn_read, *self._args,
-                     _lengths(first, self.batch, self.device), *map(ctypes.byref, into), T)
+            _enqueue(self.device.index, "co_attn_read", co_attn_read, *self._args,
+                     _lengths(first, self.batch, self.device), self._ref["_rk"], self._ref["_rv"],
+                     T)
         return k, v

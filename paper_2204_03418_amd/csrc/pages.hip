@@ -269,6 +269,42 @@ __global__ __launch_bounds__(kBlock) void select_store_kernel(PagesArgs a, const
   }
 }
 
+// Both in one workgroup, whose threads hold the new rows.
+constexpr int kHeld = 8;
+__global__ __launch_bounds__(kOne) void select_one_kernel(PagesArgs a, const int32_t* source) {
+  const int B = a.d.batch, P = a.d.page_tokens, W = a.d.stream_pages, n = B * W;
+  const int tid = threadIdx.x;
+  int page[kHeld], tokens = 0, first = 0;
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) {
+    const int i = k * kOne + tid;
+    page[k] = -1;
+    if (i >= n) continue;
+    const int b = i / W, s = i - b * W, from = source[b];
+    if (from < 0 || from >= B) continue;
+    const int end = a.s.tokens[from], low = min(max(a.s.first[from], 0), end);
+    if (int64_t(slot_page(s, low / P, W)) * P < end)
+      page[k] = valid_page(a.s.table[from * W + s], a.d.pages);
+  }
+  if (tid < B && source[tid] >= 0 && source[tid] < B) {
+    tokens = max(a.s.tokens[source[tid]], 0);
+    first = max(a.s.first[source[tid]], 0);
+  }
+  for (int p = tid; p < a.d.pages; p += kOne) ref_store(a.s.refs + p, 0);
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) {
+    const int i = k * kOne + tid;
+    if (i >= n) continue;
+    a.s.table[i] = page[k];
+    if (page[k] >= 0) ref_add(a.s.refs + page[k], 1);
+  }
+  if (tid >= B) return;
+  a.s.tokens[tid] = a.s.base[tid] = tokens;
+  a.s.first[tid] = first;
+  a.s.granted[tid] = 0;
+}
+
 // Which pages move where: one workgroup.  moves: their number, then (from, to) each; rank: which of
 // them a page is.
 __global__ __launch_bounds__(kOne) void compact_plan_kernel(PagesArgs a, int32_t* moves,
@@ -404,6 +440,12 @@ hipError_t launch_pages_select(const co_pages_desc& d, const co_pages& s, const 
                                hipStream_t stream) {
   const PagesArgs a{d, s, nullptr, 0, 0};
   int32_t* rows = static_cast<int32_t*>(s.workspace);
+  // one launch where a workgroup holds the table (64 streams of 34 pages: 3.7 us for 5.8)
+  if (d.batch <= kOne && int64_t(d.batch) * d.stream_pages <= kHeld * kOne &&
+      d.pages <= 16 * kHeld * kOne) {
+    select_one_kernel<<<1, kOne, 0, stream>>>(a, source);
+    return hipGetLastError();
+  }
   const int64_t most = std::max<int64_t>(int64_t(d.batch) * d.stream_pages, d.pages);
   const unsigned grid = unsigned(std::min<int64_t>(grid_for(most), 2048));
   select_gather_kernel<<<grid, kBlock, 0, stream>>>(a, source, rows);

@@ -130,6 +130,8 @@ def test_rotary_refuses():
     with pytest.raises(coinf.CoinfError):
         layer.forward(x, x)                                     # fine, but ...
         layer.forward(x, x.clone(), out=x, k_out=x)             # both into one place
+    with pytest.raises(ValueError):
+        layer.forward(x, x.clone(), k_out=x, positions=None, out=x[:1])
     assert layer.forward(x[:, :0]).shape == (2, 0, 4, 32)
 
 
@@ -207,6 +209,30 @@ def test_pages_and_contents_through_many_calls(P, seed):
                         want[:, b, p] = x
             assert np.array_equal(R.np64(k), want[0]), (step, what)
             assert np.array_equal(R.np64(v), want[1]), (step, what)
+
+
+@pytest.mark.parametrize("N", [9000, 2500])
+def test_pages_of_many_streams(N):
+    """More streams and pages than one workgroup's threads: reserve, fork, truncate, compact."""
+    B, W, P = 1100, 12, 16
+    rng = np.random.default_rng(5)
+    pages, model = make_pages(B, N, W, P, 1, 8), R.Streams(B, N, W, P)
+    for T, keep in ((40, 0), (100, 0), (1, 0), (30, 20), (90, 0)):
+        n = rng.integers(0, T + 1, B)
+        pages.reserve(T, i32(n.tolist()), keep=keep)
+        model.reserve(n.tolist(), keep)
+        same_tables(pages, model)
+        source = np.where(rng.random(B) < 0.5, np.arange(B), rng.integers(-1, B, B))
+        pages.select(i32(source.tolist()))
+        model.select(source.tolist())
+        same_tables(pages, model)
+        to = [int(rng.integers(0, t + 1)) if rng.random() < 0.3 else t for t in model.tokens]
+        pages.truncate(i32(to))
+        model.truncate(to)
+        pages.compact()
+        model.compact()
+        same_tables(pages, model)
+    assert (sum(model.refused) > 0) == (N == 2500)
 
 
 def test_pages_run_out():
