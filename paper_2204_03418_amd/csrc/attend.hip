@@ -114,8 +114,7 @@ hipError_t launch_attend(const co_attn_desc& d, const co_attn_cache& cache, cons
   a.slack = kSlack / a.scale_log2;
   a.group = d.heads / d.kv_heads;
   const Cut c = cut_of(d, T);
-  if (int64_t(T) * a.group + c.rows >= INT32_MAX || c.units() * c.splits >= 1 << 24 ||
-      c.units() * c.rows / 4 >= 1 << 24)
+  if (int64_t(T) * a.group + c.rows >= INT32_MAX || c.units() * c.splits >= 1 << 23)
     return hipErrorInvalidConfiguration;
   a.by_group = make_fastdiv(a.group);
   a.by_W = make_fastdiv(d.stream_pages);

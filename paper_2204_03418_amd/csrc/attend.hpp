@@ -16,6 +16,8 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
@@ -127,7 +129,7 @@ __device__ __forceinline__ float exponent_to_f32(int biased) {
 }
 
 // The 8-bit terms of 16 values, 2^{e - 4 k} the scale of term k: words[k] 16 bytes.  Two hold a
-// bfloat16 exactly down to 2^-17 of the block's largest, six a float32 to 2^-24 of it.
+// bfloat16 exactly down to 2^-17 of the block's largest.
 template <int TERMS>
 __device__ __forceinline__ void to_terms(float (&v)[16], int scale_byte, i32x4 (&words)[TERMS]) {
 #pragma unroll
@@ -155,8 +157,11 @@ __device__ __forceinline__ int query_scale(uint32_t most) {
   return max(int(most >> 23) - 7, 40);
 }
 
+// Scores.  bfloat16: keys as they are against queries in two 8-bit terms, whose instructions sum to about
+// 2^-20 of their largest product.  float32: those sums would be its error (4e-6 to 1e-5 measured), so
+// its keys become bfloat16 (exactly) and its queries three bfloat16 terms (24 bits).
 template <typename T>
-constexpr int kQueryTerms = sizeof(T) == 2 ? 2 : 6;
+constexpr int kQueryTerms = sizeof(T) == 2 ? 2 : 3;
 template <typename T>
 constexpr int kWeightTerms = sizeof(T) == 2 ? 1 : 2;
 
@@ -167,6 +172,28 @@ __device__ __forceinline__ f16x8 decode8(uint32_t w, float scale) {
   const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 2);
   const f16x2 d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 3);
   return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// Eight codes as bfloat16, times 2^{byte - 127}; NaN for 255.
+__device__ __forceinline__ bf16x8 decode8_bf16(uint32_t w, int byte) {
+  const float scale = __uint_as_float(byte == 255 ? 0x7fc00000u : uint32_t(byte) << 23);
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// Eight values as bfloat16 terms.
+template <int TERMS>
+__device__ __forceinline__ void to_bf16_terms(float (&v)[8], bf16x8 (&terms)[TERMS]) {
+#pragma unroll
+  for (int k = 0; k < TERMS; ++k)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      terms[k][i] = __bf16(v[i]);
+      v[i] -= float(terms[k][i]);
+    }
 }
 
 // Four rows of 16 columns of an LDS tile of 16-bit values, turned: lane j of 16 gets column j.

@@ -23,7 +23,13 @@ struct Few {
   // or one of four
   static constexpr int NBP = NB <= 2 ? NB : (NB + 3) / 4 * 4;
   static constexpr int FRAGS = NBP >= 4 ? NBP / 4 : 1;
-  static constexpr int MMA = NBP >= 4 ? QT * FRAGS : NBP == 2 ? QT / 2 : (QT + 3) / 4;
+  // float32: keys as bfloat16, an instruction a term and 8 of a lane's channels
+  static constexpr bool WIDE = sizeof(T) == 4;
+  static constexpr int SUBS = NBP >= 4 ? 4 : NBP;  // of a fragment
+  static constexpr int MMA = WIDE         ? QT * FRAGS * SUBS
+                             : NBP >= 4   ? QT * FRAGS
+                             : NBP == 2   ? QT / 2
+                                          : (QT + 3) / 4;
   static constexpr int CHUNKS = NB * kStep;  // 16 bytes of values of a step
   static constexpr int VC = (CHUNKS + 63) / 64;
   static constexpr int VS = NB * 32 + 16;    // rows 32 bytes beside a multiple of the banks
@@ -166,7 +172,7 @@ __global__ __launch_bounds__(kBlock, (few_waves<T, NB, CT>())) void attend_few_k
   }
 
   // queries, as 8-bit terms
-  i32x8 qo[CT][F::MMA];
+  std::conditional_t<F::WIDE, bf16x8, i32x8> qo[CT][F::MMA];
   int qs[CT][F::MMA];
   bool q_bad[CT];
 #pragma unroll
@@ -177,61 +183,89 @@ __global__ __launch_bounds__(kBlock, (few_waves<T, NB, CT>())) void attend_few_k
     const T* q = static_cast<const T*>(a.q.data) + b * a.q.batch_stride + t * a.q.token_stride +
                  int64_t(head) * a.d.head_dim;
     q_bad[c] = false;
+    if constexpr (F::WIDE) {
+      // the channels that a lane's keys have: 8 of sub m of its block's four eights
 #pragma unroll
-    for (int f = 0; f < F::FRAGS; ++f) {
-      int byte[2];
-      i32x4 words[2][F::QT];
-      // this lane's halves of 16 channels: of slots g / 2 and 2 + g / 2
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        if (w == 1 && F::NBP <= 2) {  // the same block again
-          byte[1] = byte[0];
-#pragma unroll
-          for (int k = 0; k < F::QT; ++k) words[1][k] = words[0][k];
-          continue;
-        }
-        const int blk = F::NBP == 2 ? g / 2 : F::block(f, 2 * w + g / 2);
-        float v[16];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          load4<T>(q, live ? blk * 32 + 16 * (g % 2) + 4 * i : a.d.head_dim, a.d.head_dim, a.wide,
-                   v + 4 * i);
-        uint32_t most = 0;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          v[i] *= a.q_sign;
-          most = max(most, __float_as_uint(v[i]) & 0x7fffffffu);
-        }
-        most = max(most, uint32_t(__shfl_xor(int(most), 16)));
-        const bool bad = most >= 0x7f800000u;
-        q_bad[c] |= bad;
-        byte[w] = bad ? 127 : query_scale(most);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = bad ? 0.f : v[i];
-        to_terms<F::QT>(v, byte[w], words[w]);
-      }
-      // scales: of slot g, which lanes of group 2 (g % 2) have
-      const int b0 = __shfl(byte[0], col + 32 * (g % 2)), b1 = __shfl(byte[1], col + 32 * (g % 2));
-      const int mine = g / 2 ? b1 : b0;
-#pragma unroll
-      for (int k = 0; k < F::MMA / F::FRAGS; ++k) {
-        const int j = k * F::FRAGS + f;
+      for (int i = 0; i < F::FRAGS * F::SUBS; ++i) {
+        const int f = i / F::SUBS, m = i % F::SUBS;
+        const int eight = F::NBP >= 4 ? m : F::NBP == 2 ? 2 * m + g / 2 : g;
+        const int at = F::block(f, g) * 32 + 8 * eight;
+        float v[8];
 #pragma unroll
         for (int w = 0; w < 2; ++w)
+          load4<T>(q, live ? at + 4 * w : a.d.head_dim, a.d.head_dim, a.wide, v + 4 * w);
+        uint32_t most = 0;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if constexpr (F::NBP >= 4) {
-              qo[c][j][4 * w + i] = words[w][k][i];
-            } else if constexpr (F::NBP == 2) {
-              qo[c][j][4 * w + i] = words[w][2 * k + w][i];
-            } else {
-              const int t0 = 4 * k + 2 * w;
-              const int lo = t0 < F::QT ? words[w][t0 < F::QT ? t0 : 0][i] : 0;
-              const int hi = t0 + 1 < F::QT ? words[w][t0 + 1 < F::QT ? t0 + 1 : 0][i] : 0;
-              qo[c][j][4 * w + i] = g / 2 ? hi : lo;
-            }
+        for (int k = 0; k < 8; ++k) {
+          v[k] *= a.q_sign;
+          most = max(most, __float_as_uint(v[k]) & 0x7fffffffu);
+        }
+        const bool bad = most >= 0x7f800000u;
+        q_bad[c] |= bad;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = bad ? 0.f : v[k];
+        bf16x8 terms[F::QT];
+        to_bf16_terms<F::QT>(v, terms);
+#pragma unroll
+        for (int k = 0; k < F::QT; ++k) qo[c][i * F::QT + k] = terms[k];
+      }
+    } else {
+#pragma unroll
+      for (int f = 0; f < F::FRAGS; ++f) {
+        int byte[2];
+        i32x4 words[2][F::QT];
+        // this lane's halves of 16 channels: of slots g / 2 and 2 + g / 2
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          if (w == 1 && F::NBP <= 2) {  // the same block again
+            byte[1] = byte[0];
+#pragma unroll
+            for (int k = 0; k < F::QT; ++k) words[1][k] = words[0][k];
+            continue;
           }
-        qs[c][j] = mine - 4 * (F::NBP >= 4 ? k : F::NBP == 2 ? 2 * k + g / 2 : 4 * k + g);
+          const int blk = F::NBP == 2 ? g / 2 : F::block(f, 2 * w + g / 2);
+          float v[16];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            load4<T>(q, live ? blk * 32 + 16 * (g % 2) + 4 * i : a.d.head_dim, a.d.head_dim, a.wide,
+                     v + 4 * i);
+          uint32_t most = 0;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            v[i] *= a.q_sign;
+            most = max(most, __float_as_uint(v[i]) & 0x7fffffffu);
+          }
+          most = max(most, uint32_t(__shfl_xor(int(most), 16)));
+          const bool bad = most >= 0x7f800000u;
+          q_bad[c] |= bad;
+          byte[w] = bad ? 127 : query_scale(most);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] = bad ? 0.f : v[i];
+          to_terms<F::QT>(v, byte[w], words[w]);
+        }
+        // scales: of slot g, which lanes of group 2 (g % 2) have
+        const int b0 = __shfl(byte[0], col + 32 * (g % 2)), b1 = __shfl(byte[1], col + 32 * (g % 2));
+        const int mine = g / 2 ? b1 : b0;
+#pragma unroll
+        for (int k = 0; k < F::MMA / F::FRAGS; ++k) {
+          const int j = k * F::FRAGS + f;
+#pragma unroll
+          for (int w = 0; w < 2; ++w)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              if constexpr (F::NBP >= 4) {
+                qo[c][j][4 * w + i] = words[w][k][i];
+              } else if constexpr (F::NBP == 2) {
+                qo[c][j][4 * w + i] = words[w][2 * k + w][i];
+              } else {
+                const int t0 = 4 * k + 2 * w;
+                const int lo = t0 < F::QT ? words[w][t0 < F::QT ? t0 : 0][i] : 0;
+                const int hi = t0 + 1 < F::QT ? words[w][t0 + 1 < F::QT ? t0 + 1 : 0][i] : 0;
+                qo[c][j][4 * w + i] = g / 2 ? hi : lo;
+              }
+            }
+          qs[c][j] = mine - 4 * (F::NBP >= 4 ? k : F::NBP == 2 ? 2 * k + g / 2 : 4 * k + g);
+        }
       }
     }
     // all lanes of a column
@@ -264,18 +298,38 @@ __global__ __launch_bounds__(kBlock, (few_waves<T, NB, CT>())) void attend_few_k
     // scores: the keys are used up first
     f32x4 sc[CT][2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < 2; ++i) {
 #pragma unroll
-      for (int c = 0; c < CT; ++c) {
-        sc[c][i] = f32x4{};
+      for (int c = 0; c < CT; ++c) sc[c][i] = f32x4{};
+      if constexpr (F::WIDE) {
 #pragma unroll
-        for (int j = 0; j < F::MMA; ++j) {
-          const i32x4 w = rk[i][j % F::FRAGS];
-          sc[c][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-              i32x8{w[0], w[1], w[2], w[3], 0, 0, 0, 0}, qo[c][j], sc[c][i], 4, 0, 0,
-              rks[i][j % F::FRAGS], 0, qs[c][j]);
+        for (int n = 0; n < F::FRAGS * F::SUBS; ++n) {
+          const i32x4 w = rk[i][n / F::SUBS];
+          const int m = n % F::SUBS;
+          const int eight = F::NBP >= 4   ? w[m]
+                            : F::NBP == 2 ? (g / 2 ? w[2 * m + 1] : w[2 * m])
+                            : g / 2       ? (g % 2 ? w[3] : w[2])
+                                          : (g % 2 ? w[1] : w[0]);
+          const bf16x8 key = decode8_bf16(eight, rks[i][n / F::SUBS]);
+#pragma unroll
+          for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int k = F::QT - 1; k >= 0; --k)  // the lowest terms first
+              sc[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, qo[c][n * F::QT + k],
+                                                                 sc[c][i], 0, 0, 0);
         }
+      } else {
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+          for (int j = F::MMA - 1; j >= 0; --j) {  // the lowest terms first
+            const i32x4 w = rk[i][j % F::FRAGS];
+            sc[c][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                i32x8{w[0], w[1], w[2], w[3], 0, 0, 0, 0}, qo[c][j], sc[c][i], 4, 0, 0,
+                rks[i][j % F::FRAGS], 0, qs[c][j]);
+          }
       }
+    }
     // values, as 16-bit floats into LDS
     if (pos0 < span.lowest || pos0 + kStep > hi) {  // of the stream's own tokens
 #pragma unroll

@@ -21,8 +21,11 @@ template <typename T, int NB, int W>
 struct Rows {
   static constexpr int KEYS = kCacheTile * W, HALVES = KEYS / 32;
   static constexpr int QT = kQueryTerms<T>, PT = kWeightTerms<T>;
+  // float32: keys as bfloat16, products from 0
+  static constexpr bool WIDE = sizeof(T) == 4;
   static constexpr bool EVEN = NB % 2 == 0;
-  static constexpr int MMA = QT * NB / 2;           // of a 32 x 32 tile of scores, depth 64
+  // of a 32 x 32 tile of scores: depth 64, or 16
+  static constexpr int MMA = WIDE ? QT * NB * 2 : QT * NB / 2;
   static constexpr int FRAGS = EVEN ? NB / 2 : NB;  // of keys
   static constexpr int CHUNKS = NB * kCacheTile;    // 16 bytes of codes of 16 tokens
   static constexpr int PER = (CHUNKS + 63) / 64;
@@ -98,38 +101,67 @@ __global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_r
   const bool live = row < rows;
   const T* q = static_cast<const T*>(a.q.data) + b * a.q.batch_stride +
                int64_t(live ? t : 0) * a.q.token_stride + int64_t(live ? head : 0) * a.d.head_dim;
-  i32x8 qo[R::MMA];
+  std::conditional_t<R::WIDE, bf16x8, i32x8> qo[R::MMA];
   int qs[R::MMA];
   bool q_bad = false;
+  if constexpr (R::WIDE) {
+    // instruction f, m, term: this half's channels 8 m of block 2 f + half, or 16 m + 8 half of block f
 #pragma unroll
-  for (int blk = 0; blk < NB; ++blk) {
-    float v[16];
+    for (int i = 0; i < R::MMA / R::QT; ++i) {
+      const int c = R::EVEN ? 64 * (i / 4) + 32 * half + 8 * (i % 4)
+                            : 32 * (i / 2) + 16 * (i % 2) + 8 * half;
+      float v[8];
 #pragma unroll
-    for (int w = 0; w < 4; ++w)
-      load4<T>(q, live ? blk * 32 + 16 * half + 4 * w : a.d.head_dim, a.d.head_dim, a.wide, v + 4 * w);
-    uint32_t most = 0;
+      for (int w = 0; w < 2; ++w)
+        load4<T>(q, live ? c + 4 * w : a.d.head_dim, a.d.head_dim, a.wide, v + 4 * w);
+      uint32_t most = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      v[i] *= a.q_sign;
-      most = max(most, __float_as_uint(v[i]) & 0x7fffffffu);
+      for (int k = 0; k < 8; ++k) {
+        v[k] *= a.q_sign;
+        most = max(most, __float_as_uint(v[k]) & 0x7fffffffu);
+      }
+      const bool bad = most >= 0x7f800000u;
+      q_bad |= bad;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = bad ? 0.f : v[k];
+      bf16x8 terms[R::QT];
+      to_bf16_terms<R::QT>(v, terms);
+#pragma unroll
+      for (int k = 0; k < R::QT; ++k) qo[i * R::QT + k] = terms[k];
     }
-    most = max(most, uint32_t(__shfl_xor(int(most), 32)));
-    const bool bad = most >= 0x7f800000u;
-    q_bad |= bad;
-    const int byte = bad ? 127 : query_scale(most);
+    q_bad |= __shfl_xor(int(q_bad), 32) != 0;
+  } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = bad ? 0.f : v[i];
-    i32x4 words[R::QT];
-    to_terms<R::QT>(v, byte, words);
+    for (int blk = 0; blk < NB; ++blk) {
+      float v[16];
 #pragma unroll
-    for (int j = 0; j < R::MMA; ++j) {
+      for (int w = 0; w < 4; ++w)
+        load4<T>(q, live ? blk * 32 + 16 * half + 4 * w : a.d.head_dim, a.d.head_dim, a.wide,
+                 v + 4 * w);
+      uint32_t most = 0;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if (R::block(j, h) != blk) continue;
-        const i32x4 w = words[R::term(j, h)];
+      for (int i = 0; i < 16; ++i) {
+        v[i] *= a.q_sign;
+        most = max(most, __float_as_uint(v[i]) & 0x7fffffffu);
+      }
+      most = max(most, uint32_t(__shfl_xor(int(most), 32)));
+      const bool bad = most >= 0x7f800000u;
+      q_bad |= bad;
+      const int byte = bad ? 127 : query_scale(most);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) qo[j][4 * h + i] = w[i];
-        if (h == half) qs[j] = byte - 4 * R::term(j, h);
+      for (int i = 0; i < 16; ++i) v[i] = bad ? 0.f : v[i];
+      i32x4 words[R::QT];
+      to_terms<R::QT>(v, byte, words);
+#pragma unroll
+      for (int j = 0; j < R::MMA; ++j) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (R::block(j, h) != blk) continue;
+          const i32x4 w = words[R::term(j, h)];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) qo[j][4 * h + i] = w[i];
+          if (h == half) qs[j] = byte - 4 * R::term(j, h);
+        }
       }
     }
   }
@@ -212,7 +244,7 @@ __global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_r
   f32x16 o[NB];
 #pragma unroll
   for (int i = 0; i < NB; ++i) o[i] = f32x16{};
-  // The row's reference score, and its sum.  The products begin at -reference (all 16 alike): what
+  // Minus the row's reference score, and its sum.  The products begin there (all 16 alike): what
   // they give is the difference.  over: what a difference may reach, everything before the first.
   f32x16 below = f32x16{};
   float l[2] = {0.f, 0.f}, over = -3e38f;
@@ -279,21 +311,34 @@ __global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_r
   // Scores of 32 keys (a half): those of two halves are held, and the largest of the newer one's.
   f32x16 sc[2];
   float top[2];  // of even and odd ones
-  i32x8 kf[R::FRAGS];
+  i32x4 kf[R::FRAGS];
   int ks[R::FRAGS];
   const auto load_keys = [&](int h, int slot) {
 #pragma unroll
     for (int f = 0; f < R::FRAGS; ++f) {
       const int blk = R::EVEN ? 2 * f + half : f;
       const int at = ((2 * h + col / 16) * NB + blk) * 16 + col % 16;
-      const i32x4 w = *reinterpret_cast<const i32x4*>(s.k[slot] + at * 16);
-      kf[f] = i32x8{w[0], w[1], w[2], w[3], 0, 0, 0, 0};
+      kf[f] = *reinterpret_cast<const i32x4*>(s.k[slot] + at * 16);
       ks[f] = s.ks[slot][at];
     }
   };
-  const auto score = [&](int g, int j) {  // instruction j of them
-    sc[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-        kf[j % R::FRAGS], qo[j], j ? sc[g] : below, 4, 0, 0, ks[j % R::FRAGS], 0, qs[j]);
+  bf16x8 key;
+  const auto score = [&](int g, int i) {  // instruction i of them: the lowest terms first
+    const f32x16 from = i ? sc[g] : R::WIDE ? f32x16{} : below;
+    if constexpr (R::WIDE) {
+      const int sub = i / R::QT, f = R::EVEN ? sub / 4 : sub / 2;
+      if (i % R::QT == 0)
+        key = decode8_bf16(R::EVEN ? kf[f][sub % 4] : half ? kf[f][sub % 2 * 2 + 1]
+                                                           : kf[f][sub % 2 * 2], ks[f]);
+      sc[g] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key, qo[sub * R::QT + R::QT - 1 - i % R::QT],
+                                                      from, 0, 0, 0);
+    } else {
+      const int j = R::MMA - 1 - i;
+      const i32x4 k = kf[j % R::FRAGS];
+      sc[g] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+          i32x8{k[0], k[1], k[2], k[3], 0, 0, 0, 0}, qo[j], from, 4, 0, 0, ks[j % R::FRAGS], 0,
+          qs[j]);
+    }
   };
   const auto largest = [&](int g, int i0, int i1) {
 #pragma unroll
@@ -314,7 +359,8 @@ __global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_r
     }
     const uint32_t all = __float_as_uint(fmaxf(top[0], top[1]));
     const auto both = __builtin_amdgcn_permlane32_swap(all, all, false, false);
-    const float high = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+    const float high = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) +
+                       (R::WIDE ? below[0] : 0.f);
     if (__any(high > over)) {
       const float more = high > over ? high : 0.f;
       const float down = over < 0.f ? 1.f : exp2_fast(-more * a.scale_log2);
@@ -324,8 +370,8 @@ __global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_r
 #pragma unroll
       for (int i = 0; i < NB; ++i) o[i] *= down;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        sc[g][i] -= more;
+      for (int i = 0; i < (R::WIDE ? 1 : 16); ++i) {
+        if (!R::WIDE) sc[g][i] -= more;
         below[i] -= more;
       }
     }
@@ -356,7 +402,8 @@ __global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_r
     const auto weigh = [&](int stage) {
 #pragma unroll
       for (int i = 4 * stage; i < 4 * stage + 4; ++i)
-        if (i < 16) x[i] = fmaf(sc[g][i], a.scale_log2, kLift);
+        if (i < 16)
+          x[i] = fmaf(R::WIDE ? sc[g][i] + below[0] : sc[g][i], a.scale_log2, kLift);
 #pragma unroll
       for (int i = 4 * stage - 4; i < 4 * stage; ++i)
         if (i >= 0 && i < 16) x[i] = exp2_fast(x[i]);
