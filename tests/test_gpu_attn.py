@@ -726,3 +726,17 @@ def test_far_positions_and_a_large_pool():
     pages.tokens.fill_(2 ** 31 - 4096 - 10)
     pages.first.fill_(2 ** 31 - 4096 - 10)
     assert pages.reserve(100).tolist() == [0, 0]                # no bits for them
+
+
+def test_example_streams_equal_clips():
+    import importlib.util
+    import os
+
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples",
+                        "stream_attention.py")
+    spec = importlib.util.spec_from_file_location("stream_attention", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    # as the example's own: single tokens and clips differ by the order of sums, then by roundings of
+    # bfloat16 (2^-8) in three layers and by codes that those move over a border
+    assert example.main(longest=90, tokens=6) < 0.05
