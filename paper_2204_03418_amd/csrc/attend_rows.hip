@@ -250,7 +250,8 @@ __global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_r
   float l[2] = {0.f, 0.f}, over = -3e38f;
   int E = 0;  // the values' exponent, 0: none yet
 
-  // The values into LDS, a quarter of a lane's 32 at a time.
+  // The values into LDS, a quarter of a lane's 32 at a time.  The quarters of a row's blocks change
+  // places by (row / 4) % 4, so that 16 rows' lie in all banks.
   const auto fill_values = [&](int buf, int E, int piece) {
 #pragma unroll
     for (int i = 0; i < R::PER; ++i) {
@@ -260,7 +261,7 @@ __global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_r
       const int e = max(127 + kValueLift + rvs[i] - E, 0);
       const float scale = __uint_as_float(uint32_t(rvs[i] == 0 || rvs[i] == 255 ? 0 : e) << 23);
       _Float16* dst = s.v[buf] + (wave * kCacheTile + c % 16) * R::VS + c / 16 * 32;
-      *reinterpret_cast<f16x8*>(dst + 8 * piece) = decode8(rv[i][piece], scale);
+      *reinterpret_cast<f16x8*>(dst + 8 * (piece ^ c / 4 % 4)) = decode8(rv[i][piece], scale);
     }
   };
   // the values' exponent for a tile
@@ -385,15 +386,17 @@ __global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_r
   const auto advance = [&](int h, int buf, int h_other, int h_keys, int slot_keys, auto&& beside) {
     const int g = h % 2, other = h_other % 2;
     const int j16 = lane % 16;
-    const _Float16* base = s.v[buf] + (32 * h + 4 * half + j16 / 4) * R::VS +
-                           16 * (lane / 16 % 2) + 4 * (j16 % 4);
+    const int quarter = 2 * (lane / 16 % 2) + j16 % 4 / 2;  // of a block, before they change places
+    const _Float16* base = s.v[buf] + (32 * h + 4 * half + j16 / 4) * R::VS + 4 * (j16 % 2);
+    const _Float16* lo = base + 8 * (quarter ^ half);
+    const _Float16* hi = base + 8 * R::VS + 8 * (quarter ^ (2 + half));
     const auto values = [&](int i) {  // 16 keys i / NB, block i % NB
-      const _Float16* v = base + 16 * (i / NB) * R::VS + 32 * (i % NB);
+      const int at = 16 * (i / NB) * R::VS + 32 * (i % NB);
       struct Both {
         s16x4 lo, hi;
       } r;
-      r.lo = turned4(v);
-      r.hi = turned4(v + 8 * R::VS);
+      r.lo = turned4(lo + at);
+      r.hi = turned4(hi + at);
       return __builtin_bit_cast(f16x8, r);
     };
     // weights in four groups of four, each a stage behind the one before: arguments, powers, operands
@@ -511,12 +514,12 @@ __global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_r
         // past the last tile: 0
         const int h1 = (h + 1) % R::HALVES, h2 = (h + 2) % R::HALVES;
         advance(h, buf, h1, h2, h + 2 < R::HALVES ? slot : slot1, [&](int i) {
-          // the next tiles' keys in the first but one half, values in the last, in order
-          if (h == R::HALVES - 2 && i == 0) fill_keys(page2, tile + 2, slot2);
+          // the next tiles' values and keys, as late as may be: they are on their way
           if (h == R::HALVES - 1) {
 #pragma unroll
             for (int k = 4 * i / NB; k < 4 * (i + 1) / NB; ++k)
               fill_values(buf ^ 1, E1, k);
+            if (i == NB - 1) fill_keys(page2, tile + 2, slot2);
           }
         });
       }
