@@ -10,6 +10,8 @@
 // LDS holds and moves a quarter of the bytes.  Values become 16-bit floats in LDS, once a
 // workgroup (exactly, but for what is below 2^-35 of its tile's largest scale), and the
 // weights 16-bit floats with 11 bits (two terms, 22 bits, for float32).
+#include <utility>
+
 #include "attend.hpp"
 
 namespace coinf {
@@ -34,6 +36,16 @@ struct Rows {
   static __device__ int term(int j, int h) { return EVEN ? 2 * j / NB : 2 * (j / NB) + h; }
   static __device__ int block(int j, int h) { return EVEN ? 2 * j % NB + h : j % NB; }
 };
+
+// f(0), f(1), .. f(N - 1), of constants: long bodies too, which loops are not unrolled for.
+template <typename F, int... I>
+__device__ __forceinline__ void each_of(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void each(F&& f) {
+  each_of(f, std::make_integer_sequence<int, N>{});
+}
 
 // Has v made by here.
 __device__ __forceinline__ void hold(float& v) { asm volatile("" : "+v"(v)); }
@@ -432,8 +444,7 @@ __global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_r
             __builtin_amdgcn_mfma_f32_32x32x16_f16(v[i % NB], p[k][i / NB], o[i % NB], 0, 0, 0);
     };
     constexpr int STAGES = 6;
-#pragma unroll
-    for (int j = 0; j < R::MMA; ++j) {
+    each<R::MMA>([&](auto j) {
       score(other, j);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -441,7 +452,7 @@ __global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_r
 #pragma unroll
       for (int i = NB * j / R::MMA; i < NB * (j + 1) / R::MMA; ++i) v[i] = values(i);
       __builtin_amdgcn_sched_barrier(0);
-    }
+    });
     load_keys(h_keys, slot_keys);
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
@@ -484,8 +495,7 @@ __global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_r
 #pragma unroll
     for (int i = 0; i < 4; ++i) fill_values(part.first & 1, E, i);
     load_keys(0, 0);
-#pragma unroll
-    for (int j = 0; j < R::MMA; ++j) score(0, j);
+    each<R::MMA>([&](auto j) { score(0, j); });
     largest(0, 0, 16);
     load_keys(1, 0);
     flags = s.flags[part.first & 3][lane % W];
@@ -543,8 +553,7 @@ __global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_r
 #pragma unroll
       for (int i = 0; i < 4; ++i) fill_values(buf ^ 1, E1, i);
       load_keys(0, slot1);
-#pragma unroll
-      for (int j = 0; j < R::MMA; ++j) score(0, j);
+      each<R::MMA>([&](auto j) { score(0, j); });
       largest(0, 0, 16);
       load_keys(1, slot1);
     }
