@@ -1004,7 +1004,8 @@ co_status co_pages_query(const co_pages_desc* desc, co_pages_info* info);
  * of them), and pages wholly below are freed.  Streams are served in order,
  * each wholly (granted = n) or not at all (granted = 0, refused += n): the free
  * pages must suffice for it and all before it that the table's rows have room
- * for.  New pages are the lowest free ones.  A page that another stream holds
+ * for.  A stream whose tokens need no new page always gets them.  New pages are
+ * the lowest free ones.  A page that another stream holds
  * too is replaced by a new one, to which the tiles (16 tokens) of tokens that
  * the stream holds are copied in every layer; such a page is freed, where that
  * was its last use, for the next call.
@@ -1076,7 +1077,14 @@ co_status co_attn_read(const co_attn_desc* desc, const co_attn_cache* cache, con
  * Host only. */
 co_status co_attn_workspace_bytes(const co_attn_desc* desc, int32_t T, int64_t* bytes);
 
-/* Attention of the tokens q (B, T, heads head_dim), appended before, into y. */
+/*
+ * Attention of the tokens q (B, T, heads head_dim), appended before, into y, which is rounded once.
+ * Scores and sums are float32: a score is off by about 2^-20 of its largest product for CO_BF16
+ * and by 2^-23 of the sum of its products' magnitudes for CO_F32; weights have 11 bits, for CO_F32
+ * 22, and are multiples of 2^-35 of the row's reference, which is within 2^4 of its largest.  A row
+ * whose query is not finite, or that sees a key that is not, is NaN; a value that is not makes its
+ * block of 32 channels NaN in the rows that see it.  Scores must stay in float32's range.
+ */
 co_status co_attn_forward_steps(const co_attn_desc* desc, const co_attn_cache* cache,
                                 const co_tokens* q, const co_tokens* y, int32_t T,
                                 void* workspace, int64_t workspace_bytes, void* stream);

@@ -278,7 +278,7 @@ __global__ __launch_bounds__(kBlock, (few_waves<T, NB, CT>())) void attend_few_k
   int E = 0;
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
-    m[c] = -1e30f;
+    m[c] = -3e38f;  // below every score
     l[c] = 0.f;
 #pragma unroll
     for (int i = 0; i < NB * 2; ++i) o[c][i] = f32x4{};

@@ -498,6 +498,20 @@ def test_attend_not_finite_reaches_who_sees_it(dtype, T, which, bad):
     assert torch.equal(outs[0][~hit], outs[1][~hit])
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T", [1, 3, 80])
+def test_attend_scores_far_below(dtype, T):
+    """Scores of -6e37, all alike: the weights are equal, and their mean of a constant is it (ten
+    roundings of 2^-24 relative to 2 at most, and bfloat16 has it exactly)."""
+    pages = make_pages(B=2, N=20, W=8, P=16, K=1, D=64)
+    attn = coinf.CoAttention(pages, heads=2, dtype=dtype)
+    q = torch.full((2, T, 2, 64), 1e18, dtype=dtype, device=DEV)
+    k = torch.full((2, T, 1, 64), -1e18, dtype=dtype, device=DEV)
+    pages.reserve(T)
+    got = attn.forward_steps(q, k, torch.full_like(k, 2.0))
+    assert ((got.float() - 2).abs() <= 10 * 2 ** -23).all()
+
+
 def test_attend_pieces_tokens_and_clips_agree():
     """Definition 1: one set of parameters gives a clip, pieces and single tokens the same outputs but
     for the order of sums."""
