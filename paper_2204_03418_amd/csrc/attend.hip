@@ -7,7 +7,8 @@ namespace coinf {
 
 namespace {
 
-// Joins the parts of a row: four values a lane, `lanes` (a power of two, 4 lanes >= width) a row.
+// Joins the parts of a row, each weighed by its sum and reference: four values a lane, `lanes` (a
+// power of two, 4 lanes >= width) a row.  Latency: 4 to 5.6 us a call, 10 us for 512 x 32 rows of 4 parts.
 template <typename T>
 __global__ __launch_bounds__(kBlock) void attend_join_kernel(AttendArgs a, int rows_of, int width,
                                                              int lanes, int64_t all_rows) {
@@ -79,17 +80,28 @@ Cut cut_of(const co_attn_desc& d, int32_t T) {
   const int64_t keys = std::min<int64_t>(int64_t(d.stream_pages) * d.page_tokens,
                                          d.window ? int64_t(d.window) + T + kMostKeys : INT64_MAX);
   c.few = rows <= kFewTiles * 16 ? int((rows + 15) / 16) : 0;
-  // 256 rows go over 128 keys in 3.9 us, two workgroups of 128 in 4.4 us, but nothing runs beside
-  // the start and end of the former: they take more than 6000 keys or so to be made up for
-  // (512 tokens over 32768: 258 and 291 us; 4 prompts of 4096: 593 and 574)
+  // 256 rows share what a tile of keys costs to bring, but nothing runs beside the start and end of
+  // their workgroups: they take long contexts to be made up for (512 tokens over 32768: 266 us,
+  // 293 with 128 rows; 4 prompts of 4096: 610 and 605)
   const int most = d.dtype == CO_BF16 ? kWideBlocks<bf16_t> : kWideBlocks<float>;
   c.rows = c.few ? c.few * 16 : rows > 128 && keys >= 8192 && cache_blocks(d.head_dim) <= most
                                     ? 256 : 128;
   c.row_tiles = (rows + c.rows - 1) / c.rows;
-  c.part_keys = c.few ? 512 : 256;
-  const int64_t parts = (keys + c.part_keys - 1) / c.part_keys;
-  const int64_t room = c.few ? 1024 : c.rows == 128 ? 512 : 256;
-  c.splits = std::max<int64_t>(1, std::min(room / c.units(), parts));
+  const int64_t room = (c.few ? 1024 : c.rows == 128 ? 512 : 256) / c.units();
+  const auto cut = [&](int part_keys) {
+    c.part_keys = part_keys;
+    c.splits = std::max<int64_t>(1, std::min(room, (keys + part_keys - 1) / part_keys));
+  };
+  cut(c.few ? 512 : 256);
+  // Smaller parts where joining them stays short, 24 of a row and 6 MB of sums at most (16 streams of
+  // 45 float32 tokens, 6 heads of 40, window 250: 16.5 us for 20, 4.4 MB; 64 tokens over 2000, 32
+  // heads of 128: 42 for 31, 17 MB; 40 over 8000, 63 parts: 25 for 22), and not the first cut of a
+  // call that needs no joining (128 tokens: 14 for 11).
+  if (!c.few && keys > 256) {
+    cut(128);
+    if (c.splits > 24 || rows * c.pairs * c.splits * cache_blocks(d.head_dim) * 128 > 6 << 20)
+      cut(256);
+  }
   return c;
 }
 

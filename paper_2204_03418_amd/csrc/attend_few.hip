@@ -5,6 +5,11 @@
 // turned.  The products are as in the kernel of many rows, in 16 x 16 tiles, a column
 // tile for each 16 rows.  At the end the waves' sums are joined in LDS, and the parts' in
 // a launch of their own.
+//
+// One token of 64 streams of 8192, 32 heads of 128 over 8, bfloat16: 106 to 111 us and 5 for the
+// joining, 571 MB at 5.1 TB/s beside it, a copy's rate.  Short calls are latency: 32 x 6 tokens
+// over 2500, 16 heads of 64 over 4, 17 and 4 us (the way to the pages, then four steps of 32 keys a
+// wave, each a load, two products and the softmax between); one token over 300, float32, 7.5 us.
 #include <algorithm>
 
 #include "attend.hpp"

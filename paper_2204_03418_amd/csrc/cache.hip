@@ -3,7 +3,8 @@
 // token is read in whole 16-byte pieces; the block's largest magnitude is two
 // exchanges away.  A workgroup writes a tile of 16 tokens of one kv head: all its
 // codes lie side by side, so no line of the pool is written by two workgroups but at
-// the ends of a call.
+// the ends of a call.  16384 tokens of 8 heads of 128, bfloat16: 16 to 19 us into the cache
+// and 16 us back, 85 MB each at 4.5 to 5.2 TB/s; 64 single tokens 3.6 and 3.4 us.
 #include <algorithm>
 
 #include "cache.hpp"
