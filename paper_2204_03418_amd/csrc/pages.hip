@@ -10,7 +10,7 @@
 // 64 streams of 2000 tokens, 4 layers of 8 heads of 128: select 5.3 us, reserve 7.3 and its
 // copies of half a page 5.7, truncate 2.9, all of them latency (passes over the table and the
 // counts that depend on each other).  Compaction of 9664 pages, 201 MB in 2 layers:
-// the plan 13 us (two passes over the counts by one workgroup), the moves 86 us, 4.8 TB/s of
+// the plan 8 us (one workgroup), the moves 86 us, 4.8 TB/s of
 // reading and writing.
 #include <algorithm>
 
@@ -311,44 +311,54 @@ __global__ __launch_bounds__(kOne) void select_one_kernel(PagesArgs a, const int
   a.s.granted[tid] = 0;
 }
 
+// Bit i: whether a page p + i has holders, p + i < n.
+constexpr int kEach = 8;
+__device__ __forceinline__ int used_pages(const int32_t* refs, int p, int n) {
+  int v[kEach], bits = 0;
+  if (p + kEach <= n) {
+    __builtin_memcpy(v, refs + p, sizeof(v));
+  } else {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) v[i] = p + i < n ? refs[p + i] : 0;
+  }
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) bits |= (v[i] > 0) << i;
+  return bits;
+}
+
 // Which pages move where: one workgroup.  moves: their number, then (from, to) each; rank: which of
 // them a page is.
 __global__ __launch_bounds__(kOne) void compact_plan_kernel(PagesArgs a, int32_t* moves,
                                                             int32_t* rank) {
   __shared__ int scratch[kOne / 64];
-  constexpr int EACH = 8;
+  constexpr int PASS = kEach * kOne;
   const int n = a.d.pages, tid = threadIdx.x;
-  int mine_used = 0, used;
-  for (int p0 = 0; p0 < n; p0 += EACH * kOne) {
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-      const int p = p0 + i * kOne + tid;
-      mine_used += p < n && a.s.refs[min(p, n - 1)] > 0;
-    }
+  int mine_used = 0, used, kept = 0;  // kept: the first four passes' bits
+  for (int p0 = 0; p0 < n; p0 += PASS) {
+    const int bits = used_pages(a.s.refs, p0 + kEach * tid, n);
+    mine_used += __popc(bits);
+    if (p0 < 4 * PASS) kept |= bits << (p0 / PASS * kEach);
   }
   prefix_before(mine_used, scratch, used);
   // the k-th free page below `used` takes the k-th used one above
   int holes = 0, movers = 0;
-  for (int p0 = 0; p0 < n; p0 += EACH * kOne) {
-    int mine = 0, total;
-    bool pick[EACH];
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-      const int p = p0 + EACH * tid + i;
-      pick[i] = p < n && (a.s.refs[min(p, n - 1)] > 0) != (p < used);
-      mine += pick[i] ? p < used ? 1 : 1 << 16 : 0;  // at most 8 k of either in a pass
-    }
-    int at = prefix_before(mine, scratch, total);
+  for (int p0 = 0; p0 < n; p0 += PASS) {
+    const int p = p0 + kEach * tid;
+    int bits = p0 < 4 * PASS ? kept >> (p0 / PASS * kEach) & 255 : used_pages(a.s.refs, p, n);
+    // below `used`: the free ones
+    const int below = p + kEach <= used ? 255 : p < used ? (1 << (used - p)) - 1 : 0;
+    bits ^= below;
+    int total;  // at most 8 k of either in a pass
+    const int at = prefix_before(__popc(bits & below) | __popc(bits & ~below) << 16, scratch, total);
     int hole = holes + (at & 0xffff), mover = movers + (at >> 16);
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-      const int p = p0 + EACH * tid + i;
-      if (!pick[i]) continue;
-      if (p < used) {
-        moves[2 + 2 * hole++] = p;
+    for (int i = 0; i < kEach; ++i) {
+      if (!(bits >> i & 1)) continue;
+      if (below >> i & 1) {
+        moves[2 + 2 * hole++] = p + i;
       } else {
-        rank[p] = mover;
-        moves[1 + 2 * mover++] = p;
+        rank[p + i] = mover;
+        moves[1 + 2 * mover++] = p + i;
       }
     }
     holes += total & 0xffff;

@@ -235,6 +235,26 @@ def test_pages_of_many_streams(N):
     assert (sum(model.refused) > 0) == (N == 2500)
 
 
+@pytest.mark.parametrize("N", [40001, 32768])
+def test_compact_a_pool_of_many_passes(N):
+    """More pages than the plan's passes keep: half of the streams leave, twice."""
+    B, W, P = 1100, 40, 16
+    rng = np.random.default_rng(6)
+    pages, model = make_pages(B, N, W, P, 1, 8), R.Streams(B, N, W, P)
+    for _ in range(2):
+        n = [max(W * P - t, 0) for t in model.tokens]
+        pages.reserve(W * P, i32(n))
+        model.reserve(n)
+        same_tables(pages, model)
+        assert max(p for row in model.table for p in row) >= N - W
+        to = [t if rng.random() < 0.5 else 0 for t in model.tokens]
+        pages.truncate(i32(to))
+        model.truncate(to)
+        pages.compact()
+        model.compact()
+        same_tables(pages, model)
+
+
 def test_pages_run_out():
     """Streams in order get all they ask for or nothing; one that needs no page goes on."""
     pages = make_pages(B=4, N=3, W=3, P=16)
