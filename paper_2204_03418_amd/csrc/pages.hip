@@ -9,9 +9,8 @@
 //
 // 64 streams of 2000 tokens, 4 layers of 8 heads of 128: select 5.3 us, reserve 7.3 and its
 // copies of half a page 5.7, truncate 2.9, all of them latency (passes over the table and the
-// counts that depend on each other).  Compaction of 9664 pages, 201 MB in 2 layers:
-// the plan 8 us (one workgroup), the moves 86 us, 4.8 TB/s of
-// reading and writing.
+// counts that depend on each other).  Compaction, 209 MB of pages in 2 layers:
+// the plan 8 us (one workgroup), the moves 86 us, 4.8 TB/s of reading and writing.
 #include <algorithm>
 
 #include "cache.hpp"
