@@ -87,7 +87,9 @@ Cut cut_of(const co_attn_desc& d, int32_t T) {
   c.rows = c.few ? c.few * 16 : rows > 128 && keys >= 8192 && cache_blocks(d.head_dim) <= most
                                     ? 256 : 128;
   c.row_tiles = (rows + c.rows - 1) / c.rows;
-  const int64_t room = (c.few ? 1024 : c.rows == 128 ? 512 : 256) / c.units();
+  // large heads: one a CU (2 x 1000 bfloat16 tokens, 8 heads of 256: 66 us, 84 with parts for two)
+  const bool two = c.rows == 128 && cache_blocks(d.head_dim) <= most;
+  const int64_t room = (c.few ? 1024 : two ? 512 : 256) / c.units();
   const auto cut = [&](int part_keys) {
     c.part_keys = part_keys;
     c.splits = std::max<int64_t>(1, std::min(room, (keys + part_keys - 1) / part_keys));
