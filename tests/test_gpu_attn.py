@@ -676,6 +676,36 @@ def test_block_in_a_graph():
         torch.randn(1000, device=DEV).sum().item()
 
 
+def test_page_calls_in_a_graph():
+    """All of the pages' calls in one captured graph, against the tables' model on every replay."""
+    B, N, W, P = 6, 40, 8, 16
+    rng = np.random.default_rng(8)
+    pages, model = make_pages(B, N, W, P, 2, 40, layers=2), R.Streams(B, N, W, P)
+    n, source, to = (torch.zeros(B, dtype=torch.int32, device=DEV) for _ in range(3))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pages.reserve(40, n, keep=50)
+        pages.select(source)
+        pages.truncate(to)
+        pages.compact()
+    same_tables(pages, model)                                   # a capture runs nothing
+    for i in range(8):
+        asked = rng.integers(0, 41, B).tolist()
+        model.reserve(asked, 50)
+        picked = [int(rng.integers(-1, B)) if rng.random() < 0.4 else b for b in range(B)]
+        model.select(picked)
+        ends = [max(t - int(rng.integers(0, 20)), 0) if rng.random() < 0.5 else t
+                for t in model.tokens]
+        model.truncate(ends)
+        model.compact()
+        for buf, values in ((n, asked), (source, picked), (to, ends)):
+            buf.copy_(i32(values))
+        graph.replay()
+        torch.cuda.synchronize()
+        same_tables(pages, model)
+        torch.randn(1000, device=DEV).sum().item()
+
+
 def test_two_streams_at_once():
     """Two layers' calls on streams of their own at the same time, against one after the other."""
     g = gen(81)
