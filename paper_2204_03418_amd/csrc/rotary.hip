@@ -2,8 +2,8 @@
 // position.  Bound by memory: queries and keys are read and written once, in one
 // launch.  A workgroup makes the sines and cosines of its tokens' pairs once, one
 // a thread, in LDS, and all heads use them (computed for each head they would cost
-// about as much as the memory).  16384 tokens of 40 heads of 128, bfloat16: 62 to 70 us,
-// 336 MB at 4.8 to 5.4 TB/s; 24 single tokens 3.7 us, the launch.
+// about as much as the memory).  16384 tokens of 40 heads of 128, bfloat16: 65 to 70 us,
+// 336 MB at 4.8 to 5.2 TB/s; 24 single tokens 3.6 us, the launch.
 //
 // The angle in turns is position * f / (2 pi) modulo 1, an exact 64-bit product of
 // the position and the frequency in units of 2^-64 turns; what is left of the nearest
@@ -55,6 +55,13 @@ __device__ __forceinline__ float2 sincos_turns(uint64_t frac) {
   return {quarter & 2 ? -a : a, (quarter + 1) & 2 ? -b : b};
 }
 
+// Where a pair's sine and cosine lie: of units of eight, which are 64 bytes, every other four have
+// their 16-byte parts in another order, so that eight units' first parts lie in all banks (a call 71.8 -> 69.4 us).
+template <int V>
+__device__ __forceinline__ int place(int pair) {
+  return V == 8 ? pair ^ (pair / 32 % 2 * 2) : pair;
+}
+
 // V pairs, or V values that stay, a unit.
 template <typename T, int V, bool HALF>
 __global__ __launch_bounds__(kBlock) void rotary_kernel(RotaryArgs a) {
@@ -74,7 +81,7 @@ __global__ __launch_bounds__(kBlock) void rotary_kernel(RotaryArgs a) {
                               int64_t(a.c.position_each ? 0 : t)
                         : t;
       const float2 v = sincos_turns(uint64_t(p) * a.c.turns[pair]);
-      turn[i] = {v.y * a.d.magnitude, v.x * a.d.magnitude};
+      turn[k * pairs + place<V>(pair)] = {v.y * a.d.magnitude, v.x * a.d.magnitude};
       if (pair == 0) {
         stream[k] = b;
         token[k] = t < stream_tokens(a.c.lengths, b, a.c.T) ? t : ~t;
@@ -114,13 +121,14 @@ __global__ __launch_bounds__(kBlock) void rotary_kernel(RotaryArgs a) {
         v0 = load_pack<T, V>(x + at0);
         v1 = load_pack<T, V>(x + at1);
         const float2* cs = turn + k * pairs + pair;
+        const int moved = place<V>(pair) - pair;  // of the unit's first
 #pragma unroll
         for (int i = 0; i < V; ++i) {
           // the pair's places: i of either pack, or neighbours
           T& lo = HALF ? v0.v[i] : 2 * i < V ? v0.v[2 * i % V] : v1.v[2 * i % V];
           T& hi = HALF ? v1.v[i] : 2 * i + 1 < V ? v0.v[(2 * i + 1) % V] : v1.v[(2 * i + 1) % V];
           const float p = to_f32<T>(lo), q = to_f32<T>(hi);
-          const float2 r = cs[i];
+          const float2 r = cs[i ^ moved];
           lo = from_f32<T>(fmaf(p, r.x, -(q * r.y)));
           hi = from_f32<T>(fmaf(q, r.x, p * r.y));
         }
