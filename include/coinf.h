@@ -958,7 +958,7 @@ co_status co_rotary_forward(const co_rotary_desc* desc, const co_rotary_call* ca
  *   scales of K (page_tokens / 16, NB, 16 bytes)       tile, block, token
  *   scales of V the same
  * A value is c 2^(s - 127): c by its code's lower three bits 0, 0.5, 1, 1.5, 2, 3, 4, 6
- * and its highest bit the sign; s the block's scale byte, and s = 255: NaN.
+ * and its highest bit the sign; s the block's scale byte, 7..252, or 255: NaN, or 0: all codes are 0.
  * Channels past head_dim are 0.
  */
 #define CO_ATTN_MAX_HEAD  256
@@ -1061,8 +1061,8 @@ typedef struct co_attn_cache {
  * Puts the tokens k and v (B, T, kv_heads head_dim) into their pages: a block of 32
  * channels has the scale 2^e, e the least in -120..125 with max |x| <= 7 2^e (so
  * that what is cut at 6 is off by no more than half a step), and its values go to
- * the nearest code, of two the even one.  A block with a value that is not finite
- * is NaN.  Tokens past n, and those without a page, go nowhere.
+ * the nearest code, of two the even one.  A block of magnitudes up to 2^-122 is 0, one with a
+ * value that is not finite NaN.  Tokens past n, and those without a page, go nowhere.
  */
 co_status co_attn_append(const co_attn_desc* desc, const co_attn_cache* cache, const co_tokens* k,
                          const co_tokens* v, int32_t T, void* stream);
@@ -1081,7 +1081,10 @@ co_status co_attn_workspace_bytes(const co_attn_desc* desc, int32_t T, int64_t* 
  * Attention of the tokens q (B, T, heads head_dim), appended before, into y, which is rounded once.
  * Scores and sums are float32: a score is off by about 2^-20 of its largest product for CO_BF16
  * and by 2^-23 of the sum of its products' magnitudes for CO_F32; weights have 11 bits, for CO_F32
- * 22, and are multiples of 2^-35 of the row's reference, which is within 2^4 of its largest.  A row
+ * 22, and are multiples of 2^-35 of the row's reference, which is within 2^4 of its largest.  Values
+ * are taken exactly and their sums keep float32's bits, whatever else the stream's keys hold, down to
+ * scales 2^-160 of the kv head's largest there (where they are further than 2^31, or 2^21 for
+ * CO_F32, below others, a call takes about twice as long).  A row
  * whose query is not finite, or that sees a key that is not, is NaN; a value that is not makes its
  * block of 32 channels NaN in the rows that see it.  Scores must stay in float32's range.
  */

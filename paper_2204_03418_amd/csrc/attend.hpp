@@ -50,8 +50,19 @@ constexpr int kMostKeys = 128;  // of a tile
 // Weights are 2^{x + kLift}, x <= kSlack over the row's reference: 2^15, below 16-bit floats' highest.
 // Their least step is 2^-24, 2^-35 of the row's reference.
 constexpr float kLift = 11.f, kSlack = 4.f;
-// Values are c 2^{s - E + kValueLift}, s <= E: below 6 2^12.
+// Values are 16-bit floats c 2^{s - E + kValueLift}, s <= E: below 6 2^12, and taken as that down to
+// s = E - kSpan, c = 0.5: exact for bfloat16 calls; normal (2^-14 and more) for float32, since matrix
+// instructions sum denormal ones with fewer bits (45 rows that see only values 2^20 below others moved by
+// 1 bit, 2^24 by 6e-8, 2^28 by 6.6e-7).  E, one for all channels and keys of a pass (those too that a row does
+// not see), only rises.  A pass that meets values further below it, or in which it rises by more than
+// kMostRise (sums under the first one are 2^-13 and more, and keep 24 bits above 2^-126), is lost.
+// It is taken again with values as bfloat16, c 2^{s - E + kFarLift} under the last E, which are exact
+// down to s = E - 204, and weights in bfloat16 terms: sums over 2^31 keys stay below 2^127, and those
+// of values down to s = E - 170 keep 24 bits.
 constexpr int kValueLift = 12, kValueSlack = 4;
+template <typename T>
+constexpr int kSpan = sizeof(T) == 2 ? 35 : 25;
+constexpr int kMostRise = 85, kFarLift = 78;
 
 // What a stream's rows see.
 struct Span {
@@ -95,6 +106,13 @@ __device__ __forceinline__ int wave_max(int v) {  // v >= 0
   v = dpp_max<0x142, 0xa>(v);  // lane 15 of the 16 below
   v = dpp_max<0x143, 0xc>(v);  // lane 31
   return __builtin_amdgcn_readlane(v, 63);
+}
+
+// A kernel's only argument, read again: the compiler would keep the first pass's for the second.
+__device__ __forceinline__ const AttendArgs& again(const AttendArgs&) {
+  auto p = __builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const AttendArgs*)(p);
 }
 
 // Four values of channels c.. of a row, 0 past D.
@@ -164,6 +182,8 @@ template <typename T>
 constexpr int kQueryTerms = sizeof(T) == 2 ? 2 : 3;
 template <typename T>
 constexpr int kWeightTerms = sizeof(T) == 2 ? 1 : 2;
+template <typename T>
+constexpr int kFarTerms = sizeof(T) == 2 ? 2 : 3;  // bfloat16: 16 or 24 bits
 
 // Eight codes as 16-bit floats, times the scale.
 __device__ __forceinline__ f16x8 decode8(uint32_t w, float scale) {
@@ -182,6 +202,20 @@ __device__ __forceinline__ bf16x8 decode8_bf16(uint32_t w, int byte) {
   const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2);
   const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// Whether values of scale s lie too far below E; those of scale 0 are 0.
+template <typename T>
+__device__ __forceinline__ bool lost_values(int s, int E) {
+  return uint32_t(s - 1) < uint32_t(max(E - kSpan<T> - 1, 0));
+}
+// The exponent of the pass for far values: outputs' factor 2^{E - kFarLift - 127} is in float32's range.
+__device__ __forceinline__ int far_exponent(int E) { return max(E, kFarLift + 1); }
+// Eight of them for the pass of far values.
+__device__ __forceinline__ bf16x8 decode8_far(uint32_t w, int s, int E) {
+  const int byte = 127 + kFarLift + s - E;
+  const bool some = s != 0 && s != 255 && byte > 0;
+  return decode8_bf16(some ? w : 0, some ? byte : 127);
 }
 
 // Eight values as bfloat16 terms.

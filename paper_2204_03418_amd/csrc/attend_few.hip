@@ -4,7 +4,8 @@
 // from memory as the operand that they are, values pass through the wave's own LDS to be
 // turned.  The products are as in the kernel of many rows, in 16 x 16 tiles, a column
 // tile for each 16 rows.  At the end the waves' sums are joined in LDS, and the parts' in
-// a launch of their own.
+// a launch of their own.  Values too far apart for 16-bit floats, as in that kernel: the workgroup
+// goes over its part again (64 streams of 8192: 227 us for 114).
 //
 // One token of 64 streams of 8192, 32 heads of 128 over 8, bfloat16: 106 to 111 us and 5 for the
 // joining, 571 MB at 5.1 TB/s beside it, a copy's rate.  Short calls are latency: 32 x 6 tokens
@@ -44,10 +45,12 @@ struct Few {
   }
 };
 
-// Waves a SIMD: what a kernel's registers and LDS leave room for.
+// Waves a SIMD: what the first pass's registers and LDS leave room for.
 template <typename T, int NB, int CT>
 constexpr int few_waves() {
-  return CT == 1 && (sizeof(T) == 2 || NB <= 2) && NB <= 4 ? 4 : NB <= 4 ? 2 : 1;
+  if (NB > 4) return 1;
+  if (sizeof(T) == 2) return CT == 1 || NB <= 2 ? 4 : 2;
+  return CT == 1 ? (NB <= 2 ? 4 : 3) : NB <= 1 ? 4 : NB <= 2 ? 3 : 2;
 }
 
 // One wave's values, and at the end its sums (16 rows of NB * 32, 64 bytes more each).
@@ -59,14 +62,28 @@ struct FewLds {
   };
 };
 
-template <typename T, int NB, int CT>
-__global__ __launch_bounds__(kBlock, (few_waves<T, NB, CT>())) void attend_few_kernel(
-    AttendArgs a) {
+template <typename T, int NB>
+struct FewAll {
+  FewLds<T, NB> wave[kWaves];
+  float2 stats[kWaves][16];
+  int32_t lost[kWaves];
+};
+
+// A workgroup's pass over its part, to the end or, true, until its values' range is known to be too
+// wide: E is the wave's values' exponent, 0 before the first pass, and the pass for far values takes
+// it as it is.
+template <typename T, int NB, int CT, bool FAR>
+__device__ __forceinline__ bool attend_few(const AttendArgs& a, FewAll<T, NB>& s, int& E) {
   using F = Few<T, NB>;
-  __shared__ FewLds<T, NB> lds[kWaves];
-  __shared__ float2 stats[kWaves][16];
-  const int lane = threadIdx.x % 64, col = lane % 16, g = lane / 16;
-  const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / 64);
+  using Value = std::conditional_t<FAR, bf16x8, f16x8>;
+  constexpr int PT = FAR ? kFarTerms<T> : F::PT;
+  auto& lds = s.wave;
+  auto& stats = s.stats;
+  int tid = threadIdx.x;
+  // nothing of the first pass is kept for the second
+  if constexpr (FAR) asm volatile("" : "+v"(tid));
+  const int lane = tid % 64, col = lane % 16, g = lane / 16;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int split = blockIdx.x / a.pairs, pair = blockIdx.x - split * a.pairs;
   const int b = fdiv(pair, a.by_kv), kv = pair - b * a.d.kv_heads;
   const Span span(a, b);
@@ -77,14 +94,14 @@ __global__ __launch_bounds__(kBlock, (few_waves<T, NB, CT>())) void attend_few_k
     return static_cast<T*>(a.y.data) + b * a.y.batch_stride + t * a.y.token_stride +
            int64_t(head) * a.d.head_dim;
   };
-  if (split == 0) {  // outputs of tokens that the stream does not have
+  if (!FAR && split == 0) {  // outputs of tokens that the stream does not have
     const float none[4] = {};
-    for (int i = threadIdx.x; i < (a.T - span.n) * a.group * (NB * 8); i += kBlock)
+    for (int i = tid; i < (a.T - span.n) * a.group * (NB * 8); i += kBlock)
       store4<T>(out_row(rows + i / (NB * 8)), i % (NB * 8) * 4, a.d.head_dim, a.wide, none);
   }
-  if (rows == 0) return;
+  if (rows == 0) return false;
   const Part part(a, span.lo(a, 0), span.base + span.n, split);
-  if (split >= part.parts) return;
+  if (split >= part.parts) return false;
 
   // The keys' way: pages two steps ahead, codes and scales one.  Nothing is read out of a page's
   // range, and without a page all is 0.  The two tiles of 16 tokens of a step lie in one page, or
@@ -280,7 +297,9 @@ __global__ __launch_bounds__(kBlock, (few_waves<T, NB, CT>())) void attend_few_k
 
   f32x4 o[CT][NB * 2];
   float m[CT], l[CT];
-  int E = 0;
+  int E0 = 0;         // the first exponent
+  uint64_t lost = 0;  // lanes whose values were
+  if (FAR) E = far_exponent(E);
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
     m[c] = -3e38f;  // below every score
@@ -350,7 +369,7 @@ __global__ __launch_bounds__(kBlock, (few_waves<T, NB, CT>())) void attend_few_k
       bad |= rvs[i] == 255;
       top_s = max(top_s, rvs[i] == 255 ? 0 : rvs[i]);
     }
-    if (__any(top_s > E)) {
+    if (!FAR && __any(top_s > E)) {
       const int next = wave_max(top_s) + kValueSlack;
       if (E) {
         const float down = exponent_to_f32(127 + E - next);
@@ -358,9 +377,14 @@ __global__ __launch_bounds__(kBlock, (few_waves<T, NB, CT>())) void attend_few_k
         for (int c = 0; c < CT; ++c)
 #pragma unroll
           for (int i = 0; i < NB * 2; ++i) o[c][i] *= down;
+      } else {
+        E0 = next;
       }
       E = next;
     }
+    if (!FAR)
+#pragma unroll
+      for (int i = 0; i < F::VC; ++i) lost |= __ballot(lost_values<T>(rvs[i], E));
 #pragma unroll
     for (int i = 0; i < F::VC; ++i) {
       const int c = lane + 64 * i, tile = c / (NB * 16), rest = c - tile * NB * 16;
@@ -370,7 +394,11 @@ __global__ __launch_bounds__(kBlock, (few_waves<T, NB, CT>())) void attend_few_k
       const float scale = __uint_as_float(uint32_t(rvs[i] == 0 || rvs[i] == 255 ? 0 : e) << 23);
       _Float16* dst = vbuf + (tile * 16 + rest % 16) * F::VS + rest / 16 * 32;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) *reinterpret_cast<f16x8*>(dst + 8 * k) = decode8(rv[i][k], scale);
+      for (int k = 0; k < 4; ++k)
+        if constexpr (FAR)
+          *reinterpret_cast<bf16x8*>(dst + 8 * k) = decode8_far(rv[i][k], rvs[i], E);
+        else
+          *reinterpret_cast<f16x8*>(dst + 8 * k) = decode8(rv[i][k], scale);
     }
     int raw[F::VC];
 #pragma unroll
@@ -381,7 +409,7 @@ __global__ __launch_bounds__(kBlock, (few_waves<T, NB, CT>())) void attend_few_k
       if (step + 2 * kWaves < end) fetch_pages(step + 2 * kWaves);
     }
     const bool whole = pos0 >= lo_all && pos0 + kStep - 1 <= hi_all && pages == 3;
-    f16x8 p[CT][F::PT];
+    Value p[CT][PT];
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       if (!whole || 16 * (c + 1) > rows) {
@@ -412,13 +440,25 @@ __global__ __launch_bounds__(kBlock, (few_waves<T, NB, CT>())) void attend_few_k
 #pragma unroll
         for (int k = 0; k < 2; ++k)
           w[k] = exp2_fast(fmaf(sc[c][(i + k) / 4][(i + k) % 4] - m[c], a.scale_log2, kLift));
+        if constexpr (FAR) {
+          l[c] += w[0] + w[1];
 #pragma unroll
-        for (int k = 0; k < F::PT; ++k) {
-          const f16x2 r = __builtin_convertvector(w, f16x2);
-          p[c][k][i] = r[0];
-          p[c][k][i + 1] = r[1];
-          l[c] = __builtin_amdgcn_fdot2(r, f16x2{1, 1}, l[c], false);
-          if (k + 1 < F::PT) w -= __builtin_convertvector(r, f32x2);
+          for (int k = 0; k < PT; ++k)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+              const __bf16 r = __bf16(w[n]);
+              p[c][k][i + n] = r;
+              w[n] -= float(r);
+            }
+        } else {
+#pragma unroll
+          for (int k = 0; k < PT; ++k) {
+            const f16x2 r = __builtin_convertvector(w, f16x2);
+            p[c][k][i] = r[0];
+            p[c][k][i + 1] = r[1];
+            l[c] = __builtin_amdgcn_fdot2(r, f16x2{1, 1}, l[c], false);
+            if (k + 1 < PT) w -= __builtin_convertvector(r, f32x2);
+          }
         }
       }
     }
@@ -431,12 +471,15 @@ __global__ __launch_bounds__(kBlock, (few_waves<T, NB, CT>())) void attend_few_k
       } r;
       r.lo = turned4(base + 16 * i);
       r.hi = turned4(base + 16 * F::VS + 16 * i);
-      const f16x8 v = __builtin_bit_cast(f16x8, r);
+      const Value v = __builtin_bit_cast(Value, r);
 #pragma unroll
       for (int c = 0; c < CT; ++c)
 #pragma unroll
-        for (int k = 0; k < F::PT; ++k)
-          o[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[c][k], o[c][i], 0, 0, 0);
+        for (int k = 0; k < PT; ++k)
+          if constexpr (FAR)
+            o[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[c][k], o[c][i], 0, 0, 0);
+          else
+            o[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[c][k], o[c][i], 0, 0, 0);
     }
     __builtin_amdgcn_wave_barrier();
     if (__any(bad)) {  // blocks that are not finite, to the rows that see their tokens
@@ -460,10 +503,12 @@ __global__ __launch_bounds__(kBlock, (few_waves<T, NB, CT>())) void attend_few_k
     }
   }
 
+  if (!FAR) s.lost[wave] = lost || E - E0 > kMostRise;
   // the waves' sums together, a column tile at a time
   constexpr int OS = NB * 32 + 16;
-  const float up = exponent_to_f32(E - kValueSlack);
-  const float less = exponent_to_f32(127 + kValueSlack - kValueLift);
+  // 2^{E - 127 - kValueLift} in two steps, neither out of range; 2^{E - 127 - kFarLift} is in it
+  const float up = exponent_to_f32(FAR ? E - kFarLift : E - kValueSlack);
+  const float less = FAR ? 1.f : exponent_to_f32(127 + kValueSlack - kValueLift);
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
     if (16 * c >= rows) break;
@@ -481,7 +526,13 @@ __global__ __launch_bounds__(kBlock, (few_waves<T, NB, CT>())) void attend_few_k
     }
     if (g == 0) stats[wave][col] = {m[c], l[c]};
     __syncthreads();
-    for (int i = threadIdx.x; i < 16 * NB * 8; i += kBlock) {
+    if (!FAR && c == 0) {
+      int any = 0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) any |= s.lost[w];
+      if (__builtin_expect(any, 0)) return true;
+    }
+    for (int i = tid; i < 16 * NB * 8; i += kBlock) {
       const int r = i / (NB * 8), ch = i % (NB * 8) * 4, row = 16 * c + r;
       if (row >= rows) break;
       float top = -__builtin_inff(), sum = 0.f, v[4] = {};
@@ -509,6 +560,16 @@ __global__ __launch_bounds__(kBlock, (few_waves<T, NB, CT>())) void attend_few_k
       }
     }
   }
+  return false;
+}
+
+template <typename T, int NB, int CT>
+__global__ __launch_bounds__(kBlock, (few_waves<T, NB, CT>())) void attend_few_kernel(
+    AttendArgs a) {
+  __shared__ FewAll<T, NB> s;
+  int E = 0;
+  if (__builtin_expect(attend_few<T, NB, CT, false>(a, s, E), 0))
+    attend_few<T, NB, CT, true>(again(a), s, E);
 }
 
 template <typename T, int NB>

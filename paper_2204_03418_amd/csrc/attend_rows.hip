@@ -8,9 +8,14 @@
 // instructions with a scale a block of 32 channels read 4-bit keys against queries in
 // 8-bit terms, which hold them exactly, at the rate of 16-bit products (two terms);
 // LDS holds and moves a quarter of the bytes.  Values become 16-bit floats in LDS, once a
-// workgroup (exactly, but for what is below 2^-35 of its tile's largest scale), and the
-// weights 16-bit floats with 11 bits (two terms, 22 bits, for float32).  For float32
-// the keys become bfloat16 before the first product, and the queries three terms.
+// workgroup, and the weights 16-bit floats with 11 bits (two terms, 22 bits, for float32).
+// For float32 the keys become bfloat16 before the first product, and the queries three terms.
+//
+// 16-bit floats hold values 2^31 apart exactly (attend.hpp).  A workgroup that meets others among its
+// part's keys, hidden or not, goes over them again with values as bfloat16, whose exponents span the
+// cache's, and weights in two or three bfloat16 terms: 1.7 to 2.3 times as long in all (four prompts
+// as below, every eighth token's values 2^60 larger: 1282 us for 565).  Looking for them costs nothing
+// measurable at 128 channels and 15 in 1000 of a prompt of heads of 64.
 //
 // Four prompts of 4096 tokens, 32 heads of 128 over 8, bfloat16: 575 to 605 us, 910 to 956
 // TFLOP/s (a large bfloat16 matrix product: 1258); 512 tokens over 32768: 254 to 266 us, 1.04 to
@@ -70,14 +75,21 @@ struct RowsLds {
   uint8_t ks[3][W * R::CHUNKS];
   alignas(16) uint8_t vs[4][W * R::CHUNKS];  // by tile modulo 4, 0 of keys not the stream's
   int32_t flags[4][W];           // by tile modulo 4
+  int32_t lost;
 };
 
-template <typename T, int NB, int W>
-__global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_rows_kernel(AttendArgs a) {
+// A workgroup's pass over its part, to the end or, true, until its values' range is known to be too
+// wide: E is the values' exponent, 0 before the first pass, and the pass for far values takes it as
+// it is.
+template <typename T, int NB, int W, bool FAR>
+__device__ __forceinline__ bool attend_rows(const AttendArgs& a, RowsLds<T, NB, W>& s, int& E) {
   using R = Rows<T, NB, W>;
-  constexpr int kRows = 32 * W, kKeys = R::KEYS;
-  __shared__ RowsLds<T, NB, W> s;
-  const int tid = threadIdx.x, lane = tid % 64, col = lane % 32, half = lane / 32;
+  using Value = std::conditional_t<FAR, bf16x8, f16x8>;
+  constexpr int kRows = 32 * W, kKeys = R::KEYS, PT = FAR ? kFarTerms<T> : R::PT;
+  int tid = threadIdx.x;
+  // nothing of the first pass is kept for the second
+  if constexpr (FAR) asm volatile("" : "+v"(tid));
+  const int lane = tid % 64, col = lane % 32, half = lane / 32;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
 
   // which unit: all parts and row tiles of a pair on one XCD where the pairs allow it, the rows
@@ -113,11 +125,12 @@ __global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_r
   };
   if (row0 >= rows) {
     if (split == 0) no_output();
-    return;
+    return false;
   }
   const int t_last = fdiv(min(row0 + kRows, rows) - 1, a.by_group);
   const Part part(a, span.lo(a, fdiv(row0, a.by_group)), span.base + t_last + 1, split);
-  if (split >= part.parts) return;
+  if (split >= part.parts) return false;
+  if (!FAR && tid == 0) s.lost = 0;
 
   // queries, as 8-bit terms
   const bool live = row < rows;
@@ -270,7 +283,9 @@ __global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_r
   // they give is the difference.  over: what a difference may reach, everything before the first.
   f32x16 below = f32x16{};
   float l[2] = {0.f, 0.f}, over = -3e38f;
-  int E = 0;  // the values' exponent, 0: none yet
+  int E0 = 0;         // the first exponent
+  uint64_t lost = 0;  // lanes whose values were
+  if (FAR) E = far_exponent(E);
 
   // The values into LDS, a quarter of a lane's 32 at a time.  The quarters of a row's blocks change
   // places by (row / 4) % 4, so that 16 rows' lie in all banks.
@@ -279,15 +294,24 @@ __global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_r
     for (int i = 0; i < R::PER; ++i) {
       const int c = lane + 64 * i;
       if (c >= R::CHUNKS) break;
-      // without a scale: 0
-      const int e = max(127 + kValueLift + rvs[i] - E, 0);
-      const float scale = __uint_as_float(uint32_t(rvs[i] == 0 || rvs[i] == 255 ? 0 : e) << 23);
-      _Float16* dst = s.v[buf] + (wave * kCacheTile + c % 16) * R::VS + c / 16 * 32;
-      *reinterpret_cast<f16x8*>(dst + 8 * (piece ^ c / 4 % 4)) = decode8(rv[i][piece], scale);
+      _Float16* dst = s.v[buf] + (wave * kCacheTile + c % 16) * R::VS + c / 16 * 32 +
+                      8 * (piece ^ c / 4 % 4);
+      if constexpr (FAR) {
+        *reinterpret_cast<bf16x8*>(dst) = decode8_far(rv[i][piece], rvs[i], E);
+      } else {
+        // without a scale: 0
+        const int e = max(127 + kValueLift + rvs[i] - E, 0);
+        const float scale = __uint_as_float(uint32_t(rvs[i] == 0 || rvs[i] == 255 ? 0 : e) << 23);
+        *reinterpret_cast<f16x8*>(dst) = decode8(rv[i][piece], scale);
+      }
     }
+    if (!FAR && piece == 0)
+#pragma unroll
+      for (int i = 0; i < R::PER; ++i) lost |= __ballot(lost_values<T>(rvs[i], E));
   };
   // the values' exponent for a tile
   const auto exponent = [&](int tile) {
+    if (FAR) return E;
     constexpr int WORDS = W * R::CHUNKS / 4;  // of scales
     typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
     const auto word = [&](int i) {
@@ -319,6 +343,8 @@ __global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_r
       const float down = exponent_to_f32(127 + E - next);
 #pragma unroll
       for (int i = 0; i < NB; ++i) o[i] *= down;
+    } else {
+      E0 = next;
     }
     E = next;
   };
@@ -419,10 +445,10 @@ __global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_r
       } r;
       r.lo = turned4(lo + at);
       r.hi = turned4(hi + at);
-      return __builtin_bit_cast(f16x8, r);
+      return __builtin_bit_cast(Value, r);
     };
     // weights in four groups of four, each a stage behind the one before: arguments, powers, operands
-    f16x8 p[R::PT][2], v[NB];
+    Value p[PT][2], v[NB];
     float x[16];
     const auto weigh = [&](int stage) {
 #pragma unroll
@@ -436,22 +462,38 @@ __global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_r
       for (int i = 4 * stage - 8; i < 4 * stage - 4; i += 2) {
         if (i < 0) continue;
         f32x2 w = {x[i], x[i + 1]};
+        if constexpr (FAR) {
+          l[i / 2 % 2] += w[0] + w[1];
 #pragma unroll
-        for (int k = 0; k < R::PT; ++k) {
-          const f16x2 r = __builtin_convertvector(w, f16x2);
-          p[k][i / 8][i % 8] = r[0];
-          p[k][i / 8][i % 8 + 1] = r[1];
-          // the sum of the weights as they are used
-          l[i / 2 % 2] = __builtin_amdgcn_fdot2(r, f16x2{1, 1}, l[i / 2 % 2], false);
-          if (k + 1 < R::PT) w -= __builtin_convertvector(r, f32x2);
+          for (int k = 0; k < PT; ++k)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+              const __bf16 r = __bf16(w[n]);
+              p[k][i / 8][i % 8 + n] = r;
+              w[n] -= float(r);
+            }
+        } else {
+#pragma unroll
+          for (int k = 0; k < PT; ++k) {
+            const f16x2 r = __builtin_convertvector(w, f16x2);
+            p[k][i / 8][i % 8] = r[0];
+            p[k][i / 8][i % 8 + 1] = r[1];
+            // the sum of the weights as they are used
+            l[i / 2 % 2] = __builtin_amdgcn_fdot2(r, f16x2{1, 1}, l[i / 2 % 2], false);
+            if (k + 1 < PT) w -= __builtin_convertvector(r, f32x2);
+          }
         }
       }
     };
     const auto add = [&](int i) {
 #pragma unroll
-      for (int k = 0; k < R::PT; ++k)
-        o[i % NB] =
-            __builtin_amdgcn_mfma_f32_32x32x16_f16(v[i % NB], p[k][i / NB], o[i % NB], 0, 0, 0);
+      for (int k = 0; k < PT; ++k)
+        if constexpr (FAR)
+          o[i % NB] =
+              __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[i % NB], p[k][i / NB], o[i % NB], 0, 0, 0);
+        else
+          o[i % NB] =
+              __builtin_amdgcn_mfma_f32_32x32x16_f16(v[i % NB], p[k][i / NB], o[i % NB], 0, 0, 0);
     };
     constexpr int STAGES = 6;
     each<R::MMA>([&](auto j) {
@@ -575,16 +617,21 @@ __global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_r
     __syncthreads();
   }
 
+  if constexpr (!FAR) {
+    if (lost || E - E0 > kMostRise) s.lost = 1;
+    __syncthreads();
+    if (__builtin_expect(s.lost, 0)) return true;
+  }
   float sum = l[0] + l[1];
   sum += __shfl_xor(sum, 32);
   if (!live) {
     if (split == 0) no_output();
-    return;
+    return false;
   }
   const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-  // 2^{E - 127 - kValueLift} in two steps, neither out of range
-  const float up = exponent_to_f32(E - kValueSlack);
-  const float less = exponent_to_f32(127 + kValueSlack - kValueLift);
+  // 2^{E - 127 - kValueLift} in two steps, neither out of range; 2^{E - 127 - kFarLift} is in it
+  const float up = exponent_to_f32(FAR ? E - kFarLift : E - kValueSlack);
+  const float less = FAR ? 1.f : exponent_to_f32(127 + kValueSlack - kValueLift);
   const float bad = q_bad && sum > 0.f ? __builtin_nanf("") : 0.f;
   const auto value = [&](int blk, int i) { return o[blk][i] * inv * less * up + bad; };
   if (part.parts == 1) {
@@ -597,7 +644,7 @@ __global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_r
         const float v[4] = {value(blk, i), value(blk, i + 1), value(blk, i + 2), value(blk, i + 3)};
         store4<T>(y, blk * 32 + 2 * i + 4 * half, a.d.head_dim, a.wide, v);
       }
-    return;
+    return false;
   }
   const int64_t at = ((int64_t(pair) * a.row_tiles + rt) * a.splits + split) * kRows +
                      wave * 32 + col;
@@ -611,6 +658,15 @@ __global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_r
       store_pack<float, 4>(o_part + blk * 32 + 2 * i + 4 * half, v);
     }
   if (half == 0) a.part_stat[at] = {-below[0], sum};
+  return false;
+}
+
+template <typename T, int NB, int W>
+__global__ __launch_bounds__(64 * W, NB <= kWideBlocks<T> ? 2 : 1) void attend_rows_kernel(AttendArgs a) {
+  __shared__ RowsLds<T, NB, W> s;
+  int E = 0;
+  if (__builtin_expect(attend_rows<T, NB, W, false>(a, s, E), 0))
+    attend_rows<T, NB, W, true>(again(a), s, E);
 }
 
 template <typename T, int NB>

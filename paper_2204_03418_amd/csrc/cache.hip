@@ -28,9 +28,10 @@ struct CacheArgs {
 };
 
 // The scale byte of a block whose largest magnitude has the float32 bits `most`; codes follow it:
-// 255 where that is not finite.
+// 255 where that is not finite, 0 where all codes are (up to 2^-122, half of the least one).
 __device__ __forceinline__ int scale_byte(uint32_t most) {
   if (most >= 0x7f800000u) return 255;
+  if (most <= 0x02800000u) return 0;
   // 2^k m, 1 <= m < 2: the least e with 2^k m <= 7 2^e
   const int e = int(most >> 23) - 127 - 2 + ((most & 0x7fffffu) > 0x600000u);
   return min(max(e, -120), 125) + 127;
@@ -109,7 +110,7 @@ __global__ __launch_bounds__(kBlock) void append_kernel(CacheArgs a) {
       most = max(most, uint32_t(__shfl_xor(int(most), 2)));
       const int s = scale_byte(most);
       uint32_t code = 0;
-      if (s != 255) {
+      if (s != 255 && s != 0) {
         const float scale = scale_of(s);
         code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[w][0], v[w][1], scale, 0);
         code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[w][2], v[w][3], scale, 1);
