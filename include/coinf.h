@@ -1079,8 +1079,10 @@ co_status co_attn_workspace_bytes(const co_attn_desc* desc, int32_t T, int64_t* 
 
 /*
  * Attention of the tokens q (B, T, heads head_dim), appended before, into y, which is rounded once.
- * Scores and sums are float32: a score is off by about 2^-20 of its largest product for CO_BF16
- * and by 2^-23 of the sum of its products' magnitudes for CO_F32; weights have 11 bits, for CO_F32
+ * Scores and sums are float32: a score is off by about 2^-20 of its largest product for CO_BF16,
+ * where queries of less than 2^-13 of the largest in their block of 32 channels also lose up to 2^-21
+ * of that largest, each times its key, and by 2^-23 of the sum of its products' magnitudes for
+ * CO_F32; weights have 11 bits, for CO_F32
  * 22, and are multiples of 2^-35 of the row's reference, which is within 2^4 of its largest.  Values
  * are taken exactly and their sums keep float32's bits, whatever else the stream's keys hold, down to
  * scales 2^-160 of the kv head's largest there (where they are further than 2^31, or 2^21 for

@@ -146,8 +146,10 @@ __device__ __forceinline__ float exponent_to_f32(int biased) {
   return __uint_as_float(uint32_t(min(max(biased, 0), 254)) << 23);
 }
 
-// The 8-bit terms of 16 values, 2^{e - 4 k} the scale of term k: words[k] 16 bytes.  Two hold a
-// bfloat16 exactly down to 2^-17 of the block's largest.
+// The 8-bit terms of 16 values, 2^{e - 4 k} the scale of term k: words[k] 16 bytes.  A term has 4 bits
+// and steps of 2^-9 of its scale at least.  Two, where the block's largest is 2^7 of the first scale
+// and more, hold a bfloat16 exactly down to 2^-13 of that largest, and leave up to 2^-21 of it
+// (half of 2^-13 2^-7) below.
 template <int TERMS>
 __device__ __forceinline__ void to_terms(float (&v)[16], int scale_byte, i32x4 (&words)[TERMS]) {
 #pragma unroll
@@ -176,7 +178,7 @@ __device__ __forceinline__ int query_scale(uint32_t most) {
 }
 
 // Scores.  bfloat16: keys as they are against queries in two 8-bit terms, whose instructions sum to about
-// 2^-20 of their largest product.  float32: those sums would be its error (4e-6 to 1e-5 measured), so
+// 2^-20 of their largest product; what the terms leave of a query adds to that.  float32: those sums would be its error (4e-6 to 1e-5 measured), so
 // its keys become bfloat16 (exactly) and its queries three bfloat16 terms (24 bits).
 template <typename T>
 constexpr int kQueryTerms = sizeof(T) == 2 ? 2 : 3;

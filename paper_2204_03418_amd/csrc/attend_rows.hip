@@ -6,7 +6,8 @@
 // tiles: column = row of queries), and the weights are the operand of O^T = V^T P^T without
 // leaving their lanes.  The first product takes the cache's codes as they are: matrix
 // instructions with a scale a block of 32 channels read 4-bit keys against queries in
-// 8-bit terms, which hold them exactly, at the rate of 16-bit products (two terms);
+// 8-bit terms, which hold a bfloat16 down to 2^-21 of its block's largest, at the rate of 16-bit
+// products (two terms);
 // LDS holds and moves a quarter of the bytes.  Values become 16-bit floats in LDS, once a
 // workgroup, and the weights 16-bit floats with 11 bits (two terms, 22 bits, for float32).
 // For float32 the keys become bfloat16 before the first product, and the queries three terms.

@@ -248,3 +248,37 @@ def test_far_values_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, attn.forward_steps(q, k, buf)), up
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("up", [10, 13, 16])
+@pytest.mark.parametrize("T,D", [(1, 64), (6, 96), (90, 64), (40, 256)])
+def test_queries_with_an_outlier(dtype, up, T, D):
+    """A query channel 2^up times the others whose keys are 0: the scores are the others'.
+
+    bfloat16: a block's queries are two terms of 4 bits whose least step is 2^-9 and 2^-13 of a scale
+    that is at most 2^-7 of the block's largest, so what they leave is half of 2^-13 2^-7 of that,
+    2^-21, for each of the block's keys."""
+    g = gen(107)
+    B, H, K, ctx = 2, 2, 1, 60
+    q, k, v = (randn(g, B, L, n, D, dtype=dtype) for L, n in ((T, H), (ctx + T, K), (ctx + T, K)))
+    q[..., 3] = 2.0 ** up * 1.5
+    k[..., 3] = 0
+    pages = make_pages(B, 24, 12, 16, K, D)
+    attn = coinf.CoAttention(pages, heads=H, dtype=dtype)
+    pages.reserve(ctx)
+    attn.append(k[:, :ctx].to(DEV), v[:, :ctx].to(DEV))
+    pages.reserve(T)
+    got = attn.forward_steps(q.to(DEV), k[:, ctx:].to(DEV), v[:, ctx:].to(DEV))
+    kq, vq = R.quantised(R.np64(k)), R.quantised(R.np64(v))
+    for b in range(B):
+        qb = R.np64(q[b])
+        y, (size, worst, reach) = R.attend(qb, kq[b], vq[b], ctx + np.arange(T), 0, 0, attn.scale)
+        if dtype is BF16:
+            left = 0
+            for c in range(0, D, 32):
+                keys = np.abs(kq[b][..., c:c + 32]).sum(-1).max()
+                left = left + 2.0 ** -21 * np.abs(qb[..., c:c + 32]).max(-1, keepdims=True) * keys
+            worst = worst + attn.scale * left / ((D + 16) * R.U32)
+        bound = R.attend_bound(y, (size, worst, reach), ctx + T, D, U[dtype], WEIGHT[dtype])
+        R.within(got[b], y, bound, f"stream {b}")
