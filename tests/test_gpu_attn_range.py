@@ -1,5 +1,6 @@
 """Attention where magnitudes lie far apart: values of the cache many binades below others of the same
-call, whether a row sees those or not.  Against plain 64-bit forms.
+call, whether a row sees those or not.  And each of its kernels: every number of blocks of channels and of
+column tiles.  Against plain 64-bit forms.
 
 Bounds, beside those of the attention tests: a value is exact whatever else the cache holds, so an
 output's error is relative to what its row sees of its channel.  A key whose weight is below 2^-160 of
@@ -12,7 +13,7 @@ import torch
 
 import attn_ref as R
 from paper_2204_03418_amd import coinf
-from test_gpu_attn import WEIGHT, i32, make_pages
+from test_gpu_attn import WEIGHT, attend_case, attend_check, make_pages
 from test_gpu_tokens import BF16, DEV, F32, U, gen, randn
 
 pytestmark = pytest.mark.gpu
@@ -101,8 +102,10 @@ def test_many_rows(kind, dtype, T, ctx, H, K, D):
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("kind", ["growing", "later"])
-def test_wide_workgroups(kind, dtype):
-    far_case(kind, 140, 8300, 1, 1, 64, dtype, 0, P=64, B=1)
+@pytest.mark.parametrize("D", [32, 64, 96, 128])
+def test_wide_workgroups(D, kind, dtype):
+    """More than 128 rows over 8192 keys and more: workgroups of 256 rows."""
+    far_case(kind, 140, 8300, 1, 1, D, dtype, 0, P=64, B=1)
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
@@ -282,3 +285,50 @@ def test_queries_with_an_outlier(dtype, up, T, D):
             worst = worst + attn.scale * left / ((D + 16) * R.U32)
         bound = R.attend_bound(y, (size, worst, reach), ctx + T, D, U[dtype], WEIGHT[dtype])
         R.within(got[b], y, bound, f"stream {b}")
+
+
+# ------------------------------------------------------------ every kernel of attention
+
+HEADS = [24, 40, 96, 128, 160, 192, 224, 256]                   # 1 to 8 blocks of channels
+
+
+@pytest.mark.parametrize("P", [16, 64])
+@pytest.mark.parametrize("T,H,K,rows", [(1, 1, 1, 1), (4, 8, 2, 16), (3, 12, 2, 18), (8, 4, 1, 32)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("D", HEADS)
+def test_few_rows_of_every_head(D, dtype, T, H, K, rows, P):
+    """One and two column tiles of 16 rows, over a context of several parts."""
+    assert T * H // K == rows <= 32                             # the kernel of few rows
+    case = (2, T, 1300, H, K, D, P, 0, dtype, "full", 0, 0)
+    attn, pages, q, *rest = attend_case(case, 33)
+    attend_check(case, attn, q, *rest, attn.attend(q.to(DEV)), "few rows")
+
+
+@pytest.mark.parametrize("T,ctx,H,K", [(20, 700, 2, 1), (70, 100, 2, 1)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("D", HEADS)
+def test_many_rows_of_every_head(D, dtype, T, ctx, H, K):
+    assert T * H // K > 32                                      # the kernel of many rows
+    case = (2, T, ctx, H, K, D, 32, 0, dtype, "ragged", 0, 0)
+    attn, pages, q, *rest = attend_case(case, 34)
+    attend_check(case, attn, q, *rest, attn.attend(q.to(DEV)), "many rows")
+
+
+@pytest.mark.parametrize("kind", ["blocks", "growing"])
+@pytest.mark.parametrize("T,H,K", [(1, 1, 1), (4, 6, 1), (40, 1, 1)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("D", HEADS)
+def test_far_values_of_every_head(D, dtype, T, H, K, kind):
+    far_case(kind, T, 150, H, K, D, dtype, 0, P=32, B=1)
+
+
+def test_rotary_writes_queries_and_keys_apart():
+    """One tensor may be both inputs; two outputs may not be one place."""
+    layer = coinf.CoRotary(32, device=DEV)
+    x = randn(gen(108), 2, 3, 4, 32).to(DEV)
+    a, b = layer.forward(x, x)
+    assert torch.equal(a, b) and torch.equal(a, layer.forward(x))
+    other = x.clone()
+    for k, out, k_out in ((other, x, x), (other, other, None), (other, None, x)):
+        with pytest.raises(coinf.CoinfError):
+            layer.forward(x, k, out=out, k_out=k_out)
