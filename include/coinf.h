@@ -899,7 +899,7 @@ co_status co_norm_forward_lengths(const co_norm_desc* desc, const co_norm_call* 
  * position p:  (u, w) -> m (u cos - w sin, w cos + u sin); the others stay.
  * An angle is taken modulo a turn in 64-bit integers, turns[i] = f_i / (2 pi) 2^64
  * (co_rotary_turns), so that far positions lose nothing: it is off by
- * |p| 2^-64 turns, and the float32 sine and cosine by 2^-23.  Outputs are
+ * |p| 2^-64 turns (f_i times that where f_i > 1), and the float32 sine and cosine by 2^-23.  Outputs are
  * rounded once.  y may be in place of x (the same strides).
  */
 #define CO_ROTARY_HALF         0

@@ -72,7 +72,11 @@ struct Cut {
   int64_t units() const { return pairs * row_tiles; }
 };
 
-// Workgroups that the card holds: two a CU of many rows, four of few.  A call of fewer units has its keys cut in parts.
+// A call of fewer units than the card holds workgroups has its keys cut in parts: two a CU of many
+// rows, one of large heads; four of few, which is what up to 16 bfloat16 rows of heads to 128 and float32
+// ones to 64 have, and up to 32 of half such heads (others one to three: their parts run in rounds).
+// Both counts go by the room of the
+// table's rows, which the host knows, not by what streams hold.
 Cut cut_of(const co_attn_desc& d, int32_t T) {
   Cut c;
   c.pairs = int64_t(d.batch) * d.kv_heads;

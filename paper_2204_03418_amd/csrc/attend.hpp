@@ -40,7 +40,7 @@ struct AttendArgs {
   int32_t splits;      // parts of a unit's keys at most
   int32_t keys;        // of a tile
   int32_t part_tiles;  // of a part at least
-  int32_t wide;        // q and y in pieces of 16 bytes
+  int32_t wide;        // q and y four values at a time
   float* part;         // (units, splits, rows, NB * 32) values, then (.., rows) reference score and sum
   float2* part_stat;
 };

@@ -18,12 +18,14 @@
 // as below, every eighth token's values 2^60 larger: 1282 us for 565).  Looking for them costs nothing
 // measurable at 128 channels and 15 in 1000 of a prompt of heads of 64.
 //
-// Four prompts of 4096 tokens, 32 heads of 128 over 8, bfloat16: 575 to 605 us, 910 to 956
-// TFLOP/s (a large bfloat16 matrix product: 1258); 512 tokens over 32768: 254 to 266 us, 1.04 to
+// Four prompts of 4096 tokens, 32 heads of 128 over 8, bfloat16: 565 to 605 us, 910 to 970
+// TFLOP/s (a large bfloat16 matrix product: 1287); 512 tokens over 32768: 254 to 266 us, 1.04 to
 // 1.09 PFLOP/s.  The matrix units work half of the time.  At two waves a SIMD, which the sums and
 // operands leave room for, the rest is issue and latency of the vector and LDS work between the
 // products: without any matrix instruction a call takes as long to 4 parts in 100.  Exponentials
-// and roundings of the weights are a quarter of that, reading the turned values a tenth.  No faster:
+// and roundings of the weights are a quarter of that, reading the turned values a tenth.  Heads past
+// 128 channels, past 64 in float32, have one wave a SIMD, and registers in scratch at 224 and 256
+// channels, in float32 from 192 on (the first pass by itself: 33 and 46 a lane; 26, 128 and 138).  No faster:
 // 64 rows a wave (its registers spill), the scheduler's own grouping of the instructions,
 // apart code for tiles at the mask's edge, loads for the first tiles ahead of the queries.
 #include <utility>
